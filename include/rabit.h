@@ -395,6 +395,87 @@ int rb_rmsnorm(const uint16_t *x, const uint16_t *w, uint16_t *y, int T, int n, 
 int rb_silu_mul(const uint16_t *gate, const uint16_t *up, uint16_t *y, size_t n, void *stream);
 int rb_add(const uint16_t *a, const uint16_t *b, uint16_t *y, size_t n, void *stream);
 
+/*
+ * Attention and its cache (the part of a Llama block between q, k, v and o).
+ *
+ * Heads: `heads` query heads share `kv_heads` key and value heads, heads /
+ * kv_heads of them one after the other (head h reads key head h / (heads /
+ * kv_heads)); `dim` elements each, a multiple of 8 up to 128 (RB_ERR_UNSUPPORTED
+ * above).  q is [token][head][dim] with strides of its own for token and head, in
+ * elements, multiples of 8 and at most 2^25; elements of a head are contiguous.  k and v likewise.  o is
+ * contiguous [tokens][heads][dim].  q, k, v, o are device memory of one dtype,
+ * RB_F16 or RB_BF16, 16-byte aligned.  Scores, softmax and sums are fp32; the
+ * softmax weights are rounded to dtype before they meet the values.
+ *
+ * Sequences are packed one after the other: sequence s has the tokens first[s]
+ * .. first[s + 1] - 1 (device int32 [n_seqs + 1], first[0] = 0, not decreasing;
+ * lengths of zero are allowed; at most 2^24 tokens and 2^20 sequences).  The arrays are read on the
+ * device; entries out of order or out of range give unspecified results, but
+ * nothing outside the buffers is touched.
+ *
+ * What a row does not see has no influence on it, infinities and NaN included.
+ * A row that sees no key at all gives zeros (and lse = -infinity).
+ */
+typedef struct rb_heads {
+    int heads, kv_heads, dim, dtype;
+    long long q_token, q_head, k_token, k_head, v_token, v_head;
+} rb_heads;
+
+/*
+ * Whole prompts.  Row i of a sequence sees its keys j <= i (causal), or all of
+ * them.  first_k / tokens_k: the keys' own packing where it differs from the queries' (NULL:
+ * the same, tokens_k = tokens_q); causal rows are then aligned at the end, row i of n sees
+ * j <= i + (keys - n).  scores are scale * q.k, scale > 0 (RB_ERR_VALUE).
+ * lse: NULL or fp32 [tokens_q][heads], log sum_j exp(scale * q_i.k_j), which the
+ * gradient needs.
+ */
+int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, const void *v,
+                   const int32_t *first_q, const int32_t *first_k, int n_seqs, int tokens_q, int tokens_k,
+                   int causal, float scale, void *o, float *lse, void *stream);
+
+/*
+ * A paged cache: `pages` pages of page_tokens tokens (a power of two, 8 .. 65536) of
+ * kv_heads heads of dim elements, keys and values in two arrays of the same strides
+ * (elements, multiples of 8; elements of a head are contiguous), 16-byte
+ * aligned.  Position p of sequence s lies in page table[s * width + p /
+ * page_tokens], place p % page_tokens (device int32 [n_seqs][width]; entries
+ * behind a sequence's last position are not read).
+ */
+typedef struct rb_cache {
+    void *k, *v;
+    int pages, page_tokens, kv_heads, dim, dtype;
+    long long page_stride, token_stride, head_stride;
+} rb_cache;
+
+/*
+ * New tokens enter the cache: sequence s has the tokens first[s] .. first[s + 1] - 1 of k and v (and
+ * q), which become the last of its lengths[s] positions (the length after the call; what
+ * lies before is there already).  With cos and sin (device fp32 [table_rows][rotary / 2], 16-byte
+ * aligned, row = position) the first `rotary` elements of every head of k and q are turned, in fp32 with one
+ * rounding: pairs (x, y) -> (x cos - y sin, y cos + x sin), element i with i + rotary / 2, or 2 i with 2 i + 1
+ * where `interleaved`.  rotary is a multiple of 8, at most dim.  cos and sin NULL: nothing is turned.  The
+ * turned q goes to q_out, contiguous [tokens][heads][dim] (may be q itself if that is
+ * contiguous); q and q_out NULL: no queries.  H: strides of q, k, v, and their heads, which have to be the cache's.
+ * Positions outside the page table are not stored.
+ */
+int rb_cache_append(const rb_cache *C, const rb_heads *H, const void *q, const void *k, const void *v,
+                    const float *cos, const float *sin, int table_rows, int rotary, int interleaved,
+                    const int32_t *first, const int32_t *lengths, const int32_t *table, int width,
+                    int n_seqs, int tokens, void *q_out, void *stream);
+
+/*
+ * Attention of new tokens over the cache: sequence s has the tokens first[s] ..
+ * first[s + 1] - 1 of q, which are the last of its lengths[s] positions (their
+ * keys and values are in the cache already).  A token sees the positions up to its
+ * own.  Any mix of single tokens and chunks.  workspace: rb_attn_paged_workspace_bytes
+ * bytes of device memory, 16-byte aligned.
+ */
+size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens);
+int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads,
+                  const int32_t *first, const int32_t *lengths, const int32_t *table, int width,
+                  int n_seqs, int tokens, float scale, void *o,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

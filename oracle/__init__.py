@@ -34,6 +34,11 @@ What each function follows:
                                and the addition of the residual stream, each by its
                                textbook definition.
 
+* ``attention`` / ``attention_grad`` / ``rotary``
+                             - what the same block has between q, k, v and o: softmax
+                               attention of one head and its gradient, and the rotary
+                               embedding, each by its textbook definition.
+
 All floating point is fp64.  Stored fp16 / bf16 values are widened exactly.
 """
 from __future__ import annotations
@@ -434,3 +439,58 @@ def block_forward(layers: Sequence[Tuple[np.ndarray, np.ndarray, np.ndarray]],
         if write_back:
             bufs[dst] = y.astype(np.float16)
     return outs
+
+
+# ------------------------------------------------------------- attention ---
+def _weights(q, k, sees, scale):
+    """Softmax weights [n][m] of rows that see their first sees[i] keys, and the log-sums [n]."""
+    s = (q @ k.T) * scale if k.shape[0] else np.zeros((q.shape[0], 0))
+    s = np.where(np.arange(k.shape[0])[None] < np.asarray(sees)[:, None], s, -np.inf)
+    top = s.max(1, initial=-np.inf)
+    p = np.exp(s - np.where(np.isneginf(top), 0.0, top)[:, None])
+    total = p.sum(1)
+    with np.errstate(divide="ignore"):
+        lse = np.where(np.isneginf(top), -np.inf, top + np.log(total))
+    return p / np.where(total == 0, 1.0, total)[:, None], lse
+
+
+def attention(q, k, v, sees, scale: float):
+    """One head: o_i = sum_j p_ij v_j with p_i the softmax of scale * q_i.k_j over the first sees[i] keys j.
+
+    q [n][d], k and v [m][d]; rows that see nothing give zeros and a log-sum of minus infinity.  Places
+    that a row does not see take no part at all.  Returns (o [n][d], lse [n], sum_j p_ij |v_j| [n][d]).
+    """
+    q, k, v = _f64(q), _f64(k), _f64(v)
+    with np.errstate(invalid="ignore", over="ignore"):
+        p, lse = _weights(q, k, sees, scale)
+        if np.isfinite(v).all():
+            return p @ v, lse, p @ np.abs(v)
+        rows = [(p[i, :max(n, 0)], v[:max(n, 0)]) for i, n in enumerate(sees)]
+        return np.stack([a @ b for a, b in rows]), lse, np.stack([a @ np.abs(b) for a, b in rows])
+
+
+def attention_grad(do, q, k, v, sees, scale: float):
+    """Gradients of `attention` for one head, given do [n][d]:
+    dv_j = sum_i p_ij do_i;  ds_ij = scale p_ij (do_i.v_j - do_i.o_i);  dq_i = sum_j ds_ij k_j;  dk_j = sum_i ds_ij q_i.
+
+    Returns (dq, dk, dv) and, for error bounds, the same sums over magnitudes, with |ds_ij| widened by
+    scale p_ij (|do_i|.|o_i|), which is what a rounded o_i moves it by.
+    """
+    do, q, k, v = _f64(do), _f64(q), _f64(k), _f64(v)
+    p, _ = _weights(q, k, sees, scale)
+    o = p @ v
+    ds = scale * p * (do @ v.T - (do * o).sum(1)[:, None])
+    wide = np.abs(ds) + scale * p * (np.abs(do) * np.abs(o)).sum(1)[:, None]
+    return (ds @ k, ds.T @ q, p.T @ do), (wide @ np.abs(k), wide.T @ np.abs(q), p.T @ np.abs(do))
+
+
+def rotary(x, cos, sin, interleaved: bool):
+    """x [..., d] with its first 2 * cos.shape[-1] elements turned pair by pair: (a, b) -> (a cos - b sin, b cos + a sin);
+    pairs are (i, i + half) or, interleaved, (2 i, 2 i + 1)."""
+    x = _f64(x).copy()
+    cos, sin = _f64(cos), _f64(sin)
+    half = cos.shape[-1]
+    a, b = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    u, w = x[..., a].copy(), x[..., b].copy()
+    x[..., a], x[..., b] = u * cos - w * sin, w * cos + u * sin
+    return x

@@ -33,6 +33,7 @@ EXPORTS = [
     "rb_couple", "rb_weight_grad", "rb_scale_grads", "rb_scale_grads_workspace_bytes",
     "rb_block_prepare", "rb_block_workspace_bytes", "rb_rmsnorm", "rb_silu_mul", "rb_add",
     "rb_derive_iterative", "rb_derive_workspace_bytes",
+    "rb_attn_prompt", "rb_attn_paged", "rb_attn_paged_workspace_bytes", "rb_cache_append",
     "rb_dense_gemv_f16", "rb_stream_read", "rb_stream_read_groups", "rb_version", "rb_last_path",
 ]
 
@@ -55,6 +56,17 @@ class rb_stack_op(ctypes.Structure):
 class rb_block_op(ctypes.Structure):
     _fields_ = [("layer", ctypes.c_int), ("src", ctypes.c_int), ("dst", ctypes.c_int),
                 ("norm", ctypes.c_int), ("epilogue", ctypes.c_int), ("aux", ctypes.c_int)]
+
+
+class rb_heads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("heads", "kv_heads", "dim", "dtype")] + \
+               [(n, ctypes.c_longlong) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head")]
+
+
+class rb_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int) for n in ("pages", "page_tokens", "kv_heads", "dim", "dtype")] + \
+               [(n, ctypes.c_longlong) for n in ("page_stride", "token_stride", "head_stride")]
 
 
 def _load() -> ctypes.CDLL:
@@ -100,6 +112,12 @@ def _load() -> ctypes.CDLL:
     lib.rb_scale_grads_workspace_bytes.argtypes = [i, i, i]
     lib.rb_scale_grads_workspace_bytes.restype = z
     lib.rb_scale_grads.argtypes = [p, p, p, p, i, i, i, p, p, p, z, p]
+    f, l = ctypes.c_float, ctypes.c_longlong
+    lib.rb_attn_prompt.argtypes = [ctypes.POINTER(rb_heads), p, p, p, p, p, i, i, i, i, f, p, p, p]
+    lib.rb_cache_append.argtypes = [ctypes.POINTER(rb_cache), ctypes.POINTER(rb_heads), p, p, p, p, p, i, i, i, p, p, p, i, i, i, p, p]
+    lib.rb_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(rb_cache), i, i, i]
+    lib.rb_attn_paged_workspace_bytes.restype = z
+    lib.rb_attn_paged.argtypes = [ctypes.POINTER(rb_cache), p, l, l, i, p, p, p, i, i, i, f, p, p, z, p]
     lib.rb_dense_gemv_f16.argtypes = [p, p, p, i, i, p]
     lib.rb_stream_read.argtypes = [p, z, p, p]
     lib.rb_stream_read_groups.argtypes = []
@@ -107,7 +125,8 @@ def _load() -> ctypes.CDLL:
     lib.rb_last_path.argtypes = []
     for name in EXPORTS:
         if name not in ("rb_native_bytes", "rb_workspace_bytes", "rb_noalloc_scratch_bytes",
-                        "rb_scale_grads_workspace_bytes", "rb_block_workspace_bytes", "rb_derive_workspace_bytes"):
+                        "rb_scale_grads_workspace_bytes", "rb_block_workspace_bytes", "rb_derive_workspace_bytes",
+                        "rb_attn_paged_workspace_bytes"):
             getattr(lib, name).restype = i
     return lib
 
@@ -480,6 +499,111 @@ def rb_scale_grads(G: torch.Tensor, packed: torch.Tensor, g: torch.Tensor, h: to
     _check("rb_scale_grads", lib.rb_scale_grads(G.data_ptr(), packed.data_ptr(), g.data_ptr(), h.data_ptr(), K, out, inn,
                                                 gg.data_ptr(), gh.data_ptr(), ws.data_ptr(), n, _stream()))
     return gg, gh
+
+
+# -------------------------------------------------- attention, its cache ---
+def _check_heads(x: torch.Tensor, dtype: torch.dtype, dim: int) -> None:
+    assert x.is_cuda and x.dim() == 3 and x.dtype == dtype and x.shape[2] == dim and (dim == 1 or x.stride(2) == 1)
+
+
+def _check_numbers(x: torch.Tensor, *shape) -> None:
+    assert x.is_cuda and x.dtype == torch.int32 and x.is_contiguous() and tuple(x.shape) == shape
+
+
+def _heads(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> rb_heads:
+    """Shapes and strides of q [tokens][heads][dim] and k, v [tokens][kv_heads][dim]."""
+    for x in (q, k, v):
+        _check_heads(x, k.dtype, k.shape[2])
+    assert k.shape == v.shape
+    return rb_heads(q.shape[1], k.shape[1], k.shape[2], _DTYPE_CODE[k.dtype], *q.stride()[:2], *k.stride()[:2], *v.stride()[:2])
+
+
+def rb_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, first_k: torch.Tensor = None,
+                   causal: bool = True, scale: float = None, want_lse: bool = False, o: torch.Tensor = None):
+    """Attention over packed sequences: q [tokens][heads][dim], k and v [tokens][kv_heads][dim] (fp16 or bf16, any
+    strides of tokens and heads), first int32 [n_seqs + 1]; returns o [tokens][heads][dim], or (o, lse fp32 [tokens][heads])."""
+    H = _heads(q, k, v)
+    _check_numbers(first, first.numel())
+    if first_k is not None:
+        _check_numbers(first_k, first.numel())
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert o.is_cuda and o.dtype == q.dtype and o.shape == q.shape and o.is_contiguous()
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+    _check("rb_attn_prompt", lib.rb_attn_prompt(
+        ctypes.byref(H), q.data_ptr(), k.data_ptr(), v.data_ptr(), first.data_ptr(), None if first_k is None else first_k.data_ptr(),
+        first.numel() - 1, q.shape[0], k.shape[0], int(causal), q.shape[2] ** -0.5 if scale is None else scale, o.data_ptr(),
+        lse.data_ptr() if want_lse else None, _stream()))
+    return (o, lse) if want_lse else o
+
+
+class Cache:
+    """A paged cache over two tensors [pages][page_tokens][kv_heads][dim] of equal strides (fp16 or bf16)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype
+        assert k.stride() == v.stride() and (k.shape[3] == 1 or k.stride(3) == 1)
+        self.k, self.v = k, v
+        pages, page_tokens, self.kv_heads, self.dim = k.shape
+        self._struct = rb_cache(k.data_ptr(), v.data_ptr(), pages, page_tokens, self.kv_heads, self.dim, _DTYPE_CODE[k.dtype], *k.stride()[:3])
+
+    @classmethod
+    def zeros(cls, pages: int, page_tokens: int, kv_heads: int, dim: int, dtype=torch.float16, device="cuda:0") -> "Cache":
+        return cls(*(torch.zeros((pages, page_tokens, kv_heads, dim), dtype=dtype, device=device) for _ in range(2)))
+
+    def struct(self) -> rb_cache:
+        return self._struct
+
+
+def _check_sequences(first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor) -> int:
+    n = lengths.numel()
+    _check_numbers(first, n + 1)
+    _check_numbers(lengths, n)
+    _check_numbers(table, n, table.shape[-1])
+    return n
+
+
+def rb_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
+                    q: torch.Tensor = None, cos: torch.Tensor = None, sin: torch.Tensor = None, interleaved: bool = False,
+                    q_out: torch.Tensor = None):
+    """New tokens k, v [tokens][kv_heads][dim] become the last of each sequence's lengths int32 [n_seqs] positions of the
+    cache, with the rotary embedding of cos, sin fp32 [rows][rotary / 2] on k and q [tokens][heads][dim]; returns the turned q."""
+    n = _check_sequences(first, lengths, table)
+    H = _heads(k if q is None else q, k, v)
+    assert H.kv_heads == cache.kv_heads and H.dim == cache.dim and k.dtype == cache.k.dtype
+    assert q is None or q.shape[0] == k.shape[0]
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert (q is None) == (q_out is None) and (q is None or (q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous()))
+    assert (cos is None) == (sin is None)
+    if cos is not None:
+        for x in (cos, sin):
+            assert x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.dim() == 2 and x.shape == cos.shape
+    _check("rb_cache_append", lib.rb_cache_append(
+        ctypes.byref(cache.struct()), ctypes.byref(H), None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        None if cos is None else cos.data_ptr(), None if cos is None else sin.data_ptr(), 0 if cos is None else cos.shape[0],
+        0 if cos is None else 2 * cos.shape[1], int(interleaved), first.data_ptr(), lengths.data_ptr(), table.data_ptr(), table.shape[1],
+        n, k.shape[0], None if q is None else q_out.data_ptr(), _stream()))
+    return q_out
+
+
+def rb_attn_paged(cache: Cache, q: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, scale: float = None,
+                  o: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
+    """Attention of new tokens q [tokens][heads][dim], the last of each sequence's lengths positions, over the cache."""
+    n = _check_sequences(first, lengths, table)
+    _check_heads(q, cache.k.dtype, cache.dim)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert o.is_cuda and o.dtype == q.dtype and o.shape == q.shape and o.is_contiguous()
+    C, tokens, heads = ctypes.byref(cache.struct()), q.shape[0], q.shape[1]
+    if workspace is None:
+        need = lib.rb_attn_paged_workspace_bytes(C, heads, n, tokens)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check("rb_attn_paged", lib.rb_attn_paged(
+        C, q.data_ptr(), q.stride(0), q.stride(1), heads, first.data_ptr(), lengths.data_ptr(), table.data_ptr(), table.shape[1], n, tokens,
+        cache.dim ** -0.5 if scale is None else scale, o.data_ptr(), None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel(), _stream()))
+    return o
 
 
 def rb_stack_set_option(option: int, value: int) -> None:

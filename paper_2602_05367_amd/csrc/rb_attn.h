@@ -1,0 +1,255 @@
+// What the attention kernels share: element types and their matrix instructions, tiles of keys and
+// values in LDS, and the way from a workgroup's number to the rows it has to do.
+//
+// All products are v_mfma_f32_32x32x16.  Its operands hold, per lane, row (left) or column (right)
+// lane % 32 and eight values along the contraction, of the half lane / 32; its result holds column
+// lane % 32 and rows 8 (i / 4) + 4 (lane / 32) + i % 4 for i = 0..15.  Scores are computed transposed, keys
+// by query rows: a lane then owns one query row, its softmax statistics are scalars of the lane, and
+// the weights are already where the next product's right operand wants them, with the contraction
+// index numbered 4 (lane / 32) + e % 4 + 8 (e / 4).  The left operand of that product, the transposed values,
+// is read in the same numbering from the row-major tile by ds_read_b64_tr_b16 (four rows by
+// sixteen columns per sixteen lanes, transposed on the way).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "rabit.h"
+#include "rb_device.h"
+
+namespace rb {
+namespace attn {
+
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+#define RB_NEG_INF (-__builtin_inff())
+
+// Weights are rounded to the inputs' type before they meet the values, each on its own and to
+// nearest: one rounding of relative size 2^-11 (2^-8) per weight, which averages out over a row to what
+// the rounding of the result costs.  fp16 reaches down to 2^-14 only at full precision, so its weights are
+// kept 2^BIAS times as large as the softmax defines them.
+struct F16 {
+    static constexpr int BIAS = 6, GRAD_BIAS = 14;
+    static constexpr uint32_t EXPONENT = 0x7c00u;
+    static __device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2h)); }
+    static __device__ __forceinline__ float widen(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
+};
+struct BF16 {
+    static constexpr int BIAS = 0, GRAD_BIAS = 0;
+    static constexpr uint32_t EXPONENT = 0x7f80u;
+    static __device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2b)); }
+    static __device__ __forceinline__ float widen(uint32_t bits) { return __uint_as_float(bits << 16); }
+};
+
+// an infinity or a NaN among the two 16-bit values of a word
+template <class T> __device__ __forceinline__ bool not_finite(uint32_t w)
+{
+    constexpr uint32_t E = T::EXPONENT;
+    return (w & E) == E || ((w >> 16) & E) == E;
+}
+template <class T> __device__ __forceinline__ uint32_t finite_part(uint32_t w)
+{
+    constexpr uint32_t E = T::EXPONENT;
+    return ((w & E) == E ? 0 : w & 0xffffu) | (((w >> 16) & E) == E ? 0 : w & 0xffff0000u);
+}
+
+// the sum or maximum of a lane's value and that of the lane 32 away, in both
+__device__ __forceinline__ float over_halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float over_halves_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// ------------------------------------------------------------------- tiles ---
+// A tile is ROWS rows of D elements (D = 64 or 128, a head's elements and zeros after them) in LDS,
+// 16-byte pieces of a row permuted so that 32 rows at one column and four rows at 32 columns both
+// touch every bank once: piece c of row r lies at c ^ spread(r).
+constexpr int ROWS = 64, WAVES = 4;
+template <int D> struct Tile {
+    static constexpr int ROW = D * 2, BYTES = ROWS * ROW, PIECES = D / 8;
+    static constexpr int ROWS_PER_LOAD = 1024 / ROW, LOADS = BYTES / 1024 / WAVES;     // a wavefront's load fills 1 KB
+    static __device__ __forceinline__ int spread(int r)
+    {
+        return D == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+    }
+};
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+typedef __attribute__((address_space(3))) v4u lds_v4u;
+
+// Loads past the end of a buffer give zeros, in LDS too: rows past a sequence's end and elements past a
+// head's last are zeros in every tile, whatever lies there in memory.
+constexpr uint32_t NOWHERE = 0x7fffff00u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t *p, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, (int)bytes, 0x00020000);
+}
+
+// Where this lane's part of load i of a tile lies behind the first row of that load
+template <int D> __device__ __forceinline__ void lane_offsets(uint32_t (&at)[Tile<D>::LOADS], long long stride, int dim, int wave, int lane)
+{
+    using L = Tile<D>;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+        const int r = lane / L::PIECES, row = (wave * L::LOADS + i) * L::ROWS_PER_LOAD + r;
+        const int c = (lane % L::PIECES) ^ L::spread(row);
+        at[i] = c * 8 < dim ? (uint32_t)(r * stride) + c * 16 : NOWHERE;
+    }
+}
+// `rows` rows from `base` on into the rows of a load; rows <= 0: zeros
+__device__ __forceinline__ void load_rows(const uint8_t *base, long long stride, int rows, int most, int dim, uint32_t at, uint8_t *to)
+{
+    rows = min(rows, most);
+    const uint32_t bytes = rows <= 0 ? 0u : (uint32_t)((rows - 1) * (int)stride + dim * 2);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(base, bytes), (__attribute__((address_space(3))) void *)to, 16, (int)at, 0, 0, 0);
+}
+// rows first .. first + 63 of a sequence's `len` rows, strided in memory
+template <int D>
+__device__ __forceinline__ void load_tile(const uint8_t *base, long long stride, int first, int len, int dim, const uint32_t (&at)[Tile<D>::LOADS], uint8_t *tile, int wave)
+{
+    using L = Tile<D>;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+        const int row = first + (wave * L::LOADS + i) * L::ROWS_PER_LOAD;
+        load_rows(base + row * stride, stride, len - row, L::ROWS_PER_LOAD, dim, at[i], tile + (wave * L::LOADS + i) * 1024);
+    }
+}
+
+// Reads of a tile as left operands.  Rows: row 32 b + lane % 32, elements 16 k + 8 (lane / 32) ..; columns:
+// element 32 b + lane % 32 of rows 16 k + the numbering above.
+template <int D> struct Rows {
+    uint32_t row;
+    int piece;
+    __device__ __forceinline__ Rows(int lane) : row((lane & 31) * Tile<D>::ROW), piece(((lane >> 5) ^ Tile<D>::spread(lane & 31)) * 16) {}
+    __device__ __forceinline__ v4u read(const uint8_t *tile, int b, int k) const
+    {
+        return *(const lds_v4u *)(lds_byte *)(tile + row + (piece ^ (k * 32)) + b * (32 * Tile<D>::ROW));
+    }
+};
+template <int D> struct Columns {
+    uint32_t row;
+    int piece[2];
+    __device__ __forceinline__ Columns(int lane)
+    {
+        const int h = lane >> 5, i = lane & 15, r = 4 * h + i / 4, c = (lane >> 4 & 1) * 2 + (i & 3) / 2;
+        row = r * Tile<D>::ROW + (i & 1) * 8;
+        piece[0] = (c ^ Tile<D>::spread(r)) * 16;
+        piece[1] = (c ^ Tile<D>::spread(r + 8)) * 16;
+    }
+    __device__ __forceinline__ v4u read(const uint8_t *tile, int b, int k) const
+    {
+        const uint8_t *p = tile + row + k * (16 * Tile<D>::ROW);
+        const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(lds_byte *)(p + (piece[0] ^ (b * 64)))));
+        const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(lds_byte *)(p + 8 * Tile<D>::ROW + (piece[1] ^ (b * 64)))));
+        return (v4u){lo.x, lo.y, hi.x, hi.y};
+    }
+};
+
+// Infinities and NaN in places that a row does not see: weight zero times such a value would be NaN.  Tiles of which some row of the
+// workgroup sees only a part are looked through before use: what is not finite becomes zero, and `found` says that there was some.
+template <class T, int D> __device__ __forceinline__ void make_finite(uint8_t *tile, int *found, int tid)
+{
+    using L = Tile<D>;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+        lds_v4u *at = (lds_v4u *)(lds_byte *)(tile + (i * (64 * WAVES) + tid) * 16);
+        const v4u w = *at;
+        if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) {
+            *found = 1;
+            *at = (v4u){finite_part<T>(w.x), finite_part<T>(w.y), finite_part<T>(w.z), finite_part<T>(w.w)};
+        }
+    }
+}
+// At the end, where something was found: sums [element][column of the lane] += what is not finite in row `from` (in memory), if the lane's
+// column sees it.  Any weight gives the same.
+template <class T, int D> __device__ __forceinline__ void add_not_finite(v16f (&sums)[D / 32], const uint8_t *from, int dim, int h, bool seen)
+{
+    const __amdgpu_buffer_rsrc_t row = buffer(from, dim * 2);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const v2u w = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(row, h * 8, (b * 32 + 2 * i) * 2, 0));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t bits = (j < 2 ? w.x : w.y) >> (j % 2 * 16) & 0xffffu;
+                if (seen && (bits & T::EXPONENT) == T::EXPONENT) sums[b][i + j] += T::widen(bits);
+            }
+        }
+}
+// the loads into LDS that this wavefront has asked for have arrived: a barrier alone does not wait for them
+__device__ __forceinline__ void loads_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// -------------------------------------------------------------------- work ---
+// Sequences are packed: sequence s has the tokens first[s] .. first[s + 1] - 1.  The rows of a key head are its queries, group after
+// group of the heads that share it: row = token * group + head of the group.  Blocks of BM rows are numbered so that the
+// number of a sequence's first block follows from first[s] alone, floor(first[s] group / BM) + s, without a sum over the
+// sequences before it; some numbers between two sequences belong to nobody.
+__device__ __forceinline__ int block_start(const int *first, int s, int group, int BM) { return (int)((long long)first[s] * group / BM) + s; }
+inline long long block_numbers(long long tokens, int n_seqs, int group, int BM) { return tokens * group / BM + n_seqs; }
+
+// the last of n places whose start is not beyond `value` (place 0's never is); a wavefront looks at 64 at a time
+template <class Start> __device__ __forceinline__ int last_not_beyond(int n, int value, int lane, Start start)
+{
+    const int last = n - 1;
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 63) / 64;
+        const unsigned long long below = __ballot(lane * step < n && start(min(lo + lane * step, last)) <= value);
+        const int k = max(0, __popcll(below) - 1);
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+__device__ __forceinline__ int sequence_of_block(const int *first, int n_seqs, int group, int BM, int block, int lane)
+{
+    return last_not_beyond(n_seqs, block, lane, [&](int s) { return block_start(first, s, group, BM); });
+}
+
+// One sequence's part of the work.  What the arrays say is brought into the range of the buffers: an array that
+// is not in order gives wrong results, but no access outside.
+struct Sequence {
+    int q0, n_q, k0, n_k;
+};
+__device__ __forceinline__ Sequence sequence_at(const int *first_q, const int *first_k, int s, int tokens_q, int tokens_k)
+{
+    Sequence r;
+    r.q0 = min(max(first_q[s], 0), tokens_q);
+    r.n_q = min(max(first_q[s + 1], r.q0), tokens_q) - r.q0;
+    r.k0 = min(max(first_k[s], 0), tokens_k);
+    r.n_k = min(max(first_k[s + 1], r.k0), tokens_k) - r.k0;
+    return r;
+}
+
+// Operands of a call; strides in bytes.
+struct Side {
+    Address at;
+    long long token, head;
+};
+
+}  // namespace attn
+}  // namespace rb

@@ -1,0 +1,283 @@
+// Attention over packed prompts and over a paged cache: o_i = sum_j p_ij v_j with
+// p_ij = exp(c q_i . k_j - lse_i), lse_i = log sum_j exp(c q_i . k_j) over the keys j that row i sees.
+#include <hip/hip_runtime.h>
+#include <cmath>
+
+#include "rabit.h"
+#include "rb_attn.h"
+#include "rb_attn_host.h"
+
+namespace rb {
+namespace attn {
+namespace {
+
+struct Args {
+    Side q, k, v;
+    Address o, lse, first_q, first_k;        // paged: first_k holds the sequences' lengths
+    Address table;
+    long long page;
+    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
+    int page_shift, pages, width;
+    float c;                                 // scale log2(e): the exponentials are powers of two
+};
+
+constexpr int BM = 32 * WAVES;
+// Weights are taken relative to a maximum that follows the scores only when they pass it by this many powers of two: the sums
+// are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
+constexpr float SLACK = 8.f;
+
+// One workgroup does BM rows of one key head, 32 per wavefront, over all keys that they see, 64 at a time: the next
+// tile of keys and values is on its way into LDS while one is used.
+template <class T, int D, bool PAGED>
+__global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
+{
+    using L = Tile<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * L::BYTES];       // keys, keys, values, values
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % A.kv_heads;      // the workgroups of a head go to the same XCDs
+    int block = blockIdx.x / A.kv_heads;
+    if (A.causal) block = (int)(gridDim.x / A.kv_heads) - 1 - block;      // the longest first
+    const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
+    const int s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
+    Sequence S = sequence_at(first_q, PAGED ? first_q : first_k, s, A.tokens_q, PAGED ? A.tokens_q : A.tokens_k);
+    if (PAGED) {
+        S.k0 = 0;
+        S.n_k = min(max(first_k[s], 0), (int)min((long long)A.width << A.page_shift, 0x7fffffc0ll));
+    }
+    const int row0 = (block - block_start(first_q, s, A.group, BM)) * BM, n_rows = S.n_q * A.group;
+    if (row0 < 0 || row0 >= n_rows) return;
+
+    const int my_row = row0 + wave * 32 + (lane & 31);
+    const bool real = my_row < n_rows;
+    const int row = min(my_row, n_rows - 1), token = row / A.group, head = kvh * A.group + row % A.group;
+    // the last key that a row sees; -1 or less: none
+    const int ahead = S.n_k - S.n_q;
+    auto last_key = [&](int r) { return A.causal ? min(ahead + min(r, n_rows - 1) / A.group, S.n_k - 1) : S.n_k - 1; };
+    const int limit = A.causal ? ahead + token : S.n_k - 1;
+    const int block_least = last_key(row0), block_most = last_key(row0 + BM - 1);
+    const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32 + 31));
+    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + ROWS - 1) / ROWS;
+
+    v4u q[D / 16];
+    {
+        const uint8_t *from = global_at<const uint8_t>(A.q.at) + (S.q0 + token) * A.q.token + head * A.q.head;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) q[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from + k * 32 + h * 16) : (v4u)(0u);
+    }
+
+    uint32_t k_at[L::LOADS], v_at[L::LOADS];
+    lane_offsets<D>(k_at, A.k.token, A.dim, wave, lane);
+    lane_offsets<D>(v_at, A.v.token, A.dim, wave, lane);
+    const uint8_t *k_base = global_at<const uint8_t>(A.k.at) + S.k0 * A.k.token + kvh * A.k.head;
+    const uint8_t *v_base = global_at<const uint8_t>(A.v.at) + S.k0 * A.v.token + kvh * A.v.head;
+    const int *table = PAGED ? global_at<const int>(A.table) + (long long)s * A.width : nullptr;
+    int held = 0, held_at = -1;      // 64 entries of the page table, one per lane
+    auto row_at = [&](int r) {       // where row r's key lies behind the first page
+        const int page = __builtin_amdgcn_readlane(held, (r >> A.page_shift) & 63);
+        return page * A.page + (r & ((1 << A.page_shift) - 1)) * A.k.token;
+    };
+    auto hold_pages = [&](int t) {
+        const int page0 = (t * ROWS) >> A.page_shift;
+        if (page0 >> 6 == held_at) return;
+        held_at = page0 >> 6;
+        held = min(max(table[min(held_at * 64 + lane, A.width - 1)], 0), A.pages - 1);
+    };
+    auto page_at = [&](int r) {      // the same, of a row whose page is held no longer
+        const int page = min(max(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), 0), A.pages - 1);
+        return page * A.page + (r & ((1 << A.page_shift) - 1)) * A.k.token;
+    };
+    auto load = [&](int t) {
+        uint8_t *to = lds + (t & 1) * L::BYTES;
+        if constexpr (!PAGED) {
+            load_tile<D>(k_base, A.k.token, t * ROWS, S.n_k, A.dim, k_at, to, wave);
+            load_tile<D>(v_base, A.v.token, t * ROWS, S.n_k, A.dim, v_at, to + 2 * L::BYTES, wave);
+        } else {
+            hold_pages(t);
+#pragma unroll
+            for (int i = 0; i < L::LOADS; ++i) {
+                const int part = wave * L::LOADS + i, r = t * ROWS + part * L::ROWS_PER_LOAD;
+                const long long at = row_at(r);
+                load_rows(k_base + at, A.k.token, S.n_k - r, L::ROWS_PER_LOAD, A.dim, k_at[i], to + part * 1024);
+                load_rows(v_base + at, A.v.token, S.n_k - r, L::ROWS_PER_LOAD, A.dim, v_at[i], to + 2 * L::BYTES + part * 1024);
+            }
+        }
+    };
+
+    const Rows<D> rows(lane);
+    const Columns<D> columns(lane);
+    v16f sums[D / 32] = {};
+    float top = RB_NEG_INF, total = 0.f;
+    if (tid == 0) found = 0;
+    if (n_tiles > 0) load(0);
+    for (int t = 0; t < n_tiles; ++t) {
+        loads_arrived();
+        __syncthreads();      // tile t is there, everybody has done with tile t - 1
+        uint8_t *keys = lds + (t & 1) * L::BYTES, *values = keys + 2 * L::BYTES;
+        const bool partly = block_least < min(t * ROWS + ROWS, S.n_k) - 1;      // some row of the workgroup does not see all of the tile's keys
+        if (partly) {
+            make_finite<T, D>(values, &found, tid);
+            __syncthreads();
+        }
+        v16f x[2] = {};
+        if (t * ROWS <= wave_most) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) x[b] = T::mfma(rows.read(keys, b, k), q[k], x[b]);
+        }
+        // the next tile is asked for here, behind the last ordinary read of LDS: before such a read the compiler would wait for it
+        if (t + 1 < n_tiles) load(t + 1);
+        if (t * ROWS <= wave_most) {
+            if (t * ROWS + ROWS - 1 > wave_least) {
+                const int seen = limit - t * ROWS - 4 * h;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (b * 32 + 8 * (i / 4) + i % 4 > seen) x[b][i] = RB_NEG_INF;
+            }
+            float most = x[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) most = fmaxf(most, x[i / 16][i % 16]);
+            most = over_halves_max(most) * A.c;
+            if (__ballot(most > top + SLACK)) {
+                const float now = fmaxf(top, most);
+                const float shrink = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                top = now;
+                total *= shrink;
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) sums[b] *= shrink;
+            }
+            const float zero_at = (top == RB_NEG_INF ? 0.f : top) - T::BIAS;
+            v4u p[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float a = __builtin_amdgcn_exp2f(fmaf(x[b][i], A.c, -zero_at)), z = __builtin_amdgcn_exp2f(fmaf(x[b][i + 1], A.c, -zero_at));
+                    total += a + z;
+                    w[i / 2] = T::pack(a, z);
+                }
+                p[2 * b] = (v4u){w[0], w[1], w[2], w[3]};
+                p[2 * b + 1] = (v4u){w[4], w[5], w[6], w[7]};
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) sums[b] = T::mfma(columns.read(values, b, k), p[k], sums[b]);
+        }
+    }
+
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(found))
+        for (int r = max(block_least + 1, 0) / ROWS * ROWS; r <= wave_most; ++r)
+            add_not_finite<T, D>(sums, v_base + (PAGED ? page_at(r) : r * A.v.token), A.dim, h, r <= limit);
+
+    total = over_halves_sum(total);
+    const bool empty = limit < 0;
+    if (A.lse && real && h == 0)
+        global_at<float>(A.lse)[(long long)(S.q0 + token) * A.heads + head] = empty ? RB_NEG_INF : (top - T::BIAS + __builtin_amdgcn_logf(total)) * LN2;
+    const float norm = empty ? 0.f : 1.f / total;
+    uint8_t *to = global_at<uint8_t>(A.o) + ((long long)(S.q0 + token) * A.heads + head) * (A.dim * 2);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            // elements 0-3 and 8-11 of a run of 16 are in the lower half, the others in the upper: exchanged, each half stores eight in a row
+            const auto lo = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i] * norm, sums[b][i + 1] * norm), T::pack(sums[b][i + 4] * norm, sums[b][i + 5] * norm), false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i + 2] * norm, sums[b][i + 3] * norm), T::pack(sums[b][i + 6] * norm, sums[b][i + 7] * norm), false, false);
+            const int e = b * 32 + i * 2 + h * 8;
+            if (real && e < A.dim) *(v4u *)(to + e * 2) = empty ? (v4u)(0u) : (v4u){lo[0], hi[0], lo[1], hi[1]};
+        }
+}
+
+template <class T, bool PAGED> int launch(const Args &A, hipStream_t stream)
+{
+    const long long n = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads;
+    if (n > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    if (A.dim <= 64)
+        hipLaunchKernelGGL((rows_kernel<T, 64, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
+    else
+        hipLaunchKernelGGL((rows_kernel<T, 128, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
+    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
+
+}  // namespace
+
+int check_heads(const rb_heads *H)
+{
+    if (!H) return RB_ERR_NULL;
+    if (H->heads < 1 || H->kv_heads < 1 || H->heads % H->kv_heads != 0 || H->heads > 65536) return RB_ERR_SHAPE;
+    if (H->dim < 8 || H->dim % 8 != 0) return RB_ERR_SHAPE;
+    if (H->dim > 128 || (H->dtype != RB_F16 && H->dtype != RB_BF16)) return RB_ERR_UNSUPPORTED;
+    for (const long long s : {H->q_token, H->q_head, H->k_token, H->k_head, H->v_token, H->v_head}) {
+        if (s < 0 || s > MAX_STRIDE) return RB_ERR_SHAPE;
+        if (s % 8 != 0) return RB_ERR_ALIGN;
+    }
+    return RB_OK;
+}
+
+int check_scale(float scale)
+{
+    return scale > 0.f && scale <= 3e38f ? RB_OK : RB_ERR_VALUE;
+}
+
+}  // namespace attn
+}  // namespace rb
+
+using namespace rb::attn;
+
+extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, const void *v, const int32_t *first_q, const int32_t *first_k, int n_seqs,
+                              int tokens_q, int tokens_k, int causal, float scale, void *o, float *lse, void *stream)
+{
+    const int rc = check_heads(H);
+    if (rc != RB_OK) return rc;
+    if (!q || !k || !v || !first_q || !o) return RB_ERR_NULL;
+    if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens_q < 1 || tokens_k < 0 || tokens_q > MAX_TOKENS || tokens_k > MAX_TOKENS || (!first_k && tokens_k != tokens_q)) return RB_ERR_SHAPE;
+    if (check_scale(scale) != RB_OK) return RB_ERR_VALUE;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) return RB_ERR_ALIGN;
+    if (((uintptr_t)first_q | (uintptr_t)first_k | (uintptr_t)lse) & 3) return RB_ERR_ALIGN;
+    Args A = {};
+    A.q = side(q, H->q_token, H->q_head), A.k = side(k, H->k_token, H->k_head), A.v = side(v, H->v_token, H->v_head);
+    A.o = rb::address_of(o), A.lse = rb::address_of(lse), A.first_q = rb::address_of(first_q), A.first_k = rb::address_of(first_k ? first_k : first_q);
+    A.n_seqs = n_seqs, A.tokens_q = tokens_q, A.tokens_k = tokens_k;
+    A.heads = H->heads, A.kv_heads = H->kv_heads, A.group = H->heads / H->kv_heads, A.dim = H->dim, A.causal = causal != 0;
+    A.c = scale * LOG2E;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return H->dtype == RB_F16 ? launch<F16, false>(A, st) : launch<BF16, false>(A, st);
+}
+
+extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
+{
+    if (check_cache(C) != RB_OK || heads < 1 || heads % C->kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
+    return 0;
+}
+
+extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
+                             const int32_t *table, int width, int n_seqs, int tokens, float scale, void *o, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_cache(C);
+    if (rc != RB_OK) return rc;
+    const rb_heads H = {heads, C->kv_heads, C->dim, C->dtype, q_token, q_head, C->token_stride, C->head_stride, C->token_stride, C->head_stride};
+    rc = check_heads(&H);
+    if (rc != RB_OK) return rc;
+    if (!q || !first || !lengths || !table || !o) return RB_ERR_NULL;
+    if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens < 1 || tokens > MAX_TOKENS || width < 1) return RB_ERR_SHAPE;
+    if (check_scale(scale) != RB_OK) return RB_ERR_VALUE;
+    if (((uintptr_t)q | (uintptr_t)o) & 15) return RB_ERR_ALIGN;
+    if (((uintptr_t)first | (uintptr_t)lengths | (uintptr_t)table) & 3) return RB_ERR_ALIGN;
+    if (workspace_bytes < rb_attn_paged_workspace_bytes(C, heads, n_seqs, tokens) || (workspace_bytes && !workspace)) return RB_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15) return RB_ERR_ALIGN;
+    Args A = {};
+    A.q = side(q, q_token, q_head), A.k = side(C->k, C->token_stride, C->head_stride), A.v = side(C->v, C->token_stride, C->head_stride);
+    A.o = rb::address_of(o), A.first_q = rb::address_of(first), A.first_k = rb::address_of(lengths), A.table = rb::address_of(table);
+    A.page = C->page_stride * 2, A.pages = C->pages, A.width = width, A.page_shift = __builtin_ctz((unsigned)C->page_tokens);
+    A.n_seqs = n_seqs, A.tokens_q = tokens;
+    A.heads = heads, A.kv_heads = C->kv_heads, A.group = heads / C->kv_heads, A.dim = C->dim, A.causal = 1;
+    A.c = scale * LOG2E;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return C->dtype == RB_F16 ? launch<F16, true>(A, st) : launch<BF16, true>(A, st);
+}
