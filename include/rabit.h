@@ -434,6 +434,20 @@ int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, const void *
                    int causal, float scale, void *o, float *lse, void *stream);
 
 /*
+ * Gradients of rb_attn_prompt for the same operands: go, the gradient of o, and o itself are contiguous
+ * [tokens_q][heads][dim], lse is what the forward call gave.  dq [tokens_q][heads][dim], dk and dv
+ * [tokens_k][kv_heads][dim], contiguous, of the inputs' dtype; dk and dv are summed over the query heads that share a key head.
+ * Sums are fp32; weights and score gradients are rounded to dtype before they meet the other operand
+ * (fp16: scaled by a power of two first, so small gradients keep their bits).  No atomics: the same
+ * inputs give the same bits.  workspace: rb_attn_grad_workspace_bytes bytes, 16-byte aligned.
+ */
+size_t rb_attn_grad_workspace_bytes(const rb_heads *H, int tokens_q, int tokens_k);
+int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                        const int32_t *first_q, const int32_t *first_k, int n_seqs, int tokens_q, int tokens_k,
+                        int causal, float scale, void *dq, void *dk, void *dv,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * A paged cache: `pages` pages of page_tokens tokens (a power of two, 8 .. 65536) of
  * kv_heads heads of dim elements, keys and values in two arrays of the same strides
  * (elements, multiples of 8; elements of a head are contiguous), 16-byte

@@ -33,7 +33,7 @@ EXPORTS = [
     "rb_couple", "rb_weight_grad", "rb_scale_grads", "rb_scale_grads_workspace_bytes",
     "rb_block_prepare", "rb_block_workspace_bytes", "rb_rmsnorm", "rb_silu_mul", "rb_add",
     "rb_derive_iterative", "rb_derive_workspace_bytes",
-    "rb_attn_prompt", "rb_attn_paged", "rb_attn_paged_workspace_bytes", "rb_cache_append",
+    "rb_attn_prompt", "rb_attn_prompt_grad", "rb_attn_grad_workspace_bytes", "rb_attn_paged", "rb_attn_paged_workspace_bytes", "rb_cache_append",
     "rb_dense_gemv_f16", "rb_stream_read", "rb_stream_read_groups", "rb_version", "rb_last_path",
 ]
 
@@ -114,6 +114,9 @@ def _load() -> ctypes.CDLL:
     lib.rb_scale_grads.argtypes = [p, p, p, p, i, i, i, p, p, p, z, p]
     f, l = ctypes.c_float, ctypes.c_longlong
     lib.rb_attn_prompt.argtypes = [ctypes.POINTER(rb_heads), p, p, p, p, p, i, i, i, i, f, p, p, p]
+    lib.rb_attn_grad_workspace_bytes.argtypes = [ctypes.POINTER(rb_heads), i, i]
+    lib.rb_attn_grad_workspace_bytes.restype = z
+    lib.rb_attn_prompt_grad.argtypes = [ctypes.POINTER(rb_heads), p, p, p, p, p, p, p, p, i, i, i, i, f, p, p, p, p, z, p]
     lib.rb_cache_append.argtypes = [ctypes.POINTER(rb_cache), ctypes.POINTER(rb_heads), p, p, p, p, p, i, i, i, p, p, p, i, i, i, p, p]
     lib.rb_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(rb_cache), i, i, i]
     lib.rb_attn_paged_workspace_bytes.restype = z
@@ -126,7 +129,7 @@ def _load() -> ctypes.CDLL:
     for name in EXPORTS:
         if name not in ("rb_native_bytes", "rb_workspace_bytes", "rb_noalloc_scratch_bytes",
                         "rb_scale_grads_workspace_bytes", "rb_block_workspace_bytes", "rb_derive_workspace_bytes",
-                        "rb_attn_paged_workspace_bytes"):
+                        "rb_attn_paged_workspace_bytes", "rb_attn_grad_workspace_bytes"):
             getattr(lib, name).restype = i
     return lib
 
@@ -535,6 +538,26 @@ def rb_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: tor
         first.numel() - 1, q.shape[0], k.shape[0], int(causal), q.shape[2] ** -0.5 if scale is None else scale, o.data_ptr(),
         lse.data_ptr() if want_lse else None, _stream()))
     return (o, lse) if want_lse else o
+
+
+def rb_attn_prompt_grad(go: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                        first: torch.Tensor, first_k: torch.Tensor = None, causal: bool = True, scale: float = None):
+    """(dq, dk, dv) of rb_attn_prompt, given go, the gradient of its result o, and its lse."""
+    H = _heads(q, k, v)
+    _check_numbers(first, first.numel())
+    if first_k is not None:
+        _check_numbers(first_k, first.numel())
+    for x in (go, o):
+        assert x.is_cuda and x.dtype == q.dtype and x.shape == q.shape and x.is_contiguous()
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous()
+    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+    n = lib.rb_attn_grad_workspace_bytes(ctypes.byref(H), q.shape[0], k.shape[0])
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+    _check("rb_attn_prompt_grad", lib.rb_attn_prompt_grad(
+        ctypes.byref(H), go.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), first.data_ptr(),
+        None if first_k is None else first_k.data_ptr(), first.numel() - 1, q.shape[0], k.shape[0], int(causal),
+        q.shape[2] ** -0.5 if scale is None else scale, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), n, _stream()))
+    return dq, dk, dv
 
 
 class Cache:

@@ -1,0 +1,424 @@
+// Gradient of attention over packed prompts.  With p_ij = exp(c q_i . k_j - lse_i), given do:
+//   dv_j = sum_i p_ij do_i        dp_ij = do_i . v_j        delta_i = do_i . o_i
+//   ds_ij = c p_ij (dp_ij - delta_i)        dq_i = sum_j ds_ij k_j        dk_j = sum_i ds_ij q_i
+// Two kernels, one with the keys in place and the queries going by (dk, dv: four products), one the other way
+// round (dq: three).  The scores are computed twice, seven products instead of five; in return every sum has one owner, which
+// adds in one order: no atomics, the same bits every time, and the query heads that share a key head are summed in registers.
+//
+// ds is rounded to the inputs' type before it meets k and q.  In fp16 that takes a scale: ds is p times
+// something of the size of do, and both are small.  Twice dim times the largest finite |do| and |v| bounds
+// |dp - delta|; the power of two that brings this bound to one is taken out before and put back into the sums.
+#include <hip/hip_runtime.h>
+
+#include "rabit.h"
+#include "rb_attn.h"
+#include "rb_attn_host.h"
+
+namespace rb {
+namespace attn {
+namespace {
+
+struct GradArgs {
+    Side q, k, v, o;                    // o: strides of the contiguous o, do and dq
+    Address go, lse, first_q, first_k;
+    Address delta, most_o, most_v;      // workspace: [tokens_q][heads], [blocks of 64 tokens][heads], [blocks][kv_heads]
+    Address dq, dk, dv;
+    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
+    float c, scale;
+};
+
+// ------------------------------------------------------- delta and maxima ---
+// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o, or of v.
+template <class T> __global__ __launch_bounds__(256) void delta_kernel(const GradArgs A)
+{
+    __shared__ uint32_t most[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (lane & 15) * 8;
+    const int columns = A.heads + A.kv_heads, head = blockIdx.x % columns, block = blockIdx.x / columns;
+    const bool is_v = head >= A.heads;
+    const int tokens = is_v ? A.tokens_k : A.tokens_q;
+    uint32_t top = 0;
+    for (int i = 0; i < 4; ++i) {
+        const int token = block * 64 + (wave * 4 + i) * 4 + lane / 16;
+        if (token >= tokens) continue;      // whole groups of 16 lanes
+        v4u x = (v4u)(0u), y = (v4u)(0u);
+        if (e < A.dim) {
+            const long long at = is_v ? token * A.v.token + (head - A.heads) * A.v.head : token * A.o.token + head * A.o.head;
+            x = *(const v4u *)(global_at<const uint8_t>(is_v ? A.v.at : A.go) + at + e * 2);
+            if (!is_v) y = *(const v4u *)(global_at<const uint8_t>(A.o.at) + at + e * 2);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = x[j] & 0x7fffu, hi = x[j] >> 16 & 0x7fffu;
+            top = max(top, lo < T::EXPONENT ? lo : 0u);
+            top = max(top, hi < T::EXPONENT ? hi : 0u);
+            sum += T::widen(x[j] & 0xffffu) * T::widen(y[j] & 0xffffu) + T::widen(x[j] >> 16) * T::widen(y[j] >> 16);
+        }
+        if (!is_v) {
+            for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+            if ((lane & 15) == 0) global_at<float>(A.delta)[(long long)token * A.heads + head] = sum;
+        }
+    }
+    for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    if (lane == 0) most[wave] = top;
+    __syncthreads();
+    if (threadIdx.x == 0 && block * 64 < tokens) {
+        top = max(max(most[0], most[1]), max(most[2], most[3]));
+        global_at<float>(is_v ? A.most_v : A.most_o)[(long long)block * (is_v ? A.kv_heads : A.heads) + (is_v ? head - A.heads : head)] = T::widen(top);
+    }
+}
+
+// the largest over the blocks that hold tokens t0 .. t0 + n - 1, of `heads` heads from `head` on
+__device__ __forceinline__ float most_of(const float *most, int columns, int head, int heads, int t0, int n, int lane)
+{
+    float v = 0.f;
+    if (n > 0)
+        for (int b = t0 / 64 * heads + lane; b < ((t0 + n - 1) / 64 + 1) * heads; b += 64) v = fmaxf(v, most[(long long)(b / heads) * columns + head + b % heads]);
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+// the power of two that takes 2 dim a b to between a half and one (1 where that is zero; fp16 values, so neither end of fp32 is near)
+__device__ __forceinline__ float scale_for(float a, float b, int dim)
+{
+    const uint32_t exponent = __float_as_uint(2.f * dim * a * b) >> 23;
+    return exponent ? __uint_as_float((253u - exponent) << 23) : 1.f;
+}
+
+// An infinity or a NaN in the tile?  (see make_finite: here the tile itself is needed as it is, and what is read transposed is cleaned)
+template <class T, int D> __device__ __forceinline__ void look_through(const uint8_t *tile, int *found, int tid)
+{
+    using L = Tile<D>;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+        const v4u w = *(const lds_v4u *)(lds_byte *)(tile + (i * (64 * WAVES) + tid) * 16);
+        if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) *found = 1;
+    }
+}
+template <class T> __device__ __forceinline__ v4u cleaned(v4u w, bool dirty)
+{
+    if (dirty) w = (v4u){finite_part<T>(w.x), finite_part<T>(w.y), finite_part<T>(w.z), finite_part<T>(w.w)};
+    return w;
+}
+
+// sums [element][column], element 32 b + ..., as D elements of a row of 16-bit values
+template <class T, int D> __device__ __forceinline__ void store_columns(const v16f (&sums)[D / 32], float scale, uint8_t *to, int dim, int h, bool real)
+{
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            const auto lo = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i] * scale, sums[b][i + 1] * scale), T::pack(sums[b][i + 4] * scale, sums[b][i + 5] * scale), false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i + 2] * scale, sums[b][i + 3] * scale), T::pack(sums[b][i + 6] * scale, sums[b][i + 7] * scale), false, false);
+            const int e = b * 32 + i * 2 + h * 8;
+            if (real && e < dim) *(v4u *)(to + e * 2) = (v4u){lo[0], hi[0], lo[1], hi[1]};
+        }
+}
+
+// --------------------------------------------------------------- dk and dv ---
+// A workgroup keeps 128 keys and values of one key head, 32 per wavefront as right operands in registers, and takes the queries
+// and do of all its query heads, 64 tokens at a time, through LDS.
+constexpr int BN = 32 * WAVES;
+
+template <class T, int D>
+__global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(const GradArgs A)
+{
+    using L = Tile<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * L::BYTES];       // queries, queries, do, do
+    // what the rows' sums of products start from: -lse in units of the scores, -delta
+    __shared__ __attribute__((aligned(16))) float rows_of[2][2][ROWS];
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;      // causal: the first keys have the most rows
+    const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
+    const int s = sequence_of_block(first_k, A.n_seqs, 1, BN, block, lane);
+    const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
+    const int key0 = (block - block_start(first_k, s, 1, BN)) * BN;
+    if (key0 < 0 || key0 >= S.n_k) return;
+    const int ahead = S.n_k - S.n_q;
+    const int my_key = key0 + wave * 32 + (lane & 31), key = min(my_key, S.n_k - 1);
+    const int block_last = min(key0 + BN, S.n_k) - 1, wave_first = key0 + wave * 32, wave_last = min(wave_first + 31, S.n_k - 1);
+
+    v4u kk[D / 16], vv[D / 16];
+    {
+        const uint8_t *from_k = global_at<const uint8_t>(A.k.at) + (long long)(S.k0 + key) * A.k.token + kvh * A.k.head;
+        const uint8_t *from_v = global_at<const uint8_t>(A.v.at) + (long long)(S.k0 + key) * A.v.token + kvh * A.v.head;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            kk[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_k + k * 32 + h * 16) : (v4u)(0u);
+            vv[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_v + k * 32 + h * 16) : (v4u)(0u);
+        }
+    }
+    float unit = 1.f;      // taken out of dp - delta
+    if (T::GRAD_BIAS)
+        unit = scale_for(most_of(global_at<const float>(A.most_o), A.heads, kvh * A.group, A.group, S.q0, S.n_q, lane),
+                         most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
+
+    uint32_t q_at[L::LOADS], o_at[L::LOADS];
+    lane_offsets<D>(q_at, A.q.token, A.dim, wave, lane);
+    lane_offsets<D>(o_at, A.o.token, A.dim, wave, lane);
+    const int tile0 = A.causal ? max(key0 - ahead, 0) / ROWS : 0, tiles = (S.n_q + ROWS - 1) / ROWS - tile0;
+    const int steps = __builtin_amdgcn_readfirstlane(tiles > 0 ? tiles * A.group : 0);
+    float next_lse = 0.f, next_delta = 0.f;      // of one row of the next tile, in the first wavefront
+    auto load = [&](int n) {
+        const int g = n / tiles, t = tile0 + n % tiles, head = kvh * A.group + g;
+        if (wave == 0) {
+            const int row = t * ROWS + lane;
+            const long long at = (long long)(S.q0 + min(row, S.n_q - 1)) * A.heads + head;
+            // a row past the end: no weight (do is zero there as well)
+            next_lse = row < S.n_q ? T::GRAD_BIAS / A.c - global_at<const float>(A.lse)[at] / A.scale : RB_NEG_INF;
+            next_delta = row < S.n_q ? -global_at<const float>(A.delta)[at] : 0.f;
+        }
+        uint8_t *to = lds + (n & 1) * L::BYTES;
+        load_tile<D>(global_at<const uint8_t>(A.q.at) + S.q0 * A.q.token + head * A.q.head, A.q.token, t * ROWS, S.n_q, A.dim, q_at, to, wave);
+        load_tile<D>(global_at<const uint8_t>(A.go) + S.q0 * A.o.token + head * A.o.head, A.o.token, t * ROWS, S.n_q, A.dim, o_at, to + 2 * L::BYTES, wave);
+    };
+
+    const Rows<D> rows(lane);
+    const Columns<D> columns(lane);
+    v16f sums_k[D / 32] = {}, sums_v[D / 32] = {};
+    if (tid == 0) found = 0;
+    if (steps > 0) load(0);
+    for (int n = 0; n < steps; ++n) {
+        const int t = tile0 + n % tiles;
+        if (wave == 0) {
+            rows_of[n & 1][0][lane] = next_lse;
+            rows_of[n & 1][1][lane] = next_delta;
+        }
+        loads_arrived();
+        __syncthreads();
+        const uint8_t *queries = lds + (n & 1) * L::BYTES, *outs = queries + 2 * L::BYTES;
+        const bool partly = A.causal && block_last > ahead + t * ROWS;      // some key of the workgroup is not seen by all rows
+        bool dirty = false;
+        if (partly) {
+            look_through<T, D>(queries, &found, tid);
+            look_through<T, D>(outs, &found, tid);
+            __syncthreads();
+            dirty = __builtin_amdgcn_readfirstlane(found) != 0;
+        }
+        const bool any = !A.causal || wave_first <= ahead + t * ROWS + ROWS - 1;
+        const bool masked = A.causal && wave_last > ahead + t * ROWS;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            v16f x, y;
+            if (any) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = rows_of[n & 1][0][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
+                    y[i] = rows_of[n & 1][1][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
+                }
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    x = T::mfma(rows.read(queries, b, k), kk[k], x);
+                    y = T::mfma(rows.read(outs, b, k), vv[k], y);
+                }
+            }
+            if (b == 1 && n + 1 < steps) load(n + 1);      // behind the last ordinary read of LDS
+            if (!any) continue;
+            const int least = my_key - ahead - t * ROWS - b * 32 - 4 * h;      // the first row that sees this key
+            uint32_t w[8], z[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float p[2], d[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = i + j;
+                    p[j] = __builtin_amdgcn_exp2f(x[r] * A.c);
+                    d[j] = p[j] * y[r] * unit;
+                    if (masked && 8 * (r / 4) + r % 4 < least) p[j] = d[j] = 0.f;
+                }
+                w[i / 2] = T::pack(p[0], p[1]);
+                z[i / 2] = T::pack(d[0], d[1]);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) {
+                    sums_v[e] = T::mfma(cleaned<T>(columns.read(outs, e, 2 * b + k), dirty), (v4u){w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]}, sums_v[e]);
+                    sums_k[e] = T::mfma(cleaned<T>(columns.read(queries, e, 2 * b + k), dirty), (v4u){z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]}, sums_k[e]);
+                }
+        }
+    }
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(found))      // (only the rows of tiles that were cleaned, and their keys see it)
+        for (int g = 0; g < A.group; ++g)
+            for (int r = tile0 * ROWS; r < min(S.n_q, (max(block_last - ahead, 0) + ROWS - 1) / ROWS * ROWS); ++r)
+                add_not_finite<T, D>(sums_v, global_at<const uint8_t>(A.go) + (S.q0 + r) * A.o.token + (kvh * A.group + g) * A.o.head, A.dim, h, my_key <= ahead + r);
+
+    const bool real = my_key < S.n_k;
+    const long long at = ((long long)(S.k0 + key) * A.kv_heads + kvh) * (A.dim * 2);
+    store_columns<T, D>(sums_v, 1.f / (1 << T::GRAD_BIAS), global_at<uint8_t>(A.dv) + at, A.dim, h, real);
+    store_columns<T, D>(sums_k, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dk) + at, A.dim, h, real);
+}
+
+// ---------------------------------------------------------------------- dq ---
+// As the forward kernel: 128 rows of one key head, 32 per wavefront, with q and do as right operands in registers; keys and values go by.
+template <class T, int D>
+__global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A)
+{
+    using L = Tile<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * L::BYTES];       // keys, keys, values, values
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % A.kv_heads;
+    int block = blockIdx.x / A.kv_heads;
+    if (A.causal) block = (int)(gridDim.x / A.kv_heads) - 1 - block;
+    const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
+    const int s = sequence_of_block(first_q, A.n_seqs, A.group, BN, block, lane);
+    const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
+    const int row0 = (block - block_start(first_q, s, A.group, BN)) * BN, n_rows = S.n_q * A.group;
+    if (row0 < 0 || row0 >= n_rows) return;
+
+    const int my_row = row0 + wave * 32 + (lane & 31);
+    const int row = min(my_row, n_rows - 1), token = row / A.group, head = kvh * A.group + row % A.group;
+    const int ahead = S.n_k - S.n_q;
+    auto last_key = [&](int r) { return A.causal ? min(ahead + min(r, n_rows - 1) / A.group, S.n_k - 1) : S.n_k - 1; };
+    const int limit = A.causal ? ahead + token : S.n_k - 1;
+    const int block_least = last_key(row0), block_most = last_key(row0 + BN - 1);
+    const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32 + 31));
+    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + ROWS - 1) / ROWS;
+
+    v4u q[D / 16], go[D / 16];
+    const long long row_at = (long long)(S.q0 + token) * A.o.token + head * A.o.head;
+    {
+        const uint8_t *from_q = global_at<const uint8_t>(A.q.at) + (S.q0 + token) * A.q.token + head * A.q.head, *from_o = global_at<const uint8_t>(A.go) + row_at;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            q[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_q + k * 32 + h * 16) : (v4u)(0u);
+            go[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_o + k * 32 + h * 16) : (v4u)(0u);
+        }
+    }
+    float unit = 1.f;      // here of the row alone: do is in registers
+    if (T::GRAD_BIAS) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t lo = go[k][j] & 0x7fffu, hi = go[k][j] >> 16 & 0x7fffu;
+                top = max(top, max(lo < T::EXPONENT ? lo : 0u, hi < T::EXPONENT ? hi : 0u));
+            }
+        unit = scale_for(over_halves_max(T::widen(top)), most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
+    }
+    const long long stat = (long long)(S.q0 + token) * A.heads + head;
+    const float zero_at = global_at<const float>(A.lse)[stat] * LOG2E - T::GRAD_BIAS, delta = global_at<const float>(A.delta)[stat] * unit;
+
+    uint32_t k_at[L::LOADS], v_at[L::LOADS];
+    lane_offsets<D>(k_at, A.k.token, A.dim, wave, lane);
+    lane_offsets<D>(v_at, A.v.token, A.dim, wave, lane);
+    const uint8_t *k_base = global_at<const uint8_t>(A.k.at) + S.k0 * A.k.token + kvh * A.k.head;
+    const uint8_t *v_base = global_at<const uint8_t>(A.v.at) + S.k0 * A.v.token + kvh * A.v.head;
+    auto load = [&](int t) {
+        uint8_t *to = lds + (t & 1) * L::BYTES;
+        load_tile<D>(k_base, A.k.token, t * ROWS, S.n_k, A.dim, k_at, to, wave);
+        load_tile<D>(v_base, A.v.token, t * ROWS, S.n_k, A.dim, v_at, to + 2 * L::BYTES, wave);
+    };
+
+    const Rows<D> rows(lane);
+    const Columns<D> columns(lane);
+    v16f sums[D / 32] = {};
+    if (tid == 0) found = 0;
+    if (n_tiles > 0) load(0);
+    for (int t = 0; t < n_tiles; ++t) {
+        loads_arrived();
+        __syncthreads();
+        const uint8_t *keys = lds + (t & 1) * L::BYTES, *values = keys + 2 * L::BYTES;
+        bool dirty = false;
+        if (block_least < min(t * ROWS + ROWS, S.n_k) - 1) {      // some row of the workgroup does not see all of the tile's keys
+            look_through<T, D>(keys, &found, tid);
+            __syncthreads();
+            dirty = __builtin_amdgcn_readfirstlane(found) != 0;
+        }
+        const bool any = t * ROWS <= wave_most, masked = t * ROWS + ROWS - 1 > wave_least;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            v16f x = {}, y = {};
+            if (any) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    x = T::mfma(rows.read(keys, b, k), q[k], x);
+                    y = T::mfma(rows.read(values, b, k), go[k], y);
+                }
+            }
+            if (b == 1 && t + 1 < n_tiles) load(t + 1);      // behind the last ordinary read of LDS
+            if (!any) continue;
+            const int seen = limit - t * ROWS - b * 32 - 4 * h;
+            uint32_t z[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float d[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = i + j;
+                    d[j] = __builtin_amdgcn_exp2f(fmaf(x[r], A.c, -zero_at)) * fmaf(y[r], unit, -delta);
+                    if (masked && 8 * (r / 4) + r % 4 > seen) d[j] = 0.f;
+                }
+                z[i / 2] = T::pack(d[0], d[1]);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e)
+                    sums[e] = T::mfma(cleaned<T>(columns.read(keys, e, 2 * b + k), dirty), (v4u){z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]}, sums[e]);
+        }
+    }
+    store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows);
+}
+
+template <class T, int D> int launch(const GradArgs &A, hipStream_t stream)
+{
+    const long long deltas = (long long)((max(A.tokens_q, A.tokens_k) + 63) / 64) * (A.heads + A.kv_heads);
+    const long long keys = block_numbers(A.tokens_k, A.n_seqs, 1, BN) * A.kv_heads, queries = block_numbers(A.tokens_q, A.n_seqs, A.group, BN) * A.kv_heads;
+    if (deltas > 0x7fffffffll || keys > 0x7fffffffll || queries > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    hipLaunchKernelGGL((delta_kernel<T>), dim3((unsigned)deltas), dim3(256), 0, stream, A);
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)keys), dim3(64 * WAVES), 0, stream, A);
+    hipLaunchKernelGGL((queries_kernel<T, D>), dim3((unsigned)queries), dim3(64 * WAVES), 0, stream, A);
+    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
+
+size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
+size_t delta_bytes(const rb_heads *H, int tokens_q) { return rounded((size_t)tokens_q * H->heads * 4); }
+size_t most_bytes(int tokens, int heads) { return rounded((size_t)((tokens + 63) / 64) * heads * 4); }
+
+}  // namespace
+}  // namespace attn
+}  // namespace rb
+
+using namespace rb::attn;
+
+extern "C" size_t rb_attn_grad_workspace_bytes(const rb_heads *H, int tokens_q, int tokens_k)
+{
+    if (check_heads(H) != RB_OK || tokens_q < 1 || tokens_k < 1) return 0;
+    return delta_bytes(H, tokens_q) + most_bytes(tokens_q, H->heads) + most_bytes(tokens_k, H->kv_heads);
+}
+
+extern "C" int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, const int32_t *first_q,
+                                   const int32_t *first_k, int n_seqs, int tokens_q, int tokens_k, int causal, float scale, void *dq, void *dk, void *dv, void *workspace,
+                                   size_t workspace_bytes, void *stream)
+{
+    const int rc = check_heads(H);
+    if (rc != RB_OK) return rc;
+    if (!go || !q || !k || !v || !o || !lse || !first_q || !dq || !dk || !dv) return RB_ERR_NULL;
+    if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens_q < 1 || tokens_k < 1 || tokens_q > MAX_TOKENS || tokens_k > MAX_TOKENS || (!first_k && tokens_k != tokens_q)) return RB_ERR_SHAPE;
+    if (check_scale(scale) != RB_OK) return RB_ERR_VALUE;
+    for (const void *p : {go, q, k, v, o, (const void *)dq, (const void *)dk, (const void *)dv})
+        if ((uintptr_t)p & 15) return RB_ERR_ALIGN;
+    if (((uintptr_t)first_q | (uintptr_t)first_k | (uintptr_t)lse) & 3) return RB_ERR_ALIGN;
+    if (workspace_bytes < rb_attn_grad_workspace_bytes(H, tokens_q, tokens_k) || !workspace) return RB_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15) return RB_ERR_ALIGN;
+    GradArgs A = {};
+    A.q = side(q, H->q_token, H->q_head), A.k = side(k, H->k_token, H->k_head), A.v = side(v, H->v_token, H->v_head);
+    A.o = side(o, (long long)H->heads * H->dim, H->dim);
+    A.go = rb::address_of(go), A.lse = rb::address_of(lse), A.first_q = rb::address_of(first_q), A.first_k = rb::address_of(first_k ? first_k : first_q);
+    A.delta = rb::address_of(workspace);
+    A.most_o = A.delta + delta_bytes(H, tokens_q);
+    A.most_v = A.most_o + most_bytes(tokens_q, H->heads);
+    A.dq = rb::address_of(dq), A.dk = rb::address_of(dk), A.dv = rb::address_of(dv);
+    A.n_seqs = n_seqs, A.tokens_q = tokens_q, A.tokens_k = tokens_k;
+    A.heads = H->heads, A.kv_heads = H->kv_heads, A.group = H->heads / H->kv_heads, A.dim = H->dim, A.causal = causal != 0;
+    A.c = scale * LOG2E, A.scale = scale;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (H->dtype == RB_F16) return A.dim <= 64 ? launch<F16, 64>(A, st) : launch<F16, 128>(A, st);
+    return A.dim <= 64 ? launch<BF16, 64>(A, st) : launch<BF16, 128>(A, st);
+}

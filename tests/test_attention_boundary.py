@@ -49,6 +49,28 @@ def test_prompt_refusals():
         assert _prompt(**kw) == rb.RB_ERR_ALIGN, kw
 
 
+def _grad(H=None, go=0x100, q=0x200, k=0x300, v=0x400, o=0x500, lse=0x600, first=0x700, first_k=None, n=1, tq=8, tk=8, scale=0.1, dq=0x800, dk=0x900, dv=0xa00,
+          ws=0x1000, size=1 << 30):
+    return rb.lib.rb_attn_prompt_grad(H or _H(), go, q, k, v, o, lse, first, first_k, n, tq, tk, 1, scale, dq, dk, dv, ws, size, None)
+
+
+def test_gradient_refusals():
+    for kw, code in BAD_HEADS:
+        assert _grad(H=_H(**kw)) == code, kw
+    for name in ("go", "q", "k", "v", "o", "lse", "first", "dq", "dk", "dv"):
+        assert _grad(**{name: None}) == rb.RB_ERR_NULL, name
+    for kw in (dict(n=0), dict(tq=0, tk=0), dict(tk=9), dict(tk=0, first_k=0xb00), dict(tq=(1 << 24) + 1, tk=(1 << 24) + 1)):
+        assert _grad(**kw) == rb.RB_ERR_SHAPE, kw
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert _grad(scale=scale) == rb.RB_ERR_VALUE
+    for name in ("go", "q", "k", "v", "o", "dq", "dk", "dv"):
+        assert _grad(**{name: 0x108}) == rb.RB_ERR_ALIGN, name
+    assert _grad(lse=0x602) == rb.RB_ERR_ALIGN and _grad(first=0x701) == rb.RB_ERR_ALIGN and _grad(ws=0x1004) == rb.RB_ERR_ALIGN
+    need = rb.lib.rb_attn_grad_workspace_bytes(_H(), 8, 8)
+    assert need >= 8 * 4 * 4 and _grad(size=need - 1) == rb.RB_ERR_WORKSPACE and _grad(ws=None) == rb.RB_ERR_WORKSPACE
+    assert rb.lib.rb_attn_grad_workspace_bytes(None, 8, 8) == 0 and rb.lib.rb_attn_grad_workspace_bytes(_H(), 0, 8) == 0
+
+
 def _paged(C=None, q=0x100, qt=256, qh=64, heads=4, first=0x400, lengths=0x500, table=0x600, width=3, n=2, tokens=2, scale=0.1, o=0x700, ws=0x8000, size=1 << 40):
     return rb.lib.rb_attn_paged(C or _C(), q, qt, qh, heads, first, lengths, table, width, n, tokens, scale, o, ws, size, None)
 
