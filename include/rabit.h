@@ -402,7 +402,7 @@ int rb_add(const uint16_t *a, const uint16_t *b, uint16_t *y, size_t n, void *st
  * kv_heads of them one after the other (head h reads key head h / (heads /
  * kv_heads)); `dim` elements each, a multiple of 8 up to 128 (RB_ERR_UNSUPPORTED
  * above).  q is [token][head][dim] with strides of its own for token and head, in
- * elements, multiples of 8 and at most 2^25; elements of a head are contiguous.  k and v likewise.  o is
+ * elements, multiples of 8 and at most 2^23; elements of a head are contiguous.  k and v likewise.  o is
  * contiguous [tokens][heads][dim].  q, k, v, o are device memory of one dtype,
  * RB_F16 or RB_BF16, 16-byte aligned.  Scores, softmax and sums are fp32; the
  * softmax weights are rounded to dtype before they meet the values.

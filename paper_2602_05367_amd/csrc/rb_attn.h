@@ -83,17 +83,14 @@ __device__ __forceinline__ float over_halves_sum(float v)
 }
 
 // ------------------------------------------------------------------- tiles ---
-// A tile is ROWS rows of D elements (D = 64 or 128, a head's elements and zeros after them) in LDS,
-// 16-byte pieces of a row permuted so that 32 rows at one column and four rows at 32 columns both
-// touch every bank once: piece c of row r lies at c ^ spread(r).
-constexpr int ROWS = 64, WAVES = 4;
+// A tile is some rows of D elements (D = 64 or 128, a head's elements and zeros after them) in LDS, in groups of rows that
+// one load of a wavefront fills (1 KB), 16 bytes between groups, 16-byte pieces of a row permuted: piece c of row r lies at c ^ spread(r).  So 32
+// rows at one column and four rows at 32 columns both touch every bank once, and most of what varies in an address is a constant.
 template <int D> struct Tile {
-    static constexpr int ROW = D * 2, BYTES = ROWS * ROW, PIECES = D / 8;
-    static constexpr int ROWS_PER_LOAD = 1024 / ROW, LOADS = BYTES / 1024 / WAVES;     // a wavefront's load fills 1 KB
-    static __device__ __forceinline__ int spread(int r)
-    {
-        return D == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
-    }
+    static constexpr int ROW = D * 2, PIECES = D / 8, GROUP_ROWS = 1024 / ROW, GROUP = 1024 + 16;
+    static __device__ __forceinline__ int spread(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1; }
+    static constexpr int bytes(int rows) { return rows / GROUP_ROWS * GROUP; }
+    static __device__ __forceinline__ int row_at(int r) { return r / GROUP_ROWS * GROUP + r % GROUP_ROWS * ROW; }
 };
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
@@ -108,74 +105,86 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t *p, uint3
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, (int)bytes, 0x00020000);
 }
 
-// Where this lane's part of load i of a tile lies behind the first row of that load
-template <int D> __device__ __forceinline__ void lane_offsets(uint32_t (&at)[Tile<D>::LOADS], long long stride, int dim, int wave, int lane)
-{
+// W wavefronts load a tile: the rows of a wavefront are consecutive.  Where this lane's part of load i lies behind row `behind` of the wavefront's part
+// (0: behind the tile's first row)
+template <int D, int ROWS, int W> struct Part {
     using L = Tile<D>;
+    static constexpr int LOADS = ROWS / L::GROUP_ROWS / W;
+    uint32_t at[LOADS];
+    __device__ __forceinline__ Part(long long stride, int dim, int first_row, int lane)
+    {
+        const int r = lane / L::PIECES, c = (lane % L::PIECES) ^ L::spread(r);
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-        const int r = lane / L::PIECES, row = (wave * L::LOADS + i) * L::ROWS_PER_LOAD + r;
-        const int c = (lane % L::PIECES) ^ L::spread(row);
-        at[i] = c * 8 < dim ? (uint32_t)(r * stride) + c * 16 : NOWHERE;
+        for (int i = 0; i < LOADS; ++i) at[i] = c * 8 < dim ? (uint32_t)((first_row + i * L::GROUP_ROWS + r) * stride) + c * 16 : NOWHERE;
     }
-}
-// `rows` rows from `base` on into the rows of a load; rows <= 0: zeros
-__device__ __forceinline__ void load_rows(const uint8_t *base, long long stride, int rows, int most, int dim, uint32_t at, uint8_t *to)
+    // loads FROM .. FROM + N - 1 of the part, from a buffer
+    template <int FROM, int N> __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, uint8_t *tile, int wave) const
+    {
+#pragma unroll
+        for (int i = FROM; i < FROM + N; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(tile + (wave * LOADS + i) * L::GROUP), 16, (int)at[i], 0, 0, 0);
+    }
+};
+// `rows` rows of a head from `base` on, at most `most`; rows <= 0: nothing
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const uint8_t *base, long long stride, int rows, int most, int dim)
 {
     rows = min(rows, most);
-    const uint32_t bytes = rows <= 0 ? 0u : (uint32_t)((rows - 1) * (int)stride + dim * 2);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(base, bytes), (__attribute__((address_space(3))) void *)to, 16, (int)at, 0, 0, 0);
-}
-// rows first .. first + 63 of a sequence's `len` rows, strided in memory
-template <int D>
-__device__ __forceinline__ void load_tile(const uint8_t *base, long long stride, int first, int len, int dim, const uint32_t (&at)[Tile<D>::LOADS], uint8_t *tile, int wave)
-{
-    using L = Tile<D>;
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-        const int row = first + (wave * L::LOADS + i) * L::ROWS_PER_LOAD;
-        load_rows(base + row * stride, stride, len - row, L::ROWS_PER_LOAD, dim, at[i], tile + (wave * L::LOADS + i) * 1024);
-    }
+    return buffer(base, rows <= 0 ? 0u : (uint32_t)((rows - 1) * (int)stride + dim * 2));
 }
 
 // Reads of a tile as left operands.  Rows: row 32 b + lane % 32, elements 16 k + 8 (lane / 32) ..; columns:
 // element 32 b + lane % 32 of rows 16 k + the numbering above.
 template <int D> struct Rows {
-    uint32_t row;
-    int piece;
-    __device__ __forceinline__ Rows(int lane) : row((lane & 31) * Tile<D>::ROW), piece(((lane >> 5) ^ Tile<D>::spread(lane & 31)) * 16) {}
+    int row, piece;
+    __device__ __forceinline__ Rows(int lane) : row(Tile<D>::row_at(lane & 31)), piece(((lane >> 5) ^ Tile<D>::spread(lane & 31)) * 16) {}
     __device__ __forceinline__ v4u read(const uint8_t *tile, int b, int k) const
     {
-        return *(const lds_v4u *)(lds_byte *)(tile + row + (piece ^ (k * 32)) + b * (32 * Tile<D>::ROW));
+        constexpr int MOVED = D == 128 ? 192 : 96;      // bits of a piece's place that the permutation touches
+        return *(const lds_v4u *)(lds_byte *)(tile + (row + (piece ^ (k * 32 & MOVED))) + (k * 32 & ~MOVED) + 32 / Tile<D>::GROUP_ROWS * Tile<D>::GROUP * b);
     }
 };
 template <int D> struct Columns {
-    uint32_t row;
-    int piece[2];
+    int row, piece;
     __device__ __forceinline__ Columns(int lane)
     {
         const int h = lane >> 5, i = lane & 15, r = 4 * h + i / 4, c = (lane >> 4 & 1) * 2 + (i & 3) / 2;
-        row = r * Tile<D>::ROW + (i & 1) * 8;
-        piece[0] = (c ^ Tile<D>::spread(r)) * 16;
-        piece[1] = (c ^ Tile<D>::spread(r + 8)) * 16;
+        row = Tile<D>::row_at(r) + (i & 1) * 8;
+        piece = (c ^ Tile<D>::spread(r)) * 16;
     }
     __device__ __forceinline__ v4u read(const uint8_t *tile, int b, int k) const
     {
-        const uint8_t *p = tile + row + k * (16 * Tile<D>::ROW);
-        const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(lds_byte *)(p + (piece[0] ^ (b * 64)))));
-        const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(lds_byte *)(p + 8 * Tile<D>::ROW + (piece[1] ^ (b * 64)))));
+        constexpr int EIGHT = 8 / Tile<D>::GROUP_ROWS * Tile<D>::GROUP;      // the permutation is the same eight rows on
+        const uint8_t *p = tile + (row + (piece ^ (b * 64))) + 2 * EIGHT * k;
+        const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(lds_byte *)p));
+        const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(lds_byte *)(p + EIGHT)));
         return (v4u){lo.x, lo.y, hi.x, hi.y};
     }
 };
 
+// N matrix instructions, each with a left operand from LDS that is read AHEAD instructions before its use.  The order is held: left alone, the
+// compiler puts every read right before its use and waits for it (see the figures at the kernels).
+template <int N, int AHEAD, class Read, class Use> __device__ __forceinline__ void stream_operands(Read read, Use use)
+{
+    v4u held[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) held[i] = read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        use(i, held[i % AHEAD]);
+        if (i + AHEAD < N) held[i % AHEAD] = read(i + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // Infinities and NaN in places that a row does not see: weight zero times such a value would be NaN.  Tiles of which some row of the
 // workgroup sees only a part are looked through before use: what is not finite becomes zero, and `found` says that there was some.
-template <class T, int D> __device__ __forceinline__ void make_finite(uint8_t *tile, int *found, int tid)
+template <class T, int D, int ROWS, int W> __device__ __forceinline__ void make_finite(uint8_t *tile, int *found, int tid)
 {
     using L = Tile<D>;
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-        lds_v4u *at = (lds_v4u *)(lds_byte *)(tile + (i * (64 * WAVES) + tid) * 16);
+    for (int i = 0; i < ROWS / L::GROUP_ROWS / W; ++i) {
+        lds_v4u *at = (lds_v4u *)(lds_byte *)(tile + (i * W + (tid >> 6)) * L::GROUP + (tid & 63) * 16);
         const v4u w = *at;
         if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) {
             *found = 1;
@@ -200,8 +209,18 @@ template <class T, int D> __device__ __forceinline__ void add_not_finite(v16f (&
             }
         }
 }
-// the loads into LDS that this wavefront has asked for have arrived: a barrier alone does not wait for them
-__device__ __forceinline__ void loads_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// keeps a value's computation where it is written: the compiler would move it behind the next branch
+__device__ __forceinline__ void computed_here(float &v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void computed_here(uint32_t &v) { asm volatile("" : "+v"(v)); }
+// the loads into LDS that this wavefront has asked for have arrived, all but the last LEFT: a barrier alone does not wait for them
+template <int LEFT = 0> __device__ __forceinline__ void loads_arrived() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
+// the barrier alone: __syncthreads() would wait for all loads
+__device__ __forceinline__ void meet()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 // -------------------------------------------------------------------- work ---
 // Sequences are packed: sequence s has the tokens first[s] .. first[s + 1] - 1.  The rows of a key head are its queries, group after
@@ -237,11 +256,13 @@ struct Sequence {
 };
 __device__ __forceinline__ Sequence sequence_at(const int *first_q, const int *first_k, int s, int tokens_q, int tokens_k)
 {
+    // (the same in all lanes, which the compiler has to be told: an address that it takes to differ costs a loop over the lanes)
+    auto entry = [&](const int *first, int i) { return __builtin_amdgcn_readfirstlane(first[i]); };
     Sequence r;
-    r.q0 = min(max(first_q[s], 0), tokens_q);
-    r.n_q = min(max(first_q[s + 1], r.q0), tokens_q) - r.q0;
-    r.k0 = min(max(first_k[s], 0), tokens_k);
-    r.n_k = min(max(first_k[s + 1], r.k0), tokens_k) - r.k0;
+    r.q0 = min(max(entry(first_q, s), 0), tokens_q);
+    r.n_q = min(max(entry(first_q, s + 1), r.q0), tokens_q) - r.q0;
+    r.k0 = min(max(entry(first_k, s), 0), tokens_k);
+    r.n_k = min(max(entry(first_k, s + 1), r.k0), tokens_k) - r.k0;
     return r;
 }
 

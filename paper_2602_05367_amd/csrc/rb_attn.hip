@@ -1,7 +1,7 @@
 // Attention over packed prompts and over a paged cache: o_i = sum_j p_ij v_j with
 // p_ij = exp(c q_i . k_j - lse_i), lse_i = log sum_j exp(c q_i . k_j) over the keys j that row i sees.
 #include <hip/hip_runtime.h>
-#include <cmath>
+#include <type_traits>
 
 #include "rabit.h"
 #include "rb_attn.h"
@@ -10,6 +10,8 @@
 namespace rb {
 namespace attn {
 namespace {
+
+#define RB_INLINE __attribute__((always_inline))
 
 struct Args {
     Side q, k, v;
@@ -21,18 +23,22 @@ struct Args {
     float c;                                 // scale log2(e): the exponentials are powers of two
 };
 
-constexpr int BM = 32 * WAVES;
 // Weights are taken relative to a maximum that follows the scores only when they pass it by this many powers of two: the sums
 // are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
 constexpr float SLACK = 8.f;
 
-// One workgroup does BM rows of one key head, 32 per wavefront, over all keys that they see, 64 at a time: the next
-// tile of keys and values is on its way into LDS while one is used.
+// One workgroup does 128 rows of one key head, 32 per wavefront, over all keys that they see, KEYS at a time; the next tile of keys and values
+// is on its way into LDS while one is used.  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part (one long
+// prompt of 8192 tokens, 64 query and 8 key heads of 128, causal, bf16: 1.00 ms, 1.10 PFLOP/s).  What was tried beside it: 32 keys at a time and
+// three wavefronts per SIMD, the same on long prompts and a fifth slower on short ones; a pipeline within a wavefront, scores of one half of a tile
+// beside the weights of the other, 1.08 ms; eight wavefronts and three tiles ahead, 1.09 ms; operand reads left to the compiler, 1.11 ms.
+constexpr int WAVES = 4, BM = 32 * WAVES, KEYS = 64;
 template <class T, int D, bool PAGED>
 __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
 {
     using L = Tile<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * L::BYTES];       // keys, keys, values, values
+    // tiles as variables of their own: the compiler then knows that loads into one do not concern reads of another
+    __shared__ __attribute__((aligned(16))) uint8_t keys_a[L::bytes(KEYS)], values_a[L::bytes(KEYS)], keys_b[L::bytes(KEYS)], values_b[L::bytes(KEYS)];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -44,7 +50,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     Sequence S = sequence_at(first_q, PAGED ? first_q : first_k, s, A.tokens_q, PAGED ? A.tokens_q : A.tokens_k);
     if (PAGED) {
         S.k0 = 0;
-        S.n_k = min(max(first_k[s], 0), (int)min((long long)A.width << A.page_shift, 0x7fffffc0ll));
+        S.n_k = min(max(__builtin_amdgcn_readfirstlane(first_k[s]), 0), (int)min((long long)A.width << A.page_shift, 0x7fffffc0ll));
     }
     const int row0 = (block - block_start(first_q, s, A.group, BM)) * BM, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
@@ -58,7 +64,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     const int limit = A.causal ? ahead + token : S.n_k - 1;
     const int block_least = last_key(row0), block_most = last_key(row0 + BM - 1);
     const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32 + 31));
-    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + ROWS - 1) / ROWS;
+    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS;
 
     v4u q[D / 16];
     {
@@ -67,114 +73,105 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
         for (int k = 0; k < D / 16; ++k) q[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from + k * 32 + h * 16) : (v4u)(0u);
     }
 
-    uint32_t k_at[L::LOADS], v_at[L::LOADS];
-    lane_offsets<D>(k_at, A.k.token, A.dim, wave, lane);
-    lane_offsets<D>(v_at, A.v.token, A.dim, wave, lane);
+    // rows of a page are counted from the first that the wavefront needs, others from the tile's
+    constexpr int MINE = KEYS / WAVES, LOADS = Part<D, KEYS, WAVES>::LOADS;
+    const Part<D, KEYS, WAVES> k_part(A.k.token, A.dim, PAGED ? 0 : wave * MINE, lane), v_part(A.v.token, A.dim, PAGED ? 0 : wave * MINE, lane);
     const uint8_t *k_base = global_at<const uint8_t>(A.k.at) + S.k0 * A.k.token + kvh * A.k.head;
     const uint8_t *v_base = global_at<const uint8_t>(A.v.at) + S.k0 * A.v.token + kvh * A.v.head;
     const int *table = PAGED ? global_at<const int>(A.table) + (long long)s * A.width : nullptr;
-    int held = 0, held_at = -1;      // 64 entries of the page table, one per lane
-    auto row_at = [&](int r) {       // where row r's key lies behind the first page
-        const int page = __builtin_amdgcn_readlane(held, (r >> A.page_shift) & 63);
-        return page * A.page + (r & ((1 << A.page_shift) - 1)) * A.k.token;
+    auto place = [&](int page, int r) RB_INLINE {      // of row r, behind the first page
+        return min(max(page, 0), A.pages - 1) * A.page + (r & ((1 << A.page_shift) - 1)) * A.k.token;
     };
-    auto hold_pages = [&](int t) {
-        const int page0 = (t * ROWS) >> A.page_shift;
-        if (page0 >> 6 == held_at) return;
-        held_at = page0 >> 6;
-        held = min(max(table[min(held_at * 64 + lane, A.width - 1)], 0), A.pages - 1);
-    };
-    auto page_at = [&](int r) {      // the same, of a row whose page is held no longer
-        const int page = min(max(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), 0), A.pages - 1);
-        return page * A.page + (r & ((1 << A.page_shift) - 1)) * A.k.token;
-    };
-    auto load = [&](int t) {
-        uint8_t *to = lds + (t & 1) * L::BYTES;
-        if constexpr (!PAGED) {
-            load_tile<D>(k_base, A.k.token, t * ROWS, S.n_k, A.dim, k_at, to, wave);
-            load_tile<D>(v_base, A.v.token, t * ROWS, S.n_k, A.dim, v_at, to + 2 * L::BYTES, wave);
-        } else {
-            hold_pages(t);
+    // A wavefront's part of a tile lies in one page, or, 16 rows in pages of eight, in two.  Pages are asked for one step before the rows are.
+    constexpr int PARTS = MINE / 8, PART_LOADS = LOADS / PARTS;
+    const __attribute__((address_space(4))) int *pages_at = (const __attribute__((address_space(4))) int *)table;
+    int pages[PARTS] = {};
+    auto ask_pages = [&](int t) RB_INLINE {
 #pragma unroll
-            for (int i = 0; i < L::LOADS; ++i) {
-                const int part = wave * L::LOADS + i, r = t * ROWS + part * L::ROWS_PER_LOAD;
-                const long long at = row_at(r);
-                load_rows(k_base + at, A.k.token, S.n_k - r, L::ROWS_PER_LOAD, A.dim, k_at[i], to + part * 1024);
-                load_rows(v_base + at, A.v.token, S.n_k - r, L::ROWS_PER_LOAD, A.dim, v_at[i], to + 2 * L::BYTES + part * 1024);
-            }
+        for (int i = 0; i < PARTS; ++i) pages[i] = pages_at[min((t * KEYS + wave * MINE + i * 8) >> A.page_shift, A.width - 1)];
+    };
+    auto load_one = [&](int t, const uint8_t *base, long long stride, const Part<D, KEYS, WAVES> &part, uint8_t *tile) RB_INLINE {
+        if constexpr (!PAGED) {
+            part.template load<0, LOADS>(rows_buffer(base + (long long)t * KEYS * stride, stride, S.n_k - t * KEYS, KEYS, A.dim), tile, wave);
+        } else {
+            const int r = t * KEYS + wave * MINE;
+            part.template load<0, PART_LOADS>(rows_buffer(base + place(pages[0], r), stride, S.n_k - r, 8, A.dim), tile, wave);
+            if constexpr (PARTS == 2)      // (its offsets are eight rows on)
+                part.template load<PART_LOADS, PART_LOADS>(rows_buffer(base + place(pages[1], r + 8) - 8 * stride, stride, S.n_k - r, 16, A.dim), tile, wave);
         }
+    };
+    auto load = [&](int t, uint8_t *keys, uint8_t *values) RB_INLINE {
+        load_one(t, k_base, A.k.token, k_part, keys);
+        load_one(t, v_base, A.v.token, v_part, values);
+        if constexpr (PAGED) ask_pages(t + 1);
     };
 
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
-    v16f sums[D / 32] = {};
+    constexpr int B = D / 32, H = KEYS / 32;
+    v16f sums[B] = {};
     float top = RB_NEG_INF, total = 0.f;
-    if (tid == 0) found = 0;
-    if (n_tiles > 0) load(0);
-    for (int t = 0; t < n_tiles; ++t) {
+    auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) RB_INLINE {
         loads_arrived();
         __syncthreads();      // tile t is there, everybody has done with tile t - 1
-        uint8_t *keys = lds + (t & 1) * L::BYTES, *values = keys + 2 * L::BYTES;
-        const bool partly = block_least < min(t * ROWS + ROWS, S.n_k) - 1;      // some row of the workgroup does not see all of the tile's keys
-        if (partly) {
-            make_finite<T, D>(values, &found, tid);
+        if (t + 1 < n_tiles) load(t + 1, next_keys, next_values);
+        if (block_least < min(t * KEYS + KEYS, S.n_k) - 1) {      // some row of the workgroup does not see all of the tile's keys
+            make_finite<T, D, KEYS, WAVES>(values, &found, tid);
             __syncthreads();
         }
-        v16f x[2] = {};
-        if (t * ROWS <= wave_most) {
+        if (t * KEYS > wave_most) return;
+        v16f x[H] = {};
+        stream_operands<H * D / 16, 6>([&](int i) RB_INLINE { return rows.read(keys, i % H, i / H); }, [&](int i, v4u a) RB_INLINE { x[i % H] = T::mfma(a, q[i / H], x[i % H]); });
+        if (t * KEYS + KEYS - 1 > wave_least) {
+            const int seen = limit - t * KEYS - 4 * h;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
+            for (int b = 0; b < H; ++b)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) x[b] = T::mfma(rows.read(keys, b, k), q[k], x[b]);
+                for (int i = 0; i < 16; ++i)
+                    if (b * 32 + 8 * (i / 4) + i % 4 > seen) x[b][i] = RB_NEG_INF;
         }
-        // the next tile is asked for here, behind the last ordinary read of LDS: before such a read the compiler would wait for it
-        if (t + 1 < n_tiles) load(t + 1);
-        if (t * ROWS <= wave_most) {
-            if (t * ROWS + ROWS - 1 > wave_least) {
-                const int seen = limit - t * ROWS - 4 * h;
+        float most = x[0][0];
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+        for (int i = 1; i < 16 * H; ++i) most = fmaxf(most, x[i / 16][i % 16]);
+        most = over_halves_max(most) * A.c;
+        if (__ballot(most > top + SLACK)) {
+            const float now = fmaxf(top, most);
+            const float shrink = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            total *= shrink;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (b * 32 + 8 * (i / 4) + i % 4 > seen) x[b][i] = RB_NEG_INF;
-            }
-            float most = x[0][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) most = fmaxf(most, x[i / 16][i % 16]);
-            most = over_halves_max(most) * A.c;
-            if (__ballot(most > top + SLACK)) {
-                const float now = fmaxf(top, most);
-                const float shrink = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now);
-                top = now;
-                total *= shrink;
-#pragma unroll
-                for (int b = 0; b < D / 32; ++b) sums[b] *= shrink;
-            }
-            const float zero_at = (top == RB_NEG_INF ? 0.f : top) - T::BIAS;
-            v4u p[4];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float a = __builtin_amdgcn_exp2f(fmaf(x[b][i], A.c, -zero_at)), z = __builtin_amdgcn_exp2f(fmaf(x[b][i + 1], A.c, -zero_at));
-                    total += a + z;
-                    w[i / 2] = T::pack(a, z);
-                }
-                p[2 * b] = (v4u){w[0], w[1], w[2], w[3]};
-                p[2 * b + 1] = (v4u){w[4], w[5], w[6], w[7]};
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int b = 0; b < D / 32; ++b) sums[b] = T::mfma(columns.read(values, b, k), p[k], sums[b]);
+            for (int b = 0; b < B; ++b) sums[b] *= shrink;
         }
+        const float zero_at = (top == RB_NEG_INF ? 0.f : top) - T::BIAS;
+        v4u p[2 * H];
+#pragma unroll
+        for (int b = 0; b < H; ++b) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = __builtin_amdgcn_exp2f(fmaf(x[b][i], A.c, -zero_at)), z = __builtin_amdgcn_exp2f(fmaf(x[b][i + 1], A.c, -zero_at));
+                total += a + z;
+                w[i / 2] = T::pack(a, z);
+            }
+            p[2 * b] = (v4u){w[0], w[1], w[2], w[3]};
+            p[2 * b + 1] = (v4u){w[4], w[5], w[6], w[7]};
+        }
+        stream_operands<2 * H * B, 4>([&](int i) RB_INLINE { return columns.read(values, i % B, i / B); }, [&](int i, v4u a) RB_INLINE { sums[i % B] = T::mfma(a, p[i / B], sums[i % B]); });
+    };
+    if (tid == 0) found = 0;
+    if (n_tiles > 0) {
+        if constexpr (PAGED) ask_pages(0);
+        load(0, keys_a, values_a);
+    }
+    for (int t = 0; t < n_tiles; t += 2) {
+        step(t, keys_a, values_a, keys_b, values_b);
+        if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
 
     __syncthreads();
     if (__builtin_amdgcn_readfirstlane(found))
-        for (int r = max(block_least + 1, 0) / ROWS * ROWS; r <= wave_most; ++r)
-            add_not_finite<T, D>(sums, v_base + (PAGED ? page_at(r) : r * A.v.token), A.dim, h, r <= limit);
+        for (int r = max(block_least + 1, 0) / KEYS * KEYS; r <= wave_most; ++r)
+            add_not_finite<T, D>(sums, v_base + (PAGED ? place(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), r) : r * A.v.token), A.dim, h, r <= limit);
 
     total = over_halves_sum(total);
     const bool empty = limit < 0;

@@ -18,6 +18,8 @@ namespace rb {
 namespace attn {
 namespace {
 
+constexpr int WAVES = 4, ROWS = 64;
+
 struct GradArgs {
     Side q, k, v, o;                    // o: strides of the contiguous o, do and dq
     Address go, lse, first_q, first_k;
@@ -89,8 +91,8 @@ template <class T, int D> __device__ __forceinline__ void look_through(const uin
 {
     using L = Tile<D>;
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-        const v4u w = *(const lds_v4u *)(lds_byte *)(tile + (i * (64 * WAVES) + tid) * 16);
+    for (int i = 0; i < ROWS / L::GROUP_ROWS / WAVES; ++i) {
+        const v4u w = *(const lds_v4u *)(lds_byte *)(tile + (i * WAVES + (tid >> 6)) * L::GROUP + (tid & 63) * 16);
         if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) *found = 1;
     }
 }
@@ -123,9 +125,9 @@ template <class T, int D>
 __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(const GradArgs A)
 {
     using L = Tile<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * L::BYTES];       // queries, queries, do, do
+    __shared__ __attribute__((aligned(1024))) uint8_t queries_a[L::bytes(ROWS)], outs_a[L::bytes(ROWS)], queries_b[L::bytes(ROWS)], outs_b[L::bytes(ROWS)];
     // what the rows' sums of products start from: -lse in units of the scores, -delta
-    __shared__ __attribute__((aligned(16))) float rows_of[2][2][ROWS];
+    __shared__ __attribute__((aligned(16))) float rows_a[2][ROWS], rows_b[2][ROWS];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -154,40 +156,37 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(cons
         unit = scale_for(most_of(global_at<const float>(A.most_o), A.heads, kvh * A.group, A.group, S.q0, S.n_q, lane),
                          most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
 
-    uint32_t q_at[L::LOADS], o_at[L::LOADS];
-    lane_offsets<D>(q_at, A.q.token, A.dim, wave, lane);
-    lane_offsets<D>(o_at, A.o.token, A.dim, wave, lane);
+    const Part<D, ROWS, WAVES> q_part(A.q.token, A.dim, wave * (ROWS / WAVES), lane), o_part(A.o.token, A.dim, wave * (ROWS / WAVES), lane);
     const int tile0 = A.causal ? max(key0 - ahead, 0) / ROWS : 0, tiles = (S.n_q + ROWS - 1) / ROWS - tile0;
     const int steps = __builtin_amdgcn_readfirstlane(tiles > 0 ? tiles * A.group : 0);
     float next_lse = 0.f, next_delta = 0.f;      // of one row of the next tile, in the first wavefront
-    auto load = [&](int n) {
+    auto load = [&](int n, uint8_t *queries, uint8_t *outs) {
         const int g = n / tiles, t = tile0 + n % tiles, head = kvh * A.group + g;
         if (wave == 0) {
-            const int row = t * ROWS + lane;
-            const long long at = (long long)(S.q0 + min(row, S.n_q - 1)) * A.heads + head;
-            // a row past the end: no weight (do is zero there as well)
-            next_lse = row < S.n_q ? T::GRAD_BIAS / A.c - global_at<const float>(A.lse)[at] / A.scale : RB_NEG_INF;
-            next_delta = row < S.n_q ? -global_at<const float>(A.delta)[at] : 0.f;
+            const long long at = (long long)(S.q0 + min(t * ROWS + lane, S.n_q - 1)) * A.heads + head;
+            next_lse = global_at<const float>(A.lse)[at];
+            next_delta = global_at<const float>(A.delta)[at];
         }
-        uint8_t *to = lds + (n & 1) * L::BYTES;
-        load_tile<D>(global_at<const uint8_t>(A.q.at) + S.q0 * A.q.token + head * A.q.head, A.q.token, t * ROWS, S.n_q, A.dim, q_at, to, wave);
-        load_tile<D>(global_at<const uint8_t>(A.go) + S.q0 * A.o.token + head * A.o.head, A.o.token, t * ROWS, S.n_q, A.dim, o_at, to + 2 * L::BYTES, wave);
+        const uint8_t *q_from = global_at<const uint8_t>(A.q.at) + (long long)(S.q0 + t * ROWS) * A.q.token + head * A.q.head;
+        const uint8_t *o_from = global_at<const uint8_t>(A.go) + (long long)(S.q0 + t * ROWS) * A.o.token + head * A.o.head;
+        q_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(q_from, A.q.token, S.n_q - t * ROWS, ROWS, A.dim), queries, wave);
+        o_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(o_from, A.o.token, S.n_q - t * ROWS, ROWS, A.dim), outs, wave);
     };
 
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
     v16f sums_k[D / 32] = {}, sums_v[D / 32] = {};
     if (tid == 0) found = 0;
-    if (steps > 0) load(0);
-    for (int n = 0; n < steps; ++n) {
+    auto step = [&](int n, uint8_t *queries, uint8_t *outs, float (&rows_of)[2][ROWS], uint8_t *next_queries, uint8_t *next_outs) {
         const int t = tile0 + n % tiles;
         if (wave == 0) {
-            rows_of[n & 1][0][lane] = next_lse;
-            rows_of[n & 1][1][lane] = next_delta;
+            // a row past the end: no weight (do is zero there as well)
+            rows_of[0][lane] = t * ROWS + lane < S.n_q ? T::GRAD_BIAS / A.c - next_lse / A.scale : RB_NEG_INF;
+            rows_of[1][lane] = -next_delta;
         }
         loads_arrived();
         __syncthreads();
-        const uint8_t *queries = lds + (n & 1) * L::BYTES, *outs = queries + 2 * L::BYTES;
+        if (n + 1 < steps) load(n + 1, next_queries, next_outs);
         const bool partly = A.causal && block_last > ahead + t * ROWS;      // some key of the workgroup is not seen by all rows
         bool dirty = false;
         if (partly) {
@@ -204,16 +203,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(cons
             if (any) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    x[i] = rows_of[n & 1][0][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
-                    y[i] = rows_of[n & 1][1][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
+                    x[i] = rows_of[0][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
+                    y[i] = rows_of[1][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
                 }
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    x = T::mfma(rows.read(queries, b, k), kk[k], x);
-                    y = T::mfma(rows.read(outs, b, k), vv[k], y);
-                }
+stream_operands<D / 8, 4>([&](int i) { return rows.read(i % 2 ? outs : queries, b, i / 2); },
+                                          [&](int i, v4u a) {
+                                              if (i % 2)
+                                                  y = T::mfma(a, vv[i / 2], y);
+                                              else
+                                                  x = T::mfma(a, kk[i / 2], x);
+                                          });
             }
-            if (b == 1 && n + 1 < steps) load(n + 1);      // behind the last ordinary read of LDS
             if (!any) continue;
             const int least = my_key - ahead - t * ROWS - b * 32 - 4 * h;      // the first row that sees this key
             uint32_t w[8], z[8];
@@ -230,14 +230,22 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(cons
                 w[i / 2] = T::pack(p[0], p[1]);
                 z[i / 2] = T::pack(d[0], d[1]);
             }
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e) {
-                    sums_v[e] = T::mfma(cleaned<T>(columns.read(outs, e, 2 * b + k), dirty), (v4u){w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]}, sums_v[e]);
-                    sums_k[e] = T::mfma(cleaned<T>(columns.read(queries, e, 2 * b + k), dirty), (v4u){z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]}, sums_k[e]);
-                }
+constexpr int E = D / 32;
+            const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
+            stream_operands<4 * E, 4>([&](int i) { return columns.read(i % 2 ? queries : outs, i / 2 % E, 2 * b + i / (2 * E)); },
+                                      [&](int i, v4u a) {
+                                          const int e = i / 2 % E, k = i / (2 * E);
+                                          if (i % 2)
+                                              sums_k[e] = T::mfma(cleaned<T>(a, dirty), dz[k], sums_k[e]);
+                                          else
+                                              sums_v[e] = T::mfma(cleaned<T>(a, dirty), pw[k], sums_v[e]);
+                                      });
         }
+    };
+    if (steps > 0) load(0, queries_a, outs_a);
+    for (int n = 0; n < steps; n += 2) {
+        step(n, queries_a, outs_a, rows_a, queries_b, outs_b);
+        if (n + 1 < steps) step(n + 1, queries_b, outs_b, rows_b, queries_a, outs_a);
     }
     __syncthreads();
     if (__builtin_amdgcn_readfirstlane(found))      // (only the rows of tiles that were cleaned, and their keys see it)
@@ -257,7 +265,7 @@ template <class T, int D>
 __global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A)
 {
     using L = Tile<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * L::BYTES];       // keys, keys, values, values
+    __shared__ __attribute__((aligned(1024))) uint8_t keys_a[L::bytes(ROWS)], values_a[L::bytes(ROWS)], keys_b[L::bytes(ROWS)], values_b[L::bytes(ROWS)];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -304,26 +312,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A
     const long long stat = (long long)(S.q0 + token) * A.heads + head;
     const float zero_at = global_at<const float>(A.lse)[stat] * LOG2E - T::GRAD_BIAS, delta = global_at<const float>(A.delta)[stat] * unit;
 
-    uint32_t k_at[L::LOADS], v_at[L::LOADS];
-    lane_offsets<D>(k_at, A.k.token, A.dim, wave, lane);
-    lane_offsets<D>(v_at, A.v.token, A.dim, wave, lane);
+    const Part<D, ROWS, WAVES> k_part(A.k.token, A.dim, wave * (ROWS / WAVES), lane), v_part(A.v.token, A.dim, wave * (ROWS / WAVES), lane);
     const uint8_t *k_base = global_at<const uint8_t>(A.k.at) + S.k0 * A.k.token + kvh * A.k.head;
     const uint8_t *v_base = global_at<const uint8_t>(A.v.at) + S.k0 * A.v.token + kvh * A.v.head;
-    auto load = [&](int t) {
-        uint8_t *to = lds + (t & 1) * L::BYTES;
-        load_tile<D>(k_base, A.k.token, t * ROWS, S.n_k, A.dim, k_at, to, wave);
-        load_tile<D>(v_base, A.v.token, t * ROWS, S.n_k, A.dim, v_at, to + 2 * L::BYTES, wave);
+    auto load = [&](int t, uint8_t *keys, uint8_t *values) {
+        k_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(k_base + (long long)t * ROWS * A.k.token, A.k.token, S.n_k - t * ROWS, ROWS, A.dim), keys, wave);
+        v_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(v_base + (long long)t * ROWS * A.v.token, A.v.token, S.n_k - t * ROWS, ROWS, A.dim), values, wave);
     };
 
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
     v16f sums[D / 32] = {};
     if (tid == 0) found = 0;
-    if (n_tiles > 0) load(0);
-    for (int t = 0; t < n_tiles; ++t) {
+    auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) {
         loads_arrived();
         __syncthreads();
-        const uint8_t *keys = lds + (t & 1) * L::BYTES, *values = keys + 2 * L::BYTES;
+        if (t + 1 < n_tiles) load(t + 1, next_keys, next_values);
         bool dirty = false;
         if (block_least < min(t * ROWS + ROWS, S.n_k) - 1) {      // some row of the workgroup does not see all of the tile's keys
             look_through<T, D>(keys, &found, tid);
@@ -335,13 +339,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A
         for (int b = 0; b < 2; ++b) {
             v16f x = {}, y = {};
             if (any) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    x = T::mfma(rows.read(keys, b, k), q[k], x);
-                    y = T::mfma(rows.read(values, b, k), go[k], y);
-                }
+stream_operands<D / 8, 4>([&](int i) { return rows.read(i % 2 ? values : keys, b, i / 2); },
+                                          [&](int i, v4u a) {
+                                              if (i % 2)
+                                                  y = T::mfma(a, go[i / 2], y);
+                                              else
+                                                  x = T::mfma(a, q[i / 2], x);
+                                          });
             }
-            if (b == 1 && t + 1 < n_tiles) load(t + 1);      // behind the last ordinary read of LDS
             if (!any) continue;
             const int seen = limit - t * ROWS - b * 32 - 4 * h;
             uint32_t z[8];
@@ -356,12 +361,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A
                 }
                 z[i / 2] = T::pack(d[0], d[1]);
             }
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e)
-                    sums[e] = T::mfma(cleaned<T>(columns.read(keys, e, 2 * b + k), dirty), (v4u){z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]}, sums[e]);
+constexpr int E = D / 32;
+            const v4u dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
+            stream_operands<2 * E, 4>([&](int i) { return columns.read(keys, i % E, 2 * b + i / E); },
+                                      [&](int i, v4u a) { sums[i % E] = T::mfma(cleaned<T>(a, dirty), dz[i / E], sums[i % E]); });
         }
+    };
+    if (n_tiles > 0) load(0, keys_a, values_a);
+    for (int t = 0; t < n_tiles; t += 2) {
+        step(t, keys_a, values_a, keys_b, values_b);
+        if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
     store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows);
 }

@@ -8,8 +8,8 @@
 namespace rb {
 namespace attn {
 
-// rows of a load are addressed by 32 bits, everything above them by 64
-constexpr long long MAX_STRIDE = 1ll << 25, MAX_PAGE_STRIDE = 1ll << 40;
+// the 64 rows of a tile are addressed by 32 bits, everything above them by 64
+constexpr long long MAX_STRIDE = 1ll << 23, MAX_PAGE_STRIDE = 1ll << 40;
 // products of a token and a group, and the positions of a cache, stay within 31 bits
 constexpr int MAX_SEQS = 1 << 20, MAX_TOKENS = 1 << 24, MAX_PAGE = 1 << 16;
 
