@@ -32,6 +32,7 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 #define RB_NEG_INF (-__builtin_inff())
+#define RB_INLINE __attribute__((always_inline))
 
 // Weights are rounded to the inputs' type before they meet the values, each on its own and to
 // nearest: one rounding of relative size 2^-11 (2^-8) per weight, which averages out over a row to what
@@ -68,6 +69,11 @@ template <class T> __device__ __forceinline__ uint32_t finite_part(uint32_t w)
 {
     constexpr uint32_t E = T::EXPONENT;
     return ((w & E) == E ? 0 : w & 0xffffu) | (((w >> 16) & E) == E ? 0 : w & 0xffff0000u);
+}
+
+template <class T> __device__ __forceinline__ v4u finite_part(v4u w)
+{
+    return (v4u){finite_part<T>(w.x), finite_part<T>(w.y), finite_part<T>(w.z), finite_part<T>(w.w)};
 }
 
 // the sum or maximum of a lane's value and that of the lane 32 away, in both
@@ -188,7 +194,7 @@ template <class T, int D, int ROWS, int W> __device__ __forceinline__ void make_
         const v4u w = *at;
         if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) {
             *found = 1;
-            *at = (v4u){finite_part<T>(w.x), finite_part<T>(w.y), finite_part<T>(w.z), finite_part<T>(w.w)};
+            *at = finite_part<T>(w);
         }
     }
 }
@@ -209,9 +215,20 @@ template <class T, int D> __device__ __forceinline__ void add_not_finite(v16f (&
             }
         }
 }
-// keeps a value's computation where it is written: the compiler would move it behind the next branch
-__device__ __forceinline__ void computed_here(float &v) { asm volatile("" : "+v"(v)); }
-__device__ __forceinline__ void computed_here(uint32_t &v) { asm volatile("" : "+v"(v)); }
+// sums [element][column], element 32 b + 8 (i / 4) + 4 h + i % 4, as a row of 16-bit values per column; `empty`: zeros whatever they are
+template <class T, int D> __device__ __forceinline__ void store_columns(const v16f (&sums)[D / 32], float scale, uint8_t *to, int dim, int h, bool real, bool empty)
+{
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            // elements 0-3 and 8-11 of a run of 16 are in the lower half, the others in the upper: exchanged, each half stores eight in a row
+            const auto lo = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i] * scale, sums[b][i + 1] * scale), T::pack(sums[b][i + 4] * scale, sums[b][i + 5] * scale), false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i + 2] * scale, sums[b][i + 3] * scale), T::pack(sums[b][i + 6] * scale, sums[b][i + 7] * scale), false, false);
+            const int e = b * 32 + i * 2 + h * 8;
+            if (real && e < dim) *(v4u *)(to + e * 2) = empty ? (v4u)(0u) : (v4u){lo[0], hi[0], lo[1], hi[1]};
+        }
+}
 // the loads into LDS that this wavefront has asked for have arrived, all but the last LEFT: a barrier alone does not wait for them
 template <int LEFT = 0> __device__ __forceinline__ void loads_arrived() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 // the barrier alone: __syncthreads() would wait for all loads
@@ -271,6 +288,20 @@ struct Side {
     Address at;
     long long token, head;
 };
+struct Args {
+    Side q, k, v;
+    Address o, lse, first_q, first_k;        // paged: first_k holds the sequences' lengths
+    Address table;
+    long long page;
+    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
+    int page_shift, pages, width;
+    float c;                                 // scale log2(e): the exponentials are powers of two
+};
+
+
+// Weights are taken relative to a maximum that follows the scores only when they pass it by this many powers of two: the sums
+// are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
+constexpr float SLACK = 8.f;
 
 }  // namespace attn
 }  // namespace rb

@@ -6,26 +6,11 @@
 #include "rabit.h"
 #include "rb_attn.h"
 #include "rb_attn_host.h"
+#include "rb_internal.h"
 
 namespace rb {
 namespace attn {
 namespace {
-
-#define RB_INLINE __attribute__((always_inline))
-
-struct Args {
-    Side q, k, v;
-    Address o, lse, first_q, first_k;        // paged: first_k holds the sequences' lengths
-    Address table;
-    long long page;
-    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
-    int page_shift, pages, width;
-    float c;                                 // scale log2(e): the exponentials are powers of two
-};
-
-// Weights are taken relative to a maximum that follows the scores only when they pass it by this many powers of two: the sums
-// are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
-constexpr float SLACK = 8.f;
 
 // One workgroup does 128 rows of one key head, 32 per wavefront, over all keys that they see, KEYS at a time; the next tile of keys and values
 // is on its way into LDS while one is used.  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part (one long
@@ -177,18 +162,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     const bool empty = limit < 0;
     if (A.lse && real && h == 0)
         global_at<float>(A.lse)[(long long)(S.q0 + token) * A.heads + head] = empty ? RB_NEG_INF : (top - T::BIAS + __builtin_amdgcn_logf(total)) * LN2;
-    const float norm = empty ? 0.f : 1.f / total;
     uint8_t *to = global_at<uint8_t>(A.o) + ((long long)(S.q0 + token) * A.heads + head) * (A.dim * 2);
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 8) {
-            // elements 0-3 and 8-11 of a run of 16 are in the lower half, the others in the upper: exchanged, each half stores eight in a row
-            const auto lo = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i] * norm, sums[b][i + 1] * norm), T::pack(sums[b][i + 4] * norm, sums[b][i + 5] * norm), false, false);
-            const auto hi = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i + 2] * norm, sums[b][i + 3] * norm), T::pack(sums[b][i + 6] * norm, sums[b][i + 7] * norm), false, false);
-            const int e = b * 32 + i * 2 + h * 8;
-            if (real && e < A.dim) *(v4u *)(to + e * 2) = empty ? (v4u)(0u) : (v4u){lo[0], hi[0], lo[1], hi[1]};
-        }
+    store_columns<T, D>(sums, empty ? 0.f : 1.f / total, to, A.dim, h, real, empty);
 }
 
 template <class T, bool PAGED> int launch(const Args &A, hipStream_t stream)
@@ -250,7 +225,7 @@ extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, c
 extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
 {
     if (check_cache(C) != RB_OK || heads < 1 || heads % C->kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
-    return 0;
+    return few_applies(tokens, n_seqs, heads / C->kv_heads) ? few_workspace_bytes(C->kv_heads, C->dim, rb::mx::device_groups()) : 0;
 }
 
 extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
@@ -276,5 +251,6 @@ extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token
     A.heads = heads, A.kv_heads = C->kv_heads, A.group = heads / C->kv_heads, A.dim = C->dim, A.causal = 1;
     A.c = scale * LOG2E;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (few_applies(tokens, n_seqs, A.group)) return launch_few(A, C->dtype, rb::mx::device_groups(), workspace, st);
     return C->dtype == RB_F16 ? launch<F16, true>(A, st) : launch<BF16, true>(A, st);
 }

@@ -1,0 +1,394 @@
+// Attention of few new tokens per sequence over a paged cache (a decoding batch, drafts to verify): the time is that of reading the cache once.
+//
+// A job is up to 32 rows (tokens times the heads of a group) of one sequence and key head; its work is a row of tiles of 32 keys.  The tiles of
+// all jobs of a key head, one after the other, are cut into equal shares, one per wavefront, wherever that falls: contexts of any mix of lengths load every
+// compute unit alike.  A wavefront keeps two tiles of keys and values on their way into LDS of its own, across jobs, and meets nobody.  What it has
+// of a job that it does not have all of goes to the workspace, unnormalised, and a second launch joins the parts in a fixed order.
+#include <hip/hip_runtime.h>
+
+#include "rabit.h"
+#include "rb_attn.h"
+#include "rb_attn_host.h"
+
+namespace rb {
+namespace attn {
+namespace {
+
+constexpr int KEYS = 32, JOB = 32, WAVES = 4;
+
+// Where the work of a sequence lies among all tiles of a key head
+struct Shape {
+    int rows, blocks, tiles;
+    __device__ __forceinline__ long long count() const { return (long long)blocks * tiles; }
+};
+__device__ __forceinline__ int positions(int length, int width, int page_shift)
+{
+    return min(max(length, 0), (int)min((long long)width << page_shift, 0x7fffffc0ll));
+}
+__device__ __forceinline__ Shape shape_of(const Args &A, int q0, int q1, int length)
+{
+    q0 = min(max(q0, 0), A.tokens_q);
+    q1 = min(max(q1, q0), A.tokens_q);
+    const int rows = (q1 - q0) * A.group;
+    // a sequence that has rows but no positions: one tile, of which they see nothing
+    return {rows, (rows + JOB - 1) / JOB, rows ? max((positions(length, A.width, A.page_shift) + KEYS - 1) / KEYS, 1) : 0};
+}
+// Sums over the sequences, 64 at a time.  total(): all tiles; locate(at): the sequence that has tile `at` (at < total), which becomes the tile among its own
+struct Sums {
+    const Args &A;
+    const int *first, *lengths;
+    int lane;
+    __device__ __forceinline__ long long count(int s) const { return s < A.n_seqs ? shape_of(A, first[s], first[s + 1], lengths[s]).count() : 0; }
+    static __device__ __forceinline__ long long from_lane(long long v, int from)
+    {
+        return (long long)(unsigned)__shfl((int)v, from) | (long long)__shfl((int)(v >> 32), from) << 32;
+    }
+    static __device__ __forceinline__ long long up_to_lane(long long v, int lane)
+    {
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long u = from_lane(v, max(lane - d, 0));
+            if (lane >= d) v += u;
+        }
+        return v;
+    }
+    // the tiles before sequence `end`
+    __device__ __forceinline__ long long before(int end) const
+    {
+        long long sum = 0;
+        for (int s = lane; s < end; s += 64) sum += count(s);
+        return from_lane(up_to_lane(sum, lane), 63);
+    }
+    __device__ __forceinline__ int locate(long long &at) const
+    {
+        for (int s = 0; s < A.n_seqs; s += 64) {
+            const long long upto = up_to_lane(count(s + lane), lane), here = from_lane(upto, 63);
+            if (at < here) {
+                const int l = __popcll(__ballot(upto <= at));
+                if (l) at -= from_lane(upto, l - 1);
+                return s + l;
+            }
+            at -= here;
+        }
+        return A.n_seqs;
+    }
+};
+// share w of `all` tiles in `shares`, of which there are never more than tiles: no share is empty
+__device__ __forceinline__ int shares_of(long long all, int wavefronts) { return (int)min((long long)wavefronts, max(all, 1ll)); }
+__device__ __forceinline__ long long share_start(long long all, int w, int shares) { return all * w / shares; }
+
+// a part of a job in the workspace: the maxima and sums of its rows, then a row of D each
+template <int D> struct PartOfJob {
+    static constexpr size_t FLOATS = JOB * (2 + D);
+    float *at;
+    __device__ __forceinline__ PartOfJob(Address workspace, int kvh, int wavefronts, int w, int which) : at(global_at<float>(workspace) + (((size_t)kvh * wavefronts + w) * 2 + which) * FLOATS) {}
+    __device__ __forceinline__ float *top(int row) const { return at + row; }
+    __device__ __forceinline__ float *total(int row) const { return at + JOB + row; }
+    __device__ __forceinline__ float *row(int row) const { return at + 2 * JOB + row * D; }
+};
+
+// a position in the row of tiles
+struct Cursor {
+    int s, block, t;
+    Shape shape;
+    int n_k;
+};
+
+template <class T, int D>
+__global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A, Address workspace)
+{
+    using L = Tile<D>;
+    __shared__ __attribute__((aligned(16))) uint8_t keys_a[WAVES * L::bytes(KEYS)], values_a[WAVES * L::bytes(KEYS)], keys_b[WAVES * L::bytes(KEYS)], values_b[WAVES * L::bytes(KEYS)];
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % A.kv_heads, wavefronts = (int)(gridDim.x / A.kv_heads) * WAVES, w = (int)(blockIdx.x / A.kv_heads) * WAVES + wave;
+    const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
+    typedef const __attribute__((address_space(4))) int *Uniform;
+    const Uniform first_u = (Uniform)first, lengths_u = (Uniform)lengths, table_u = (Uniform)global_at<const int>(A.table);
+    const Sums sums_of = {A, first, lengths, lane};
+    const long long all = sums_of.before(A.n_seqs);
+    const int shares = __builtin_amdgcn_readfirstlane(shares_of(all, wavefronts));
+    if (w >= shares) return;
+    long long begin = share_start(all, w, shares);
+    const int n = __builtin_amdgcn_readfirstlane((int)(share_start(all, w + 1, shares) - begin));
+    if (n <= 0) return;
+
+    auto visit = [&](Cursor &c) RB_INLINE {      // sequence c.s, or nothing behind the last
+        if (c.s >= A.n_seqs) {
+            c.shape = {0, 1, 0x7fffffff};
+            c.n_k = 0;
+            return;
+        }
+        c.shape = shape_of(A, first_u[c.s], first_u[c.s + 1], lengths_u[c.s]);
+        c.n_k = positions(lengths_u[c.s], A.width, A.page_shift);
+    };
+    auto advance = [&](Cursor &c) RB_INLINE {
+        if (++c.t < c.shape.tiles) return;
+        c.t = 0;
+        if (++c.block < c.shape.blocks) return;
+        c.block = 0;
+        do {
+            ++c.s;
+            visit(c);
+        } while (c.shape.blocks == 0);
+    };
+    Cursor at = {}, ahead = {};      // the tile at hand, and the next to be asked for
+    at.s = __builtin_amdgcn_readfirstlane(sums_of.locate(begin));
+    if (at.s >= A.n_seqs) return;
+    visit(at);
+    at.block = __builtin_amdgcn_readfirstlane((int)(begin / at.shape.tiles));
+    at.t = __builtin_amdgcn_readfirstlane((int)(begin % at.shape.tiles));
+    ahead = at;
+
+    constexpr int LOADS = Part<D, KEYS, 1>::LOADS;
+    const Part<D, KEYS, 1> part(A.k.token, A.dim, 0, lane);
+    const uint8_t *k_base = global_at<const uint8_t>(A.k.at) + kvh * A.k.head, *v_base = global_at<const uint8_t>(A.v.at) + kvh * A.v.head;
+    auto place = [&](int page, int r) RB_INLINE { return min(max(page, 0), A.pages - 1) * A.page + (r & ((1 << A.page_shift) - 1)) * A.k.token; };
+    int pages[4] = {};      // of the tile to be asked for next
+    auto ask_pages = [&](const Cursor &c) RB_INLINE {
+        const Uniform row = table_u + (long long)min(c.s, A.n_seqs - 1) * A.width;
+        if (A.page_shift >= 5) {
+            pages[0] = row[min((c.t * KEYS) >> A.page_shift, A.width - 1)];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pages[i] = row[min((c.t * KEYS + i * 8) >> A.page_shift, A.width - 1)];
+        }
+    };
+    // tile number i of the share, which `ahead` stands at; past the share's end loads count, but fetch nothing
+    auto load = [&](int i, const uint8_t *base, uint8_t *tile) RB_INLINE {
+        const int r = ahead.t * KEYS, len = i < n ? ahead.n_k - r : 0;
+        if (A.page_shift >= 5) {
+            part.template load<0, LOADS>(rows_buffer(base + place(pages[0], r), A.k.token, len, KEYS, A.dim), tile, 0);
+        } else {
+            constexpr int P = LOADS / 4;      // a load's offsets count from the tile's first row
+            part.template load<0, P>(rows_buffer(base + place(pages[0], r), A.k.token, len, 8, A.dim), tile, 0);
+            part.template load<P, P>(rows_buffer(base + place(pages[1], r + 8) - 8 * A.k.token, A.k.token, len, 16, A.dim), tile, 0);
+            part.template load<2 * P, P>(rows_buffer(base + place(pages[2], r + 16) - 16 * A.k.token, A.k.token, len, 24, A.dim), tile, 0);
+            part.template load<3 * P, P>(rows_buffer(base + place(pages[3], r + 24) - 24 * A.k.token, A.k.token, len, 32, A.dim), tile, 0);
+        }
+    };
+    auto next_ahead = [&]() RB_INLINE {
+        advance(ahead);
+        ask_pages(ahead);
+    };
+
+    const Rows<D> rows(lane);
+    const Columns<D> columns(lane);
+    constexpr int B = D / 32;
+    v4u q[D / 16];
+    v16f sums[B];
+    float top, total;
+    int limit, least, from_t, token, head;
+    bool real, found;
+    auto start = [&]() RB_INLINE {
+        const int q0 = min(max(first_u[at.s], 0), A.tokens_q), n_q = at.shape.rows / A.group, row0 = at.block * JOB;
+        const int row = min(row0 + (lane & 31), at.shape.rows - 1);
+        real = row0 + (lane & 31) < at.shape.rows;
+        token = q0 + row / A.group;
+        head = kvh * A.group + row % A.group;
+        limit = at.n_k - n_q + row / A.group;
+        least = at.n_k - n_q + row0 / A.group;
+        from_t = at.t;
+        const uint8_t *from = global_at<const uint8_t>(A.q.at) + token * A.q.token + head * A.q.head;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) q[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from + k * 32 + h * 16) : (v4u)(0u);
+        // waited for here, once a job: where they are used, the compiler would wait for all loads at every tile
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) asm volatile("" : "+v"(q[k]));
+#pragma unroll
+        for (int b = 0; b < B; ++b) sums[b] = (v16f)(0.f);
+        top = RB_NEG_INF;
+        total = 0.f;
+        found = false;
+    };
+    bool first_job = true;
+    auto finish = [&]() RB_INLINE {      // with tile at.t
+        if (found)
+            for (int r = max(max(least + 1, 0) / KEYS, from_t) * KEYS; r < min((at.t + 1) * KEYS, at.n_k); ++r) {
+                const int page = table_u[(long long)at.s * A.width + (r >> A.page_shift)];
+                add_not_finite<T, D>(sums, v_base + place(page, r), A.dim, h, r <= limit);
+            }
+        total = over_halves_sum(total);
+        if (from_t == 0 && at.t == at.shape.tiles - 1) {
+            const bool empty = limit < 0;
+            store_columns<T, D>(sums, empty ? 0.f : 1.f / total, global_at<uint8_t>(A.o) + ((long long)token * A.heads + head) * (A.dim * 2), A.dim, h, real, empty);
+        } else if (real) {
+            const PartOfJob<D> to(workspace, kvh, wavefronts, w, first_job ? 0 : 1);
+            const int row = lane & 31;
+            if (h == 0) {
+                *to.top(row) = top;
+                *to.total(row) = total;
+            }
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) *(v4f *)(to.row(row) + b * 32 + 2 * i + 4 * h) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
+        }
+        first_job = false;
+    };
+
+    auto step = [&](int i, uint8_t *keys, uint8_t *values) RB_INLINE {
+        if (i == 0 || at.t == 0) start();
+        loads_arrived<3 * LOADS>();
+        v16f x = {};
+        stream_operands<D / 16, 4>([&](int k) RB_INLINE { return rows.read(keys, 0, k); }, [&](int k, v4u a) RB_INLINE { x = T::mfma(a, q[k], x); });
+        load(i + 2, k_base, keys);
+        const int first_key = at.t * KEYS;
+        if (first_key + KEYS - 1 > least) {
+            const int seen = limit - first_key - 4 * h;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (8 * (e / 4) + e % 4 > seen) x[e] = RB_NEG_INF;
+        }
+        float most = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) most = fmaxf(most, x[e]);
+        most = over_halves_max(most) * A.c;
+        if (__ballot(most > top + SLACK)) {
+            const float now = fmaxf(top, most), shrink = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            total *= shrink;
+#pragma unroll
+            for (int b = 0; b < B; ++b) sums[b] *= shrink;
+        }
+        const float zero_at = (top == RB_NEG_INF ? 0.f : top) - T::BIAS;
+        uint32_t wt[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float a = __builtin_amdgcn_exp2f(fmaf(x[e], A.c, -zero_at)), z = __builtin_amdgcn_exp2f(fmaf(x[e + 1], A.c, -zero_at));
+            total += a + z;
+            wt[e / 2] = T::pack(a, z);
+        }
+        const v4u p[2] = {{wt[0], wt[1], wt[2], wt[3]}, {wt[4], wt[5], wt[6], wt[7]}};
+        loads_arrived<3 * LOADS>();
+        if (least < min(first_key + KEYS, at.n_k) - 1) {      // some row does not see all of the tile's keys: see make_finite
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                lds_v4u *v = (lds_v4u *)(lds_byte *)(values + j * L::GROUP + lane * 16);
+                const v4u was = *v, is = finite_part<T>(was);
+                if (was.x != is.x || was.y != is.y || was.z != is.z || was.w != is.w) {
+                    any = true;
+                    *v = is;
+                }
+            }
+            found |= __ballot(any) != 0;
+        }
+        stream_operands<2 * B, 4>([&](int k) RB_INLINE { return columns.read(values, k % B, k / B); }, [&](int k, v4u a) RB_INLINE { sums[k % B] = T::mfma(a, p[k / B], sums[k % B]); });
+        load(i + 2, v_base, values);
+        next_ahead();
+        if (i == n - 1 || at.t == at.shape.tiles - 1) finish();
+        advance(at);
+    };
+
+    uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS), *const kb = keys_b + wave * L::bytes(KEYS), *const vb = values_b + wave * L::bytes(KEYS);
+    ask_pages(ahead);
+    load(0, k_base, ka);
+    load(0, v_base, va);
+    next_ahead();
+    load(1, k_base, kb);
+    load(1, v_base, vb);
+    next_ahead();
+    for (int i = 0; i < n; i += 2) {
+        step(i, ka, va);
+        if (i + 1 < n) step(i + 1, kb, vb);
+    }
+    loads_arrived();
+}
+
+// A job that several wavefronts had parts of: o = sum of the parts' rows, each times 2^(its maximum - the largest), over the sum of their totals
+// likewise, in the order of the parts.  A thread takes four elements; up to eight groups of threads share out the rows, or, where there are few, the parts.
+template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, Address workspace, int wavefronts)
+{
+    constexpr int COLUMNS = D / 4, GROUPS = 256 / COLUMNS;
+    __shared__ float joined[GROUPS][D], totals[GROUPS], tops[GROUPS];
+    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;
+    const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
+    const int s = sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
+    const Shape shape = shape_of(A, first[s], first[s + 1], lengths[s]);
+    const int b = block - block_start(first, s, A.group, JOB);
+    if (b < 0 || b >= shape.blocks) return;
+    const Sums sums_of = {A, first, lengths, lane};
+    const long long all = sums_of.before(A.n_seqs), from = sums_of.before(s) + (long long)b * shape.tiles;
+    const int shares = shares_of(all, wavefronts);
+    // the shares that have its first and its last tile: the last that start no later
+    auto share_of = [&](long long tile) { return (int)(((tile + 1) * shares - 1) / all); };
+    const int w0 = share_of(from), w1 = share_of(from + shape.tiles - 1);
+    if (w0 == w1) return;      // it has stored the result
+    const bool starts_inside = share_start(all, w0, shares) < from;      // the first part is that share's last, all others are their shares' first
+
+    const int n_rows = min(shape.rows - b * JOB, JOB), column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
+    const int n_q = shape.rows / A.group, n_k = positions(lengths[s], A.width, A.page_shift), q0 = min(max(first[s], 0), A.tokens_q);
+    int rows_at_once = 1;
+    while (rows_at_once < n_rows && rows_at_once < GROUPS) rows_at_once *= 2;
+    const int parts = GROUPS / rows_at_once;      // groups per row
+    for (int r0 = 0; r0 < n_rows; r0 += rows_at_once) {
+        const int r = r0 + group % rows_at_once, p = group / rows_at_once;
+        float top = RB_NEG_INF, total = 0.f;
+        v4f sum = {};
+        if (r < n_rows)
+            for (int w = w0 + p; w <= w1; w += parts) {
+                const PartOfJob<D> part(workspace, kvh, wavefronts, w, w == w0 && starts_inside ? 1 : 0);
+                const float t = *part.top(r);
+                const v4f x = *(const v4f *)(part.row(r) + column * 4);
+                const float now = fmaxf(top, t), mine = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(t - now), others = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                total = total * others + *part.total(r) * mine;
+                sum = sum * others + x * mine;
+                top = now;
+            }
+        __syncthreads();
+        *(v4f *)&joined[group][column * 4] = sum;
+        if (column == 0) totals[group] = total, tops[group] = top;
+        __syncthreads();
+        if (p == 0 && r < n_rows) {
+            float most = RB_NEG_INF;
+            for (int i = 0; i < parts; ++i) most = fmaxf(most, tops[group + i * rows_at_once]);
+            v4f out = {};
+            float all_of = 0.f;
+            for (int i = 0; i < parts; ++i) {
+                const int g = group + i * rows_at_once;
+                const float f = tops[g] == RB_NEG_INF && most == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(tops[g] - most);
+                out += *(const v4f *)&joined[g][column * 4] * f;
+                all_of += totals[g] * f;
+            }
+            const int row = b * JOB + r, token = row / A.group;
+            const bool empty = n_k - n_q + token < 0;
+            const float norm = 1.f / all_of;
+            if (column * 4 < A.dim)
+                *(v2u *)(global_at<uint8_t>(A.o) + (((long long)(q0 + token) * A.heads + kvh * A.group + row % A.group) * A.dim + column * 4) * 2) =
+                    empty ? (v2u)(0u) : (v2u){T::pack(out[0] * norm, out[1] * norm), T::pack(out[2] * norm, out[3] * norm)};
+        }
+    }
+}
+
+// one workgroup per compute unit, shared out over the key heads
+int groups_per_head(const Args &A, int compute_units) { return compute_units > A.kv_heads ? compute_units / A.kv_heads : 1; }
+
+template <class T, int D> int launch(const Args &A, int compute_units, void *workspace, hipStream_t stream)
+{
+    const int groups = groups_per_head(A, compute_units);
+    const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, JOB) * A.kv_heads;
+    if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
+    hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES), 0, stream, A, address_of(workspace));
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs), dim3(256), 0, stream, A, address_of(workspace), groups * WAVES);
+    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
+
+}  // namespace
+
+bool few_applies(int tokens, int n_seqs, int group) { return (long long)tokens * group <= (long long)JOB * n_seqs; }
+
+size_t few_workspace_bytes(int kv_heads, int dim, int compute_units)
+{
+    Args A = {};
+    A.kv_heads = kv_heads;
+    return (size_t)kv_heads * groups_per_head(A, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfJob<64>::FLOATS : PartOfJob<128>::FLOATS) * 4;
+}
+
+int launch_few(const Args &A, int dtype, int compute_units, void *workspace, hipStream_t stream)
+{
+    if (dtype == RB_F16) return A.dim <= 64 ? launch<F16, 64>(A, compute_units, workspace, stream) : launch<F16, 128>(A, compute_units, workspace, stream);
+    return A.dim <= 64 ? launch<BF16, 64>(A, compute_units, workspace, stream) : launch<BF16, 128>(A, compute_units, workspace, stream);
+}
+
+}  // namespace attn
+}  // namespace rb

@@ -96,25 +96,7 @@ template <class T, int D> __device__ __forceinline__ void look_through(const uin
         if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) *found = 1;
     }
 }
-template <class T> __device__ __forceinline__ v4u cleaned(v4u w, bool dirty)
-{
-    if (dirty) w = (v4u){finite_part<T>(w.x), finite_part<T>(w.y), finite_part<T>(w.z), finite_part<T>(w.w)};
-    return w;
-}
-
-// sums [element][column], element 32 b + ..., as D elements of a row of 16-bit values
-template <class T, int D> __device__ __forceinline__ void store_columns(const v16f (&sums)[D / 32], float scale, uint8_t *to, int dim, int h, bool real)
-{
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 8) {
-            const auto lo = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i] * scale, sums[b][i + 1] * scale), T::pack(sums[b][i + 4] * scale, sums[b][i + 5] * scale), false, false);
-            const auto hi = __builtin_amdgcn_permlane32_swap(T::pack(sums[b][i + 2] * scale, sums[b][i + 3] * scale), T::pack(sums[b][i + 6] * scale, sums[b][i + 7] * scale), false, false);
-            const int e = b * 32 + i * 2 + h * 8;
-            if (real && e < dim) *(v4u *)(to + e * 2) = (v4u){lo[0], hi[0], lo[1], hi[1]};
-        }
-}
+template <class T> __device__ __forceinline__ v4u cleaned(v4u w, bool dirty) { return dirty ? finite_part<T>(w) : w; }
 
 // --------------------------------------------------------------- dk and dv ---
 // A workgroup keeps 128 keys and values of one key head, 32 per wavefront as right operands in registers, and takes the queries
@@ -255,8 +237,8 @@ constexpr int E = D / 32;
 
     const bool real = my_key < S.n_k;
     const long long at = ((long long)(S.k0 + key) * A.kv_heads + kvh) * (A.dim * 2);
-    store_columns<T, D>(sums_v, 1.f / (1 << T::GRAD_BIAS), global_at<uint8_t>(A.dv) + at, A.dim, h, real);
-    store_columns<T, D>(sums_k, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dk) + at, A.dim, h, real);
+    store_columns<T, D>(sums_v, 1.f / (1 << T::GRAD_BIAS), global_at<uint8_t>(A.dv) + at, A.dim, h, real, false);
+    store_columns<T, D>(sums_k, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dk) + at, A.dim, h, real, false);
 }
 
 // ---------------------------------------------------------------------- dq ---
@@ -372,7 +354,7 @@ constexpr int E = D / 32;
         step(t, keys_a, values_a, keys_b, values_b);
         if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
-    store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows);
+    store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, false);
 }
 
 template <class T, int D> int launch(const GradArgs &A, hipStream_t stream)
