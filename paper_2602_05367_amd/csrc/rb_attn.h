@@ -295,6 +295,8 @@ struct Args {
     long long page;
     int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
     int page_shift, pages, width;
+    Address parts;                           // workspace
+    int splits;                              // workgroups that share the keys of the same rows
     float c;                                 // scale log2(e): the exponentials are powers of two
 };
 
@@ -302,6 +304,80 @@ struct Args {
 // Weights are taken relative to a maximum that follows the scores only when they pass it by this many powers of two: the sums
 // are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
 constexpr float SLACK = 8.f;
+
+// positions of a sequence in a cache: what its length says, as far as the page table reaches
+__device__ __forceinline__ int positions(int length, int width, int page_shift)
+{
+    return min(max(length, 0), (int)min((long long)width << page_shift, 0x7fffffc0ll));
+}
+// workgroups that share `tiles` tiles: two tiles each at least
+__device__ __forceinline__ int splits_of(int tiles, int splits) { return max(min(splits, tiles / 2), 1); }
+
+// Parts of the same rows over different keys, unnormalised, in memory: the rows' maxima and sums, then the rows.
+template <int D, int N> struct PartOfRows {
+    static constexpr size_t FLOATS = N * (2 + D);
+    float *at;
+    __device__ __forceinline__ PartOfRows(Address workspace, size_t which) : at(global_at<float>(workspace) + which * FLOATS) {}
+    __device__ __forceinline__ float *top(int row) const { return at + row; }
+    __device__ __forceinline__ float *total(int row) const { return at + N + row; }
+    __device__ __forceinline__ float *row(int row) const { return at + 2 * N + row * D; }
+    // from the lane that has column `row` of the sums, both halves of the wavefront
+    __device__ __forceinline__ void store(const v16f (&sums)[D / 32], float row_top, float row_total, int r, int h) const
+    {
+        if (h == 0) {
+            *top(r) = row_top;
+            *total(r) = row_total;
+        }
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *(v4f *)(row(r) + b * 32 + 2 * i + 4 * h) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
+    }
+};
+// Joins n_parts of rows row0 .. row0 + n_rows - 1: o = sum of the parts' rows, each times 2^(its maximum - the largest), over the sum of their totals
+// likewise, in the order of the parts.  256 threads; a thread takes four elements; its groups share out the rows, or, where there are few, the parts.
+// part(i): a PartOfRows; out(row): where the result goes; empty(row): it sees nothing.
+template <class T, int D, class Part_, class Out, class Empty>
+__device__ __forceinline__ void join_rows(int n_parts, int row0, int n_rows, int dim, Part_ part, Out out, Empty empty)
+{
+    constexpr int COLUMNS = D / 4, GROUPS = 256 / COLUMNS;
+    __shared__ float joined[GROUPS][D], totals[GROUPS], tops[GROUPS];
+    const int column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
+    int rows_at_once = 1;
+    while (rows_at_once < n_rows && rows_at_once < GROUPS) rows_at_once *= 2;
+    const int sharing = GROUPS / rows_at_once;      // groups per row
+    auto weight = [](float top, float most) { return most == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - most); };
+    for (int r0 = 0; r0 < n_rows; r0 += rows_at_once) {
+        const int i = r0 + group % rows_at_once, r = row0 + i, p = group / rows_at_once;
+        float top = RB_NEG_INF, total = 0.f;
+        v4f sum = {};
+        if (i < n_rows)
+            for (int w = p; w < n_parts; w += sharing) {
+                const auto from = part(w);
+                const float t = *from.top(r), now = fmaxf(top, t), mine = weight(t, now), others = weight(top, now);
+                const v4f x = *(const v4f *)(from.row(r) + column * 4);
+                total = total * others + *from.total(r) * mine;
+                sum = sum * others + x * mine;
+                top = now;
+            }
+        __syncthreads();
+        *(v4f *)&joined[group][column * 4] = sum;
+        if (column == 0) totals[group] = total, tops[group] = top;
+        __syncthreads();
+        if (p == 0 && i < n_rows && column * 4 < dim) {
+            float most = RB_NEG_INF, all = 0.f;
+            for (int g = group; g < GROUPS; g += rows_at_once) most = fmaxf(most, tops[g]);
+            v4f o = {};
+            for (int g = group; g < GROUPS; g += rows_at_once) {
+                const float f = weight(tops[g], most);
+                o += *(const v4f *)&joined[g][column * 4] * f;
+                all += totals[g] * f;
+            }
+            const float norm = 1.f / all;
+            *(v2u *)(out(r) + column * 8) = empty(r) ? (v2u)(0u) : (v2u){T::pack(o[0] * norm, o[1] * norm), T::pack(o[2] * norm, o[3] * norm)};
+        }
+    }
+}
 
 }  // namespace attn
 }  // namespace rb

@@ -1,7 +1,7 @@
 // Attention over packed prompts and over a paged cache: o_i = sum_j p_ij v_j with
 // p_ij = exp(c q_i . k_j - lse_i), lse_i = log sum_j exp(c q_i . k_j) over the keys j that row i sees.
 #include <hip/hip_runtime.h>
-#include <type_traits>
+#include <algorithm>
 
 #include "rabit.h"
 #include "rb_attn.h"
@@ -29,13 +29,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kvh = blockIdx.x % A.kv_heads;      // the workgroups of a head go to the same XCDs
     int block = blockIdx.x / A.kv_heads;
-    if (A.causal) block = (int)(gridDim.x / A.kv_heads) - 1 - block;      // the longest first
+    const int split = PAGED ? block % A.splits : 0, n_blocks = (int)(gridDim.x / A.kv_heads) / (PAGED ? A.splits : 1);
+    if (PAGED) block /= A.splits;
+    if (A.causal) block = n_blocks - 1 - block;      // the longest first
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     const int s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
     Sequence S = sequence_at(first_q, PAGED ? first_q : first_k, s, A.tokens_q, PAGED ? A.tokens_q : A.tokens_k);
     if (PAGED) {
         S.k0 = 0;
-        S.n_k = min(max(__builtin_amdgcn_readfirstlane(first_k[s]), 0), (int)min((long long)A.width << A.page_shift, 0x7fffffc0ll));
+        S.n_k = positions(__builtin_amdgcn_readfirstlane(first_k[s]), A.width, A.page_shift);
     }
     const int row0 = (block - block_start(first_q, s, A.group, BM)) * BM, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
@@ -49,7 +51,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     const int limit = A.causal ? ahead + token : S.n_k - 1;
     const int block_least = last_key(row0), block_most = last_key(row0 + BM - 1);
     const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32 + 31));
-    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS;
+    const int tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS, parts = PAGED ? splits_of(tiles, A.splits) : 1;
+    if (split >= parts) return;
+    const int first_tile = tiles * split / parts, n_tiles = tiles * (split + 1) / parts;      // (the end of this workgroup's)
 
     v4u q[D / 16];
     {
@@ -144,36 +148,77 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
         stream_operands<2 * H * B, 4>([&](int i) RB_INLINE { return columns.read(values, i % B, i / B); }, [&](int i, v4u a) RB_INLINE { sums[i % B] = T::mfma(a, p[i / B], sums[i % B]); });
     };
     if (tid == 0) found = 0;
-    if (n_tiles > 0) {
-        if constexpr (PAGED) ask_pages(0);
-        load(0, keys_a, values_a);
+    if (first_tile < n_tiles) {
+        if constexpr (PAGED) ask_pages(first_tile);
+        load(first_tile, keys_a, values_a);
     }
-    for (int t = 0; t < n_tiles; t += 2) {
+    for (int t = first_tile; t < n_tiles; t += 2) {
         step(t, keys_a, values_a, keys_b, values_b);
         if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
 
     __syncthreads();
     if (__builtin_amdgcn_readfirstlane(found))
-        for (int r = max(block_least + 1, 0) / KEYS * KEYS; r <= wave_most; ++r)
+        for (int r = max(max(block_least + 1, 0) / KEYS, first_tile) * KEYS; r <= min(wave_most, n_tiles * KEYS - 1); ++r)
             add_not_finite<T, D>(sums, v_base + (PAGED ? place(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), r) : r * A.v.token), A.dim, h, r <= limit);
 
     total = over_halves_sum(total);
     const bool empty = limit < 0;
+    if (parts > 1) {
+        if (real) PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + split).store(sums, top, total, wave * 32 + (lane & 31), h);
+        return;
+    }
     if (A.lse && real && h == 0)
         global_at<float>(A.lse)[(long long)(S.q0 + token) * A.heads + head] = empty ? RB_NEG_INF : (top - T::BIAS + __builtin_amdgcn_logf(total)) * LN2;
     uint8_t *to = global_at<uint8_t>(A.o) + ((long long)(S.q0 + token) * A.heads + head) * (A.dim * 2);
     store_columns<T, D>(sums, empty ? 0.f : 1.f / total, to, A.dim, h, real, empty);
 }
 
+// What several workgroups had parts of; 32 rows per workgroup
+template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A)
+{
+    constexpr int QUARTER = BM / 4;
+    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads / 4, row0 = blockIdx.x / A.kv_heads % 4 * QUARTER;
+    const int *first = global_at<const int>(A.first_q);
+    const int s = sequence_of_block(first, A.n_seqs, A.group, BM, block, lane);
+    const Sequence S = sequence_at(first, first, s, A.tokens_q, A.tokens_q);
+    const int before = (block - block_start(first, s, A.group, BM)) * BM, n_rows = S.n_q * A.group - before;
+    if (before < 0 || row0 >= n_rows) return;
+    const int ahead = positions(global_at<const int>(A.first_k)[s], A.width, A.page_shift) - S.n_q;
+    const int most = ahead + (before + min(n_rows, BM) - 1) / A.group, parts = splits_of((max(most + 1, 0) + KEYS - 1) / KEYS, A.splits);
+    if (parts == 1) return;
+    join_rows<T, D>(
+        parts, row0, min(n_rows - row0, QUARTER), A.dim, [&](int i) { return PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + i); },
+        [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(S.q0 + (before + r) / A.group) * A.heads + kvh * A.group + (before + r) % A.group) * (A.dim * 2); },
+        [&](int r) { return ahead + (before + r) / A.group < 0; });
+}
+
+// A cache is read by two workgroups per compute unit at least, if its keys allow: where the rows alone are fewer, several share the keys
+int splits_for(int tokens, int n_seqs, int kv_heads, int group, int compute_units)
+{
+    const long long n = block_numbers(tokens, n_seqs, group, BM) * kv_heads;
+    return (int)std::max(1ll, std::min(16ll, 2ll * compute_units / std::max(n, 1ll)));
+}
+size_t splits_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, int dim, int compute_units)
+{
+    const int splits = splits_for(tokens, n_seqs, kv_heads, group, compute_units);
+    return splits < 2 ? 0 : (size_t)block_numbers(tokens, n_seqs, group, BM) * kv_heads * splits * (dim <= 64 ? PartOfRows<64, BM>::FLOATS : PartOfRows<128, BM>::FLOATS) * 4;
+}
+
 template <class T, bool PAGED> int launch(const Args &A, hipStream_t stream)
 {
-    const long long n = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads;
-    if (n > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = PAGED ? blocks * A.splits : blocks;
+    if (n > 0x1fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     if (A.dim <= 64)
         hipLaunchKernelGGL((rows_kernel<T, 64, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
     else
         hipLaunchKernelGGL((rows_kernel<T, 128, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
+    if (PAGED && A.splits > 1) {
+        if (A.dim <= 64)
+            hipLaunchKernelGGL((join_kernel<T, 64>), dim3((unsigned)(blocks * 4)), dim3(256), 0, stream, A);
+        else
+            hipLaunchKernelGGL((join_kernel<T, 128>), dim3((unsigned)(blocks * 4)), dim3(256), 0, stream, A);
+    }
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
 
@@ -225,7 +270,8 @@ extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, c
 extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
 {
     if (check_cache(C) != RB_OK || heads < 1 || heads % C->kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
-    return few_applies(tokens, n_seqs, heads / C->kv_heads) ? few_workspace_bytes(C->kv_heads, C->dim, rb::mx::device_groups()) : 0;
+    const int units = rb::mx::device_groups(), group = heads / C->kv_heads;
+    return few_applies(tokens, n_seqs, group) ? few_workspace_bytes(C->kv_heads, C->dim, units) : splits_workspace_bytes(tokens, n_seqs, C->kv_heads, group, C->dim, units);
 }
 
 extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
@@ -250,7 +296,9 @@ extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token
     A.n_seqs = n_seqs, A.tokens_q = tokens;
     A.heads = heads, A.kv_heads = C->kv_heads, A.group = heads / C->kv_heads, A.dim = C->dim, A.causal = 1;
     A.c = scale * LOG2E;
+    A.parts = rb::address_of(workspace);
+    A.splits = splits_for(tokens, n_seqs, A.kv_heads, A.group, rb::mx::device_groups());
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_applies(tokens, n_seqs, A.group)) return launch_few(A, C->dtype, rb::mx::device_groups(), workspace, st);
+    if (few_applies(tokens, n_seqs, A.group)) return launch_few(A, C->dtype, rb::mx::device_groups(), st);
     return C->dtype == RB_F16 ? launch<F16, true>(A, st) : launch<BF16, true>(A, st);
 }

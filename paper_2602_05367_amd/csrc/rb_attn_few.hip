@@ -21,10 +21,6 @@ struct Shape {
     int rows, blocks, tiles;
     __device__ __forceinline__ long long count() const { return (long long)blocks * tiles; }
 };
-__device__ __forceinline__ int positions(int length, int width, int page_shift)
-{
-    return min(max(length, 0), (int)min((long long)width << page_shift, 0x7fffffc0ll));
-}
 __device__ __forceinline__ Shape shape_of(const Args &A, int q0, int q1, int length)
 {
     q0 = min(max(q0, 0), A.tokens_q);
@@ -76,15 +72,11 @@ struct Sums {
 __device__ __forceinline__ int shares_of(long long all, int wavefronts) { return (int)min((long long)wavefronts, max(all, 1ll)); }
 __device__ __forceinline__ long long share_start(long long all, int w, int shares) { return all * w / shares; }
 
-// a part of a job in the workspace: the maxima and sums of its rows, then a row of D each
-template <int D> struct PartOfJob {
-    static constexpr size_t FLOATS = JOB * (2 + D);
-    float *at;
-    __device__ __forceinline__ PartOfJob(Address workspace, int kvh, int wavefronts, int w, int which) : at(global_at<float>(workspace) + (((size_t)kvh * wavefronts + w) * 2 + which) * FLOATS) {}
-    __device__ __forceinline__ float *top(int row) const { return at + row; }
-    __device__ __forceinline__ float *total(int row) const { return at + JOB + row; }
-    __device__ __forceinline__ float *row(int row) const { return at + 2 * JOB + row * D; }
-};
+// the part of a job that share w has: its first (0) or its last (1)
+template <int D> __device__ __forceinline__ PartOfRows<D, JOB> part_of(Address workspace, int kvh, int wavefronts, int w, int which)
+{
+    return PartOfRows<D, JOB>(workspace, ((size_t)kvh * wavefronts + w) * 2 + which);
+}
 
 // a position in the row of tiles
 struct Cursor {
@@ -94,7 +86,7 @@ struct Cursor {
 };
 
 template <class T, int D>
-__global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A, Address workspace)
+__global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
 {
     using L = Tile<D>;
     __shared__ __attribute__((aligned(16))) uint8_t keys_a[WAVES * L::bytes(KEYS)], values_a[WAVES * L::bytes(KEYS)], keys_b[WAVES * L::bytes(KEYS)], values_b[WAVES * L::bytes(KEYS)];
@@ -212,16 +204,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A, Addres
             const bool empty = limit < 0;
             store_columns<T, D>(sums, empty ? 0.f : 1.f / total, global_at<uint8_t>(A.o) + ((long long)token * A.heads + head) * (A.dim * 2), A.dim, h, real, empty);
         } else if (real) {
-            const PartOfJob<D> to(workspace, kvh, wavefronts, w, first_job ? 0 : 1);
-            const int row = lane & 31;
-            if (h == 0) {
-                *to.top(row) = top;
-                *to.total(row) = total;
-            }
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) *(v4f *)(to.row(row) + b * 32 + 2 * i + 4 * h) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
+            part_of<D>(A.parts, kvh, wavefronts, w, first_job ? 0 : 1).store(sums, top, total, lane & 31, h);
         }
         first_job = false;
     };
@@ -295,12 +278,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A, Addres
     loads_arrived();
 }
 
-// A job that several wavefronts had parts of: o = sum of the parts' rows, each times 2^(its maximum - the largest), over the sum of their totals
-// likewise, in the order of the parts.  A thread takes four elements; up to eight groups of threads share out the rows, or, where there are few, the parts.
-template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, Address workspace, int wavefronts)
+// A job that several wavefronts had parts of
+template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, int wavefronts)
 {
-    constexpr int COLUMNS = D / 4, GROUPS = 256 / COLUMNS;
-    __shared__ float joined[GROUPS][D], totals[GROUPS], tops[GROUPS];
     const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
     const int s = sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
@@ -316,60 +296,25 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
     if (w0 == w1) return;      // it has stored the result
     const bool starts_inside = share_start(all, w0, shares) < from;      // the first part is that share's last, all others are their shares' first
 
-    const int n_rows = min(shape.rows - b * JOB, JOB), column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
     const int n_q = shape.rows / A.group, n_k = positions(lengths[s], A.width, A.page_shift), q0 = min(max(first[s], 0), A.tokens_q);
-    int rows_at_once = 1;
-    while (rows_at_once < n_rows && rows_at_once < GROUPS) rows_at_once *= 2;
-    const int parts = GROUPS / rows_at_once;      // groups per row
-    for (int r0 = 0; r0 < n_rows; r0 += rows_at_once) {
-        const int r = r0 + group % rows_at_once, p = group / rows_at_once;
-        float top = RB_NEG_INF, total = 0.f;
-        v4f sum = {};
-        if (r < n_rows)
-            for (int w = w0 + p; w <= w1; w += parts) {
-                const PartOfJob<D> part(workspace, kvh, wavefronts, w, w == w0 && starts_inside ? 1 : 0);
-                const float t = *part.top(r);
-                const v4f x = *(const v4f *)(part.row(r) + column * 4);
-                const float now = fmaxf(top, t), mine = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(t - now), others = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now);
-                total = total * others + *part.total(r) * mine;
-                sum = sum * others + x * mine;
-                top = now;
-            }
-        __syncthreads();
-        *(v4f *)&joined[group][column * 4] = sum;
-        if (column == 0) totals[group] = total, tops[group] = top;
-        __syncthreads();
-        if (p == 0 && r < n_rows) {
-            float most = RB_NEG_INF;
-            for (int i = 0; i < parts; ++i) most = fmaxf(most, tops[group + i * rows_at_once]);
-            v4f out = {};
-            float all_of = 0.f;
-            for (int i = 0; i < parts; ++i) {
-                const int g = group + i * rows_at_once;
-                const float f = tops[g] == RB_NEG_INF && most == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(tops[g] - most);
-                out += *(const v4f *)&joined[g][column * 4] * f;
-                all_of += totals[g] * f;
-            }
-            const int row = b * JOB + r, token = row / A.group;
-            const bool empty = n_k - n_q + token < 0;
-            const float norm = 1.f / all_of;
-            if (column * 4 < A.dim)
-                *(v2u *)(global_at<uint8_t>(A.o) + (((long long)(q0 + token) * A.heads + kvh * A.group + row % A.group) * A.dim + column * 4) * 2) =
-                    empty ? (v2u)(0u) : (v2u){T::pack(out[0] * norm, out[1] * norm), T::pack(out[2] * norm, out[3] * norm)};
-        }
-    }
+    auto token = [&](int r) { return (b * JOB + r) / A.group; };
+    join_rows<T, D>(
+        w1 - w0 + 1, 0, min(shape.rows - b * JOB, JOB), A.dim,
+        [&](int i) { return part_of<D>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
+        [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + token(r)) * A.heads + kvh * A.group + (b * JOB + r) % A.group) * (A.dim * 2); },
+        [&](int r) { return n_k - n_q + token(r) < 0; });
 }
 
 // one workgroup per compute unit, shared out over the key heads
 int groups_per_head(const Args &A, int compute_units) { return compute_units > A.kv_heads ? compute_units / A.kv_heads : 1; }
 
-template <class T, int D> int launch(const Args &A, int compute_units, void *workspace, hipStream_t stream)
+template <class T, int D> int launch(const Args &A, int compute_units, hipStream_t stream)
 {
     const int groups = groups_per_head(A, compute_units);
     const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, JOB) * A.kv_heads;
     if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
-    hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES), 0, stream, A, address_of(workspace));
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs), dim3(256), 0, stream, A, address_of(workspace), groups * WAVES);
+    hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES), 0, stream, A);
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs), dim3(256), 0, stream, A, groups * WAVES);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
 
@@ -381,13 +326,13 @@ size_t few_workspace_bytes(int kv_heads, int dim, int compute_units)
 {
     Args A = {};
     A.kv_heads = kv_heads;
-    return (size_t)kv_heads * groups_per_head(A, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfJob<64>::FLOATS : PartOfJob<128>::FLOATS) * 4;
+    return (size_t)kv_heads * groups_per_head(A, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfRows<64, JOB>::FLOATS : PartOfRows<128, JOB>::FLOATS) * 4;
 }
 
-int launch_few(const Args &A, int dtype, int compute_units, void *workspace, hipStream_t stream)
+int launch_few(const Args &A, int dtype, int compute_units, hipStream_t stream)
 {
-    if (dtype == RB_F16) return A.dim <= 64 ? launch<F16, 64>(A, compute_units, workspace, stream) : launch<F16, 128>(A, compute_units, workspace, stream);
-    return A.dim <= 64 ? launch<BF16, 64>(A, compute_units, workspace, stream) : launch<BF16, 128>(A, compute_units, workspace, stream);
+    if (dtype == RB_F16) return A.dim <= 64 ? launch<F16, 64>(A, compute_units, stream) : launch<F16, 128>(A, compute_units, stream);
+    return A.dim <= 64 ? launch<BF16, 64>(A, compute_units, stream) : launch<BF16, 128>(A, compute_units, stream);
 }
 
 }  // namespace attn

@@ -33,7 +33,7 @@ inline int check_cache(const rb_cache *C)
 // paged calls with few rows per sequence (rb_attn_few.hip)
 bool few_applies(int tokens, int n_seqs, int group);
 size_t few_workspace_bytes(int kv_heads, int dim, int compute_units);
-int launch_few(const Args &A, int dtype, int compute_units, void *workspace, hipStream_t stream);
+int launch_few(const Args &A, int dtype, int compute_units, hipStream_t stream);
 
 inline Side side(const void *p, long long token, long long head) { return {rb::address_of(p), token * 2, head * 2}; }
 
