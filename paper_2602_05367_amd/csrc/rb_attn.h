@@ -244,7 +244,7 @@ __device__ __forceinline__ void meet()
 // group of the heads that share it: row = token * group + head of the group.  Blocks of BM rows are numbered so that the
 // number of a sequence's first block follows from first[s] alone, floor(first[s] group / BM) + s, without a sum over the
 // sequences before it; some numbers between two sequences belong to nobody.
-__device__ __forceinline__ int block_start(const int *first, int s, int group, int BM) { return (int)((long long)first[s] * group / BM) + s; }
+__device__ __forceinline__ int block_start(int first, int s, int group, int BM) { return (int)((long long)first * group / BM) + s; }
 inline long long block_numbers(long long tokens, int n_seqs, int group, int BM) { return tokens * group / BM + n_seqs; }
 
 // the last of n places whose start is not beyond `value` (place 0's never is); a wavefront looks at 64 at a time
@@ -263,7 +263,7 @@ template <class Start> __device__ __forceinline__ int last_not_beyond(int n, int
 }
 __device__ __forceinline__ int sequence_of_block(const int *first, int n_seqs, int group, int BM, int block, int lane)
 {
-    return last_not_beyond(n_seqs, block, lane, [&](int s) { return block_start(first, s, group, BM); });
+    return last_not_beyond(n_seqs, block, lane, [&](int s) { return block_start(first[s], s, group, BM); });
 }
 
 // One sequence's part of the work.  What the arrays say is brought into the range of the buffers: an array that
@@ -334,48 +334,54 @@ template <int D, int N> struct PartOfRows {
             for (int i = 0; i < 16; i += 4) *(v4f *)(row(r) + b * 32 + 2 * i + 4 * h) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
     }
 };
-// Joins n_parts of rows row0 .. row0 + n_rows - 1: o = sum of the parts' rows, each times 2^(its maximum - the largest), over the sum of their totals
-// likewise, in the order of the parts.  256 threads; a thread takes four elements; its groups share out the rows, or, where there are few, the parts.
-// part(i): a PartOfRows; out(row): where the result goes; empty(row): it sees nothing.
+// Joins n_parts of the `joined` rows (two, four or eight) from row0 on, of which n_rows are there: o = sum of the parts' rows, each times 2^(its maximum - the
+// largest), over the sum of their totals likewise, in the order of the parts.  256 threads, four elements each; the groups of threads that make up a row share
+// out the parts.  Bound: latency, so all loads of sixteen parts and group are on their way before the first is used.  part(i): a PartOfRows; out(row): where
+// the result goes; empty(row): it sees nothing.
 template <class T, int D, class Part_, class Out, class Empty>
-__device__ __forceinline__ void join_rows(int n_parts, int row0, int n_rows, int dim, Part_ part, Out out, Empty empty)
+__device__ __forceinline__ void join_rows(int joined, int n_parts, int row0, int n_rows, int dim, Part_ part, Out out, Empty empty)
 {
-    constexpr int COLUMNS = D / 4, GROUPS = 256 / COLUMNS;
-    __shared__ float joined[GROUPS][D], totals[GROUPS], tops[GROUPS];
-    const int column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
-    int rows_at_once = 1;
-    while (rows_at_once < n_rows && rows_at_once < GROUPS) rows_at_once *= 2;
-    const int sharing = GROUPS / rows_at_once;      // groups per row
+    constexpr int COLUMNS = D / 4, GROUPS = 256 / COLUMNS, HELD = 16;
+    __shared__ float sums[GROUPS][D], tops[GROUPS], totals[GROUPS];
+    const int column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS, lg = 31 - __builtin_clz(joined), sharing = GROUPS >> lg;
+    const int i = group & (joined - 1), p0 = group >> lg, r = row0 + i;
+    const bool mine = i < n_rows;
     auto weight = [](float top, float most) { return most == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - most); };
-    for (int r0 = 0; r0 < n_rows; r0 += rows_at_once) {
-        const int i = r0 + group % rows_at_once, r = row0 + i, p = group / rows_at_once;
-        float top = RB_NEG_INF, total = 0.f;
-        v4f sum = {};
-        if (i < n_rows)
-            for (int w = p; w < n_parts; w += sharing) {
-                const auto from = part(w);
-                const float t = *from.top(r), now = fmaxf(top, t), mine = weight(t, now), others = weight(top, now);
-                const v4f x = *(const v4f *)(from.row(r) + column * 4);
-                total = total * others + *from.total(r) * mine;
-                sum = sum * others + x * mine;
-                top = now;
-            }
-        __syncthreads();
-        *(v4f *)&joined[group][column * 4] = sum;
-        if (column == 0) totals[group] = total, tops[group] = top;
-        __syncthreads();
-        if (p == 0 && i < n_rows && column * 4 < dim) {
-            float most = RB_NEG_INF, all = 0.f;
-            for (int g = group; g < GROUPS; g += rows_at_once) most = fmaxf(most, tops[g]);
-            v4f o = {};
-            for (int g = group; g < GROUPS; g += rows_at_once) {
-                const float f = weight(tops[g], most);
-                o += *(const v4f *)&joined[g][column * 4] * f;
-                all += totals[g] * f;
-            }
-            const float norm = 1.f / all;
-            *(v2u *)(out(r) + column * 8) = empty(r) ? (v2u)(0u) : (v2u){T::pack(o[0] * norm, o[1] * norm), T::pack(o[2] * norm, o[3] * norm)};
+    float most = RB_NEG_INF, total = 0.f;      // of this group's parts
+    v4f sum = {};
+    for (int w0 = p0; w0 < n_parts; w0 += HELD * sharing) {
+        v4f x[HELD];
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) x[j] = mine && w0 + j * sharing < n_parts ? *(const v4f *)(part(w0 + j * sharing).row(r) + column * 4) : (v4f)(0.f);
+        // the parts' maxima and totals, one per lane
+        const bool has = mine && column < HELD && w0 + column * sharing < n_parts;
+        float t = has ? *part(w0 + column * sharing).top(r) : RB_NEG_INF, part_total = has ? *part(w0 + column * sharing).total(r) : 0.f;
+        float now = t;
+        for (int d = COLUMNS / 2; d > 0; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+        now = fmaxf(now, most);
+        const float before = weight(most, now), w = weight(t, now);
+        most = now;
+        part_total *= w;
+        for (int d = COLUMNS / 2; d > 0; d >>= 1) part_total += __shfl_xor(part_total, d);
+        total = total * before + part_total;
+        sum *= before;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) sum += x[j] * __shfl(w, j, COLUMNS);
+    }
+    *(v4f *)&sums[group][column * 4] = sum;
+    if (column == 0) tops[group] = most, totals[group] = total;
+    __syncthreads();
+    if (p0 == 0 && mine && column * 4 < dim) {
+        for (int g = group; g < GROUPS; g += joined) most = fmaxf(most, tops[g]);
+        sum = (v4f)(0.f);
+        total = 0.f;
+        for (int g = group; g < GROUPS; g += joined) {
+            const float f = weight(tops[g], most);
+            sum += *(const v4f *)&sums[g][column * 4] * f;
+            total += totals[g] * f;
         }
+        const float norm = 1.f / total;
+        *(v2u *)(out(r) + column * 8) = empty(r) ? (v2u)(0u) : (v2u){T::pack(sum[0] * norm, sum[1] * norm), T::pack(sum[2] * norm, sum[3] * norm)};
     }
 }
 

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
         S.k0 = 0;
         S.n_k = positions(__builtin_amdgcn_readfirstlane(first_k[s]), A.width, A.page_shift);
     }
-    const int row0 = (block - block_start(first_q, s, A.group, BM)) * BM, n_rows = S.n_q * A.group;
+    const int row0 = (block - block_start(first_q[s], s, A.group, BM)) * BM, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
 
     const int my_row = row0 + wave * 32 + (lane & 31);
@@ -174,21 +174,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     store_columns<T, D>(sums, empty ? 0.f : 1.f / total, to, A.dim, h, real, empty);
 }
 
-// What several workgroups had parts of; 32 rows per workgroup
-template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A)
+// What several workgroups had parts of
+template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, int joined)
 {
-    constexpr int QUARTER = BM / 4;
-    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads / 4, row0 = blockIdx.x / A.kv_heads % 4 * QUARTER;
+    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads, row0 = blockIdx.y * joined;
     const int *first = global_at<const int>(A.first_q);
     const int s = sequence_of_block(first, A.n_seqs, A.group, BM, block, lane);
     const Sequence S = sequence_at(first, first, s, A.tokens_q, A.tokens_q);
-    const int before = (block - block_start(first, s, A.group, BM)) * BM, n_rows = S.n_q * A.group - before;
+    const int before = (block - block_start(first[s], s, A.group, BM)) * BM, n_rows = S.n_q * A.group - before;
     if (before < 0 || row0 >= n_rows) return;
     const int ahead = positions(global_at<const int>(A.first_k)[s], A.width, A.page_shift) - S.n_q;
     const int most = ahead + (before + min(n_rows, BM) - 1) / A.group, parts = splits_of((max(most + 1, 0) + KEYS - 1) / KEYS, A.splits);
     if (parts == 1) return;
     join_rows<T, D>(
-        parts, row0, min(n_rows - row0, QUARTER), A.dim, [&](int i) { return PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + i); },
+        joined, parts, row0, min(n_rows - row0, joined), A.dim, [&](int i) { return PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + i); },
         [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(S.q0 + (before + r) / A.group) * A.heads + kvh * A.group + (before + r) % A.group) * (A.dim * 2); },
         [&](int r) { return ahead + (before + r) / A.group < 0; });
 }
@@ -197,7 +196,7 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
 int splits_for(int tokens, int n_seqs, int kv_heads, int group, int compute_units)
 {
     const long long n = block_numbers(tokens, n_seqs, group, BM) * kv_heads;
-    return (int)std::max(1ll, std::min(16ll, 2ll * compute_units / std::max(n, 1ll)));
+    return n >= 2ll * compute_units ? 1 : (int)std::min(16ll, (2ll * compute_units + n - 1) / std::max(n, 1ll));
 }
 size_t splits_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, int dim, int compute_units)
 {
@@ -214,10 +213,11 @@ template <class T, bool PAGED> int launch(const Args &A, hipStream_t stream)
     else
         hipLaunchKernelGGL((rows_kernel<T, 128, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
     if (PAGED && A.splits > 1) {
+        const int joined = rows_joined(blocks, BM);
         if (A.dim <= 64)
-            hipLaunchKernelGGL((join_kernel<T, 64>), dim3((unsigned)(blocks * 4)), dim3(256), 0, stream, A);
+            hipLaunchKernelGGL((join_kernel<T, 64>), dim3((unsigned)blocks, BM / joined), dim3(256), 0, stream, A, joined);
         else
-            hipLaunchKernelGGL((join_kernel<T, 128>), dim3((unsigned)(blocks * 4)), dim3(256), 0, stream, A);
+            hipLaunchKernelGGL((join_kernel<T, 128>), dim3((unsigned)blocks, BM / joined), dim3(256), 0, stream, A, joined);
     }
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
@@ -271,7 +271,9 @@ extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, in
 {
     if (check_cache(C) != RB_OK || heads < 1 || heads % C->kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
     const int units = rb::mx::device_groups(), group = heads / C->kv_heads;
-    return few_applies(tokens, n_seqs, group) ? few_workspace_bytes(C->kv_heads, C->dim, units) : splits_workspace_bytes(tokens, n_seqs, C->kv_heads, group, C->dim, units);
+    // whichever kernel the table's width will choose
+    const size_t few = few_applies(tokens, n_seqs, group, 0) ? few_workspace_bytes(C->kv_heads, C->dim, units) : 0;
+    return std::max(few, splits_workspace_bytes(tokens, n_seqs, C->kv_heads, group, C->dim, units));
 }
 
 extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
@@ -299,6 +301,6 @@ extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token
     A.parts = rb::address_of(workspace);
     A.splits = splits_for(tokens, n_seqs, A.kv_heads, A.group, rb::mx::device_groups());
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_applies(tokens, n_seqs, A.group)) return launch_few(A, C->dtype, rb::mx::device_groups(), st);
+    if (few_applies(tokens, n_seqs, A.group, (long long)width * C->page_tokens)) return launch_few(A, C->dtype, rb::mx::device_groups(), st);
     return C->dtype == RB_F16 ? launch<F16, true>(A, st) : launch<BF16, true>(A, st);
 }

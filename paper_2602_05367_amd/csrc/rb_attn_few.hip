@@ -5,6 +5,7 @@
 // compute unit alike.  A wavefront keeps two tiles of keys and values on their way into LDS of its own, across jobs, and meets nobody.  What it has
 // of a job that it does not have all of goes to the workspace, unnormalised, and a second launch joins the parts in a fixed order.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 
 #include "rabit.h"
 #include "rb_attn.h"
@@ -16,10 +17,10 @@ namespace {
 
 constexpr int KEYS = 32, JOB = 32, WAVES = 4;
 
-// Where the work of a sequence lies among all tiles of a key head
+// Where the work of a sequence lies among all tiles of a key head.  (All of them, as many as rows and positions allow, are counted in 31 bits: see few_applies.)
 struct Shape {
     int rows, blocks, tiles;
-    __device__ __forceinline__ long long count() const { return (long long)blocks * tiles; }
+    __device__ __forceinline__ int count() const { return blocks * tiles; }
 };
 __device__ __forceinline__ Shape shape_of(const Args &A, int q0, int q1, int length)
 {
@@ -29,38 +30,58 @@ __device__ __forceinline__ Shape shape_of(const Args &A, int q0, int q1, int len
     // a sequence that has rows but no positions: one tile, of which they see nothing
     return {rows, (rows + JOB - 1) / JOB, rows ? max((positions(length, A.width, A.page_shift) + KEYS - 1) / KEYS, 1) : 0};
 }
-// Sums over the sequences, 64 at a time.  total(): all tiles; locate(at): the sequence that has tile `at` (at < total), which becomes the tile among its own
+// Sums over the sequences, 64 at a time, the first 64 looked at once
 struct Sums {
     const Args &A;
     const int *first, *lengths;
-    int lane;
-    __device__ __forceinline__ long long count(int s) const { return s < A.n_seqs ? shape_of(A, first[s], first[s + 1], lengths[s]).count() : 0; }
-    static __device__ __forceinline__ long long from_lane(long long v, int from)
+    int lane, q0, q1, length, upto;      // what the arrays say of sequence `lane`; the tiles of sequences 0 .. lane
+    __device__ __forceinline__ Sums(const Args &A_, const int *first_, const int *lengths_, int lane_) : A(A_), first(first_), lengths(lengths_), lane(lane_)
     {
-        return (long long)(unsigned)__shfl((int)v, from) | (long long)__shfl((int)(v >> 32), from) << 32;
+        const int s = min(lane, A.n_seqs - 1);
+        q0 = first[s], q1 = first[s + 1], length = lengths[s];
+        upto = up_to_lane(lane < A.n_seqs ? shape_of(A, q0, q1, length).count() : 0);
     }
-    static __device__ __forceinline__ long long up_to_lane(long long v, int lane)
+    __device__ __forceinline__ int count(int s) const { return s < A.n_seqs ? shape_of(A, first[s], first[s + 1], lengths[s]).count() : 0; }
+    __device__ __forceinline__ int up_to_lane(int v) const
     {
         for (int d = 1; d < 64; d <<= 1) {
-            const long long u = from_lane(v, max(lane - d, 0));
+            const int u = __shfl_up(v, d);
             if (lane >= d) v += u;
         }
         return v;
     }
-    // the tiles before sequence `end`
-    __device__ __forceinline__ long long before(int end) const
+    __device__ __forceinline__ void entries(int s, int &from, int &to, int &len) const      // of one sequence
     {
-        long long sum = 0;
-        for (int s = lane; s < end; s += 64) sum += count(s);
-        return from_lane(up_to_lane(sum, lane), 63);
+        if (s < 64) {      // at hand
+            from = __builtin_amdgcn_readlane(q0, s), to = __builtin_amdgcn_readlane(q1, s), len = __builtin_amdgcn_readlane(length, s);
+        } else {
+            typedef const __attribute__((address_space(4))) int *Uniform;
+            from = ((Uniform)first)[s], to = ((Uniform)first)[s + 1], len = ((Uniform)lengths)[s];
+        }
     }
-    __device__ __forceinline__ int locate(long long &at) const
+    __device__ __forceinline__ int of_block(int block) const
     {
+        if (A.n_seqs > 64) return sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
+        return max(__popcll(__ballot(lane < A.n_seqs && block_start(q0, lane, A.group, JOB) <= block)) - 1, 0);
+    }
+    // the tiles before sequence `end`
+    __device__ __forceinline__ int before(int end) const
+    {
+        if (end <= 64) return end > 0 ? __builtin_amdgcn_readlane(upto, end - 1) : 0;
+        int sum = 0;
+        for (int s = 64 + lane; s < end; s += 64) sum += count(s);
+        return __builtin_amdgcn_readlane(upto, 63) + __builtin_amdgcn_readlane(up_to_lane(sum), 63);
+    }
+    // the sequence that has tile `at` (which exists); `at` becomes the tile among its own
+    __device__ __forceinline__ int locate(int &at) const
+    {
+        int now = upto;
         for (int s = 0; s < A.n_seqs; s += 64) {
-            const long long upto = up_to_lane(count(s + lane), lane), here = from_lane(upto, 63);
+            if (s) now = up_to_lane(count(s + lane));
+            const int here = __builtin_amdgcn_readlane(now, 63);
             if (at < here) {
-                const int l = __popcll(__ballot(upto <= at));
-                if (l) at -= from_lane(upto, l - 1);
+                const int l = __popcll(__ballot(now <= at));
+                if (l) at -= __builtin_amdgcn_readlane(now, l - 1);
                 return s + l;
             }
             at -= here;
@@ -68,9 +89,17 @@ struct Sums {
         return A.n_seqs;
     }
 };
-// share w of `all` tiles in `shares`, of which there are never more than tiles: no share is empty
-__device__ __forceinline__ int shares_of(long long all, int wavefronts) { return (int)min((long long)wavefronts, max(all, 1ll)); }
-__device__ __forceinline__ long long share_start(long long all, int w, int shares) { return all * w / shares; }
+// All tiles in equal shares, the first ones longer by one; never more shares than tiles: none is empty
+struct Shares {
+    int n, each, longer;
+    __device__ __forceinline__ Shares(int all, int wavefronts) : n(min(wavefronts, max(all, 1))), each((int)((unsigned)all / (unsigned)n)), longer(all - each * n) {}
+    __device__ __forceinline__ int start(int w) const { return w * each + min(w, longer); }
+    __device__ __forceinline__ int of(int tile) const
+    {
+        const unsigned in_longer = (unsigned)(each + 1) * longer;
+        return (unsigned)tile < in_longer ? (int)((unsigned)tile / (unsigned)(each + 1)) : longer + (int)(((unsigned)tile - in_longer) / (unsigned)each);
+    }
+};
 
 // the part of a job that share w has: its first (0) or its last (1)
 template <int D> __device__ __forceinline__ PartOfRows<D, JOB> part_of(Address workspace, int kvh, int wavefronts, int w, int which)
@@ -82,7 +111,7 @@ template <int D> __device__ __forceinline__ PartOfRows<D, JOB> part_of(Address w
 struct Cursor {
     int s, block, t;
     Shape shape;
-    int n_k;
+    int q0, n_k;
 };
 
 template <class T, int D>
@@ -95,13 +124,12 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     const int kvh = blockIdx.x % A.kv_heads, wavefronts = (int)(gridDim.x / A.kv_heads) * WAVES, w = (int)(blockIdx.x / A.kv_heads) * WAVES + wave;
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
     typedef const __attribute__((address_space(4))) int *Uniform;
-    const Uniform first_u = (Uniform)first, lengths_u = (Uniform)lengths, table_u = (Uniform)global_at<const int>(A.table);
-    const Sums sums_of = {A, first, lengths, lane};
-    const long long all = sums_of.before(A.n_seqs);
-    const int shares = __builtin_amdgcn_readfirstlane(shares_of(all, wavefronts));
-    if (w >= shares) return;
-    long long begin = share_start(all, w, shares);
-    const int n = __builtin_amdgcn_readfirstlane((int)(share_start(all, w + 1, shares) - begin));
+    const Uniform table_u = (Uniform)global_at<const int>(A.table);
+    const Sums sums_of(A, first, lengths, lane);
+    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
+    if (w >= shares.n) return;
+    int begin = shares.start(w);
+    const int n = shares.start(w + 1) - begin;
     if (n <= 0) return;
 
     auto visit = [&](Cursor &c) RB_INLINE {      // sequence c.s, or nothing behind the last
@@ -110,8 +138,11 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
             c.n_k = 0;
             return;
         }
-        c.shape = shape_of(A, first_u[c.s], first_u[c.s + 1], lengths_u[c.s]);
-        c.n_k = positions(lengths_u[c.s], A.width, A.page_shift);
+        int q0, q1, length;
+        sums_of.entries(c.s, q0, q1, length);
+        c.q0 = min(max(q0, 0), A.tokens_q);
+        c.shape = shape_of(A, q0, q1, length);
+        c.n_k = positions(length, A.width, A.page_shift);
     };
     auto advance = [&](Cursor &c) RB_INLINE {
         if (++c.t < c.shape.tiles) return;
@@ -127,8 +158,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     at.s = __builtin_amdgcn_readfirstlane(sums_of.locate(begin));
     if (at.s >= A.n_seqs) return;
     visit(at);
-    at.block = __builtin_amdgcn_readfirstlane((int)(begin / at.shape.tiles));
-    at.t = __builtin_amdgcn_readfirstlane((int)(begin % at.shape.tiles));
+    at.block = __builtin_amdgcn_readfirstlane((int)((unsigned)begin / (unsigned)at.shape.tiles));
+    at.t = begin - at.block * at.shape.tiles;
     ahead = at;
 
     constexpr int LOADS = Part<D, KEYS, 1>::LOADS;
@@ -172,10 +203,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     int limit, least, from_t, token, head;
     bool real, found;
     auto start = [&]() RB_INLINE {
-        const int q0 = min(max(first_u[at.s], 0), A.tokens_q), n_q = at.shape.rows / A.group, row0 = at.block * JOB;
+        const int n_q = at.shape.rows / A.group, row0 = at.block * JOB;
         const int row = min(row0 + (lane & 31), at.shape.rows - 1);
         real = row0 + (lane & 31) < at.shape.rows;
-        token = q0 + row / A.group;
+        token = at.q0 + row / A.group;
         head = kvh * A.group + row % A.group;
         limit = at.n_k - n_q + row / A.group;
         least = at.n_k - n_q + row0 / A.group;
@@ -183,14 +214,16 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         const uint8_t *from = global_at<const uint8_t>(A.q.at) + token * A.q.token + head * A.q.head;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) q[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from + k * 32 + h * 16) : (v4u)(0u);
-        // waited for here, once a job: where they are used, the compiler would wait for all loads at every tile
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) asm volatile("" : "+v"(q[k]));
 #pragma unroll
         for (int b = 0; b < B; ++b) sums[b] = (v16f)(0.f);
         top = RB_NEG_INF;
         total = 0.f;
         found = false;
+    };
+    // Waited for once a job: where the rows are used, the compiler would wait for all loads at every tile
+    auto rows_arrived = [&]() RB_INLINE {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) asm volatile("" : "+v"(q[k]));
     };
     bool first_job = true;
     auto finish = [&]() RB_INLINE {      // with tile at.t
@@ -210,7 +243,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     };
 
     auto step = [&](int i, uint8_t *keys, uint8_t *values) RB_INLINE {
-        if (i == 0 || at.t == 0) start();
+        if (i > 0 && at.t == 0) {
+            start();
+            rows_arrived();
+        }
         loads_arrived<3 * LOADS>();
         v16f x = {};
         stream_operands<D / 16, 4>([&](int k) RB_INLINE { return rows.read(keys, 0, k); }, [&](int k, v4u a) RB_INLINE { x = T::mfma(a, q[k], x); });
@@ -265,12 +301,14 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
 
     uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS), *const kb = keys_b + wave * L::bytes(KEYS), *const vb = values_b + wave * L::bytes(KEYS);
     ask_pages(ahead);
+    start();
     load(0, k_base, ka);
     load(0, v_base, va);
     next_ahead();
     load(1, k_base, kb);
     load(1, v_base, vb);
     next_ahead();
+    rows_arrived();
     for (int i = 0; i < n; i += 2) {
         step(i, ka, va);
         if (i + 1 < n) step(i + 1, kb, vb);
@@ -279,27 +317,26 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
 }
 
 // A job that several wavefronts had parts of
-template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, int wavefronts)
+template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, int wavefronts, int joined)
 {
-    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;
+    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads, row0 = blockIdx.y * joined;
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
-    const int s = sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
-    const Shape shape = shape_of(A, first[s], first[s + 1], lengths[s]);
-    const int b = block - block_start(first, s, A.group, JOB);
-    if (b < 0 || b >= shape.blocks) return;
-    const Sums sums_of = {A, first, lengths, lane};
-    const long long all = sums_of.before(A.n_seqs), from = sums_of.before(s) + (long long)b * shape.tiles;
-    const int shares = shares_of(all, wavefronts);
-    // the shares that have its first and its last tile: the last that start no later
-    auto share_of = [&](long long tile) { return (int)(((tile + 1) * shares - 1) / all); };
-    const int w0 = share_of(from), w1 = share_of(from + shape.tiles - 1);
+    const Sums sums_of(A, first, lengths, lane);
+    const int s = __builtin_amdgcn_readfirstlane(sums_of.of_block(block));
+    int q0, q1, length;
+    sums_of.entries(s, q0, q1, length);
+    const Shape shape = shape_of(A, q0, q1, length);
+    const int b = block - block_start(q0, s, A.group, JOB);
+    if (b < 0 || b >= shape.blocks || b * JOB + row0 >= shape.rows) return;
+    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
+    const int from = sums_of.before(s) + b * shape.tiles, w0 = shares.of(from), w1 = shares.of(from + shape.tiles - 1);
     if (w0 == w1) return;      // it has stored the result
-    const bool starts_inside = share_start(all, w0, shares) < from;      // the first part is that share's last, all others are their shares' first
-
-    const int n_q = shape.rows / A.group, n_k = positions(lengths[s], A.width, A.page_shift), q0 = min(max(first[s], 0), A.tokens_q);
+    const bool starts_inside = shares.start(w0) < from;      // the first part is that share's last, all others are their shares' first
+    const int n_q = shape.rows / A.group, n_k = positions(length, A.width, A.page_shift);
+    q0 = min(max(q0, 0), A.tokens_q);
     auto token = [&](int r) { return (b * JOB + r) / A.group; };
     join_rows<T, D>(
-        w1 - w0 + 1, 0, min(shape.rows - b * JOB, JOB), A.dim,
+        joined, w1 - w0 + 1, row0, min(shape.rows - b * JOB - row0, joined), A.dim,
         [&](int i) { return part_of<D>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
         [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + token(r)) * A.heads + kvh * A.group + (b * JOB + r) % A.group) * (A.dim * 2); },
         [&](int r) { return n_k - n_q + token(r) < 0; });
@@ -314,13 +351,18 @@ template <class T, int D> int launch(const Args &A, int compute_units, hipStream
     const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, JOB) * A.kv_heads;
     if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
     hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES), 0, stream, A);
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs), dim3(256), 0, stream, A, groups * WAVES);
+    const int rows = (int)std::min((long long)JOB, (long long)A.tokens_q * A.group), joined = rows_joined(jobs, rows);      // rows of one job, at most
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs, (rows + joined - 1) / joined), dim3(256), 0, stream, A, groups * WAVES, joined);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
 
 }  // namespace
 
-bool few_applies(int tokens, int n_seqs, int group) { return (long long)tokens * group <= (long long)JOB * n_seqs; }
+bool few_applies(int tokens, int n_seqs, int group, long long positions)
+{
+    const long long tiles = block_numbers(tokens, n_seqs, group, JOB) * (std::min(positions, 0x7fffffffll) / KEYS + 1);
+    return (long long)tokens * group <= (long long)JOB * n_seqs && tiles < 0x7fffffffll;
+}
 
 size_t few_workspace_bytes(int kv_heads, int dim, int compute_units)
 {

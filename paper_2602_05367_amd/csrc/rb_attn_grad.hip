@@ -117,7 +117,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(cons
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     const int s = sequence_of_block(first_k, A.n_seqs, 1, BN, block, lane);
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
-    const int key0 = (block - block_start(first_k, s, 1, BN)) * BN;
+    const int key0 = (block - block_start(first_k[s], s, 1, BN)) * BN;
     if (key0 < 0 || key0 >= S.n_k) return;
     const int ahead = S.n_k - S.n_q;
     const int my_key = key0 + wave * 32 + (lane & 31), key = min(my_key, S.n_k - 1);
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     const int s = sequence_of_block(first_q, A.n_seqs, A.group, BN, block, lane);
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
-    const int row0 = (block - block_start(first_q, s, A.group, BN)) * BN, n_rows = S.n_q * A.group;
+    const int row0 = (block - block_start(first_q[s], s, A.group, BN)) * BN, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
 
     const int my_row = row0 + wave * 32 + (lane & 31);
