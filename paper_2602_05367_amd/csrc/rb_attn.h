@@ -143,6 +143,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const uint8_t *bas
 template <int D> struct Rows {
     int row, piece;
     __device__ __forceinline__ Rows(int lane) : row(Tile<D>::row_at(lane & 31)), piece(((lane >> 5) ^ Tile<D>::spread(lane & 31)) * 16) {}
+    __device__ __forceinline__ void write(uint8_t *tile, int b, int k, v4u v) const
+    {
+        *(lds_v4u *)(lds_byte *)(tile + (row + (piece ^ (k * 32 & (D == 128 ? 192 : 96)))) + (k * 32 & (D == 128 ? ~192 : ~96)) + 32 / Tile<D>::GROUP_ROWS * Tile<D>::GROUP * b) = v;
+    }
     __device__ __forceinline__ v4u read(const uint8_t *tile, int b, int k) const
     {
         constexpr int MOVED = D == 128 ? 192 : 96;      // bits of a piece's place that the permutation touches

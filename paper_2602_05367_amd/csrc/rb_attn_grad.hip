@@ -1,9 +1,13 @@
 // Gradient of attention over packed prompts.  With p_ij = exp(c q_i . k_j - lse_i), given do:
 //   dv_j = sum_i p_ij do_i        dp_ij = do_i . v_j        delta_i = do_i . o_i
 //   ds_ij = c p_ij (dp_ij - delta_i)        dq_i = sum_j ds_ij k_j        dk_j = sum_i ds_ij q_i
-// Two kernels, one with the keys in place and the queries going by (dk, dv: four products), one the other way
-// round (dq: three).  The scores are computed twice, seven products instead of five; in return every sum has one owner, which
-// adds in one order: no atomics, the same bits every time, and the query heads that share a key head are summed in registers.
+// Two kernels, one with the queries in place and the keys going by (dq), then one the other way round (dk, dv).  The scores are computed twice; in return
+// every sum has one owner, which adds in one order: no atomics, the same bits every time, and the query heads that share a key head are summed in registers.
+//
+// o comes rounded, so do_i . o_i is off by some 2^-12 |do_i| |o_i|: as much as the rounding of ds does to dq and dk again.  The first kernel mends that: over a row,
+// sum_j p_ij (dp_ij - delta_i) is what delta_i lacks (the weights add up to one), so it sums that beside dq, and sum_j p_ij k_j, which
+// the missing part would have been multiplied with, and stores the full delta for the second kernel.  One product more than the
+// five of the definition and the two that are computed twice.
 //
 // ds is rounded to the inputs' type before it meets k and q.  In fp16 that takes a scale: ds is p times
 // something of the size of do, and both are small.  Twice dim times the largest finite |do| and |v| bounds
@@ -18,7 +22,7 @@ namespace rb {
 namespace attn {
 namespace {
 
-constexpr int WAVES = 4, ROWS = 64;
+constexpr int ROWS = 64;
 
 struct GradArgs {
     Side q, k, v, o;                    // o: strides of the contiguous o, do and dq
@@ -87,32 +91,52 @@ __device__ __forceinline__ float scale_for(float a, float b, int dim)
 }
 
 // An infinity or a NaN in the tile?  (see make_finite: here the tile itself is needed as it is, and what is read transposed is cleaned)
-template <class T, int D> __device__ __forceinline__ void look_through(const uint8_t *tile, int *found, int tid)
+template <class T, int D, int R, int W> __device__ __forceinline__ void look_through(const uint8_t *tile, int *found, int tid)
 {
     using L = Tile<D>;
 #pragma unroll
-    for (int i = 0; i < ROWS / L::GROUP_ROWS / WAVES; ++i) {
-        const v4u w = *(const lds_v4u *)(lds_byte *)(tile + (i * WAVES + (tid >> 6)) * L::GROUP + (tid & 63) * 16);
+    for (int i = 0; i < R / L::GROUP_ROWS / W; ++i) {
+        const v4u w = *(const lds_v4u *)(lds_byte *)(tile + (i * W + (tid >> 6)) * L::GROUP + (tid & 63) * 16);
         if (not_finite<T>(w.x) || not_finite<T>(w.y) || not_finite<T>(w.z) || not_finite<T>(w.w)) *found = 1;
     }
 }
-template <class T> __device__ __forceinline__ v4u cleaned(v4u w, bool dirty) { return dirty ? finite_part<T>(w) : w; }
+// sums of the second of two wavefronts are added to the first's, by way of LDS (all wavefronts of the workgroup call this); true in the first
+template <int E> __device__ __forceinline__ bool add_halves(v16f (&sums)[E], uint8_t *by, int half, int lane)
+{
+    if (half == 1)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *(v4f *)(by + (e * 4 + i / 4) * 1024 + lane * 16) = (v4f){sums[e][i], sums[e][i + 1], sums[e][i + 2], sums[e][i + 3]};
+    __syncthreads();
+    if (half == 0)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const v4f other = *(const v4f *)(by + (e * 4 + i / 4) * 1024 + lane * 16);
+                sums[e][i] += other[0], sums[e][i + 1] += other[1], sums[e][i + 2] += other[2], sums[e][i + 3] += other[3];
+            }
+    __syncthreads();
+    return half == 0;
+}
 
 // --------------------------------------------------------------- dk and dv ---
-// A workgroup keeps 128 keys and values of one key head, 32 per wavefront as right operands in registers, and takes the queries
-// and do of all its query heads, 64 tokens at a time, through LDS.
-constexpr int BN = 32 * WAVES;
+// A workgroup keeps 128 keys and values of one key head in LDS and takes the queries and do of all its query heads, 64 rows at a
+// time, through LDS.  Eight wavefronts: four times 32 keys, by the upper and the lower 32 rows of a tile, whose sums are added at the end.
+constexpr int BN = 128;
 
 template <class T, int D>
-__global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(const GradArgs A)
+__global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
 {
     using L = Tile<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t queries_a[L::bytes(ROWS)], outs_a[L::bytes(ROWS)], queries_b[L::bytes(ROWS)], outs_b[L::bytes(ROWS)];
+    constexpr int W = 8, LOADS = Part<D, ROWS, W>::LOADS, E = D / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t queries_a[L::bytes(ROWS)], outs_a[L::bytes(ROWS)], queries_b[L::bytes(ROWS)], outs_b[L::bytes(ROWS)], keys[L::bytes(BN)], values[L::bytes(BN)];
     // what the rows' sums of products start from: -lse in units of the scores, -delta
     __shared__ __attribute__((aligned(16))) float rows_a[2][ROWS], rows_b[2][ROWS];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3, half = wave >> 2;
     const int kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;      // causal: the first keys have the most rows
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     const int s = sequence_of_block(first_k, A.n_seqs, 1, BN, block, lane);
@@ -120,47 +144,47 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(cons
     const int key0 = (block - block_start(first_k[s], s, 1, BN)) * BN;
     if (key0 < 0 || key0 >= S.n_k) return;
     const int ahead = S.n_k - S.n_q;
-    const int my_key = key0 + wave * 32 + (lane & 31), key = min(my_key, S.n_k - 1);
-    const int block_last = min(key0 + BN, S.n_k) - 1, wave_first = key0 + wave * 32, wave_last = min(wave_first + 31, S.n_k - 1);
+    const int my_key = key0 + part * 32 + (lane & 31), key = min(my_key, S.n_k - 1);
+    const int block_last = min(key0 + BN, S.n_k) - 1, wave_first = key0 + part * 32, wave_last = min(wave_first + 31, S.n_k - 1);
 
-    v4u kk[D / 16], vv[D / 16];
-    {
-        const uint8_t *from_k = global_at<const uint8_t>(A.k.at) + (long long)(S.k0 + key) * A.k.token + kvh * A.k.head;
-        const uint8_t *from_v = global_at<const uint8_t>(A.v.at) + (long long)(S.k0 + key) * A.v.token + kvh * A.v.head;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            kk[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_k + k * 32 + h * 16) : (v4u)(0u);
-            vv[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_v + k * 32 + h * 16) : (v4u)(0u);
-        }
-    }
     float unit = 1.f;      // taken out of dp - delta
     if (T::GRAD_BIAS)
         unit = scale_for(most_of(global_at<const float>(A.most_o), A.heads, kvh * A.group, A.group, S.q0, S.n_q, lane),
                          most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
 
-    const Part<D, ROWS, WAVES> q_part(A.q.token, A.dim, wave * (ROWS / WAVES), lane), o_part(A.o.token, A.dim, wave * (ROWS / WAVES), lane);
+    const Part<D, ROWS, W> q_part(A.q.token, A.dim, wave * (ROWS / W), lane), o_part(A.o.token, A.dim, wave * (ROWS / W), lane);
     const int tile0 = A.causal ? max(key0 - ahead, 0) / ROWS : 0, tiles = (S.n_q + ROWS - 1) / ROWS - tile0;
     const int steps = __builtin_amdgcn_readfirstlane(tiles > 0 ? tiles * A.group : 0);
     float next_lse = 0.f, next_delta = 0.f;      // of one row of the next tile, in the first wavefront
-    auto load = [&](int n, uint8_t *queries, uint8_t *outs) {
-        const int g = n / tiles, t = tile0 + n % tiles, head = kvh * A.group + g;
+    int load_g = 0, load_t = tile0, t = tile0;      // the tile to be asked for, and the one at hand
+    auto load = [&](uint8_t *queries, uint8_t *outs) RB_INLINE {
+        const int head = kvh * A.group + load_g, row = S.q0 + load_t * ROWS, rows = S.n_q - load_t * ROWS;
         if (wave == 0) {
-            const long long at = (long long)(S.q0 + min(t * ROWS + lane, S.n_q - 1)) * A.heads + head;
+            const long long at = (long long)(row + min(lane, rows - 1)) * A.heads + head;
             next_lse = global_at<const float>(A.lse)[at];
             next_delta = global_at<const float>(A.delta)[at];
         }
-        const uint8_t *q_from = global_at<const uint8_t>(A.q.at) + (long long)(S.q0 + t * ROWS) * A.q.token + head * A.q.head;
-        const uint8_t *o_from = global_at<const uint8_t>(A.go) + (long long)(S.q0 + t * ROWS) * A.o.token + head * A.o.head;
-        q_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(q_from, A.q.token, S.n_q - t * ROWS, ROWS, A.dim), queries, wave);
-        o_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(o_from, A.o.token, S.n_q - t * ROWS, ROWS, A.dim), outs, wave);
+        const uint8_t *q_from = global_at<const uint8_t>(A.q.at) + (long long)row * A.q.token + head * A.q.head;
+        const uint8_t *o_from = global_at<const uint8_t>(A.go) + (long long)row * A.o.token + head * A.o.head;
+        q_part.template load<0, LOADS>(rows_buffer(q_from, A.q.token, rows, ROWS, A.dim), queries, wave);
+        o_part.template load<0, LOADS>(rows_buffer(o_from, A.o.token, rows, ROWS, A.dim), outs, wave);
+        if (++load_t == tile0 + tiles) load_t = tile0, ++load_g;
     };
+
+    if (tid == 0) found = 0;
+    if (steps > 0) load(queries_a, outs_a);
+    {
+        const Part<D, BN, W> k_part(A.k.token, A.dim, wave * (BN / W), lane), v_part(A.v.token, A.dim, wave * (BN / W), lane);
+        const uint8_t *from_k = global_at<const uint8_t>(A.k.at) + (long long)(S.k0 + key0) * A.k.token + kvh * A.k.head;
+        const uint8_t *from_v = global_at<const uint8_t>(A.v.at) + (long long)(S.k0 + key0) * A.v.token + kvh * A.v.head;
+        k_part.template load<0, BN / L::GROUP_ROWS / W>(rows_buffer(from_k, A.k.token, S.n_k - key0, BN, A.dim), keys, wave);
+        v_part.template load<0, BN / L::GROUP_ROWS / W>(rows_buffer(from_v, A.v.token, S.n_k - key0, BN, A.dim), values, wave);
+    }
 
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
-    v16f sums_k[D / 32] = {}, sums_v[D / 32] = {};
-    if (tid == 0) found = 0;
-    auto step = [&](int n, uint8_t *queries, uint8_t *outs, float (&rows_of)[2][ROWS], uint8_t *next_queries, uint8_t *next_outs) {
-        const int t = tile0 + n % tiles;
+    v16f sums_k[E] = {}, sums_v[E] = {};
+    auto step = [&](int n, uint8_t *queries, uint8_t *outs, float (&rows_of)[2][ROWS], uint8_t *next_queries, uint8_t *next_outs) RB_INLINE {
         if (wave == 0) {
             // a row past the end: no weight (do is zero there as well)
             rows_of[0][lane] = t * ROWS + lane < S.n_q ? T::GRAD_BIAS / A.c - next_lse / A.scale : RB_NEG_INF;
@@ -168,73 +192,88 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void keys_kernel(cons
         }
         loads_arrived();
         __syncthreads();
-        if (n + 1 < steps) load(n + 1, next_queries, next_outs);
-        const bool partly = A.causal && block_last > ahead + t * ROWS;      // some key of the workgroup is not seen by all rows
+        if (n + 1 < steps) load(next_queries, next_outs);
         bool dirty = false;
-        if (partly) {
-            look_through<T, D>(queries, &found, tid);
-            look_through<T, D>(outs, &found, tid);
+        if (A.causal && block_last > ahead + t * ROWS) {      // some key of the workgroup is not seen by all rows
+            look_through<T, D, ROWS, W>(queries, &found, tid);
+            look_through<T, D, ROWS, W>(outs, &found, tid);
             __syncthreads();
             dirty = __builtin_amdgcn_readfirstlane(found) != 0;
         }
-        const bool any = !A.causal || wave_first <= ahead + t * ROWS + ROWS - 1;
-        const bool masked = A.causal && wave_last > ahead + t * ROWS;
+        const int row0 = t * ROWS + half * 32;
+        if (++t == tile0 + tiles) t = tile0;
+        const bool any = !A.causal || wave_first <= ahead + row0 + 31;
+        v16f x, y;
+        if (any) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            v16f x, y;
-            if (any) {
+            for (int i = 0; i < 16; ++i) {
+                x[i] = rows_of[0][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
+                y[i] = rows_of[1][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
+            }
+            // both operands come from LDS
+            constexpr int AHEAD = 3;
+            auto right = [&](int i) RB_INLINE { return rows.read(i % 2 ? values : keys, part, i / 2); };
+            v4u r[AHEAD];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[i] = rows_of[0][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
-                    y[i] = rows_of[1][b * 32 + 8 * (i / 4) + 4 * h + i % 4];
-                }
-stream_operands<D / 8, 4>([&](int i) { return rows.read(i % 2 ? outs : queries, b, i / 2); },
-                                          [&](int i, v4u a) {
+            for (int i = 0; i < AHEAD; ++i) r[i] = right(i);
+            stream_operands<D / 8, AHEAD>([&](int i) RB_INLINE { return rows.read(i % 2 ? outs : queries, half, i / 2); },
+                                          [&](int i, v4u a) RB_INLINE {
                                               if (i % 2)
-                                                  y = T::mfma(a, vv[i / 2], y);
+                                                  y = T::mfma(a, r[i % AHEAD], y);
                                               else
-                                                  x = T::mfma(a, kk[i / 2], x);
+                                                  x = T::mfma(a, r[i % AHEAD], x);
+                                              if (i + AHEAD < D / 8) r[i % AHEAD] = right(i + AHEAD);
                                           });
-            }
-            if (!any) continue;
-            const int least = my_key - ahead - t * ROWS - b * 32 - 4 * h;      // the first row that sees this key
-            uint32_t w[8], z[8];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float p[2], d[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = i + j;
-                    p[j] = __builtin_amdgcn_exp2f(x[r] * A.c);
-                    d[j] = p[j] * y[r] * unit;
-                    if (masked && 8 * (r / 4) + r % 4 < least) p[j] = d[j] = 0.f;
-                }
-                w[i / 2] = T::pack(p[0], p[1]);
-                z[i / 2] = T::pack(d[0], d[1]);
-            }
-constexpr int E = D / 32;
-            const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
-            stream_operands<4 * E, 4>([&](int i) { return columns.read(i % 2 ? queries : outs, i / 2 % E, 2 * b + i / (2 * E)); },
-                                      [&](int i, v4u a) {
-                                          const int e = i / 2 % E, k = i / (2 * E);
-                                          if (i % 2)
-                                              sums_k[e] = T::mfma(cleaned<T>(a, dirty), dz[k], sums_k[e]);
-                                          else
-                                              sums_v[e] = T::mfma(cleaned<T>(a, dirty), pw[k], sums_v[e]);
-                                      });
         }
+        if (dirty) {      // everybody has the scores: what is read transposed is cleaned
+            __syncthreads();
+            make_finite<T, D, ROWS, W>(queries, &found, tid);
+            make_finite<T, D, ROWS, W>(outs, &found, tid);
+            __syncthreads();
+        }
+        if (!any) return;
+        const bool masked = A.causal && wave_last > ahead + row0;
+        const int least = my_key - ahead - row0 - 4 * h;      // the first row that sees this key
+        uint32_t w[8], z[8];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            float p[2], d[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = i + j;
+                p[j] = __builtin_amdgcn_exp2f(x[r] * A.c);
+                d[j] = p[j] * y[r] * unit;
+                if (masked && 8 * (r / 4) + r % 4 < least) p[j] = d[j] = 0.f;
+            }
+            w[i / 2] = T::pack(p[0], p[1]);
+            z[i / 2] = T::pack(d[0], d[1]);
+        }
+        const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
+        stream_operands<4 * E, 4>([&](int i) RB_INLINE { return columns.read(i % 2 ? queries : outs, i / 2 % E, 2 * half + i / (2 * E)); },
+                                  [&](int i, v4u a) RB_INLINE {
+                                      const int e = i / 2 % E, k = i / (2 * E);
+                                      if (i % 2)
+                                          sums_k[e] = T::mfma(a, dz[k], sums_k[e]);
+                                      else
+                                          sums_v[e] = T::mfma(a, pw[k], sums_v[e]);
+                                  });
     };
-    if (steps > 0) load(0, queries_a, outs_a);
     for (int n = 0; n < steps; n += 2) {
         step(n, queries_a, outs_a, rows_a, queries_b, outs_b);
         if (n + 1 < steps) step(n + 1, queries_b, outs_b, rows_b, queries_a, outs_a);
     }
+    loads_arrived();      // (the values, where there are no rows)
     __syncthreads();
-    if (__builtin_amdgcn_readfirstlane(found))      // (only the rows of tiles that were cleaned, and their keys see it)
+    if (__builtin_amdgcn_readfirstlane(found) && half == 0)      // (only the rows of tiles that were cleaned, and their keys see it)
         for (int g = 0; g < A.group; ++g)
             for (int r = tile0 * ROWS; r < min(S.n_q, (max(block_last - ahead, 0) + ROWS - 1) / ROWS * ROWS); ++r)
-                add_not_finite<T, D>(sums_v, global_at<const uint8_t>(A.go) + (S.q0 + r) * A.o.token + (kvh * A.group + g) * A.o.head, A.dim, h, my_key <= ahead + r);
+                add_not_finite<T, D>(sums_v, global_at<const uint8_t>(A.go) + (long long)(S.q0 + r) * A.o.token + (kvh * A.group + g) * A.o.head, A.dim, h, my_key <= ahead + r);
 
+    uint8_t *const mine = part == 0 ? queries_a : part == 1 ? outs_a : part == 2 ? queries_b : outs_b;
+    static_assert(E * 4096 <= L::bytes(ROWS), "sums of 32 keys");
+    add_halves<E>(sums_v, mine, half, lane);
+    add_halves<E>(sums_k, mine, half, lane);
+    if (half == 1) return;
     const bool real = my_key < S.n_k;
     const long long at = ((long long)(S.k0 + key) * A.kv_heads + kvh) * (A.dim * 2);
     store_columns<T, D>(sums_v, 1.f / (1 << T::GRAD_BIAS), global_at<uint8_t>(A.dv) + at, A.dim, h, real, false);
@@ -242,15 +281,19 @@ constexpr int E = D / 32;
 }
 
 // ---------------------------------------------------------------------- dq ---
-// As the forward kernel: 128 rows of one key head, 32 per wavefront, with q and do as right operands in registers; keys and values go by.
+// The same the other way round: 128 rows' q and do of one key head stay in LDS, keys and values go by, 64 at a time.  Eight wavefronts: four times 32 rows,
+// by the first and the second 32 keys of a tile, whose sums are added at the end.
 template <class T, int D>
-__global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A)
+__global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
 {
     using L = Tile<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t keys_a[L::bytes(ROWS)], values_a[L::bytes(ROWS)], keys_b[L::bytes(ROWS)], values_b[L::bytes(ROWS)];
+    constexpr int W = 8, KEYS = 64, LOADS = Part<D, KEYS, W>::LOADS, E = D / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t keys_a[L::bytes(KEYS)], values_a[L::bytes(KEYS)], keys_b[L::bytes(KEYS)], values_b[L::bytes(KEYS)];
+    __shared__ __attribute__((aligned(16))) uint8_t queries[L::bytes(BN)], outs[L::bytes(BN)];
+    __shared__ float lacking_of[2][BN];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3, half = wave >> 2;
     const int kvh = blockIdx.x % A.kv_heads;
     int block = blockIdx.x / A.kv_heads;
     if (A.causal) block = (int)(gridDim.x / A.kv_heads) - 1 - block;
@@ -260,101 +303,126 @@ __global__ __launch_bounds__(64 * WAVES, 2) void queries_kernel(const GradArgs A
     const int row0 = (block - block_start(first_q[s], s, A.group, BN)) * BN, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
 
-    const int my_row = row0 + wave * 32 + (lane & 31);
+    const int my_row = row0 + part * 32 + (lane & 31);
     const int row = min(my_row, n_rows - 1), token = row / A.group, head = kvh * A.group + row % A.group;
     const int ahead = S.n_k - S.n_q;
     auto last_key = [&](int r) { return A.causal ? min(ahead + min(r, n_rows - 1) / A.group, S.n_k - 1) : S.n_k - 1; };
     const int limit = A.causal ? ahead + token : S.n_k - 1;
     const int block_least = last_key(row0), block_most = last_key(row0 + BN - 1);
-    const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32 + 31));
-    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + ROWS - 1) / ROWS;
+    const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + part * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + part * 32 + 31));
+    const int n_tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS;
 
-    v4u q[D / 16], go[D / 16];
-    const long long row_at = (long long)(S.q0 + token) * A.o.token + head * A.o.head;
-    {
-        const uint8_t *from_q = global_at<const uint8_t>(A.q.at) + (S.q0 + token) * A.q.token + head * A.q.head, *from_o = global_at<const uint8_t>(A.go) + row_at;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            q[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_q + k * 32 + h * 16) : (v4u)(0u);
-            go[k] = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_o + k * 32 + h * 16) : (v4u)(0u);
-        }
-    }
-    float unit = 1.f;      // here of the row alone: do is in registers
-    if (T::GRAD_BIAS) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t lo = go[k][j] & 0x7fffu, hi = go[k][j] >> 16 & 0x7fffu;
-                top = max(top, max(lo < T::EXPONENT ? lo : 0u, hi < T::EXPONENT ? hi : 0u));
-            }
-        unit = scale_for(over_halves_max(T::widen(top)), most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
-    }
-    const long long stat = (long long)(S.q0 + token) * A.heads + head;
-    const float zero_at = global_at<const float>(A.lse)[stat] * LOG2E - T::GRAD_BIAS, delta = global_at<const float>(A.delta)[stat] * unit;
-
-    const Part<D, ROWS, WAVES> k_part(A.k.token, A.dim, wave * (ROWS / WAVES), lane), v_part(A.v.token, A.dim, wave * (ROWS / WAVES), lane);
+    const Part<D, KEYS, W> k_part(A.k.token, A.dim, wave * (KEYS / W), lane), v_part(A.v.token, A.dim, wave * (KEYS / W), lane);
     const uint8_t *k_base = global_at<const uint8_t>(A.k.at) + S.k0 * A.k.token + kvh * A.k.head;
     const uint8_t *v_base = global_at<const uint8_t>(A.v.at) + S.k0 * A.v.token + kvh * A.v.head;
-    auto load = [&](int t, uint8_t *keys, uint8_t *values) {
-        k_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(k_base + (long long)t * ROWS * A.k.token, A.k.token, S.n_k - t * ROWS, ROWS, A.dim), keys, wave);
-        v_part.template load<0, ROWS / L::GROUP_ROWS / WAVES>(rows_buffer(v_base + (long long)t * ROWS * A.v.token, A.v.token, S.n_k - t * ROWS, ROWS, A.dim), values, wave);
+    auto load = [&](int t, uint8_t *keys, uint8_t *values) RB_INLINE {
+        k_part.template load<0, LOADS>(rows_buffer(k_base + (long long)t * KEYS * A.k.token, A.k.token, S.n_k - t * KEYS, KEYS, A.dim), keys, wave);
+        v_part.template load<0, LOADS>(rows_buffer(v_base + (long long)t * KEYS * A.v.token, A.v.token, S.n_k - t * KEYS, KEYS, A.dim), values, wave);
     };
+    if (tid == 0) found = 0;
+    if (n_tiles > 0) load(0, keys_a, values_a);
 
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
-    v16f sums[D / 32] = {};
-    if (tid == 0) found = 0;
-    auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) {
+    const long long row_at = (long long)(S.q0 + token) * A.o.token + head * A.o.head;
+    float unit = 1.f;      // here of the row alone
+    {
+        const uint8_t *from_q = global_at<const uint8_t>(A.q.at) + (S.q0 + token) * A.q.token + head * A.q.head, *from_o = global_at<const uint8_t>(A.go) + row_at;
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const v4u o = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_o + k * 32 + h * 16) : (v4u)(0u);
+            if (half == 0) {
+                rows.write(queries, part, k, k * 16 + h * 8 < A.dim ? *(const v4u *)(from_q + k * 32 + h * 16) : (v4u)(0u));
+                rows.write(outs, part, k, o);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t lo = o[j] & 0x7fffu, hi = o[j] >> 16 & 0x7fffu;
+                top = max(top, max(lo < T::EXPONENT ? lo : 0u, hi < T::EXPONENT ? hi : 0u));
+            }
+        }
+        if (T::GRAD_BIAS) unit = scale_for(over_halves_max(T::widen(top)), most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
+    }
+    const long long stat = (long long)(S.q0 + token) * A.heads + head;
+    const float delta = global_at<const float>(A.delta)[stat], zero_at = global_at<const float>(A.lse)[stat] * LOG2E - T::GRAD_BIAS;
+    const float less = -delta * unit;
+
+    v16f sums[E] = {}, means[E] = {};      // sum_j ds_ij k_j, sum_j p_ij k_j
+    float lacking = 0.f;                   // sum_j ds_ij
+    auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) RB_INLINE {
         loads_arrived();
-        __syncthreads();
+        meet();
         if (t + 1 < n_tiles) load(t + 1, next_keys, next_values);
         bool dirty = false;
-        if (block_least < min(t * ROWS + ROWS, S.n_k) - 1) {      // some row of the workgroup does not see all of the tile's keys
-            look_through<T, D>(keys, &found, tid);
-            __syncthreads();
+        if (block_least < min(t * KEYS + KEYS, S.n_k) - 1) {      // some row of the workgroup does not see all of the tile's keys
+            look_through<T, D, KEYS, W>(keys, &found, tid);
+            meet();
             dirty = __builtin_amdgcn_readfirstlane(found) != 0;
         }
-        const bool any = t * ROWS <= wave_most, masked = t * ROWS + ROWS - 1 > wave_least;
+        const int key0 = t * KEYS + half * 32;
+        const bool any = key0 <= wave_most;
+        v16f x = {}, y = {};
+        if (any) {
+            constexpr int AHEAD = 3;
+            auto right = [&](int i) RB_INLINE { return rows.read(i % 2 ? outs : queries, part, i / 2); };
+            v4u r[AHEAD];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            v16f x = {}, y = {};
-            if (any) {
-stream_operands<D / 8, 4>([&](int i) { return rows.read(i % 2 ? values : keys, b, i / 2); },
-                                          [&](int i, v4u a) {
+            for (int i = 0; i < AHEAD; ++i) r[i] = right(i);
+            stream_operands<D / 8, AHEAD>([&](int i) RB_INLINE { return rows.read(i % 2 ? values : keys, half, i / 2); },
+                                          [&](int i, v4u a) RB_INLINE {
                                               if (i % 2)
-                                                  y = T::mfma(a, go[i / 2], y);
+                                                  y = T::mfma(a, r[i % AHEAD], y);
                                               else
-                                                  x = T::mfma(a, q[i / 2], x);
+                                                  x = T::mfma(a, r[i % AHEAD], x);
+                                              if (i + AHEAD < D / 8) r[i % AHEAD] = right(i + AHEAD);
                                           });
-            }
-            if (!any) continue;
-            const int seen = limit - t * ROWS - b * 32 - 4 * h;
-            uint32_t z[8];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float d[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = i + j;
-                    d[j] = __builtin_amdgcn_exp2f(fmaf(x[r], A.c, -zero_at)) * fmaf(y[r], unit, -delta);
-                    if (masked && 8 * (r / 4) + r % 4 > seen) d[j] = 0.f;
-                }
-                z[i / 2] = T::pack(d[0], d[1]);
-            }
-constexpr int E = D / 32;
-            const v4u dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
-            stream_operands<2 * E, 4>([&](int i) { return columns.read(keys, i % E, 2 * b + i / E); },
-                                      [&](int i, v4u a) { sums[i % E] = T::mfma(cleaned<T>(a, dirty), dz[i / E], sums[i % E]); });
         }
+        if (dirty) {      // everybody has the scores: what is read transposed is cleaned
+            meet();
+            make_finite<T, D, KEYS, W>(keys, &found, tid);
+            meet();
+        }
+        if (!any) return;
+        const bool masked = key0 + 31 > wave_least;
+        const int seen = limit - key0 - 4 * h;
+        uint32_t w[8], z[8];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            float p[2], d[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = i + j;
+                p[j] = __builtin_amdgcn_exp2f(fmaf(x[r], A.c, -zero_at));
+                d[j] = p[j] * fmaf(y[r], unit, less);
+                if (masked && 8 * (r / 4) + r % 4 > seen) p[j] = d[j] = 0.f;
+            }
+            lacking += d[0] + d[1];
+            w[i / 2] = T::pack(p[0], p[1]);
+            z[i / 2] = T::pack(d[0], d[1]);
+        }
+        const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
+        stream_operands<2 * E, 4>([&](int i) RB_INLINE { return columns.read(keys, i % E, 2 * half + i / E); },
+                                  [&](int i, v4u a) RB_INLINE {
+                                      sums[i % E] = T::mfma(a, dz[i / E], sums[i % E]);
+                                      means[i % E] = T::mfma(a, pw[i / E], means[i % E]);
+                                  });
     };
-    if (n_tiles > 0) load(0, keys_a, values_a);
     for (int t = 0; t < n_tiles; t += 2) {
         step(t, keys_a, values_a, keys_b, values_b);
         if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
-    store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, false);
+    lacking = over_halves_sum(lacking) / (1 << T::GRAD_BIAS);      // in units of 2^GRAD_BIAS unit
+    if (h == 0) lacking_of[half][part * 32 + (lane & 31)] = lacking;
+    __syncthreads();
+    lacking = lacking_of[0][part * 32 + (lane & 31)] + lacking_of[1][part * 32 + (lane & 31)];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[e] -= means[e] * lacking;
+    uint8_t *const mine = part == 0 ? keys_a : part == 1 ? keys_b : part == 2 ? values_a : values_b;
+    static_assert(E * 4096 <= L::bytes(KEYS), "sums of 32 rows");
+    if (!add_halves<E>(sums, mine, half, lane)) return;
+    if (h == 0 && my_row < n_rows) global_at<float>(A.delta)[stat] = delta + lacking / unit;
+    store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, limit < 0);
 }
 
 template <class T, int D> int launch(const GradArgs &A, hipStream_t stream)
@@ -363,8 +431,8 @@ template <class T, int D> int launch(const GradArgs &A, hipStream_t stream)
     const long long keys = block_numbers(A.tokens_k, A.n_seqs, 1, BN) * A.kv_heads, queries = block_numbers(A.tokens_q, A.n_seqs, A.group, BN) * A.kv_heads;
     if (deltas > 0x7fffffffll || keys > 0x7fffffffll || queries > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     hipLaunchKernelGGL((delta_kernel<T>), dim3((unsigned)deltas), dim3(256), 0, stream, A);
-    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)keys), dim3(64 * WAVES), 0, stream, A);
-    hipLaunchKernelGGL((queries_kernel<T, D>), dim3((unsigned)queries), dim3(64 * WAVES), 0, stream, A);
+    hipLaunchKernelGGL((queries_kernel<T, D>), dim3((unsigned)queries), dim3(512), 0, stream, A);
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)keys), dim3(512), 0, stream, A);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
 
