@@ -505,20 +505,27 @@ def rb_scale_grads(G: torch.Tensor, packed: torch.Tensor, g: torch.Tensor, h: to
 
 
 # -------------------------------------------------- attention, its cache ---
-def _check_heads(x: torch.Tensor, dtype: torch.dtype, dim: int) -> None:
-    assert x.is_cuda and x.dim() == 3 and x.dtype == dtype and x.shape[2] == dim and (dim == 1 or x.stride(2) == 1)
-
-
-def _check_numbers(x: torch.Tensor, *shape) -> None:
-    assert x.is_cuda and x.dtype == torch.int32 and x.is_contiguous() and tuple(x.shape) == shape
+# (A call of these is a few microseconds of kernel: each attribute of a tensor is asked for once.)
+_I32 = torch.int32
 
 
 def _heads(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> rb_heads:
-    """Shapes and strides of q [tokens][heads][dim] and k, v [tokens][kv_heads][dim]."""
-    for x in (q, k, v):
-        _check_heads(x, k.dtype, k.shape[2])
-    assert k.shape == v.shape
-    return rb_heads(q.shape[1], k.shape[1], k.shape[2], _DTYPE_CODE[k.dtype], *q.stride()[:2], *k.stride()[:2], *v.stride()[:2])
+    """Shapes and strides of q [tokens][heads][dim] and k, v [tokens][kv_heads][dim], elements of a head contiguous."""
+    qs, ks, vs, dtype = q.stride(), k.stride(), v.stride(), k.dtype
+    _, heads, dim = q.shape
+    assert k.is_cuda and v.is_cuda and q.is_cuda and q.dtype is dtype and v.dtype is dtype and k.shape == v.shape
+    assert qs[2] == ks[2] == vs[2] == 1 and k.shape[2] == dim
+    return rb_heads(heads, k.shape[1], dim, _DTYPE_CODE[dtype], qs[0], qs[1], ks[0], ks[1], vs[0], vs[1])
+
+
+def _starts(first: torch.Tensor, first_k: torch.Tensor = None):
+    """Address of first int32 [n_seqs + 1], of first_k of the same length or None, and n_seqs."""
+    n = first.shape[0]
+    assert first.is_cuda and first.dtype is _I32 and first.dim() == 1 and first.is_contiguous()
+    if first_k is None:
+        return first.data_ptr(), None, n - 1
+    assert first_k.is_cuda and first_k.dtype is _I32 and first_k.shape == first.shape and first_k.is_contiguous()
+    return first.data_ptr(), first_k.data_ptr(), n - 1
 
 
 def rb_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, first_k: torch.Tensor = None,
@@ -526,17 +533,16 @@ def rb_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: tor
     """Attention over packed sequences: q [tokens][heads][dim], k and v [tokens][kv_heads][dim] (fp16 or bf16, any
     strides of tokens and heads), first int32 [n_seqs + 1]; returns o [tokens][heads][dim], or (o, lse fp32 [tokens][heads])."""
     H = _heads(q, k, v)
-    _check_numbers(first, first.numel())
-    if first_k is not None:
-        _check_numbers(first_k, first.numel())
+    at, at_k, n = _starts(first, first_k)
+    shape = q.shape
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert o.is_cuda and o.dtype == q.dtype and o.shape == q.shape and o.is_contiguous()
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+        o = torch.empty(shape, dtype=q.dtype, device=q.device)
+    else:
+        assert o.is_cuda and o.dtype is q.dtype and o.shape == shape and o.is_contiguous()
+    lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
     _check("rb_attn_prompt", lib.rb_attn_prompt(
-        ctypes.byref(H), q.data_ptr(), k.data_ptr(), v.data_ptr(), first.data_ptr(), None if first_k is None else first_k.data_ptr(),
-        first.numel() - 1, q.shape[0], k.shape[0], int(causal), q.shape[2] ** -0.5 if scale is None else scale, o.data_ptr(),
-        lse.data_ptr() if want_lse else None, _stream()))
+        ctypes.byref(H), q.data_ptr(), k.data_ptr(), v.data_ptr(), at, at_k, n, shape[0], k.shape[0], causal,
+        shape[2] ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr() if want_lse else None, _stream()))
     return (o, lse) if want_lse else o
 
 
@@ -544,19 +550,17 @@ def rb_attn_prompt_grad(go: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
                         first: torch.Tensor, first_k: torch.Tensor = None, causal: bool = True, scale: float = None):
     """(dq, dk, dv) of rb_attn_prompt, given go, the gradient of its result o, and its lse."""
     H = _heads(q, k, v)
-    _check_numbers(first, first.numel())
-    if first_k is not None:
-        _check_numbers(first_k, first.numel())
+    at, at_k, n = _starts(first, first_k)
+    shape, dtype, device = q.shape, q.dtype, q.device
     for x in (go, o):
-        assert x.is_cuda and x.dtype == q.dtype and x.shape == q.shape and x.is_contiguous()
-    assert lse.is_cuda and lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous()
-    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
-    n = lib.rb_attn_grad_workspace_bytes(ctypes.byref(H), q.shape[0], k.shape[0])
-    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+        assert x.is_cuda and x.dtype is dtype and x.shape == shape and x.is_contiguous()
+    assert lse.is_cuda and lse.dtype is torch.float32 and lse.shape == shape[:2] and lse.is_contiguous()
+    dq, dk, dv = (torch.empty(s, dtype=dtype, device=device) for s in (shape, k.shape, k.shape))
+    need = lib.rb_attn_grad_workspace_bytes(ctypes.byref(H), shape[0], k.shape[0])
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
     _check("rb_attn_prompt_grad", lib.rb_attn_prompt_grad(
-        ctypes.byref(H), go.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), first.data_ptr(),
-        None if first_k is None else first_k.data_ptr(), first.numel() - 1, q.shape[0], k.shape[0], int(causal),
-        q.shape[2] ** -0.5 if scale is None else scale, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), n, _stream()))
+        ctypes.byref(H), go.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), at, at_k, n, shape[0], k.shape[0],
+        causal, shape[2] ** -0.5 if scale is None else scale, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), need, _stream()))
     return dq, dk, dv
 
 
@@ -564,11 +568,12 @@ class Cache:
     """A paged cache over two tensors [pages][page_tokens][kv_heads][dim] of equal strides (fp16 or bf16)."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype
-        assert k.stride() == v.stride() and (k.shape[3] == 1 or k.stride(3) == 1)
-        self.k, self.v = k, v
+        assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype is v.dtype
+        strides = k.stride()
+        assert strides == v.stride() and strides[3] == 1
+        self.k, self.v, self.dtype = k, v, k.dtype
         pages, page_tokens, self.kv_heads, self.dim = k.shape
-        self._struct = rb_cache(k.data_ptr(), v.data_ptr(), pages, page_tokens, self.kv_heads, self.dim, _DTYPE_CODE[k.dtype], *k.stride()[:3])
+        self._struct = rb_cache(k.data_ptr(), v.data_ptr(), pages, page_tokens, self.kv_heads, self.dim, _DTYPE_CODE[k.dtype], *strides[:3])
 
     @classmethod
     def zeros(cls, pages: int, page_tokens: int, kv_heads: int, dim: int, dtype=torch.float16, device="cuda:0") -> "Cache":
@@ -578,12 +583,13 @@ class Cache:
         return self._struct
 
 
-def _check_sequences(first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor) -> int:
-    n = lengths.numel()
-    _check_numbers(first, n + 1)
-    _check_numbers(lengths, n)
-    _check_numbers(table, n, table.shape[-1])
-    return n
+def _sequences(first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
+    """Addresses of first int32 [n_seqs + 1], lengths [n_seqs] and table [n_seqs][width]; width, n_seqs."""
+    n, width = table.shape
+    assert first.is_cuda and lengths.is_cuda and table.is_cuda and first.dtype is _I32 and lengths.dtype is _I32 and table.dtype is _I32
+    assert first.shape == (n + 1,) and lengths.shape == (n,)
+    assert first.is_contiguous() and lengths.is_contiguous() and table.is_contiguous()
+    return first.data_ptr(), lengths.data_ptr(), table.data_ptr(), width, n
 
 
 def rb_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
@@ -591,41 +597,50 @@ def rb_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, first: torch
                     q_out: torch.Tensor = None):
     """New tokens k, v [tokens][kv_heads][dim] become the last of each sequence's lengths int32 [n_seqs] positions of the
     cache, with the rotary embedding of cos, sin fp32 [rows][rotary / 2] on k and q [tokens][heads][dim]; returns the turned q."""
-    n = _check_sequences(first, lengths, table)
+    at = _sequences(first, lengths, table)
     H = _heads(k if q is None else q, k, v)
-    assert H.kv_heads == cache.kv_heads and H.dim == cache.dim and k.dtype == cache.k.dtype
-    assert q is None or q.shape[0] == k.shape[0]
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert (q is None) == (q_out is None) and (q is None or (q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous()))
-    assert (cos is None) == (sin is None)
+    assert H.kv_heads == cache.kv_heads and H.dim == cache.dim and k.dtype is cache.dtype
+    tokens, from_q, to_q = k.shape[0], None, None
+    if q is not None:
+        shape = q.shape
+        assert shape[0] == tokens
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        else:
+            assert q_out.is_cuda and q_out.dtype is q.dtype and q_out.shape == shape and q_out.is_contiguous()
+        from_q, to_q = q.data_ptr(), q_out.data_ptr()
+    assert (q is None) == (q_out is None) and (cos is None) == (sin is None)
+    at_cos = at_sin = None
+    rows = half = 0
     if cos is not None:
-        for x in (cos, sin):
-            assert x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.dim() == 2 and x.shape == cos.shape
+        rows, half = cos.shape
+        assert cos.is_cuda and sin.is_cuda and cos.dtype is sin.dtype is torch.float32 and sin.shape == cos.shape
+        assert cos.is_contiguous() and sin.is_contiguous()
+        at_cos, at_sin = cos.data_ptr(), sin.data_ptr()
     _check("rb_cache_append", lib.rb_cache_append(
-        ctypes.byref(cache.struct()), ctypes.byref(H), None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
-        None if cos is None else cos.data_ptr(), None if cos is None else sin.data_ptr(), 0 if cos is None else cos.shape[0],
-        0 if cos is None else 2 * cos.shape[1], int(interleaved), first.data_ptr(), lengths.data_ptr(), table.data_ptr(), table.shape[1],
-        n, k.shape[0], None if q is None else q_out.data_ptr(), _stream()))
+        ctypes.byref(cache._struct), ctypes.byref(H), from_q, k.data_ptr(), v.data_ptr(), at_cos, at_sin, rows, 2 * half, interleaved,
+        *at, tokens, to_q, _stream()))
     return q_out
 
 
 def rb_attn_paged(cache: Cache, q: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, scale: float = None,
                   o: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """Attention of new tokens q [tokens][heads][dim], the last of each sequence's lengths positions, over the cache."""
-    n = _check_sequences(first, lengths, table)
-    _check_heads(q, cache.k.dtype, cache.dim)
+    at = _sequences(first, lengths, table)
+    shape, strides = q.shape, q.stride()
+    tokens, heads, dim = shape
+    assert q.is_cuda and q.dtype is cache.dtype and dim == cache.dim and strides[2] == 1
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert o.is_cuda and o.dtype == q.dtype and o.shape == q.shape and o.is_contiguous()
-    C, tokens, heads = ctypes.byref(cache.struct()), q.shape[0], q.shape[1]
+        o = torch.empty(shape, dtype=q.dtype, device=q.device)
+    else:
+        assert o.is_cuda and o.dtype is q.dtype and o.shape == shape and o.is_contiguous()
+    C = ctypes.byref(cache._struct)
     if workspace is None:
-        need = lib.rb_attn_paged_workspace_bytes(C, heads, n, tokens)
+        need = lib.rb_attn_paged_workspace_bytes(C, heads, at[4], tokens)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    at_ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     _check("rb_attn_paged", lib.rb_attn_paged(
-        C, q.data_ptr(), q.stride(0), q.stride(1), heads, first.data_ptr(), lengths.data_ptr(), table.data_ptr(), table.shape[1], n, tokens,
-        cache.dim ** -0.5 if scale is None else scale, o.data_ptr(), None if workspace is None else workspace.data_ptr(),
-        0 if workspace is None else workspace.numel(), _stream()))
+        C, q.data_ptr(), strides[0], strides[1], heads, *at, tokens, dim ** -0.5 if scale is None else scale, o.data_ptr(), at_ws, size, _stream()))
     return o
 
 
