@@ -270,6 +270,37 @@ __device__ __forceinline__ int sequence_of_block(const int *first, int n_seqs, i
     return last_not_beyond(n_seqs, block, lane, [&](int s) { return block_start(first[s], s, group, BM); });
 }
 
+// Of up to MOST_ORDERED sequences: their blocks in descending order of work, so that the longest start first and short ones fill the gaps.  count(n_q, n_k, x): how many
+// blocks of such a sequence have a work of x or more, all of them for x = 0; `most`: a bound on the work.  Lane s holds sequence s.  False: there are not so many blocks.
+// (Five sequences of 1 to 2048 tokens, 32 query and 8 key heads: see the kernels.)
+constexpr int MOST_ORDERED = 16;
+template <class Count> __device__ __forceinline__ bool nth_heaviest(int n_seqs, int n_q, int n_k, int nth, int most, int lane, int &s, int &block, Count count)
+{
+    auto all = [&](int x) {
+        int sum = 0;
+        for (int i = 0; i < n_seqs; ++i) sum += count(__builtin_amdgcn_readlane(n_q, i), __builtin_amdgcn_readlane(n_k, i), x);
+        return sum;
+    };
+    if (all(0) <= nth) return false;
+    int lo = 0, n = most + 1;      // the largest x of which there are more than nth lies in lo .. lo + n - 1; a lane looks at one x
+    while (n > 1) {
+        const int step = (n + 63) / 64, x = lo + min(lane * step, n - 1);
+        const int k = max(0, __popcll(__ballot(lane * step < n && all(x) > nth)) - 1);
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    const int here = lane < n_seqs ? count(n_q, n_k, lo) : 0, heavier = lane < n_seqs ? count(n_q, n_k, lo + 1) : 0;
+    nth -= all(lo + 1);      // among those of work lo, in the order of the sequences
+    int upto = here - heavier;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int v = __shfl_up(upto, d);
+        if (lane >= d) upto += v;
+    }
+    s = __builtin_amdgcn_readfirstlane(__popcll(__ballot(upto <= nth)));
+    block = __builtin_amdgcn_readlane(heavier, s) + nth - (s ? __builtin_amdgcn_readlane(upto, s - 1) : 0);
+    return true;
+}
+
 // One sequence's part of the work.  What the arrays say is brought into the range of the buffers: an array that
 // is not in order gives wrong results, but no access outside.
 struct Sequence {
@@ -285,6 +316,45 @@ __device__ __forceinline__ Sequence sequence_at(const int *first_q, const int *f
     r.k0 = min(max(entry(first_k, s), 0), tokens_k);
     r.n_k = min(max(entry(first_k, s + 1), r.k0), tokens_k) - r.k0;
     return r;
+}
+
+// Which sequence and which of its blocks a workgroup's number stands for; false: none.  Blocks of BM rows (keys: BM keys), heaviest first: causal rows see more the
+// later they are, causal keys are seen by more the earlier they are.
+template <int BM>
+__device__ __forceinline__ bool rows_of_workgroup(const int *first_q, const int *first_k, int n_seqs, int tokens_q, int tokens_k, int group, bool causal, int number, int numbers, int lane, int &s, int &block)
+{
+    if (n_seqs > 1 && n_seqs <= MOST_ORDERED) {
+        const int i = min(lane, n_seqs - 1);
+        const int q0 = min(max(first_q[i], 0), tokens_q), n_q = min(max(first_q[i + 1], q0), tokens_q) - q0, k0 = min(max(first_k[i], 0), tokens_k), n_k = min(max(first_k[i + 1], k0), tokens_k) - k0;
+        auto blocks = [&](int rows) { return (rows * group + BM - 1) / BM; };
+        if (!nth_heaviest(n_seqs, n_q, n_k, number, tokens_k, lane, s, block, [&](int q, int k, int x) {
+                if (x == 0 || !causal) return k >= x ? blocks(q) : 0;
+                return k < x ? 0 : min(blocks(q), (int)((long long)(k - x) * group / BM) + 1);
+            }))
+            return false;
+        if (causal) block = blocks(__builtin_amdgcn_readlane(n_q, s)) - 1 - block;
+        return true;
+    }
+    if (causal) number = numbers - 1 - number;
+    s = sequence_of_block(first_q, n_seqs, group, BM, number, lane);
+    block = number - block_start(first_q[s], s, group, BM);
+    return true;
+}
+template <int BM>
+__device__ __forceinline__ bool keys_of_workgroup(const int *first_q, const int *first_k, int n_seqs, int tokens_q, int tokens_k, bool causal, int number, int lane, int &s, int &block)
+{
+    if (n_seqs > 1 && n_seqs <= MOST_ORDERED) {
+        const int i = min(lane, n_seqs - 1);
+        const int q0 = min(max(first_q[i], 0), tokens_q), n_q = min(max(first_q[i + 1], q0), tokens_q) - q0, k0 = min(max(first_k[i], 0), tokens_k), n_k = min(max(first_k[i + 1], k0), tokens_k) - k0;
+        return nth_heaviest(n_seqs, n_q, n_k, number, tokens_q, lane, s, block, [&](int q, int k, int x) {
+            const int blocks = (k + BM - 1) / BM;
+            if (x == 0 || !causal) return q >= x ? blocks : 0;
+            return q < x || k < x ? 0 : min(blocks, (k - x) / BM + 1);
+        });
+    }
+    s = sequence_of_block(first_k, n_seqs, 1, BM, number, lane);
+    block = number - block_start(first_k[s], s, 1, BM);
+    return true;
 }
 
 // Operands of a call; strides in bytes.

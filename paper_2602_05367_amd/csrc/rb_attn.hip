@@ -17,32 +17,42 @@ namespace {
 // prompt of 8192 tokens, 64 query and 8 key heads of 128, causal, bf16: 1.00 ms, 1.10 PFLOP/s).  What was tried beside it: 32 keys at a time and
 // three wavefronts per SIMD, the same on long prompts and a fifth slower on short ones; a pipeline within a wavefront, scores of one half of a tile
 // beside the weights of the other, 1.08 ms; eight wavefronts and three tiles ahead, 1.09 ms; operand reads left to the compiler, 1.11 ms.
-constexpr int WAVES = 4, BM = 32 * WAVES, KEYS = 64;
-template <class T, int D, bool PAGED>
-__global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
+//
+// HALVES = 2: eight wavefronts, four of them with the first 32 keys of every tile and four with the second, joined at the end.  A step then takes little more than half
+// as long where a workgroup has a compute unit to itself; where there is a second one to fill it, there is nothing to gain.
+constexpr int BM = 128, KEYS = 64;
+template <class T, int D, bool PAGED, int HALVES>
+__global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 {
     using L = Tile<D>;
+    constexpr int WAVES = 4 * HALVES;
     // tiles as variables of their own: the compiler then knows that loads into one do not concern reads of another
     __shared__ __attribute__((aligned(16))) uint8_t keys_a[L::bytes(KEYS)], values_a[L::bytes(KEYS)], keys_b[L::bytes(KEYS)], values_b[L::bytes(KEYS)];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), quarter = wave & 3, half = wave >> 2;
     const int kvh = blockIdx.x % A.kv_heads;      // the workgroups of a head go to the same XCDs
     int block = blockIdx.x / A.kv_heads;
     const int split = PAGED ? block % A.splits : 0, n_blocks = (int)(gridDim.x / A.kv_heads) / (PAGED ? A.splits : 1);
     if (PAGED) block /= A.splits;
-    if (A.causal) block = n_blocks - 1 - block;      // the longest first
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
-    const int s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
+    int s, of_sequence;
+    if constexpr (PAGED) {
+        block = n_blocks - 1 - block;      // the longest first
+        s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
+        of_sequence = block - block_start(first_q[s], s, A.group, BM);
+    } else if (!rows_of_workgroup<BM>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.group, A.causal, block, n_blocks, lane, s, of_sequence)) {
+        return;
+    }
     Sequence S = sequence_at(first_q, PAGED ? first_q : first_k, s, A.tokens_q, PAGED ? A.tokens_q : A.tokens_k);
     if (PAGED) {
         S.k0 = 0;
         S.n_k = positions(__builtin_amdgcn_readfirstlane(first_k[s]), A.width, A.page_shift);
     }
-    const int row0 = (block - block_start(first_q[s], s, A.group, BM)) * BM, n_rows = S.n_q * A.group;
+    const int row0 = of_sequence * BM, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
 
-    const int my_row = row0 + wave * 32 + (lane & 31);
+    const int my_row = row0 + quarter * 32 + (lane & 31);
     const bool real = my_row < n_rows;
     const int row = min(my_row, n_rows - 1), token = row / A.group, head = kvh * A.group + row % A.group;
     // the last key that a row sees; -1 or less: none
@@ -50,7 +60,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     auto last_key = [&](int r) { return A.causal ? min(ahead + min(r, n_rows - 1) / A.group, S.n_k - 1) : S.n_k - 1; };
     const int limit = A.causal ? ahead + token : S.n_k - 1;
     const int block_least = last_key(row0), block_most = last_key(row0 + BM - 1);
-    const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + wave * 32 + 31));
+    const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + quarter * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + quarter * 32 + 31));
     const int tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS, parts = PAGED ? splits_of(tiles, A.splits) : 1;
     if (split >= parts) return;
     const int first_tile = tiles * split / parts, n_tiles = tiles * (split + 1) / parts;      // (the end of this workgroup's)
@@ -97,7 +107,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
 
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
-    constexpr int B = D / 32, H = KEYS / 32;
+    constexpr int B = D / 32, H = KEYS / 32 / HALVES;      // 32s of elements, and of keys of a tile
     v16f sums[B] = {};
     float top = RB_NEG_INF, total = 0.f;
     auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) RB_INLINE {
@@ -108,11 +118,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
             make_finite<T, D, KEYS, WAVES>(values, &found, tid);
             __syncthreads();
         }
-        if (t * KEYS > wave_most) return;
+        const int first_key = t * KEYS + half * 32;
+        if (first_key > wave_most) return;
         v16f x[H] = {};
-        stream_operands<H * D / 16, 6>([&](int i) RB_INLINE { return rows.read(keys, i % H, i / H); }, [&](int i, v4u a) RB_INLINE { x[i % H] = T::mfma(a, q[i / H], x[i % H]); });
-        if (t * KEYS + KEYS - 1 > wave_least) {
-            const int seen = limit - t * KEYS - 4 * h;
+        stream_operands<H * D / 16, 6>([&](int i) RB_INLINE { return rows.read(keys, half * H + i % H, i / H); }, [&](int i, v4u a) RB_INLINE { x[i % H] = T::mfma(a, q[i / H], x[i % H]); });
+        if (first_key + 32 * H - 1 > wave_least) {
+            const int seen = limit - first_key - 4 * h;
 #pragma unroll
             for (int b = 0; b < H; ++b)
 #pragma unroll
@@ -145,7 +156,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
             p[2 * b] = (v4u){w[0], w[1], w[2], w[3]};
             p[2 * b + 1] = (v4u){w[4], w[5], w[6], w[7]};
         }
-        stream_operands<2 * H * B, 4>([&](int i) RB_INLINE { return columns.read(values, i % B, i / B); }, [&](int i, v4u a) RB_INLINE { sums[i % B] = T::mfma(a, p[i / B], sums[i % B]); });
+        stream_operands<2 * H * B, 4>([&](int i) RB_INLINE { return columns.read(values, i % B, 2 * half * H + i / B); }, [&](int i, v4u a) RB_INLINE { sums[i % B] = T::mfma(a, p[i / B], sums[i % B]); });
     };
     if (tid == 0) found = 0;
     if (first_tile < n_tiles) {
@@ -158,6 +169,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     }
 
     __syncthreads();
+    if constexpr (HALVES == 2) {      // the second half's sums to the first, in units of the larger maximum
+        __shared__ float tops[BM], totals[BM];
+        static_assert(B * 4096 <= L::bytes(KEYS), "sums of 32 rows");
+        uint8_t *const by = quarter == 0 ? keys_a : quarter == 1 ? keys_b : quarter == 2 ? values_a : values_b;
+        const int r = quarter * 32 + (lane & 31);
+        total = over_halves_sum(total);
+        if (half == 1) {
+            if (h == 0) tops[r] = top, totals[r] = total;
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) *(v4f *)(by + (b * 4 + i / 4) * 1024 + lane * 16) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
+        }
+        __syncthreads();
+        if (half == 1) return;
+        const float now = fmaxf(top, tops[r]), mine = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(top - now), theirs = now == RB_NEG_INF ? 1.f : __builtin_amdgcn_exp2f(tops[r] - now);
+        top = now;
+        total = 0.5f * (total * mine + totals[r] * theirs);      // (both halves of the wavefront have all of it, and are added below)
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums[b][i] = sums[b][i] * mine + ((const v4f *)(by + (b * 4 + i / 4) * 1024 + lane * 16))[0][i % 4] * theirs;
+    }
     if (__builtin_amdgcn_readfirstlane(found))
         for (int r = max(max(block_least + 1, 0) / KEYS, first_tile) * KEYS; r <= min(wave_most, n_tiles * KEYS - 1); ++r)
             add_not_finite<T, D>(sums, v_base + (PAGED ? place(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), r) : r * A.v.token), A.dim, h, r <= limit);
@@ -165,7 +199,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void rows_kernel(const Args A)
     total = over_halves_sum(total);
     const bool empty = limit < 0;
     if (parts > 1) {
-        if (real) PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + split).store(sums, top, total, wave * 32 + (lane & 31), h);
+        if (real) PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + split).store(sums, top, total, quarter * 32 + (lane & 31), h);
         return;
     }
     if (A.lse && real && h == 0)
@@ -204,22 +238,26 @@ size_t splits_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, i
     return splits < 2 ? 0 : (size_t)block_numbers(tokens, n_seqs, group, BM) * kv_heads * splits * (dim <= 64 ? PartOfRows<64, BM>::FLOATS : PartOfRows<128, BM>::FLOATS) * 4;
 }
 
-template <class T, bool PAGED> int launch(const Args &A, hipStream_t stream)
+template <class T, int D> int launch_rows(const Args &A, bool paged, int compute_units, hipStream_t stream)
 {
-    const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = PAGED ? blocks * A.splits : blocks;
+    const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = paged ? blocks * A.splits : blocks;
     if (n > 0x1fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
-    if (A.dim <= 64)
-        hipLaunchKernelGGL((rows_kernel<T, 64, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
-    else
-        hipLaunchKernelGGL((rows_kernel<T, 128, PAGED>), dim3((unsigned)n), dim3(64 * WAVES), 0, stream, A);
-    if (PAGED && A.splits > 1) {
+    const dim3 grid((unsigned)n);
+    if (paged) {
+        hipLaunchKernelGGL((rows_kernel<T, D, true, 1>), grid, dim3(256), 0, stream, A);
         const int joined = rows_joined(blocks, BM);
-        if (A.dim <= 64)
-            hipLaunchKernelGGL((join_kernel<T, 64>), dim3((unsigned)blocks, BM / joined), dim3(256), 0, stream, A, joined);
-        else
-            hipLaunchKernelGGL((join_kernel<T, 128>), dim3((unsigned)blocks, BM / joined), dim3(256), 0, stream, A, joined);
+        if (A.splits > 1) hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)blocks, BM / joined), dim3(256), 0, stream, A, joined);
+    } else if (n <= compute_units) {
+        hipLaunchKernelGGL((rows_kernel<T, D, false, 2>), grid, dim3(512), 0, stream, A);
+    } else {
+        hipLaunchKernelGGL((rows_kernel<T, D, false, 1>), grid, dim3(256), 0, stream, A);
     }
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
+int launch(const Args &A, int dtype, bool paged, int compute_units, hipStream_t stream)
+{
+    if (dtype == RB_F16) return A.dim <= 64 ? launch_rows<F16, 64>(A, paged, compute_units, stream) : launch_rows<F16, 128>(A, paged, compute_units, stream);
+    return A.dim <= 64 ? launch_rows<BF16, 64>(A, paged, compute_units, stream) : launch_rows<BF16, 128>(A, paged, compute_units, stream);
 }
 
 }  // namespace
@@ -263,8 +301,7 @@ extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, c
     A.n_seqs = n_seqs, A.tokens_q = tokens_q, A.tokens_k = tokens_k;
     A.heads = H->heads, A.kv_heads = H->kv_heads, A.group = H->heads / H->kv_heads, A.dim = H->dim, A.causal = causal != 0;
     A.c = scale * LOG2E;
-    const hipStream_t st = static_cast<hipStream_t>(stream);
-    return H->dtype == RB_F16 ? launch<F16, false>(A, st) : launch<BF16, false>(A, st);
+    return launch(A, H->dtype, false, rb::mx::device_groups(), static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
@@ -299,8 +336,9 @@ extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token
     A.heads = heads, A.kv_heads = C->kv_heads, A.group = heads / C->kv_heads, A.dim = C->dim, A.causal = 1;
     A.c = scale * LOG2E;
     A.parts = rb::address_of(workspace);
-    A.splits = splits_for(tokens, n_seqs, A.kv_heads, A.group, rb::mx::device_groups());
+    const int units = rb::mx::device_groups();
+    A.splits = splits_for(tokens, n_seqs, A.kv_heads, A.group, units);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_applies(tokens, n_seqs, A.group, (long long)width * C->page_tokens)) return launch_few(A, C->dtype, rb::mx::device_groups(), st);
-    return C->dtype == RB_F16 ? launch<F16, true>(A, st) : launch<BF16, true>(A, st);
+    if (few_applies(tokens, n_seqs, A.group, (long long)width * C->page_tokens)) return launch_few(A, C->dtype, units, st);
+    return launch(A, C->dtype, true, units, st);
 }

@@ -139,9 +139,10 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3, half = wave >> 2;
     const int kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;      // causal: the first keys have the most rows
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
-    const int s = sequence_of_block(first_k, A.n_seqs, 1, BN, block, lane);
+    int s, of_sequence;
+    if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.causal, block, lane, s, of_sequence)) return;
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
-    const int key0 = (block - block_start(first_k[s], s, 1, BN)) * BN;
+    const int key0 = of_sequence * BN;
     if (key0 < 0 || key0 >= S.n_k) return;
     const int ahead = S.n_k - S.n_q;
     const int my_key = key0 + part * 32 + (lane & 31), key = min(my_key, S.n_k - 1);
@@ -295,12 +296,11 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3, half = wave >> 2;
     const int kvh = blockIdx.x % A.kv_heads;
-    int block = blockIdx.x / A.kv_heads;
-    if (A.causal) block = (int)(gridDim.x / A.kv_heads) - 1 - block;
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
-    const int s = sequence_of_block(first_q, A.n_seqs, A.group, BN, block, lane);
+    int s, of_sequence;
+    if (!rows_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.group, A.causal, blockIdx.x / A.kv_heads, gridDim.x / A.kv_heads, lane, s, of_sequence)) return;
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
-    const int row0 = (block - block_start(first_q[s], s, A.group, BN)) * BN, n_rows = S.n_q * A.group;
+    const int row0 = of_sequence * BN, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
 
     const int my_row = row0 + part * 32 + (lane & 31);
