@@ -370,7 +370,8 @@ struct Args {
     int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
     int page_shift, pages, width;
     Address parts;                           // workspace
-    int splits;                              // workgroups that share the keys of the same rows
+    int wanted;                              // workgroups per key head that the work is shared out to; 0: one per block of rows
+    float per_tile;                          // how many of them for a tile
     float c;                                 // scale log2(e): the exponentials are powers of two
 };
 
@@ -384,6 +385,85 @@ __device__ __forceinline__ int positions(int length, int width, int page_shift)
 {
     return min(max(length, 0), (int)min((long long)width << page_shift, 0x7fffffc0ll));
 }
+// Work over a cache, shared out evenly: that of a key head is a row of tiles, sequence after sequence and job (a block of rows) after job, cut into equal shares wherever that
+// falls.  Shape says what a sequence has of it: of(A, q0, q1, length), count() tiles, blocks of JOB rows.
+//
+// Sums over the sequences, 64 at a time, the first 64 looked at once
+template <class Shape> struct Sums {
+    static constexpr int JOB = Shape::JOB;
+    const Args &A;
+    const int *first, *lengths;
+    int lane, q0, q1, length, upto;      // what the arrays say of sequence `lane`; the tiles of sequences 0 .. lane
+    __device__ __forceinline__ Sums(const Args &A_, const int *first_, const int *lengths_, int lane_) : A(A_), first(first_), lengths(lengths_), lane(lane_)
+    {
+        const int s = min(lane, A.n_seqs - 1);
+        q0 = first[s], q1 = first[s + 1], length = lengths[s];
+        count_first();
+    }
+    __device__ __forceinline__ void count_first()
+    {
+        upto = up_to_lane(lane < A.n_seqs ? Shape::of(A, q0, q1, length).count() : 0);
+    }
+    __device__ __forceinline__ int count(int s) const { return s < A.n_seqs ? Shape::of(A, first[s], first[s + 1], lengths[s]).count() : 0; }
+    __device__ __forceinline__ int up_to_lane(int v) const
+    {
+        for (int d = 1; d < 64; d <<= 1) {
+            const int u = __shfl_up(v, d);
+            if (lane >= d) v += u;
+        }
+        return v;
+    }
+    __device__ __forceinline__ void entries(int s, int &from, int &to, int &len) const      // of one sequence
+    {
+        if (s < 64) {      // at hand
+            from = __builtin_amdgcn_readlane(q0, s), to = __builtin_amdgcn_readlane(q1, s), len = __builtin_amdgcn_readlane(length, s);
+        } else {
+            typedef const __attribute__((address_space(4))) int *Uniform;
+            from = ((Uniform)first)[s], to = ((Uniform)first)[s + 1], len = ((Uniform)lengths)[s];
+        }
+    }
+    __device__ __forceinline__ int of_block(int block) const
+    {
+        if (A.n_seqs > 64) return sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
+        return max(__popcll(__ballot(lane < A.n_seqs && block_start(q0, lane, A.group, JOB) <= block)) - 1, 0);
+    }
+    // the tiles before sequence `end`
+    __device__ __forceinline__ int before(int end) const
+    {
+        if (end <= 64) return end > 0 ? __builtin_amdgcn_readlane(upto, end - 1) : 0;
+        int sum = 0;
+        for (int s = 64 + lane; s < end; s += 64) sum += count(s);
+        return __builtin_amdgcn_readlane(upto, 63) + __builtin_amdgcn_readlane(up_to_lane(sum), 63);
+    }
+    // the sequence that has tile `at` (which exists); `at` becomes the tile among its own
+    __device__ __forceinline__ int locate(int &at) const
+    {
+        int now = upto;
+        for (int s = 0; s < A.n_seqs; s += 64) {
+            if (s) now = up_to_lane(count(s + lane));
+            const int here = __builtin_amdgcn_readlane(now, 63);
+            if (at < here) {
+                const int l = __popcll(__ballot(now <= at));
+                if (l) at -= __builtin_amdgcn_readlane(now, l - 1);
+                return s + l;
+            }
+            at -= here;
+        }
+        return A.n_seqs;
+    }
+};
+// All tiles in up to `most` equal shares of at least `least` tiles, the first ones longer by one
+struct Shares {
+    int n, each, longer;
+    __device__ __forceinline__ Shares(int all, int most, int least) : n(max(min(most, (int)((unsigned)all / (unsigned)least)), 1)), each((int)((unsigned)all / (unsigned)n)), longer(all - each * n) {}
+    __device__ __forceinline__ int start(int w) const { return w * each + min(w, longer); }
+    __device__ __forceinline__ int of(int tile) const
+    {
+        const unsigned in_longer = (unsigned)(each + 1) * longer;
+        return (unsigned)tile < in_longer ? (int)((unsigned)tile / (unsigned)(each + 1)) : longer + (int)(((unsigned)tile - in_longer) / (unsigned)each);
+    }
+};
+
 // workgroups that share `tiles` tiles: two tiles each at least
 __device__ __forceinline__ int splits_of(int tiles, int splits) { return max(min(splits, tiles / 2), 1); }
 
@@ -408,6 +488,11 @@ template <int D, int N> struct PartOfRows {
             for (int i = 0; i < 16; i += 4) *(v4f *)(row(r) + b * 32 + 2 * i + 4 * h) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
     }
 };
+// the part that a share has of a job of N rows which it does not have all of: of its first job (0) or its last (1)
+template <int D, int N> __device__ __forceinline__ PartOfRows<D, N> part_of(Address workspace, int kvh, int shares, int share, int which)
+{
+    return PartOfRows<D, N>(workspace, ((size_t)kvh * shares + share) * 2 + which);
+}
 // Joins n_parts of the `joined` rows (two, four or eight) from row0 on, of which n_rows are there: o = sum of the parts' rows, each times 2^(its maximum - the
 // largest), over the sum of their totals likewise, in the order of the parts.  256 threads, four elements each; the groups of threads that make up a row share
 // out the parts.  Bound: latency, so all loads of sixteen parts and group are on their way before the first is used.  part(i): a PartOfRows; out(row): where

@@ -12,6 +12,56 @@ namespace rb {
 namespace attn {
 namespace {
 
+constexpr int BM = 128, KEYS = 64;
+
+// A cache is shared out to workgroups by what the lengths ask for: a block of rows has as many, each with a part of the keys, as it takes for none to have more than some number
+// of tiles.  That is the smallest such number, from the tiles per workgroup wanted up to twice those, for which no more workgroups start than run at once, and where the blocks
+// are too many for any, the least of them: workgroups then take turns.  (fp16, against the same number of parts for every block: 700, 64, 33 and 200 new tokens on 100, 4000, 9000 and
+// 2000, 64 query and 8 key heads of 128, 181 -> 82 us; 128 tokens on 30000, 8 heads, 53 -> 39; 512 tokens on 7500, 32 and 8 heads, where all parts are alike, 85 -> 88.  Sharing
+// the tiles out exactly, workgroups going on from one block to the next, took 121, 40 and 98: every start of a block costs some 4 us.)
+constexpr float LEAST = 8.f;               // tiles of a part (512 new tokens: 23 us, with 4 26)
+constexpr long long GROUPS = 2, MANY = 4;  // workgroups per compute unit: wanted, and those of whole blocks that need no sharing
+constexpr long long JOINING = 2048;        // workgroups that join: all at once (8192, most of which find no work, 10 us more)
+struct Blocks {
+    static constexpr int JOB = BM;
+    int blocks, tiles, parts;      // (tiles of a block on average)
+    static __device__ __forceinline__ Blocks of(const Args &A, int q0, int q1, int length)
+    {
+        q0 = min(max(q0, 0), A.tokens_q);
+        q1 = min(max(q1, q0), A.tokens_q);
+        const int n_q = q1 - q0, n_k = positions(length, A.width, A.page_shift);
+        const int first = max((n_k - n_q) / KEYS, 0) + 1, last = n_k / KEYS + 1, tiles = first + (last - first) / 2;
+        return {(n_q * A.group + BM - 1) / BM, tiles, max((int)(tiles * A.per_tile + 0.98f), 1)};
+    }
+};
+struct Groups : Blocks {
+    __device__ __forceinline__ Groups(const Blocks &b) : Blocks(b) {}
+    __device__ __forceinline__ int count() const { return blocks * parts; }
+    static __device__ __forceinline__ Groups of(const Args &A, int q0, int q1, int length) { return Blocks::of(A, q0, q1, length); }
+};
+struct Tiles : Blocks {
+    __device__ __forceinline__ Tiles(const Blocks &b) : Blocks(b) {}
+    __device__ __forceinline__ int count() const { return blocks * tiles; }
+    static __device__ __forceinline__ Tiles of(const Args &A, int q0, int q1, int length) { return Blocks::of(A, q0, q1, length); }
+};
+struct Slots : Blocks {      // of the workspace: one for each workgroup that has a part
+    __device__ __forceinline__ Slots(const Blocks &b) : Blocks(b) {}
+    __device__ __forceinline__ int count() const { return parts > 1 ? blocks * parts : 0; }
+    static __device__ __forceinline__ Slots of(const Args &A, int q0, int q1, int length) { return Blocks::of(A, q0, q1, length); }
+};
+__device__ __forceinline__ Args with_shares(Args A, const int *first, const int *lengths, int lane)
+{
+    const float share = max(Sums<Tiles>(A, first, lengths, lane).before(A.n_seqs) / (float)A.wanted, LEAST);
+    Sums<Groups> groups(A, first, lengths, lane);
+    for (float f = 1.f; f < 2.f; f += 0.1f) {
+        A.per_tile = 1.f / (share * f);
+        groups.count_first();
+        if (groups.before(A.n_seqs) <= A.wanted) return A;
+    }
+    A.per_tile = 1.f / share;
+    return A;
+}
+
 // One workgroup does 128 rows of one key head, 32 per wavefront, over all keys that they see, KEYS at a time; the next tile of keys and values
 // is on its way into LDS while one is used.  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part (one long
 // prompt of 8192 tokens, 64 query and 8 key heads of 128, causal, bf16: 1.00 ms, 1.10 PFLOP/s).  What was tried beside it: 32 keys at a time and
@@ -20,7 +70,6 @@ namespace {
 //
 // HALVES = 2: eight wavefronts, four of them with the first 32 keys of every tile and four with the second, joined at the end.  A step then takes little more than half
 // as long where a workgroup has a compute unit to itself; where there is a second one to fill it, there is nothing to gain.
-constexpr int BM = 128, KEYS = 64;
 template <class T, int D, bool PAGED, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 {
@@ -31,18 +80,32 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), quarter = wave & 3, half = wave >> 2;
-    const int kvh = blockIdx.x % A.kv_heads;      // the workgroups of a head go to the same XCDs
-    int block = blockIdx.x / A.kv_heads;
-    const int split = PAGED ? block % A.splits : 0, n_blocks = (int)(gridDim.x / A.kv_heads) / (PAGED ? A.splits : 1);
-    if (PAGED) block /= A.splits;
+    const int kvh = blockIdx.x % A.kv_heads, number = blockIdx.x / A.kv_heads, numbers = (int)gridDim.x / A.kv_heads;      // the workgroups of a head go to the same XCDs
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
-    int s, of_sequence;
-    if constexpr (PAGED) {
-        block = n_blocks - 1 - block;      // the longest first
+    int s, of_sequence, split = 0, splits = 1;
+    [[maybe_unused]] int slot = 0;      // of this workgroup's part
+    if constexpr (!PAGED) {
+        if (!rows_of_workgroup<BM>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.group, A.causal, number, numbers, lane, s, of_sequence)) return;
+    } else if (!A.wanted) {
+        const int block = numbers - 1 - number;      // the longest first
         s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
         of_sequence = block - block_start(first_q[s], s, A.group, BM);
-    } else if (!rows_of_workgroup<BM>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.group, A.causal, block, n_blocks, lane, s, of_sequence)) {
-        return;
+    } else {
+        const Args B = with_shares(A, first_q, first_k, lane);
+        const Sums<Groups> groups(B, first_q, first_k, lane);
+        int at = groups.before(A.n_seqs) - 1 - number;
+        if (at < 0) return;
+        s = __builtin_amdgcn_readfirstlane(groups.locate(at));
+        if (s >= A.n_seqs) return;
+        int q0, q1, length;
+        groups.entries(s, q0, q1, length);
+        splits = __builtin_amdgcn_readfirstlane(Blocks::of(B, q0, q1, length).parts);
+        of_sequence = __builtin_amdgcn_readfirstlane((int)((unsigned)at / (unsigned)splits));
+        split = __builtin_amdgcn_readfirstlane((int)((unsigned)at % (unsigned)splits));
+        if (splits > 1) {
+            slot = Sums<Slots>(B, first_q, first_k, lane).before(s) + at;
+            if (slot < 0 || slot >= 2 * A.wanted) return;      // (arrays that are not in order)
+        }
     }
     Sequence S = sequence_at(first_q, PAGED ? first_q : first_k, s, A.tokens_q, PAGED ? A.tokens_q : A.tokens_k);
     if (PAGED) {
@@ -61,7 +124,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
     const int limit = A.causal ? ahead + token : S.n_k - 1;
     const int block_least = last_key(row0), block_most = last_key(row0 + BM - 1);
     const int wave_least = __builtin_amdgcn_readfirstlane(last_key(row0 + quarter * 32)), wave_most = __builtin_amdgcn_readfirstlane(last_key(row0 + quarter * 32 + 31));
-    const int tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS, parts = PAGED ? splits_of(tiles, A.splits) : 1;
+    const int tiles = __builtin_amdgcn_readfirstlane(max(block_most + 1, 0) + KEYS - 1) / KEYS, parts = PAGED ? splits_of(tiles, splits) : 1;
     if (split >= parts) return;
     const int first_tile = tiles * split / parts, n_tiles = tiles * (split + 1) / parts;      // (the end of this workgroup's)
 
@@ -199,7 +262,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
     total = over_halves_sum(total);
     const bool empty = limit < 0;
     if (parts > 1) {
-        if (real) PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + split).store(sums, top, total, quarter * 32 + (lane & 31), h);
+        if (real) PartOfRows<D, BM>(A.parts, (size_t)slot * A.kv_heads + kvh).store(sums, top, total, quarter * 32 + (lane & 31), h);
         return;
     }
     if (A.lse && real && h == 0)
@@ -211,42 +274,54 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 // What several workgroups had parts of
 template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, int joined)
 {
-    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads, row0 = blockIdx.y * joined;
-    const int *first = global_at<const int>(A.first_q);
-    const int s = sequence_of_block(first, A.n_seqs, A.group, BM, block, lane);
-    const Sequence S = sequence_at(first, first, s, A.tokens_q, A.tokens_q);
-    const int before = (block - block_start(first[s], s, A.group, BM)) * BM, n_rows = S.n_q * A.group - before;
-    if (before < 0 || row0 >= n_rows) return;
-    const int ahead = positions(global_at<const int>(A.first_k)[s], A.width, A.page_shift) - S.n_q;
-    const int most = ahead + (before + min(n_rows, BM) - 1) / A.group, parts = splits_of((max(most + 1, 0) + KEYS - 1) / KEYS, A.splits);
+    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;
+    const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
+    const Args B = with_shares(A, first, lengths, lane);
+    const Sums<Slots> slots(B, first, lengths, lane);
+    const int s = __builtin_amdgcn_readfirstlane(slots.of_block(block));
+    int q0, q1, length;
+    slots.entries(s, q0, q1, length);
+    const Blocks shape = Blocks::of(B, q0, q1, length);
+    const int b = block - block_start(q0, s, A.group, BM);
+    if (b < 0 || b >= shape.blocks || shape.parts == 1) return;
+    q0 = min(max(q0, 0), A.tokens_q);
+    const int n_q = min(max(q1, q0), A.tokens_q) - q0, before = b * BM, n_rows = n_q * A.group - before, ahead = positions(length, A.width, A.page_shift) - n_q;
+    const int most = ahead + (before + min(n_rows, BM) - 1) / A.group, parts = splits_of((max(most + 1, 0) + KEYS - 1) / KEYS, shape.parts);
     if (parts == 1) return;
-    join_rows<T, D>(
-        joined, parts, row0, min(n_rows - row0, joined), A.dim, [&](int i) { return PartOfRows<D, BM>(A.parts, ((size_t)block * A.kv_heads + kvh) * A.splits + i); },
-        [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(S.q0 + (before + r) / A.group) * A.heads + kvh * A.group + (before + r) % A.group) * (A.dim * 2); },
-        [&](int r) { return ahead + (before + r) / A.group < 0; });
+    const int slot = slots.before(s) + b * shape.parts;
+    if (slot < 0 || slot > 2 * A.wanted - parts) return;
+    for (int row0 = blockIdx.y * joined; row0 < min(n_rows, BM); row0 += gridDim.y * joined) {
+        join_rows<T, D>(
+            joined, parts, row0, min(n_rows - row0, joined), A.dim, [&](int i) { return PartOfRows<D, BM>(A.parts, (size_t)(slot + i) * A.kv_heads + kvh); },
+            [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + (before + r) / A.group) * A.heads + kvh * A.group + (before + r) % A.group) * (A.dim * 2); },
+            [&](int r) { return ahead + (before + r) / A.group < 0; });
+        __syncthreads();
+    }
 }
 
-// A cache is read by two workgroups per compute unit at least, if its keys allow: where the rows alone are fewer, several share the keys
-int splits_for(int tokens, int n_seqs, int kv_heads, int group, int compute_units)
+// Workgroups per key head that the work over a cache is shared out to; 0: one per block of rows, where those are many, or the tiles are not counted in 31 bits
+int groups_wanted(int tokens, int n_seqs, int kv_heads, int group, long long most_positions, int compute_units)
 {
-    const long long n = block_numbers(tokens, n_seqs, group, BM) * kv_heads;
-    return n >= 2ll * compute_units ? 1 : (int)std::min(16ll, (2ll * compute_units + n - 1) / std::max(n, 1ll));
+    const long long blocks = block_numbers(tokens, n_seqs, group, BM);
+    if (blocks * kv_heads >= MANY * compute_units || blocks * (most_positions / KEYS + 2) >= 0x7fffffffll) return 0;
+    return (int)std::max(GROUPS * compute_units / kv_heads, 1ll);
 }
-size_t splits_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, int dim, int compute_units)
+// Blocks of more than one part have at most twice the workgroups wanted: a block that x > 1 would do for has less than x + 1
+size_t parts_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, int dim, int compute_units)
 {
-    const int splits = splits_for(tokens, n_seqs, kv_heads, group, compute_units);
-    return splits < 2 ? 0 : (size_t)block_numbers(tokens, n_seqs, group, BM) * kv_heads * splits * (dim <= 64 ? PartOfRows<64, BM>::FLOATS : PartOfRows<128, BM>::FLOATS) * 4;
+    const size_t slots = (size_t)groups_wanted(tokens, n_seqs, kv_heads, group, 0, compute_units) * 2;
+    return slots * kv_heads * (dim <= 64 ? PartOfRows<64, BM>::FLOATS : PartOfRows<128, BM>::FLOATS) * 4;
 }
 
 template <class T, int D> int launch_rows(const Args &A, bool paged, int compute_units, hipStream_t stream)
 {
-    const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = paged ? blocks * A.splits : blocks;
+    const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = blocks + (long long)A.wanted * A.kv_heads;      // (a block that has a share of x has at most x + 1)
     if (n > 0x1fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     const dim3 grid((unsigned)n);
     if (paged) {
         hipLaunchKernelGGL((rows_kernel<T, D, true, 1>), grid, dim3(256), 0, stream, A);
         const int joined = rows_joined(blocks, BM);
-        if (A.splits > 1) hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)blocks, BM / joined), dim3(256), 0, stream, A, joined);
+        if (A.wanted) hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)blocks, (unsigned)std::min((long long)BM / joined, std::max(JOINING / blocks, 1ll))), dim3(256), 0, stream, A, joined);
     } else if (n <= compute_units) {
         hipLaunchKernelGGL((rows_kernel<T, D, false, 2>), grid, dim3(512), 0, stream, A);
     } else {
@@ -310,7 +385,7 @@ extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, in
     const int units = rb::mx::device_groups(), group = heads / C->kv_heads;
     // whichever kernel the table's width will choose
     const size_t few = few_applies(tokens, n_seqs, group, 0) ? few_workspace_bytes(C->kv_heads, C->dim, units) : 0;
-    return std::max(few, splits_workspace_bytes(tokens, n_seqs, C->kv_heads, group, C->dim, units));
+    return std::max(few, parts_workspace_bytes(tokens, n_seqs, C->kv_heads, group, C->dim, units));
 }
 
 extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
@@ -337,7 +412,7 @@ extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token
     A.c = scale * LOG2E;
     A.parts = rb::address_of(workspace);
     const int units = rb::mx::device_groups();
-    A.splits = splits_for(tokens, n_seqs, A.kv_heads, A.group, units);
+    A.wanted = groups_wanted(tokens, n_seqs, A.kv_heads, A.group, std::min((long long)width * C->page_tokens, 0x7fffffffll), units);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (few_applies(tokens, n_seqs, A.group, (long long)width * C->page_tokens)) return launch_few(A, C->dtype, units, st);
     return launch(A, C->dtype, true, units, st);

@@ -15,98 +15,22 @@ namespace rb {
 namespace attn {
 namespace {
 
-constexpr int KEYS = 32, JOB = 32, WAVES = 4;
+constexpr int KEYS = 32, ROWS = 32, WAVES = 4;
 
 // Where the work of a sequence lies among all tiles of a key head.  (All of them, as many as rows and positions allow, are counted in 31 bits: see few_applies.)
 struct Shape {
+    static constexpr int JOB = ROWS;
     int rows, blocks, tiles;
     __device__ __forceinline__ int count() const { return blocks * tiles; }
-};
-__device__ __forceinline__ Shape shape_of(const Args &A, int q0, int q1, int length)
-{
-    q0 = min(max(q0, 0), A.tokens_q);
-    q1 = min(max(q1, q0), A.tokens_q);
-    const int rows = (q1 - q0) * A.group;
-    // a sequence that has rows but no positions: one tile, of which they see nothing
-    return {rows, (rows + JOB - 1) / JOB, rows ? max((positions(length, A.width, A.page_shift) + KEYS - 1) / KEYS, 1) : 0};
-}
-// Sums over the sequences, 64 at a time, the first 64 looked at once
-struct Sums {
-    const Args &A;
-    const int *first, *lengths;
-    int lane, q0, q1, length, upto;      // what the arrays say of sequence `lane`; the tiles of sequences 0 .. lane
-    __device__ __forceinline__ Sums(const Args &A_, const int *first_, const int *lengths_, int lane_) : A(A_), first(first_), lengths(lengths_), lane(lane_)
+    static __device__ __forceinline__ Shape of(const Args &A, int q0, int q1, int length)
     {
-        const int s = min(lane, A.n_seqs - 1);
-        q0 = first[s], q1 = first[s + 1], length = lengths[s];
-        upto = up_to_lane(lane < A.n_seqs ? shape_of(A, q0, q1, length).count() : 0);
-    }
-    __device__ __forceinline__ int count(int s) const { return s < A.n_seqs ? shape_of(A, first[s], first[s + 1], lengths[s]).count() : 0; }
-    __device__ __forceinline__ int up_to_lane(int v) const
-    {
-        for (int d = 1; d < 64; d <<= 1) {
-            const int u = __shfl_up(v, d);
-            if (lane >= d) v += u;
-        }
-        return v;
-    }
-    __device__ __forceinline__ void entries(int s, int &from, int &to, int &len) const      // of one sequence
-    {
-        if (s < 64) {      // at hand
-            from = __builtin_amdgcn_readlane(q0, s), to = __builtin_amdgcn_readlane(q1, s), len = __builtin_amdgcn_readlane(length, s);
-        } else {
-            typedef const __attribute__((address_space(4))) int *Uniform;
-            from = ((Uniform)first)[s], to = ((Uniform)first)[s + 1], len = ((Uniform)lengths)[s];
-        }
-    }
-    __device__ __forceinline__ int of_block(int block) const
-    {
-        if (A.n_seqs > 64) return sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
-        return max(__popcll(__ballot(lane < A.n_seqs && block_start(q0, lane, A.group, JOB) <= block)) - 1, 0);
-    }
-    // the tiles before sequence `end`
-    __device__ __forceinline__ int before(int end) const
-    {
-        if (end <= 64) return end > 0 ? __builtin_amdgcn_readlane(upto, end - 1) : 0;
-        int sum = 0;
-        for (int s = 64 + lane; s < end; s += 64) sum += count(s);
-        return __builtin_amdgcn_readlane(upto, 63) + __builtin_amdgcn_readlane(up_to_lane(sum), 63);
-    }
-    // the sequence that has tile `at` (which exists); `at` becomes the tile among its own
-    __device__ __forceinline__ int locate(int &at) const
-    {
-        int now = upto;
-        for (int s = 0; s < A.n_seqs; s += 64) {
-            if (s) now = up_to_lane(count(s + lane));
-            const int here = __builtin_amdgcn_readlane(now, 63);
-            if (at < here) {
-                const int l = __popcll(__ballot(now <= at));
-                if (l) at -= __builtin_amdgcn_readlane(now, l - 1);
-                return s + l;
-            }
-            at -= here;
-        }
-        return A.n_seqs;
+        q0 = min(max(q0, 0), A.tokens_q);
+        q1 = min(max(q1, q0), A.tokens_q);
+        const int rows = (q1 - q0) * A.group;
+        // a sequence that has rows but no positions: one tile, of which they see nothing
+        return {rows, (rows + ROWS - 1) / ROWS, rows ? max((positions(length, A.width, A.page_shift) + KEYS - 1) / KEYS, 1) : 0};
     }
 };
-// All tiles in equal shares, the first ones longer by one; never more shares than tiles: none is empty
-struct Shares {
-    int n, each, longer;
-    __device__ __forceinline__ Shares(int all, int wavefronts) : n(min(wavefronts, max(all, 1))), each((int)((unsigned)all / (unsigned)n)), longer(all - each * n) {}
-    __device__ __forceinline__ int start(int w) const { return w * each + min(w, longer); }
-    __device__ __forceinline__ int of(int tile) const
-    {
-        const unsigned in_longer = (unsigned)(each + 1) * longer;
-        return (unsigned)tile < in_longer ? (int)((unsigned)tile / (unsigned)(each + 1)) : longer + (int)(((unsigned)tile - in_longer) / (unsigned)each);
-    }
-};
-
-// the part of a job that share w has: its first (0) or its last (1)
-template <int D> __device__ __forceinline__ PartOfRows<D, JOB> part_of(Address workspace, int kvh, int wavefronts, int w, int which)
-{
-    return PartOfRows<D, JOB>(workspace, ((size_t)kvh * wavefronts + w) * 2 + which);
-}
-
 // a position in the row of tiles
 struct Cursor {
     int s, block, t;
@@ -125,8 +49,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
     typedef const __attribute__((address_space(4))) int *Uniform;
     const Uniform table_u = (Uniform)global_at<const int>(A.table);
-    const Sums sums_of(A, first, lengths, lane);
-    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
+    const Sums<Shape> sums_of(A, first, lengths, lane);
+    const Shares shares(sums_of.before(A.n_seqs), wavefronts, 1);
     if (w >= shares.n) return;
     int begin = shares.start(w);
     const int n = shares.start(w + 1) - begin;
@@ -141,7 +65,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         int q0, q1, length;
         sums_of.entries(c.s, q0, q1, length);
         c.q0 = min(max(q0, 0), A.tokens_q);
-        c.shape = shape_of(A, q0, q1, length);
+        c.shape = Shape::of(A, q0, q1, length);
         c.n_k = positions(length, A.width, A.page_shift);
     };
     auto advance = [&](Cursor &c) RB_INLINE {
@@ -158,8 +82,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     at.s = __builtin_amdgcn_readfirstlane(sums_of.locate(begin));
     if (at.s >= A.n_seqs) return;
     visit(at);
-    at.block = __builtin_amdgcn_readfirstlane((int)((unsigned)begin / (unsigned)at.shape.tiles));
-    at.t = begin - at.block * at.shape.tiles;
+    if (begin < 0 || at.shape.blocks == 0) return;      // (arrays that are not in order)
+    at.block = min(__builtin_amdgcn_readfirstlane((int)((unsigned)begin / (unsigned)at.shape.tiles)), at.shape.blocks - 1);
+    at.t = min(begin - at.block * at.shape.tiles, at.shape.tiles - 1);
     ahead = at;
 
     constexpr int LOADS = Part<D, KEYS, 1>::LOADS;
@@ -203,7 +128,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     int limit, least, from_t, token, head;
     bool real, found;
     auto start = [&]() RB_INLINE {
-        const int n_q = at.shape.rows / A.group, row0 = at.block * JOB;
+        const int n_q = at.shape.rows / A.group, row0 = at.block * ROWS;
         const int row = min(row0 + (lane & 31), at.shape.rows - 1);
         real = row0 + (lane & 31) < at.shape.rows;
         token = at.q0 + row / A.group;
@@ -237,7 +162,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
             const bool empty = limit < 0;
             store_columns<T, D>(sums, empty ? 0.f : 1.f / total, global_at<uint8_t>(A.o) + ((long long)token * A.heads + head) * (A.dim * 2), A.dim, h, real, empty);
         } else if (real) {
-            part_of<D>(A.parts, kvh, wavefronts, w, first_job ? 0 : 1).store(sums, top, total, lane & 31, h);
+            part_of<D, ROWS>(A.parts, kvh, wavefronts, w, first_job ? 0 : 1).store(sums, top, total, lane & 31, h);
         }
         first_job = false;
     };
@@ -321,24 +246,24 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
 {
     const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads, row0 = blockIdx.y * joined;
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
-    const Sums sums_of(A, first, lengths, lane);
+    const Sums<Shape> sums_of(A, first, lengths, lane);
     const int s = __builtin_amdgcn_readfirstlane(sums_of.of_block(block));
     int q0, q1, length;
     sums_of.entries(s, q0, q1, length);
-    const Shape shape = shape_of(A, q0, q1, length);
-    const int b = block - block_start(q0, s, A.group, JOB);
-    if (b < 0 || b >= shape.blocks || b * JOB + row0 >= shape.rows) return;
-    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
+    const Shape shape = Shape::of(A, q0, q1, length);
+    const int b = block - block_start(q0, s, A.group, ROWS);
+    if (b < 0 || b >= shape.blocks || b * ROWS + row0 >= shape.rows) return;
+    const Shares shares(sums_of.before(A.n_seqs), wavefronts, 1);
     const int from = sums_of.before(s) + b * shape.tiles, w0 = shares.of(from), w1 = shares.of(from + shape.tiles - 1);
     if (w0 == w1) return;      // it has stored the result
     const bool starts_inside = shares.start(w0) < from;      // the first part is that share's last, all others are their shares' first
     const int n_q = shape.rows / A.group, n_k = positions(length, A.width, A.page_shift);
     q0 = min(max(q0, 0), A.tokens_q);
-    auto token = [&](int r) { return (b * JOB + r) / A.group; };
+    auto token = [&](int r) { return (b * ROWS + r) / A.group; };
     join_rows<T, D>(
-        joined, w1 - w0 + 1, row0, min(shape.rows - b * JOB - row0, joined), A.dim,
-        [&](int i) { return part_of<D>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
-        [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + token(r)) * A.heads + kvh * A.group + (b * JOB + r) % A.group) * (A.dim * 2); },
+        joined, w1 - w0 + 1, row0, min(shape.rows - b * ROWS - row0, joined), A.dim,
+        [&](int i) { return part_of<D, ROWS>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
+        [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + token(r)) * A.heads + kvh * A.group + (b * ROWS + r) % A.group) * (A.dim * 2); },
         [&](int r) { return n_k - n_q + token(r) < 0; });
 }
 
@@ -348,10 +273,10 @@ int groups_per_head(const Args &A, int compute_units) { return compute_units > A
 template <class T, int D> int launch(const Args &A, int compute_units, hipStream_t stream)
 {
     const int groups = groups_per_head(A, compute_units);
-    const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, JOB) * A.kv_heads;
+    const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, ROWS) * A.kv_heads;
     if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
     hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES), 0, stream, A);
-    const int rows = (int)std::min((long long)JOB, (long long)A.tokens_q * A.group), joined = rows_joined(jobs, rows);      // rows of one job, at most
+    const int rows = (int)std::min((long long)ROWS, (long long)A.tokens_q * A.group), joined = rows_joined(jobs, rows);      // rows of one job, at most
     hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs, (rows + joined - 1) / joined), dim3(256), 0, stream, A, groups * WAVES, joined);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
@@ -360,15 +285,15 @@ template <class T, int D> int launch(const Args &A, int compute_units, hipStream
 
 bool few_applies(int tokens, int n_seqs, int group, long long positions)
 {
-    const long long tiles = block_numbers(tokens, n_seqs, group, JOB) * (std::min(positions, 0x7fffffffll) / KEYS + 1);
-    return (long long)tokens * group <= (long long)JOB * n_seqs && tiles < 0x7fffffffll;
+    const long long tiles = block_numbers(tokens, n_seqs, group, ROWS) * (std::min(positions, 0x7fffffffll) / KEYS + 1);
+    return (long long)tokens * group <= (long long)ROWS * n_seqs && tiles < 0x7fffffffll;
 }
 
 size_t few_workspace_bytes(int kv_heads, int dim, int compute_units)
 {
     Args A = {};
     A.kv_heads = kv_heads;
-    return (size_t)kv_heads * groups_per_head(A, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfRows<64, JOB>::FLOATS : PartOfRows<128, JOB>::FLOATS) * 4;
+    return (size_t)kv_heads * groups_per_head(A, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfRows<64, ROWS>::FLOATS : PartOfRows<128, ROWS>::FLOATS) * 4;
 }
 
 int launch_few(const Args &A, int dtype, int compute_units, hipStream_t stream)
