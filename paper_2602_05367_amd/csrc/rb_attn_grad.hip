@@ -2,7 +2,8 @@
 //   dv_j = sum_i p_ij do_i        dp_ij = do_i . v_j        delta_i = do_i . o_i
 //   ds_ij = c p_ij (dp_ij - delta_i)        dq_i = sum_j ds_ij k_j        dk_j = sum_i ds_ij q_i
 // Two kernels, one with the queries in place and the keys going by (dq), then one the other way round (dk, dv).  The scores are computed twice; in return
-// every sum has one owner, which adds in one order: no atomics, the same bits every time, and the query heads that share a key head are summed in registers.
+// every sum has one owner, which adds in one order: no atomics, the same bits every time, and the query heads that share a key head are summed in registers, or
+// where keys are few by a few workgroups each of which has some of them, and a last kernel adds those up.
 //
 // o comes rounded, so do_i . o_i is off by some 2^-12 |do_i| |o_i|: as much as the rounding of ds does to dq and dk again.  The first kernel mends that: over a row,
 // sum_j p_ij (dp_ij - delta_i) is what delta_i lacks (the weights add up to one), so it sums that beside dq, and sum_j p_ij k_j, which
@@ -13,10 +14,12 @@
 // something of the size of do, and both are small.  Twice dim times the largest finite |do| and |v| bounds
 // |dp - delta|; the power of two that brings this bound to one is taken out before and put back into the sums.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 
 #include "rabit.h"
 #include "rb_attn.h"
 #include "rb_attn_host.h"
+#include "rb_internal.h"
 
 namespace rb {
 namespace attn {
@@ -28,7 +31,9 @@ struct GradArgs {
     Side q, k, v, o;                    // o: strides of the contiguous o, do and dq
     Address go, lse, first_q, first_k;
     Address delta, most_o, most_v;      // workspace: [tokens_q][heads], [blocks of 64 tokens][heads], [blocks][kv_heads]
+    Address parts;                      // workspace: [splits][dk, dv][tokens_k][kv_heads][dim] fp32, where there are several splits
     Address dq, dk, dv;
+    int splits;                         // workgroups that share the query heads of the same keys
     int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
     float c, scale;
 };
@@ -125,6 +130,10 @@ template <int E> __device__ __forceinline__ bool add_halves(v16f (&sums)[E], uin
 // A workgroup keeps 128 keys and values of one key head in LDS and takes the queries and do of all its query heads, 64 rows at a
 // time, through LDS.  Eight wavefronts: four times 32 keys, by the upper and the lower 32 rows of a tile, whose sums are added at the end.
 constexpr int BN = 128;
+__device__ __forceinline__ float *part_at(const GradArgs &A, int split, int which, long long row)
+{
+    return global_at<float>(A.parts) + ((long long)(split * 2 + which) * A.tokens_k * A.kv_heads + row) * A.dim;
+}
 
 template <class T, int D>
 __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
@@ -137,7 +146,8 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3, half = wave >> 2;
-    const int kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;      // causal: the first keys have the most rows
+    const int kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads, split = blockIdx.y;      // causal: the first keys have the most rows
+    const int first_g = A.group * split / A.splits, heads_of = A.group * (split + 1) / A.splits - first_g;
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     int s, of_sequence;
     if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.causal, block, lane, s, of_sequence)) return;
@@ -155,9 +165,9 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
 
     const Part<D, ROWS, W> q_part(A.q.token, A.dim, wave * (ROWS / W), lane), o_part(A.o.token, A.dim, wave * (ROWS / W), lane);
     const int tile0 = A.causal ? max(key0 - ahead, 0) / ROWS : 0, tiles = (S.n_q + ROWS - 1) / ROWS - tile0;
-    const int steps = __builtin_amdgcn_readfirstlane(tiles > 0 ? tiles * A.group : 0);
+    const int steps = __builtin_amdgcn_readfirstlane(tiles > 0 ? tiles * heads_of : 0);
     float next_lse = 0.f, next_delta = 0.f;      // of one row of the next tile, in the first wavefront
-    int load_g = 0, load_t = tile0, t = tile0;      // the tile to be asked for, and the one at hand
+    int load_g = first_g, load_t = tile0, t = tile0;      // the tile to be asked for, and the one at hand
     auto load = [&](uint8_t *queries, uint8_t *outs) RB_INLINE {
         const int head = kvh * A.group + load_g, row = S.q0 + load_t * ROWS, rows = S.n_q - load_t * ROWS;
         if (wave == 0) {
@@ -266,7 +276,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     loads_arrived();      // (the values, where there are no rows)
     __syncthreads();
     if (__builtin_amdgcn_readfirstlane(found) && half == 0)      // (only the rows of tiles that were cleaned, and their keys see it)
-        for (int g = 0; g < A.group; ++g)
+        for (int g = first_g; g < first_g + heads_of; ++g)
             for (int r = tile0 * ROWS; r < min(S.n_q, (max(block_last - ahead, 0) + ROWS - 1) / ROWS * ROWS); ++r)
                 add_not_finite<T, D>(sums_v, global_at<const uint8_t>(A.go) + (long long)(S.q0 + r) * A.o.token + (kvh * A.group + g) * A.o.head, A.dim, h, my_key <= ahead + r);
 
@@ -276,10 +286,56 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     add_halves<E>(sums_k, mine, half, lane);
     if (half == 1) return;
     const bool real = my_key < S.n_k;
-    const long long at = ((long long)(S.k0 + key) * A.kv_heads + kvh) * (A.dim * 2);
-    store_columns<T, D>(sums_v, 1.f / (1 << T::GRAD_BIAS), global_at<uint8_t>(A.dv) + at, A.dim, h, real, false);
-    store_columns<T, D>(sums_k, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dk) + at, A.dim, h, real, false);
+    const long long at = (long long)(S.k0 + key) * A.kv_heads + kvh;
+    const float scale_v = 1.f / (1 << T::GRAD_BIAS), scale_k = A.scale / (1 << T::GRAD_BIAS) / unit;
+    if (A.splits > 1) {
+        float *const k_part_at = part_at(A, split, 0, at), *const v_part_at = part_at(A, split, 1, at);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int to = e * 32 + 2 * i + 4 * h;
+                if (!real || to >= A.dim) continue;
+                *(v4f *)(k_part_at + to) = (v4f){sums_k[e][i], sums_k[e][i + 1], sums_k[e][i + 2], sums_k[e][i + 3]} * scale_k;
+                *(v4f *)(v_part_at + to) = (v4f){sums_v[e][i], sums_v[e][i + 1], sums_v[e][i + 2], sums_v[e][i + 3]} * scale_v;
+            }
+        return;
+    }
+    store_columns<T, D>(sums_v, scale_v, global_at<uint8_t>(A.dv) + at * (A.dim * 2), A.dim, h, real, false);
+    store_columns<T, D>(sums_k, scale_k, global_at<uint8_t>(A.dk) + at * (A.dim * 2), A.dim, h, real, false);
 }
+
+// The splits' sums, one after the other: eight keys per workgroup, four elements per thread
+template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const GradArgs A)
+{
+    constexpr int COLUMNS = D / 4, KEYS = 256 / COLUMNS;
+    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, e = threadIdx.x % COLUMNS * 4;
+    const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
+    int s, of_sequence;
+    if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.causal, blockIdx.x / A.kv_heads, lane, s, of_sequence)) return;
+    const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
+    const int key0 = of_sequence * BN, key = key0 + blockIdx.y * KEYS + threadIdx.x / COLUMNS;
+    if (key0 < 0 || key >= S.n_k || e >= A.dim) return;
+    const long long at = (long long)(S.k0 + key) * A.kv_heads + kvh;
+    v4f sums[2] = {};
+    for (int split = 0; split < A.splits; split += 4) {
+        v4f x[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int which = 0; which < 2; ++which) x[i][which] = split + i < A.splits ? *(const v4f *)(part_at(A, split + i, which, at) + e) : (v4f)(0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int which = 0; which < 2; ++which) sums[which] += x[i][which];
+    }
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+        *(v2u *)(global_at<uint8_t>(which ? A.dv : A.dk) + (at * A.dim + e) * 2) = (v2u){T::pack(sums[which][0], sums[which][1]), T::pack(sums[which][2], sums[which][3])};
+}
+
+// A workgroup has a compute unit to itself.  Where the keys are too few to give each one, the heads that share a key head are shared out as well.
+int splits_for(long long blocks, int kv_heads, int group, int compute_units) { return (int)std::clamp(compute_units / std::max(blocks * kv_heads, 1ll), 1ll, (long long)group); }
 
 // ---------------------------------------------------------------------- dq ---
 // The same the other way round: 128 rows' q and do of one key head stay in LDS, keys and values go by, 64 at a time.  Eight wavefronts: four times 32 rows,
@@ -425,19 +481,26 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
     store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, limit < 0);
 }
 
-template <class T, int D> int launch(const GradArgs &A, hipStream_t stream)
+template <class T, int D> int launch(GradArgs A, int compute_units, hipStream_t stream)
 {
     const long long deltas = (long long)((max(A.tokens_q, A.tokens_k) + 63) / 64) * (A.heads + A.kv_heads);
     const long long keys = block_numbers(A.tokens_k, A.n_seqs, 1, BN) * A.kv_heads, queries = block_numbers(A.tokens_q, A.n_seqs, A.group, BN) * A.kv_heads;
     if (deltas > 0x7fffffffll || keys > 0x7fffffffll || queries > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    A.splits = splits_for(block_numbers(A.tokens_k, A.n_seqs, 1, BN), A.kv_heads, A.group, compute_units);
     hipLaunchKernelGGL((delta_kernel<T>), dim3((unsigned)deltas), dim3(256), 0, stream, A);
     hipLaunchKernelGGL((queries_kernel<T, D>), dim3((unsigned)queries), dim3(512), 0, stream, A);
-    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)keys), dim3(512), 0, stream, A);
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)keys, A.splits), dim3(512), 0, stream, A);
+    if (A.splits > 1) hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)keys, BN * D / 1024), dim3(256), 0, stream, A);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
 
 size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
 size_t delta_bytes(const rb_heads *H, int tokens_q) { return rounded((size_t)tokens_q * H->heads * 4); }
+size_t parts_bytes(const rb_heads *H, int tokens_k)      // (more sequences are not fewer blocks)
+{
+    const int splits = splits_for((tokens_k + BN - 1) / BN, H->kv_heads, H->heads / H->kv_heads, rb::mx::device_groups());
+    return splits < 2 ? 0 : (size_t)splits * 2 * tokens_k * H->kv_heads * H->dim * 4;
+}
 size_t most_bytes(int tokens, int heads) { return rounded((size_t)((tokens + 63) / 64) * heads * 4); }
 
 }  // namespace
@@ -449,7 +512,7 @@ using namespace rb::attn;
 extern "C" size_t rb_attn_grad_workspace_bytes(const rb_heads *H, int tokens_q, int tokens_k)
 {
     if (check_heads(H) != RB_OK || tokens_q < 1 || tokens_k < 1) return 0;
-    return delta_bytes(H, tokens_q) + most_bytes(tokens_q, H->heads) + most_bytes(tokens_k, H->kv_heads);
+    return delta_bytes(H, tokens_q) + most_bytes(tokens_q, H->heads) + most_bytes(tokens_k, H->kv_heads) + parts_bytes(H, tokens_k);
 }
 
 extern "C" int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, const int32_t *first_q,
@@ -473,11 +536,13 @@ extern "C" int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void
     A.delta = rb::address_of(workspace);
     A.most_o = A.delta + delta_bytes(H, tokens_q);
     A.most_v = A.most_o + most_bytes(tokens_q, H->heads);
+    A.parts = A.most_v + most_bytes(tokens_k, H->kv_heads);
     A.dq = rb::address_of(dq), A.dk = rb::address_of(dk), A.dv = rb::address_of(dv);
     A.n_seqs = n_seqs, A.tokens_q = tokens_q, A.tokens_k = tokens_k;
     A.heads = H->heads, A.kv_heads = H->kv_heads, A.group = H->heads / H->kv_heads, A.dim = H->dim, A.causal = causal != 0;
     A.c = scale * LOG2E, A.scale = scale;
+    const int units = rb::mx::device_groups();
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (H->dtype == RB_F16) return A.dim <= 64 ? launch<F16, 64>(A, st) : launch<F16, 128>(A, st);
-    return A.dim <= 64 ? launch<BF16, 64>(A, st) : launch<BF16, 128>(A, st);
+    if (H->dtype == RB_F16) return A.dim <= 64 ? launch<F16, 64>(A, units, st) : launch<F16, 128>(A, units, st);
+    return A.dim <= 64 ? launch<BF16, 64>(A, units, st) : launch<BF16, 128>(A, units, st);
 }
