@@ -453,7 +453,7 @@ int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void *q, const 
  * (elements, multiples of 8; elements of a head are contiguous), 16-byte
  * aligned.  Position p of sequence s lies in page table[s * width + p /
  * page_tokens], place p % page_tokens (device int32 [n_seqs][width]; entries
- * behind a sequence's last position are not read).
+ * behind a sequence's last position are not used).
  */
 typedef struct rb_cache {
     void *k, *v;

@@ -271,32 +271,36 @@ __device__ __forceinline__ int sequence_of_block(const int *first, int n_seqs, i
 }
 
 // Of up to MOST_ORDERED sequences: their blocks in descending order of work, so that the longest start first and short ones fill the gaps.  count(n_q, n_k, x): how many
-// blocks of such a sequence have a work of x or more, all of them for x = 0; `most`: a bound on the work.  Lane s holds sequence s.  False: there are not so many blocks.
-// (Five sequences of 1 to 2048 tokens, 32 query and 8 key heads: see the kernels.)
+// blocks of such a sequence have a work of x or more, all of them for x = 0; `most`: a bound on the work.  n_q, n_k: of sequence lane % pad, where pad is
+// the power of two that holds n_seqs (zeros past them): so many lanes add up a count, and the groups of them look at several x at once.  False: there are not so many blocks.
+// Every workgroup does this for itself, in one to five microseconds.  (Heads of 128, 32 query and 8 key heads, against the order of the sequences: two sequences of 4000 tokens in all
+// 87 -> 83 us; five of 6000 the same forwards and the keys' part of the gradient 289 -> 259; eleven of 6300, not causal, 12 and 4 heads of 64, 46 -> 41; sixteen of 6000 60 -> 58.5;
+// 17 of 6000 52 -> 61; 40 of 8000 55 -> 79; and where all workgroups run at once only the time for it is left, sixteen of 1000 8.3 -> 9.6.)
 constexpr int MOST_ORDERED = 16;
+__device__ __forceinline__ int padded(int n_seqs) { return 1 << (32 - __builtin_clz(n_seqs - 1)); }      // (n_seqs >= 2)
 template <class Count> __device__ __forceinline__ bool nth_heaviest(int n_seqs, int n_q, int n_k, int nth, int most, int lane, int &s, int &block, Count count)
 {
-    auto all = [&](int x) {
-        int sum = 0;
-        for (int i = 0; i < n_seqs; ++i) sum += count(__builtin_amdgcn_readlane(n_q, i), __builtin_amdgcn_readlane(n_k, i), x);
-        return sum;
+    const int pad = padded(n_seqs), groups = 64 / pad, group = lane / pad;
+    auto over_sequences = [&](int v) {
+        for (int d = 1; d < pad; d <<= 1) v += __shfl_xor(v, d);
+        return v;
     };
-    if (all(0) <= nth) return false;
-    int lo = 0, n = most + 1;      // the largest x of which there are more than nth lies in lo .. lo + n - 1; a lane looks at one x
+    if (__builtin_amdgcn_readfirstlane(over_sequences(count(n_q, n_k, 0))) <= nth) return false;
+    int lo = 0, n = most + 1;      // the largest x of which there are more than nth lies in lo .. lo + n - 1
     while (n > 1) {
-        const int step = (n + 63) / 64, x = lo + min(lane * step, n - 1);
-        const int k = max(0, __popcll(__ballot(lane * step < n && all(x) > nth)) - 1);
-        lo += k * step;
-        n = min(step, n - k * step);
+        const int step = (n + groups) / (groups + 1), at = (group + 1) * step;
+        const int more = __popcll(__ballot(over_sequences(count(n_q, n_k, lo + min(at, n))) > nth && at < n)) / pad;
+        lo += more * step;
+        n = min(step, n - more * step);
     }
-    const int here = lane < n_seqs ? count(n_q, n_k, lo) : 0, heavier = lane < n_seqs ? count(n_q, n_k, lo + 1) : 0;
-    nth -= all(lo + 1);      // among those of work lo, in the order of the sequences
+    const int here = count(n_q, n_k, lo), heavier = count(n_q, n_k, lo + 1);
+    nth -= __builtin_amdgcn_readfirstlane(over_sequences(heavier));      // among those of work lo, in the order of the sequences
     int upto = here - heavier;
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < pad; d <<= 1) {
         const int v = __shfl_up(upto, d);
         if (lane >= d) upto += v;
     }
-    s = __builtin_amdgcn_readfirstlane(__popcll(__ballot(upto <= nth)));
+    s = min(__builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < n_seqs && upto <= nth))), n_seqs - 1);
     block = __builtin_amdgcn_readlane(heavier, s) + nth - (s ? __builtin_amdgcn_readlane(upto, s - 1) : 0);
     return true;
 }
@@ -318,18 +322,23 @@ __device__ __forceinline__ Sequence sequence_at(const int *first_q, const int *f
     return r;
 }
 
-// Which sequence and which of its blocks a workgroup's number stands for; false: none.  Blocks of BM rows (keys: BM keys), heaviest first: causal rows see more the
-// later they are, causal keys are seen by more the earlier they are.
+// `running`: how many workgroups run at once
+inline bool ordered_for(int n_seqs, long long workgroups, long long running) { return n_seqs > 1 && n_seqs <= MOST_ORDERED && workgroups > running; }
+
+// Which sequence and which of its blocks a workgroup's number stands for; false: none.  Blocks of BM rows (keys: BM keys), if `ordered` heaviest first, by steps of 64 keys (rows): causal
+// rows see more the later they are, causal keys are seen by more the earlier they are.
 template <int BM>
-__device__ __forceinline__ bool rows_of_workgroup(const int *first_q, const int *first_k, int n_seqs, int tokens_q, int tokens_k, int group, bool causal, int number, int numbers, int lane, int &s, int &block)
+__device__ __forceinline__ bool rows_of_workgroup(const int *first_q, const int *first_k, int n_seqs, bool ordered, int tokens_q, int tokens_k, int group, bool causal, int number, int numbers, int lane, int &s, int &block)
 {
-    if (n_seqs > 1 && n_seqs <= MOST_ORDERED) {
-        const int i = min(lane, n_seqs - 1);
-        const int q0 = min(max(first_q[i], 0), tokens_q), n_q = min(max(first_q[i + 1], q0), tokens_q) - q0, k0 = min(max(first_k[i], 0), tokens_k), n_k = min(max(first_k[i + 1], k0), tokens_k) - k0;
+    if (ordered) {
+        const int at = lane & (padded(n_seqs) - 1), i = min(at, n_seqs - 1);
+        const int q0 = min(max(first_q[i], 0), tokens_q), k0 = min(max(first_k[i], 0), tokens_k);
+        const int n_q = at < n_seqs ? min(max(first_q[i + 1], q0), tokens_q) - q0 : 0, n_k = at < n_seqs ? min(max(first_k[i + 1], k0), tokens_k) - k0 : 0;
         auto blocks = [&](int rows) { return (rows * group + BM - 1) / BM; };
-        if (!nth_heaviest(n_seqs, n_q, n_k, number, tokens_k, lane, s, block, [&](int q, int k, int x) {
-                if (x == 0 || !causal) return k >= x ? blocks(q) : 0;
-                return k < x ? 0 : min(blocks(q), (int)((long long)(k - x) * group / BM) + 1);
+        if (!nth_heaviest(n_seqs, n_q, n_k, number, tokens_k / 64, lane, s, block, [&](int q, int k, int x) {
+                const int beyond = k - x * 64;
+                if (x == 0 || !causal) return beyond >= 0 ? blocks(q) : 0;
+                return beyond < 0 ? 0 : min(blocks(q), (int)((long long)beyond * group / BM) + 1);
             }))
             return false;
         if (causal) block = blocks(__builtin_amdgcn_readlane(n_q, s)) - 1 - block;
@@ -341,15 +350,16 @@ __device__ __forceinline__ bool rows_of_workgroup(const int *first_q, const int 
     return true;
 }
 template <int BM>
-__device__ __forceinline__ bool keys_of_workgroup(const int *first_q, const int *first_k, int n_seqs, int tokens_q, int tokens_k, bool causal, int number, int lane, int &s, int &block)
+__device__ __forceinline__ bool keys_of_workgroup(const int *first_q, const int *first_k, int n_seqs, bool ordered, int tokens_q, int tokens_k, bool causal, int number, int lane, int &s, int &block)
 {
-    if (n_seqs > 1 && n_seqs <= MOST_ORDERED) {
-        const int i = min(lane, n_seqs - 1);
-        const int q0 = min(max(first_q[i], 0), tokens_q), n_q = min(max(first_q[i + 1], q0), tokens_q) - q0, k0 = min(max(first_k[i], 0), tokens_k), n_k = min(max(first_k[i + 1], k0), tokens_k) - k0;
-        return nth_heaviest(n_seqs, n_q, n_k, number, tokens_q, lane, s, block, [&](int q, int k, int x) {
+    if (ordered) {
+        const int at = lane & (padded(n_seqs) - 1), i = min(at, n_seqs - 1);
+        const int q0 = min(max(first_q[i], 0), tokens_q), k0 = min(max(first_k[i], 0), tokens_k);
+        const int n_q = at < n_seqs ? min(max(first_q[i + 1], q0), tokens_q) - q0 : 0, n_k = at < n_seqs ? min(max(first_k[i + 1], k0), tokens_k) - k0 : 0;
+        return nth_heaviest(n_seqs, n_q, n_k, number, tokens_q / 64, lane, s, block, [&](int q, int k, int x) {
             const int blocks = (k + BM - 1) / BM;
-            if (x == 0 || !causal) return q >= x ? blocks : 0;
-            return q < x || k < x ? 0 : min(blocks, (k - x) / BM + 1);
+            if (x == 0 || !causal) return q >= x * 64 ? blocks : 0;
+            return q < x * 64 || k < x * 64 ? 0 : min(blocks, (k - x * 64) / BM + 1);
         });
     }
     s = sequence_of_block(first_k, n_seqs, 1, BM, number, lane);
@@ -367,7 +377,7 @@ struct Args {
     Address o, lse, first_q, first_k;        // paged: first_k holds the sequences' lengths
     Address table;
     long long page;
-    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
+    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal, ordered;
     int page_shift, pages, width;
     Address parts;                           // workspace
     int wanted;                              // workgroups per key head that the work is shared out to; 0: one per block of rows

@@ -68,8 +68,9 @@ __device__ __forceinline__ Args with_shares(Args A, const int *first, const int 
 // three wavefronts per SIMD, the same on long prompts and a fifth slower on short ones; a pipeline within a wavefront, scores of one half of a tile
 // beside the weights of the other, 1.08 ms; eight wavefronts and three tiles ahead, 1.09 ms; operand reads left to the compiler, 1.11 ms.
 //
-// HALVES = 2: eight wavefronts, four of them with the first 32 keys of every tile and four with the second, joined at the end.  A step then takes little more than half
-// as long where a workgroup has a compute unit to itself; where there is a second one to fill it, there is nothing to gain.
+// HALVES = 2: eight wavefronts, four of them with the first 32 keys of every tile and four with the second, joined at the end.  For calls of no more workgroups than compute units: a step
+// takes less time where a workgroup has one to itself (fp16, heads of 128, causal: 64 tokens of 8 heads 12.4 -> 9.9 us, 333 of 32 13.4 -> 12.3, 512 of 32 16.3 -> 15.3, 8192 of one head
+// 141 -> 111), while two workgroups fill a compute unit as well as one of twice the size, without the join.
 template <class T, int D, bool PAGED, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 {
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
     int s, of_sequence, split = 0, splits = 1;
     [[maybe_unused]] int slot = 0;      // of this workgroup's part
     if constexpr (!PAGED) {
-        if (!rows_of_workgroup<BM>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.group, A.causal, number, numbers, lane, s, of_sequence)) return;
+        if (!rows_of_workgroup<BM>(first_q, first_k, A.n_seqs, A.ordered, A.tokens_q, A.tokens_k, A.group, A.causal, number, numbers, lane, s, of_sequence)) return;
     } else if (!A.wanted) {
         const int block = numbers - 1 - number;      // the longest first
         s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
@@ -313,10 +314,11 @@ size_t parts_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, in
     return slots * kv_heads * (dim <= 64 ? PartOfRows<64, BM>::FLOATS : PartOfRows<128, BM>::FLOATS) * 4;
 }
 
-template <class T, int D> int launch_rows(const Args &A, bool paged, int compute_units, hipStream_t stream)
+template <class T, int D> int launch_rows(Args A, bool paged, int compute_units, hipStream_t stream)
 {
     const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = blocks + (long long)A.wanted * A.kv_heads;      // (a block that has a share of x has at most x + 1)
     if (n > 0x1fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    A.ordered = ordered_for(A.n_seqs, n, 2ll * compute_units);
     const dim3 grid((unsigned)n);
     if (paged) {
         hipLaunchKernelGGL((rows_kernel<T, D, true, 1>), grid, dim3(256), 0, stream, A);

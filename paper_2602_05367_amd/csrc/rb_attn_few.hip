@@ -4,6 +4,10 @@
 // all jobs of a key head, one after the other, are cut into equal shares, one per wavefront, wherever that falls: contexts of any mix of lengths load every
 // compute unit alike.  A wavefront keeps two tiles of keys and values on their way into LDS of its own, across jobs, and meets nobody.  What it has
 // of a job that it does not have all of goes to the workspace, unnormalised, and a second launch joins the parts in a fixed order.
+//
+// Bound: bytes, where there are enough of them (48 sequences of 250000 positions in all, 64 query and 8 key heads of 128, bf16: 178 us and 6 for the join, 5.7 TB/s;
+// six sequences of 3 to 5 drafts on 8500 positions, 40 heads: 34 and 5); else a chain of latencies, the arrays, the table, the keys, their scores, and a launch
+// for the join (one token on 2000 positions, 32 heads, fp16: 11 and 5 us).
 #include <hip/hip_runtime.h>
 #include <algorithm>
 

@@ -34,12 +34,13 @@ struct GradArgs {
     Address parts;                      // workspace: [splits][dk, dv][tokens_k][kv_heads][dim] fp32, where there are several splits
     Address dq, dk, dv;
     int splits;                         // workgroups that share the query heads of the same keys
-    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal;
+    int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal, ordered, ordered_keys;
     float c, scale;
 };
 
 // ------------------------------------------------------- delta and maxima ---
-// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o, or of v.
+// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o, or of v.  Bound: bytes (6000 tokens of 32 heads of 128, bf16: 19.5 us,
+// 5.1 TB/s).
 template <class T> __global__ __launch_bounds__(256) void delta_kernel(const GradArgs A)
 {
     __shared__ uint32_t most[4];
@@ -128,7 +129,10 @@ template <int E> __device__ __forceinline__ bool add_halves(v16f (&sums)[E], uin
 
 // --------------------------------------------------------------- dk and dv ---
 // A workgroup keeps 128 keys and values of one key head in LDS and takes the queries and do of all its query heads, 64 rows at a
-// time, through LDS.  Eight wavefronts: four times 32 keys, by the upper and the lower 32 rows of a tile, whose sums are added at the end.
+// time, through LDS.  Eight wavefronts: four times 32 keys, by the upper and the lower 32 rows of a tile, whose sums are added at the end.  All operands come from LDS,
+// since the two sums of 32 keys fill half of the registers (with keys and values in registers they spilled, which costs more than twice the time: what is spilled waits behind
+// the loads).  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part, and the power the former may draw (five sequences of 6000 tokens in all,
+// 32 heads of 128, causal, bf16: 259 us, 0.66 PFLOP/s for its four products).  Blocks in the order of the sequences instead of the heaviest first: 289 us.
 constexpr int BN = 128;
 __device__ __forceinline__ float *part_at(const GradArgs &A, int split, int which, long long row)
 {
@@ -150,7 +154,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     const int first_g = A.group * split / A.splits, heads_of = A.group * (split + 1) / A.splits - first_g;
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     int s, of_sequence;
-    if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.causal, block, lane, s, of_sequence)) return;
+    if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.ordered_keys, A.tokens_q, A.tokens_k, A.causal, block, lane, s, of_sequence)) return;
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
     const int key0 = of_sequence * BN;
     if (key0 < 0 || key0 >= S.n_k) return;
@@ -305,14 +309,14 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     store_columns<T, D>(sums_k, scale_k, global_at<uint8_t>(A.dk) + at * (A.dim * 2), A.dim, h, real, false);
 }
 
-// The splits' sums, one after the other: eight keys per workgroup, four elements per thread
+// The splits' sums, one after the other, in fp32: four elements per thread.  Bound: latency, so four parts are on their way at once (four splits of 230 tokens: 4 us).
 template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const GradArgs A)
 {
     constexpr int COLUMNS = D / 4, KEYS = 256 / COLUMNS;
     const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, e = threadIdx.x % COLUMNS * 4;
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     int s, of_sequence;
-    if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.causal, blockIdx.x / A.kv_heads, lane, s, of_sequence)) return;
+    if (!keys_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.ordered_keys, A.tokens_q, A.tokens_k, A.causal, blockIdx.x / A.kv_heads, lane, s, of_sequence)) return;
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
     const int key0 = of_sequence * BN, key = key0 + blockIdx.y * KEYS + threadIdx.x / COLUMNS;
     if (key0 < 0 || key >= S.n_k || e >= A.dim) return;
@@ -334,12 +338,14 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
         *(v2u *)(global_at<uint8_t>(which ? A.dv : A.dk) + (at * A.dim + e) * 2) = (v2u){T::pack(sums[which][0], sums[which][1]), T::pack(sums[which][2], sums[which][3])};
 }
 
-// A workgroup has a compute unit to itself.  Where the keys are too few to give each one, the heads that share a key head are shared out as well.
+// A workgroup has a compute unit to itself.  Where the keys are too few to give each one, the heads that share a key head are shared out as well (230 tokens of 8 query and
+// 2 key heads of 96 33 -> 16.5 us and 4 for the join; 2000 tokens of 16 and 1 of 128 all kernels 937 -> 154 us).
 int splits_for(long long blocks, int kv_heads, int group, int compute_units) { return (int)std::clamp(compute_units / std::max(blocks * kv_heads, 1ll), 1ll, (long long)group); }
 
 // ---------------------------------------------------------------------- dq ---
 // The same the other way round: 128 rows' q and do of one key head stay in LDS, keys and values go by, 64 at a time.  Eight wavefronts: four times 32 rows,
-// by the first and the second 32 keys of a tile, whose sums are added at the end.
+// by the first and the second 32 keys of a tile, whose sums are added at the end.  (The same sequences: 240 us, 0.71 PFLOP/s for four products.  Four wavefronts that keep q and do
+// in registers, 32 keys at a time: 205 to 213 us there, but 28 instead of 23.5 where a workgroup has a compute unit to itself, 512 tokens of 32 heads.)
 template <class T, int D>
 __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
 {
@@ -354,7 +360,7 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
     const int kvh = blockIdx.x % A.kv_heads;
     const int *first_q = global_at<const int>(A.first_q), *first_k = global_at<const int>(A.first_k);
     int s, of_sequence;
-    if (!rows_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.tokens_q, A.tokens_k, A.group, A.causal, blockIdx.x / A.kv_heads, gridDim.x / A.kv_heads, lane, s, of_sequence)) return;
+    if (!rows_of_workgroup<BN>(first_q, first_k, A.n_seqs, A.ordered, A.tokens_q, A.tokens_k, A.group, A.causal, blockIdx.x / A.kv_heads, gridDim.x / A.kv_heads, lane, s, of_sequence)) return;
     const Sequence S = sequence_at(first_q, first_k, s, A.tokens_q, A.tokens_k);
     const int row0 = of_sequence * BN, n_rows = S.n_q * A.group;
     if (row0 < 0 || row0 >= n_rows) return;
@@ -487,6 +493,7 @@ template <class T, int D> int launch(GradArgs A, int compute_units, hipStream_t 
     const long long keys = block_numbers(A.tokens_k, A.n_seqs, 1, BN) * A.kv_heads, queries = block_numbers(A.tokens_q, A.n_seqs, A.group, BN) * A.kv_heads;
     if (deltas > 0x7fffffffll || keys > 0x7fffffffll || queries > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     A.splits = splits_for(block_numbers(A.tokens_k, A.n_seqs, 1, BN), A.kv_heads, A.group, compute_units);
+    A.ordered = ordered_for(A.n_seqs, queries, compute_units), A.ordered_keys = ordered_for(A.n_seqs, keys * A.splits, compute_units);
     hipLaunchKernelGGL((delta_kernel<T>), dim3((unsigned)deltas), dim3(256), 0, stream, A);
     hipLaunchKernelGGL((queries_kernel<T, D>), dim3((unsigned)queries), dim3(512), 0, stream, A);
     hipLaunchKernelGGL((keys_kernel<T, D>), dim3((unsigned)keys, A.splits), dim3(512), 0, stream, A);

@@ -219,7 +219,7 @@ def run(state):
         for layers, norms in state["blocks"]:
             q, k, v, o, gate, up, down = layers
             n = rb.rb_rmsnorm(x, norms[0], 1e-5)
-            kv += [rb.rb_linear_gemm(m, n) for m in (q, k, v)]      # attention is not this library's: o reads v
+            kv += [rb.rb_linear_gemm(m, n) for m in (q, k, v)]      # the linear layers alone, without attention: o reads v
             x = rb.rb_add(rb.rb_linear_gemm(o, kv[-1]), x)
             n = rb.rb_rmsnorm(x, norms[1], 1e-5)
             a = rb.rb_silu_mul(rb.rb_linear_gemm(gate, n), rb.rb_linear_gemm(up, n))

@@ -82,3 +82,18 @@ def test_drafts_of_many_sequences():
     lengths = [int(x) + n for x, n in zip(np.exp(rng.uniform(0, 7, 90)), new)]
     cache, table, hold = build_cache(rng, lengths, 32, 2, 128, BF16)
     check_paged(_rand(rng, sum(new), 8, 128, dtype=BF16, gain=2.0), cache, table, hold, new, lengths)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens", [[700, 450], [64, 700, 1, 450, 0, 333, 200, 90], [130, 0, 1, 257, 33, 90, 412, 128, 77, 5, 300, 64, 18, 201, 2, 60]])
+def test_sequences_whose_blocks_are_taken_heaviest_first(lens, causal):
+    """More blocks than run at once, of up to sixteen sequences."""
+    rng = synth.child_rng(365, len(lens), causal)
+    t, other = sum(lens), [int(x) for x in rng.permutation(lens)]
+    for heads, kv, lens_k in ((60, 60, lens), (42, 14, other)):
+        q, go = (_rand(rng, t, heads, 64, gain=g) for g in (2.0, 0.01))
+        k, v = (_rand(rng, t, kv, 64) for _ in range(2))
+        check_prompt(q, k, v, lens, lens_k, causal)
+        if heads == 42:
+            grad.check(go, q, k, v, lens, lens_k, causal)
+            grad.check(go, q, k, v, lens, lens, causal)
