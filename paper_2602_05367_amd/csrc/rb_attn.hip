@@ -68,9 +68,11 @@ __device__ __forceinline__ Args with_shares(Args A, const int *first, const int 
 // three wavefronts per SIMD, the same on long prompts and a fifth slower on short ones; a pipeline within a wavefront, scores of one half of a tile
 // beside the weights of the other, 1.08 ms; eight wavefronts and three tiles ahead, 1.09 ms; operand reads left to the compiler, 1.11 ms.
 //
-// HALVES = 2: eight wavefronts, four of them with the first 32 keys of every tile and four with the second, joined at the end.  For calls of no more workgroups than compute units: a step
-// takes less time where a workgroup has one to itself (fp16, heads of 128, causal: 64 tokens of 8 heads 12.4 -> 9.9 us, 333 of 32 13.4 -> 12.3, 512 of 32 16.3 -> 15.3, 8192 of one head
-// 141 -> 111), while two workgroups fill a compute unit as well as one of twice the size, without the join.
+// HALVES = 2: eight wavefronts, four of them with the first 32 keys of every tile and four with the second, joined at the end.  For calls of no more workgroups than compute units, and
+// of one sequence up to twice as many: a step takes less time where a workgroup has a compute unit to itself, and the longest blocks of one long sequence decide its time (fp16, causal,
+// heads of 128: 64 tokens of 8 heads 12.4 -> 9.9 us, 512 of 32 16.3 -> 15.3, 1200 of 32 and 8 28.6 -> 25.3, 8192 of one head 141 -> 111, 6000 of 8 116 -> 96; heads of 64 3 to 10 %).
+// Beyond, two workgroups fill a compute unit as well as one of twice the size, without the join (2600 tokens of 32 and 8 heads, 656 workgroups, 67 and 78 us; eight sequences of 1000
+// tokens in all, 312 workgroups, 11.5 and 16.8).
 template <class T, int D, bool PAGED, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 {
@@ -324,7 +326,7 @@ template <class T, int D> int launch_rows(Args A, bool paged, int compute_units,
         hipLaunchKernelGGL((rows_kernel<T, D, true, 1>), grid, dim3(256), 0, stream, A);
         const int joined = rows_joined(blocks, BM);
         if (A.wanted) hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)blocks, (unsigned)std::min((long long)BM / joined, std::max(JOINING / blocks, 1ll))), dim3(256), 0, stream, A, joined);
-    } else if (n <= compute_units) {
+    } else if (n <= (A.n_seqs == 1 ? 2 : 1) * compute_units) {
         hipLaunchKernelGGL((rows_kernel<T, D, false, 2>), grid, dim3(512), 0, stream, A);
     } else {
         hipLaunchKernelGGL((rows_kernel<T, D, false, 1>), grid, dim3(256), 0, stream, A);

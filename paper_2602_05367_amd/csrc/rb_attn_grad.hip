@@ -132,7 +132,7 @@ template <int E> __device__ __forceinline__ bool add_halves(v16f (&sums)[E], uin
 // time, through LDS.  Eight wavefronts: four times 32 keys, by the upper and the lower 32 rows of a tile, whose sums are added at the end.  All operands come from LDS,
 // since the two sums of 32 keys fill half of the registers (with keys and values in registers they spilled, which costs more than twice the time: what is spilled waits behind
 // the loads).  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part, and the power the former may draw (five sequences of 6000 tokens in all,
-// 32 heads of 128, causal, bf16: 259 us, 0.66 PFLOP/s for its four products).  Blocks in the order of the sequences instead of the heaviest first: 289 us.
+// 32 heads of 128, causal, bf16: 265 us, 0.65 PFLOP/s for its four products).  Blocks in the order of the sequences instead of the heaviest first: 289 us.
 constexpr int BN = 128;
 __device__ __forceinline__ float *part_at(const GradArgs &A, int split, int which, long long row)
 {
