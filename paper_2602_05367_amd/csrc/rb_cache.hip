@@ -23,21 +23,37 @@ union Four {
 
 // Element pairs (x, y) of a head become (x cos - y sin, y cos + x sin), products and sum in fp32 and rounded once.  Eight elements per thread, so every load is of eight or sixteen
 // bytes: four of either half of a head, or eight in a row where pairs are neighbours or nothing is turned.  A workgroup has elements of one token and finds its sequence itself.
-// Bound: bytes (sixteen prompts of 6000 tokens in all, 64 and 8 heads of 128, bf16: 43 us, 5.7 TB/s); one token: latencies, 3.0 us.
+// Bound: bytes (sixteen prompts of 6000 tokens in all, 64 and 8 heads of 128, bf16: 42 us, 5.8 TB/s); one token: latencies, 3 us.  The elements are
+// on their way while the place is looked up (after it: 44 us).
 template <class T, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append_kernel(const AppendArgs A)
 {
     const int token = blockIdx.x / A.blocks, part = blockIdx.x % A.blocks, lane = threadIdx.x & 63;
-    const int *first = global_at<const int>(A.first);
-    const int s = last_not_beyond(A.n_seqs, token, lane, [&](int i) { return first[i]; });
-    const long long position = (long long)global_at<const int>(A.lengths)[s] - first[s + 1] + token;
-    const bool inside = position >= 0 && position < (long long)A.width << A.page_shift;
     const int pieces = A.dim / 8, unit = part * 256 + threadIdx.x, head = unit / pieces, piece = unit % pieces;
-    if (head >= A.heads + 2 * A.kv_heads) return;
-    const bool is_q = head < A.heads, is_v = head >= A.heads + A.kv_heads;
+    const bool there = head < A.heads + 2 * A.kv_heads;
+    const bool is_q = head < A.heads, is_v = head >= A.heads + A.kv_heads, turned = !is_v && piece * 8 < A.rotary;
     const int kvh = is_q ? head : head - A.heads - (is_v ? A.kv_heads : 0);
-    const Side &from_side = is_q ? A.q : is_v ? A.v : A.k;
-    const uint8_t *from = global_at<const uint8_t>(from_side.at) + token * from_side.token + kvh * from_side.head;
+    const int at_x = piece * (INTERLEAVED || !turned ? 16 : 8), at_y = INTERLEAVED || !turned ? at_x + 8 : at_x + A.rotary;      // bytes
+    Four a = {}, b = {};
+    if (there) {      // on the way while the place is looked up
+        const Side &from_side = is_q ? A.q : is_v ? A.v : A.k;
+        const uint8_t *from = global_at<const uint8_t>(from_side.at) + token * from_side.token + kvh * from_side.head;
+        a.w = *(const v2u *)(from + at_x);
+        b.w = *(const v2u *)(from + at_y);
+    }
+    const int *first = global_at<const int>(A.first), *lengths = global_at<const int>(A.lengths);
+    int s, end, length;      // the token's sequence, where it ends, its positions
+    if (A.n_seqs < 64) {
+        const int starts = first[min(lane, A.n_seqs)], all = lengths[min(lane, A.n_seqs - 1)];
+        s = max(__popcll(__ballot(lane < A.n_seqs && starts <= token)) - 1, 0);
+        end = __builtin_amdgcn_readlane(starts, s + 1), length = __builtin_amdgcn_readlane(all, s);
+    } else {
+        s = last_not_beyond(A.n_seqs, token, lane, [&](int i) { return first[i]; });
+        end = first[s + 1], length = lengths[s];
+    }
+    const long long position = (long long)length - end + token;
+    const bool inside = position >= 0 && position < (long long)A.width << A.page_shift;
+    if (!there) return;
     uint8_t *to;
     if (is_q) {
         to = global_at<uint8_t>(A.q_to) + ((long long)token * A.heads + head) * (A.dim * 2);
@@ -46,16 +62,12 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs A)
         const int p = (int)position, page = min(max(global_at<const int>(A.table)[(long long)s * A.width + (p >> A.page_shift)], 0), A.pages - 1);
         to = global_at<uint8_t>(is_v ? A.v_to : A.k_to) + page * A.page + (p & ((1 << A.page_shift) - 1)) * A.token_stride + kvh * A.head_stride;
     }
-    if (is_v || piece * 8 >= A.rotary) {
-        *(v4u *)(to + piece * 16) = *(const v4u *)(from + piece * 16);
+    if (!turned) {
+        *(v4u *)(to + at_x) = (v4u){a.w.x, a.w.y, b.w.x, b.w.y};
         return;
     }
     const long long row = min(max(position, 0ll), (long long)A.table_rows - 1) * (A.rotary / 2) + piece * 4;
     const v4f c = *(const v4f *)(global_at<const float>(A.cos) + row), sn = *(const v4f *)(global_at<const float>(A.sin) + row);
-    const int at_x = piece * (INTERLEAVED ? 16 : 8), at_y = INTERLEAVED ? at_x + 8 : at_x + A.rotary;      // bytes
-    Four a, b;
-    a.w = *(const v2u *)(from + at_x);
-    b.w = *(const v2u *)(from + at_y);
     float x[4], y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
