@@ -21,8 +21,8 @@ union Four {
     uint16_t h[4];
 };
 
-// Element pairs (x, y) of a head become (x cos - y sin, y cos + x sin), products and sum in fp32 and rounded once.  Eight elements per thread, so every load is of eight or sixteen
-// bytes: four of either half of a head, or eight in a row where pairs are neighbours or nothing is turned.  A workgroup has elements of one token and finds its sequence itself.
+// Element pairs (x, y) of a head become (x cos - y sin, y cos + x sin), products and sum in fp32 and rounded once.  Eight elements per thread, so loads and stores are
+// of eight bytes or sixteen: four of either half of a head, or eight in a row where pairs are neighbours or nothing is turned.  A workgroup has elements of one token and finds its sequence itself.
 // Bound: bytes (sixteen prompts of 6000 tokens in all, 64 and 8 heads of 128, bf16: 42 us, 5.8 TB/s); one token: latencies, 3 us.  The elements are
 // on their way while the place is looked up (after it: 44 us).
 template <class T, bool INTERLEAVED>
