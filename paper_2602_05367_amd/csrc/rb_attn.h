@@ -408,9 +408,9 @@ template <class Shape> struct Sums {
     {
         const int s = min(lane, A.n_seqs - 1);
         q0 = first[s], q1 = first[s + 1], length = lengths[s];
-        count_first();
+        upto = up_to_lane(lane < A.n_seqs ? Shape::of(A, q0, q1, length).count() : 0);
     }
-    __device__ __forceinline__ void count_first()
+    template <class Other> __device__ __forceinline__ Sums(const Args &A_, const Sums<Other> &o) : A(A_), first(o.first), lengths(o.lengths), lane(o.lane), q0(o.q0), q1(o.q1), length(o.length)
     {
         upto = up_to_lane(lane < A.n_seqs ? Shape::of(A, q0, q1, length).count() : 0);
     }

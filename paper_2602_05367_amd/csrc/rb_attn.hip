@@ -15,10 +15,10 @@ namespace {
 constexpr int BM = 128, KEYS = 64;
 
 // A cache is shared out to workgroups by what the lengths ask for: a block of rows has as many, each with a part of the keys, as it takes for none to have more than some number
-// of tiles.  That is the smallest such number, from the tiles per workgroup wanted up to twice those, for which no more workgroups start than run at once, and where the blocks
-// are too many for any, the least of them: workgroups then take turns.  (fp16, against the same number of parts for every block: 700, 64, 33 and 200 new tokens on 100, 4000, 9000 and
-// 2000, 64 query and 8 key heads of 128, 181 -> 82 us; 128 tokens on 30000, 8 heads, 53 -> 39; 512 tokens on 7500, 32 and 8 heads, where all parts are alike, 85 -> 88.  Sharing
-// the tiles out exactly, workgroups going on from one block to the next, took 121, 40 and 98: every start of a block costs some 4 us.)
+// of tiles.  That is the smallest of some numbers, from the tiles per workgroup wanted up to twice those, for which no more workgroups start than run at once, and where the blocks
+// are too many for any, or the sequences too many to try, the first: workgroups then take turns.  (fp16, against the same number of parts for every block: 700, 64, 33 and 200 new tokens
+// on 100, 4000, 9000 and 2000, 64 query and 8 key heads of 128, 181 -> 82 us; 128 tokens on 30000, 8 heads, 53 -> 39; 512 tokens on 7500, 32 and 8 heads, where all parts are alike,
+// 85 -> 88.  Sharing the tiles out exactly, workgroups going on from one block to the next, took 121, 40 and 98: every start of a block costs some 4 us.)
 constexpr float LEAST = 8.f;               // tiles of a part (512 new tokens: 23 us, with 4 26)
 constexpr long long GROUPS = 2, MANY = 4;  // workgroups per compute unit: wanted, and those of whole blocks that need no sharing
 constexpr long long JOINING = 2048;        // workgroups that join: all at once (8192, most of which find no work, 10 us more)
@@ -49,16 +49,21 @@ struct Slots : Blocks {      // of the workspace: one for each workgroup that ha
     __device__ __forceinline__ int count() const { return parts > 1 ? blocks * parts : 0; }
     static __device__ __forceinline__ Slots of(const Args &A, int q0, int q1, int length) { return Blocks::of(A, q0, q1, length); }
 };
-__device__ __forceinline__ Args with_shares(Args A, const int *first, const int *lengths, int lane)
+__device__ __forceinline__ Args with_shares(Args A, const Sums<Tiles> &tiles)
 {
-    const float share = max(Sums<Tiles>(A, first, lengths, lane).before(A.n_seqs) / (float)A.wanted, LEAST);
-    Sums<Groups> groups(A, first, lengths, lane);
-    for (float f = 1.f; f < 2.f; f += 0.1f) {
-        A.per_tile = 1.f / (share * f);
-        groups.count_first();
-        if (groups.before(A.n_seqs) <= A.wanted) return A;
+    const float share = max(tiles.before(A.n_seqs) / (float)A.wanted, LEAST);
+    float times = 1.f;
+    if (A.n_seqs <= 32) {      // each group of lanes tries another number
+        const int pad = A.n_seqs > 1 ? padded(A.n_seqs) : 1, s = tiles.lane & (pad - 1);
+        const int q0 = __shfl(tiles.q0, s), q1 = __shfl(tiles.q1, s), length = __shfl(tiles.length, s);
+        const float mine = 1.f + (float)(tiles.lane / pad) * pad / 64.f;
+        A.per_tile = 1.f / (share * mine);
+        int groups = s < A.n_seqs ? Groups::of(A, q0, q1, length).count() : 0;
+        for (int d = 1; d < pad; d <<= 1) groups += __shfl_xor(groups, d);
+        const unsigned long long fits = __ballot(groups <= A.wanted);
+        if (fits) times = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __builtin_ctzll(fits)));
     }
-    A.per_tile = 1.f / share;
+    A.per_tile = 1.f / (share * times);
     return A;
 }
 
@@ -94,8 +99,9 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
         s = sequence_of_block(first_q, A.n_seqs, A.group, BM, block, lane);
         of_sequence = block - block_start(first_q[s], s, A.group, BM);
     } else {
-        const Args B = with_shares(A, first_q, first_k, lane);
-        const Sums<Groups> groups(B, first_q, first_k, lane);
+        const Sums<Tiles> tiles_of(A, first_q, first_k, lane);
+        const Args B = with_shares(A, tiles_of);
+        const Sums<Groups> groups(B, tiles_of);
         int at = groups.before(A.n_seqs) - 1 - number;
         if (at < 0) return;
         s = __builtin_amdgcn_readfirstlane(groups.locate(at));
@@ -106,7 +112,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
         of_sequence = __builtin_amdgcn_readfirstlane((int)((unsigned)at / (unsigned)splits));
         split = __builtin_amdgcn_readfirstlane((int)((unsigned)at % (unsigned)splits));
         if (splits > 1) {
-            slot = Sums<Slots>(B, first_q, first_k, lane).before(s) + at;
+            slot = Sums<Slots>(B, tiles_of).before(s) + at;
             if (slot < 0 || slot >= 2 * A.wanted) return;      // (arrays that are not in order)
         }
     }
@@ -279,8 +285,9 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
 {
     const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads;
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
-    const Args B = with_shares(A, first, lengths, lane);
-    const Sums<Slots> slots(B, first, lengths, lane);
+    const Sums<Tiles> tiles_of(A, first, lengths, lane);
+    const Args B = with_shares(A, tiles_of);
+    const Sums<Slots> slots(B, tiles_of);
     const int s = __builtin_amdgcn_readfirstlane(slots.of_block(block));
     int q0, q1, length;
     slots.entries(s, q0, q1, length);
