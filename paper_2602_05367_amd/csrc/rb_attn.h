@@ -111,8 +111,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t *p, uint3
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, (int)bytes, 0x00020000);
 }
 
-// W wavefronts load a tile: the rows of a wavefront are consecutive.  Where this lane's part of load i lies behind row `behind` of the wavefront's part
-// (0: behind the tile's first row)
+// W wavefronts load a tile, each some consecutive rows of it.  at[i]: where this lane's piece of load i lies behind the start of the buffer, whose row 0 is the row
+// `first_row` rows before the wavefront's own
 template <int D, int ROWS, int W> struct Part {
     using L = Tile<D>;
     static constexpr int LOADS = ROWS / L::GROUP_ROWS / W;
@@ -385,7 +385,6 @@ struct Args {
     float c;                                 // scale log2(e): the exponentials are powers of two
 };
 
-
 // Weights are taken relative to a maximum that follows the scores only when they pass it by this many powers of two: the sums
 // are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
 constexpr float SLACK = 8.f;
@@ -395,8 +394,8 @@ __device__ __forceinline__ int positions(int length, int width, int page_shift)
 {
     return min(max(length, 0), (int)min((long long)width << page_shift, 0x7fffffc0ll));
 }
-// Work over a cache, shared out evenly: that of a key head is a row of tiles, sequence after sequence and job (a block of rows) after job, cut into equal shares wherever that
-// falls.  Shape says what a sequence has of it: of(A, q0, q1, length), count() tiles, blocks of JOB rows.
+// Work over a cache: that of a key head is a row of pieces (tiles, workgroups), sequence after sequence and job (a block of JOB rows) after job.  Shape says what a sequence has
+// of it: of(A, q0, q1, length), and count() pieces.
 //
 // Sums over the sequences, 64 at a time, the first 64 looked at once
 template <class Shape> struct Sums {
@@ -462,18 +461,6 @@ template <class Shape> struct Sums {
         return A.n_seqs;
     }
 };
-// All tiles in up to `most` equal shares of at least `least` tiles, the first ones longer by one
-struct Shares {
-    int n, each, longer;
-    __device__ __forceinline__ Shares(int all, int most, int least) : n(max(min(most, (int)((unsigned)all / (unsigned)least)), 1)), each((int)((unsigned)all / (unsigned)n)), longer(all - each * n) {}
-    __device__ __forceinline__ int start(int w) const { return w * each + min(w, longer); }
-    __device__ __forceinline__ int of(int tile) const
-    {
-        const unsigned in_longer = (unsigned)(each + 1) * longer;
-        return (unsigned)tile < in_longer ? (int)((unsigned)tile / (unsigned)(each + 1)) : longer + (int)(((unsigned)tile - in_longer) / (unsigned)each);
-    }
-};
-
 // workgroups that share `tiles` tiles: two tiles each at least
 __device__ __forceinline__ int splits_of(int tiles, int splits) { return max(min(splits, tiles / 2), 1); }
 
@@ -498,11 +485,6 @@ template <int D, int N> struct PartOfRows {
             for (int i = 0; i < 16; i += 4) *(v4f *)(row(r) + b * 32 + 2 * i + 4 * h) = (v4f){sums[b][i], sums[b][i + 1], sums[b][i + 2], sums[b][i + 3]};
     }
 };
-// the part that a share has of a job of N rows which it does not have all of: of its first job (0) or its last (1)
-template <int D, int N> __device__ __forceinline__ PartOfRows<D, N> part_of(Address workspace, int kvh, int shares, int share, int which)
-{
-    return PartOfRows<D, N>(workspace, ((size_t)kvh * shares + share) * 2 + which);
-}
 // Joins n_parts of the `joined` rows (two, four or eight) from row0 on, of which n_rows are there: o = sum of the parts' rows, each times 2^(its maximum - the
 // largest), over the sum of their totals likewise, in the order of the parts.  256 threads, four elements each; the groups of threads that make up a row share
 // out the parts.  Bound: latency, so all loads of sixteen parts and group are on their way before the first is used.  part(i): a PartOfRows; out(row): where

@@ -35,6 +35,24 @@ struct Shape {
         return {rows, (rows + ROWS - 1) / ROWS, rows ? max((positions(length, A.width, A.page_shift) + KEYS - 1) / KEYS, 1) : 0};
     }
 };
+// All tiles in equal shares, the first ones longer by one; never more shares than tiles: none is empty
+struct Shares {
+    int n, each, longer;
+    __device__ __forceinline__ Shares(int all, int wavefronts) : n(min(wavefronts, max(all, 1))), each((int)((unsigned)all / (unsigned)n)), longer(all - each * n) {}
+    __device__ __forceinline__ int start(int w) const { return w * each + min(w, longer); }
+    __device__ __forceinline__ int of(int tile) const
+    {
+        const unsigned in_longer = (unsigned)(each + 1) * longer;
+        return (unsigned)tile < in_longer ? (int)((unsigned)tile / (unsigned)(each + 1)) : longer + (int)(((unsigned)tile - in_longer) / (unsigned)each);
+    }
+};
+
+// the part that share w has of a job of which it does not have all: its first job (0) or its last (1)
+template <int D> __device__ __forceinline__ PartOfRows<D, ROWS> part_of(Address workspace, int kvh, int wavefronts, int w, int which)
+{
+    return PartOfRows<D, ROWS>(workspace, ((size_t)kvh * wavefronts + w) * 2 + which);
+}
+
 // a position in the row of tiles
 struct Cursor {
     int s, block, t;
@@ -54,7 +72,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     typedef const __attribute__((address_space(4))) int *Uniform;
     const Uniform table_u = (Uniform)global_at<const int>(A.table);
     const Sums<Shape> sums_of(A, first, lengths, lane);
-    const Shares shares(sums_of.before(A.n_seqs), wavefronts, 1);
+    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
     if (w >= shares.n) return;
     int begin = shares.start(w);
     const int n = shares.start(w + 1) - begin;
@@ -166,7 +184,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
             const bool empty = limit < 0;
             store_columns<T, D>(sums, empty ? 0.f : 1.f / total, global_at<uint8_t>(A.o) + ((long long)token * A.heads + head) * (A.dim * 2), A.dim, h, real, empty);
         } else if (real) {
-            part_of<D, ROWS>(A.parts, kvh, wavefronts, w, first_job ? 0 : 1).store(sums, top, total, lane & 31, h);
+            part_of<D>(A.parts, kvh, wavefronts, w, first_job ? 0 : 1).store(sums, top, total, lane & 31, h);
         }
         first_job = false;
     };
@@ -263,7 +281,7 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
     const Shape shape = Shape::of(A, q0, q1, length);
     const int b = block - block_start(q0, s, A.group, ROWS);
     if (b < 0 || b >= shape.blocks || b * ROWS + row0 >= shape.rows) return;
-    const Shares shares(sums_of.before(A.n_seqs), wavefronts, 1);
+    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
     const int from = sums_of.before(s) + b * shape.tiles, w0 = shares.of(from), w1 = shares.of(from + shape.tiles - 1);
     if (w0 == w1) return;      // it has stored the result
     const bool starts_inside = shares.start(w0) < from;      // the first part is that share's last, all others are their shares' first
@@ -272,7 +290,7 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
     auto token = [&](int r) { return (b * ROWS + r) / A.group; };
     join_rows<T, D>(
         joined, w1 - w0 + 1, row0, min(shape.rows - b * ROWS - row0, joined), A.dim,
-        [&](int i) { return part_of<D, ROWS>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
+        [&](int i) { return part_of<D>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
         [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + token(r)) * A.heads + kvh * A.group + (b * ROWS + r) % A.group) * (A.dim * 2); },
         [&](int r) { return n_k - n_q + token(r) < 0; });
 }

@@ -97,3 +97,33 @@ def test_sequences_whose_blocks_are_taken_heaviest_first(lens, causal):
         if heads == 42:
             grad.check(go, q, k, v, lens, lens_k, causal)
             grad.check(go, q, k, v, lens, lens, causal)
+
+
+def test_chunks_and_gradients_in_a_graph():
+    """Captured once, replayed with other lengths and other operands, each replay against the eager calls."""
+    rng = synth.child_rng(366)
+    new, lengths = [90, 1, 40], [1500, 300, 700]
+    cache, table, _ = build_cache(rng, lengths, 16, 2, 128, F16)
+    q, first, now = _rand(rng, sum(new), 8, 128), _starts(new), torch.tensor(lengths, dtype=torch.int32).cuda()
+    p, go = _rand(rng, sum(new), 8, 128), _rand(rng, sum(new), 8, 128)
+    k, v = _rand(rng, sum(new), 2, 128), _rand(rng, sum(new), 2, 128)
+
+    def run():
+        o, lse = rb.rb_attn_prompt(p, k, v, first, want_lse=True)
+        return (rb.rb_attn_paged(cache, q, first, now, table), o, *rb.rb_attn_prompt_grad(go, p, k, v, o, lse, first))
+
+    run()
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        got = run()
+    for i in range(3):
+        now.copy_(torch.tensor([1500 - 400 * i, 300 - 7 * i, 700], dtype=torch.int32))
+        q.copy_(_rand(rng, *q.shape))
+        k.copy_(_rand(rng, *k.shape))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
