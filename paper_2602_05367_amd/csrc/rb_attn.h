@@ -47,6 +47,8 @@ struct F16 {
     }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2h)); }
     static __device__ __forceinline__ float widen(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
+    // a packed pair's sum, in fp32, on top of another
+    static __device__ __forceinline__ float sum(uint32_t w, float on) { return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, w), (v2h){(_Float16)1.f, (_Float16)1.f}, on, false); }
 };
 struct BF16 {
     static constexpr int BIAS = 0, GRAD_BIAS = 0;
@@ -57,6 +59,7 @@ struct BF16 {
     }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2b)); }
     static __device__ __forceinline__ float widen(uint32_t bits) { return __uint_as_float(bits << 16); }
+    static __device__ __forceinline__ float sum(uint32_t w, float on) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2b, w), (v2b){(__bf16)1.f, (__bf16)1.f}, on, false); }
 };
 
 // an infinity or a NaN among the two 16-bit values of a word

@@ -8,7 +8,8 @@
 // o comes rounded, so do_i . o_i is off by some 2^-12 |do_i| |o_i|: as much as the rounding of ds does to dq and dk again.  The first kernel mends that: over a row,
 // sum_j p_ij (dp_ij - delta_i) is what delta_i lacks (the weights add up to one), so it sums that beside dq, and sum_j p_ij k_j, which
 // the missing part would have been multiplied with, and stores the full delta for the second kernel.  One product more than the
-// five of the definition and the two that are computed twice.
+// five of the definition and the two that are computed twice.  In dq the missing part is taken from ds as rounded for the product, so where one key has nearly all the
+// weight both cancel to the last bits; the second kernel subtracts delta from the same dp, product by product, as the first, and where one key has all of it ds is exactly zero.
 //
 // ds is rounded to the inputs' type before it meets k and q.  In fp16 that takes a scale: ds is p times
 // something of the size of do, and both are small.  Twice dim times the largest finite |do| and |v| bounds
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     using L = Tile<D>;
     constexpr int W = 8, LOADS = Part<D, ROWS, W>::LOADS, E = D / 32;
     __shared__ __attribute__((aligned(16))) uint8_t queries_a[L::bytes(ROWS)], outs_a[L::bytes(ROWS)], queries_b[L::bytes(ROWS)], outs_b[L::bytes(ROWS)], keys[L::bytes(BN)], values[L::bytes(BN)];
-    // what the rows' sums of products start from: -lse in units of the scores, -delta
+    // of the rows: -lse in units of the scores, which their sums of products start from, and delta
     __shared__ __attribute__((aligned(16))) float rows_a[2][ROWS], rows_b[2][ROWS];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
         if (wave == 0) {
             // a row past the end: no weight (do is zero there as well)
             rows_of[0][lane] = t * ROWS + lane < S.n_q ? T::GRAD_BIAS / A.c - next_lse / A.scale : RB_NEG_INF;
-            rows_of[1][lane] = -next_delta;
+            rows_of[1][lane] = next_delta;
         }
         loads_arrived();
         __syncthreads();
@@ -218,13 +219,10 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
         const int row0 = t * ROWS + half * 32;
         if (++t == tile0 + tiles) t = tile0;
         const bool any = !A.causal || wave_first <= ahead + row0 + 31;
-        v16f x, y;
+        v16f x, y = {};
         if (any) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = rows_of[0][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
-                y[i] = rows_of[1][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
-            }
+            for (int i = 0; i < 16; ++i) x[i] = rows_of[0][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
             // both operands come from LDS
             constexpr int AHEAD = 3;
             auto right = [&](int i) RB_INLINE { return rows.read(i % 2 ? values : keys, part, i / 2); };
@@ -249,6 +247,9 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
         if (!any) return;
         const bool masked = A.causal && wave_last > ahead + row0;
         const int least = my_key - ahead - row0 - 4 * h;      // the first row that sees this key
+        float delta[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) delta[i] = rows_of[1][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
         uint32_t w[8], z[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
             for (int j = 0; j < 2; ++j) {
                 const int r = i + j;
                 p[j] = __builtin_amdgcn_exp2f(x[r] * A.c);
-                d[j] = p[j] * y[r] * unit;
+                d[j] = p[j] * (y[r] - delta[r]) * unit;      // (y as queries_kernel has it, bit for bit)
                 if (masked && 8 * (r / 4) + r % 4 < least) p[j] = d[j] = 0.f;
             }
             w[i / 2] = T::pack(p[0], p[1]);
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
     constexpr int W = 8, KEYS = 64, LOADS = Part<D, KEYS, W>::LOADS, E = D / 32;
     __shared__ __attribute__((aligned(16))) uint8_t keys_a[L::bytes(KEYS)], values_a[L::bytes(KEYS)], keys_b[L::bytes(KEYS)], values_b[L::bytes(KEYS)];
     __shared__ __attribute__((aligned(16))) uint8_t queries[L::bytes(BN)], outs[L::bytes(BN)];
-    __shared__ float lacking_of[2][BN];
+    __shared__ float lacking_of[2][BN], rounded_of[2][BN];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave & 3, half = wave >> 2;
@@ -411,7 +412,8 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
     const float less = -delta * unit;
 
     v16f sums[E] = {}, means[E] = {};      // sum_j ds_ij k_j, sum_j p_ij k_j
-    float lacking = 0.f;                   // sum_j ds_ij
+    float lacking = 0.f, rounded = 0.f;    // sum_j ds_ij, and of them as the products have them
+    float first_dp = 0.f;                  // dp of the first key (h = 0)
     auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) RB_INLINE {
         loads_arrived();
         meet();
@@ -446,6 +448,7 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
             meet();
         }
         if (!any) return;
+        if (t == 0) first_dp = y[0];
         const bool masked = key0 + 31 > wave_least;
         const int seen = limit - key0 - 4 * h;
         uint32_t w[8], z[8];
@@ -462,6 +465,7 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
             lacking += d[0] + d[1];
             w[i / 2] = T::pack(p[0], p[1]);
             z[i / 2] = T::pack(d[0], d[1]);
+            rounded = T::sum(z[i / 2], rounded);
         }
         const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
         stream_operands<2 * E, 4>([&](int i) RB_INLINE { return columns.read(keys, i % E, 2 * half + i / E); },
@@ -475,16 +479,21 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
         if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
     lacking = over_halves_sum(lacking) / (1 << T::GRAD_BIAS);      // in units of 2^GRAD_BIAS unit
-    if (h == 0) lacking_of[half][part * 32 + (lane & 31)] = lacking;
+    rounded = over_halves_sum(rounded) / (1 << T::GRAD_BIAS);
+    const int in_block = part * 32 + (lane & 31);
+    if (h == 0) lacking_of[half][in_block] = lacking, rounded_of[half][in_block] = rounded;
     __syncthreads();
-    lacking = lacking_of[0][part * 32 + (lane & 31)] + lacking_of[1][part * 32 + (lane & 31)];
+    lacking = lacking_of[0][in_block] + lacking_of[1][in_block];
+    rounded = rounded_of[0][in_block] + rounded_of[1][in_block];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sums[e] -= means[e] * lacking;
+    for (int e = 0; e < E; ++e) sums[e] -= means[e] * rounded;
     uint8_t *const mine = part == 0 ? keys_a : part == 1 ? keys_b : part == 2 ? values_a : values_b;
     static_assert(E * 4096 <= L::bytes(KEYS), "sums of 32 rows");
     if (!add_halves<E>(sums, mine, half, lane)) return;
-    if (h == 0 && my_row < n_rows) global_at<float>(A.delta)[stat] = delta + lacking / unit;
-    store_columns<T, D>(sums, A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, limit < 0);
+    // A row that sees one key: its weight is one, dp = delta and ds = 0 by definition, whatever the rounding of scores, sums and lse left (times zero: NaN stays)
+    const bool one = limit == 0;
+    if (h == 0 && my_row < n_rows) global_at<float>(A.delta)[stat] = one ? first_dp : delta + lacking / unit;
+    store_columns<T, D>(sums, one ? 0.f : A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, limit < 0);
 }
 
 template <class T, int D> int launch(GradArgs A, int compute_units, hipStream_t stream)
