@@ -11,9 +11,9 @@
 // five of the definition and the two that are computed twice.  In dq the missing part is taken from ds as rounded for the product, so where one key has nearly all the
 // weight both cancel to the last bits; the second kernel subtracts delta from the same dp, product by product, as the first, and where one key has all of it ds is exactly zero.
 //
-// ds is rounded to the inputs' type before it meets k and q.  In fp16 that takes a scale: ds is p times
-// something of the size of do, and both are small.  Twice dim times the largest finite |do| and |v| bounds
-// |dp - delta|; the power of two that brings this bound to one is taken out before and put back into the sums.
+// ds is rounded to the inputs' type before it meets k and q.  In fp16 that takes a scale: ds is p times something of the size of do, and both are small.  As the forward pass follows a row's
+// maximum, each row's dq, and each key's dk, has a power of two of its own that follows the largest |ds| met so far (Unit): what a row or a key does not see takes no part in it, and
+// what comes before a larger one keeps its bits, since the sums are fp32.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 
@@ -31,7 +31,7 @@ constexpr int ROWS = 64;
 struct GradArgs {
     Side q, k, v, o;                    // o: strides of the contiguous o, do and dq
     Address go, lse, first_q, first_k;
-    Address delta, most_o, most_v;      // workspace: [tokens_q][heads], [blocks of 64 tokens][heads], [blocks][kv_heads]
+    Address delta;                      // workspace: [tokens_q][heads] fp32
     Address parts;                      // workspace: [splits][dk, dv][tokens_k][kv_heads][dim] fp32, where there are several splits
     Address dq, dk, dv;
     int splits;                         // workgroups that share the query heads of the same keys
@@ -39,63 +39,52 @@ struct GradArgs {
     float c, scale;
 };
 
-// ------------------------------------------------------- delta and maxima ---
-// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o, or of v.  Bound: bytes (6000 tokens of 32 heads of 128, bf16: 19.5 us,
-// 5.1 TB/s).
+// ------------------------------------------------------------------ delta ---
+// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o.  Bound: bytes.
 template <class T> __global__ __launch_bounds__(256) void delta_kernel(const GradArgs A)
 {
-    __shared__ uint32_t most[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (lane & 15) * 8;
-    const int columns = A.heads + A.kv_heads, head = blockIdx.x % columns, block = blockIdx.x / columns;
-    const bool is_v = head >= A.heads;
-    const int tokens = is_v ? A.tokens_k : A.tokens_q;
-    uint32_t top = 0;
+    const int head = blockIdx.x % A.heads, block = blockIdx.x / A.heads;
     for (int i = 0; i < 4; ++i) {
         const int token = block * 64 + (wave * 4 + i) * 4 + lane / 16;
-        if (token >= tokens) continue;      // whole groups of 16 lanes
+        if (token >= A.tokens_q) continue;      // whole groups of 16 lanes
         v4u x = (v4u)(0u), y = (v4u)(0u);
         if (e < A.dim) {
-            const long long at = is_v ? token * A.v.token + (head - A.heads) * A.v.head : token * A.o.token + head * A.o.head;
-            x = *(const v4u *)(global_at<const uint8_t>(is_v ? A.v.at : A.go) + at + e * 2);
-            if (!is_v) y = *(const v4u *)(global_at<const uint8_t>(A.o.at) + at + e * 2);
+            const long long at = token * A.o.token + head * A.o.head;
+            x = *(const v4u *)(global_at<const uint8_t>(A.go) + at + e * 2);
+            y = *(const v4u *)(global_at<const uint8_t>(A.o.at) + at + e * 2);
         }
         float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = x[j] & 0x7fffu, hi = x[j] >> 16 & 0x7fffu;
-            top = max(top, lo < T::EXPONENT ? lo : 0u);
-            top = max(top, hi < T::EXPONENT ? hi : 0u);
-            sum += T::widen(x[j] & 0xffffu) * T::widen(y[j] & 0xffffu) + T::widen(x[j] >> 16) * T::widen(y[j] >> 16);
-        }
-        if (!is_v) {
-            for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-            if ((lane & 15) == 0) global_at<float>(A.delta)[(long long)token * A.heads + head] = sum;
-        }
-    }
-    for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    if (lane == 0) most[wave] = top;
-    __syncthreads();
-    if (threadIdx.x == 0 && block * 64 < tokens) {
-        top = max(max(most[0], most[1]), max(most[2], most[3]));
-        global_at<float>(is_v ? A.most_v : A.most_o)[(long long)block * (is_v ? A.kv_heads : A.heads) + (is_v ? head - A.heads : head)] = T::widen(top);
+        for (int j = 0; j < 4; ++j) sum += T::widen(x[j] & 0xffffu) * T::widen(y[j] & 0xffffu) + T::widen(x[j] >> 16) * T::widen(y[j] >> 16);
+        for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        if ((lane & 15) == 0) global_at<float>(A.delta)[(long long)token * A.heads + head] = sum;
     }
 }
 
-// the largest over the blocks that hold tokens t0 .. t0 + n - 1, of `heads` heads from `head` on
-__device__ __forceinline__ float most_of(const float *most, int columns, int head, int heads, int t0, int n, int lane)
-{
-    float v = 0.f;
-    if (n > 0)
-        for (int b = t0 / 64 * heads + lane; b < ((t0 + n - 1) / 64 + 1) * heads; b += 64) v = fmaxf(v, most[(long long)(b / heads) * columns + head + b % heads]);
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
-}
-// the power of two that takes 2 dim a b to between a half and one (1 where that is zero; fp16 values, so neither end of fp32 is near)
-__device__ __forceinline__ float scale_for(float a, float b, int dim)
-{
-    const uint32_t exponent = __float_as_uint(2.f * dim * a * b) >> 23;
-    return exponent ? __uint_as_float((253u - exponent) << 23) : 1.f;
-}
+// The power of two that the ds of a lane's column (a row's, a key's) are held in; 1 where the type has fp32's range.  It starts at 2^60, where fp16 resolves ds of 2^-98, and
+// falls to bring the largest to 2^10 whenever one passes 2^15: 24 binades below stay at full precision, and it seldom moves.  It does not fall below 2^-60, which holds every finite ds.
+template <class T> struct Unit {
+    float unit = T::GRAD_BIAS ? 0x1p60f : 1.f;
+    static __device__ __forceinline__ float power(uint32_t field) { return __uint_as_float(field << 23); }
+    __device__ __forceinline__ float inverse() const { return power(254u - (__float_as_uint(unit) >> 23)); }
+    // d: 16 of the column, with `unit` in them already; both halves of the wavefront call it.  What is held in the unit is to be multiplied by `moved`, the d are already
+    __device__ __forceinline__ bool follow(v16f &d, float &moved)
+    {
+        if constexpr (!T::GRAD_BIAS) return false;
+        float most = fabsf(d[0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, fabsf(d[i]));
+        most = over_halves_max(most);
+        if (!__ballot(most > 0x1p15f)) return false;
+        const int field = __float_as_uint(unit) >> 23, now = most > 0x1p15f ? max(field + 137 - (int)(__float_as_uint(most) >> 23), 67) : field;
+        moved = power(127 + now - field);
+        unit = power(now);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) d[i] *= moved;
+        return true;
+    }
+};
 
 // An infinity or a NaN in the tile?  (see make_finite: here the tile itself is needed as it is, and what is read transposed is cleaned)
 template <class T, int D, int R, int W> __device__ __forceinline__ void look_through(const uint8_t *tile, int *found, int tid)
@@ -163,11 +152,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     const int my_key = key0 + part * 32 + (lane & 31), key = min(my_key, S.n_k - 1);
     const int block_last = min(key0 + BN, S.n_k) - 1, wave_first = key0 + part * 32, wave_last = min(wave_first + 31, S.n_k - 1);
 
-    float unit = 1.f;      // taken out of dp - delta
-    if (T::GRAD_BIAS)
-        unit = scale_for(most_of(global_at<const float>(A.most_o), A.heads, kvh * A.group, A.group, S.q0, S.n_q, lane),
-                         most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
-
+    Unit<T> held;
     const Part<D, ROWS, W> q_part(A.q.token, A.dim, wave * (ROWS / W), lane), o_part(A.o.token, A.dim, wave * (ROWS / W), lane);
     const int tile0 = A.causal ? max(key0 - ahead, 0) / ROWS : 0, tiles = (S.n_q + ROWS - 1) / ROWS - tile0;
     const int steps = __builtin_amdgcn_readfirstlane(tiles > 0 ? tiles * heads_of : 0);
@@ -253,17 +238,22 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
         uint32_t w[8], z[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            float p[2], d[2];
+            float p[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int r = i + j;
                 p[j] = __builtin_amdgcn_exp2f(x[r] * A.c);
-                d[j] = p[j] * (y[r] - delta[r]) * unit;      // (y as queries_kernel has it, bit for bit)
-                if (masked && 8 * (r / 4) + r % 4 < least) p[j] = d[j] = 0.f;
+                y[r] = p[j] * (y[r] - delta[r]) * held.unit;      // ds, from the dp that queries_kernel has, bit for bit
+                if (masked && 8 * (r / 4) + r % 4 < least) p[j] = y[r] = 0.f;
             }
             w[i / 2] = T::pack(p[0], p[1]);
-            z[i / 2] = T::pack(d[0], d[1]);
         }
+        float moved;
+        if (held.follow(y, moved))
+#pragma unroll
+            for (int e = 0; e < E; ++e) sums_k[e] *= moved;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) z[i / 2] = T::pack(y[i], y[i + 1]);
         const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
         stream_operands<4 * E, 4>([&](int i) RB_INLINE { return columns.read(i % 2 ? queries : outs, i / 2 % E, 2 * half + i / (2 * E)); },
                                   [&](int i, v4u a) RB_INLINE {
@@ -287,12 +277,15 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
 
     uint8_t *const mine = part == 0 ? queries_a : part == 1 ? outs_a : part == 2 ? queries_b : outs_b;
     static_assert(E * 4096 <= L::bytes(ROWS), "sums of 32 keys");
+    if constexpr (T::GRAD_BIAS)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums_k[e] *= held.inverse();      // (each half has a unit of its own)
     add_halves<E>(sums_v, mine, half, lane);
     add_halves<E>(sums_k, mine, half, lane);
     if (half == 1) return;
     const bool real = my_key < S.n_k;
     const long long at = (long long)(S.k0 + key) * A.kv_heads + kvh;
-    const float scale_v = 1.f / (1 << T::GRAD_BIAS), scale_k = A.scale / (1 << T::GRAD_BIAS) / unit;
+    const float scale_v = 1.f / (1 << T::GRAD_BIAS), scale_k = A.scale / (1 << T::GRAD_BIAS);
     if (A.splits > 1) {
         float *const k_part_at = part_at(A, split, 0, at), *const v_part_at = part_at(A, split, 1, at);
 #pragma unroll
@@ -388,31 +381,22 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
     const long long row_at = (long long)(S.q0 + token) * A.o.token + head * A.o.head;
-    float unit = 1.f;      // here of the row alone
     {
         const uint8_t *from_q = global_at<const uint8_t>(A.q.at) + (S.q0 + token) * A.q.token + head * A.q.head, *from_o = global_at<const uint8_t>(A.go) + row_at;
-        uint32_t top = 0;
+        if (half == 0)
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            const v4u o = k * 16 + h * 8 < A.dim ? *(const v4u *)(from_o + k * 32 + h * 16) : (v4u)(0u);
-            if (half == 0) {
+            for (int k = 0; k < D / 16; ++k) {
                 rows.write(queries, part, k, k * 16 + h * 8 < A.dim ? *(const v4u *)(from_q + k * 32 + h * 16) : (v4u)(0u));
-                rows.write(outs, part, k, o);
+                rows.write(outs, part, k, k * 16 + h * 8 < A.dim ? *(const v4u *)(from_o + k * 32 + h * 16) : (v4u)(0u));
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t lo = o[j] & 0x7fffu, hi = o[j] >> 16 & 0x7fffu;
-                top = max(top, max(lo < T::EXPONENT ? lo : 0u, hi < T::EXPONENT ? hi : 0u));
-            }
-        }
-        if (T::GRAD_BIAS) unit = scale_for(over_halves_max(T::widen(top)), most_of(global_at<const float>(A.most_v), A.kv_heads, kvh, 1, S.k0, S.n_k, lane), A.dim);
     }
     const long long stat = (long long)(S.q0 + token) * A.heads + head;
     const float delta = global_at<const float>(A.delta)[stat], zero_at = global_at<const float>(A.lse)[stat] * LOG2E - T::GRAD_BIAS;
-    const float less = -delta * unit;
+    Unit<T> held;
+    float less = -delta * held.unit;
 
     v16f sums[E] = {}, means[E] = {};      // sum_j ds_ij k_j, sum_j p_ij k_j
-    float lacking = 0.f, rounded = 0.f;    // sum_j ds_ij, and of them as the products have them
+    float lacking = 0.f, rounded = 0.f;    // sum_j ds_ij, and of them as the products have them, in the unit
     float first_dp = 0.f;                  // dp of the first key (h = 0)
     auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) RB_INLINE {
         loads_arrived();
@@ -454,17 +438,26 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
         uint32_t w[8], z[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            float p[2], d[2];
+            float p[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int r = i + j;
                 p[j] = __builtin_amdgcn_exp2f(fmaf(x[r], A.c, -zero_at));
-                d[j] = p[j] * fmaf(y[r], unit, less);
-                if (masked && 8 * (r / 4) + r % 4 > seen) p[j] = d[j] = 0.f;
+                y[r] = p[j] * fmaf(y[r], held.unit, less);      // ds
+                if (masked && 8 * (r / 4) + r % 4 > seen) p[j] = y[r] = 0.f;
             }
-            lacking += d[0] + d[1];
             w[i / 2] = T::pack(p[0], p[1]);
-            z[i / 2] = T::pack(d[0], d[1]);
+        }
+        float moved;
+        if (held.follow(y, moved)) {
+            less *= moved, lacking *= moved, rounded *= moved;
+#pragma unroll
+            for (int e = 0; e < E; ++e) sums[e] *= moved;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            lacking += y[i] + y[i + 1];
+            z[i / 2] = T::pack(y[i], y[i + 1]);
             rounded = T::sum(z[i / 2], rounded);
         }
         const v4u pw[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}}, dz[2] = {{z[0], z[1], z[2], z[3]}, {z[4], z[5], z[6], z[7]}};
@@ -478,27 +471,28 @@ __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
         step(t, keys_a, values_a, keys_b, values_b);
         if (t + 1 < n_tiles) step(t + 1, keys_b, values_b, keys_a, values_a);
     }
-    lacking = over_halves_sum(lacking) / (1 << T::GRAD_BIAS);      // in units of 2^GRAD_BIAS unit
-    rounded = over_halves_sum(rounded) / (1 << T::GRAD_BIAS);
+    const float outside = held.inverse();      // (each half has a unit of its own)
+    lacking = over_halves_sum(lacking) / (1 << T::GRAD_BIAS) * outside;
+    rounded = over_halves_sum(rounded) / (1 << T::GRAD_BIAS) * outside;
     const int in_block = part * 32 + (lane & 31);
     if (h == 0) lacking_of[half][in_block] = lacking, rounded_of[half][in_block] = rounded;
     __syncthreads();
     lacking = lacking_of[0][in_block] + lacking_of[1][in_block];
     rounded = rounded_of[0][in_block] + rounded_of[1][in_block];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sums[e] -= means[e] * rounded;
+    for (int e = 0; e < E; ++e) sums[e] = sums[e] * outside - means[e] * rounded;
     uint8_t *const mine = part == 0 ? keys_a : part == 1 ? keys_b : part == 2 ? values_a : values_b;
     static_assert(E * 4096 <= L::bytes(KEYS), "sums of 32 rows");
     if (!add_halves<E>(sums, mine, half, lane)) return;
     // A row that sees one key: its weight is one, dp = delta and ds = 0 by definition, whatever the rounding of scores, sums and lse left (times zero: NaN stays)
     const bool one = limit == 0;
-    if (h == 0 && my_row < n_rows) global_at<float>(A.delta)[stat] = one ? first_dp : delta + lacking / unit;
-    store_columns<T, D>(sums, one ? 0.f : A.scale / (1 << T::GRAD_BIAS) / unit, global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, limit < 0);
+    if (h == 0 && my_row < n_rows) global_at<float>(A.delta)[stat] = one ? first_dp : delta + lacking;
+    store_columns<T, D>(sums, one ? 0.f : A.scale / (1 << T::GRAD_BIAS), global_at<uint8_t>(A.dq) + row_at, A.dim, h, my_row < n_rows, limit < 0);
 }
 
 template <class T, int D> int launch(GradArgs A, int compute_units, hipStream_t stream)
 {
-    const long long deltas = (long long)((max(A.tokens_q, A.tokens_k) + 63) / 64) * (A.heads + A.kv_heads);
+    const long long deltas = (long long)((A.tokens_q + 63) / 64) * A.heads;
     const long long keys = block_numbers(A.tokens_k, A.n_seqs, 1, BN) * A.kv_heads, queries = block_numbers(A.tokens_q, A.n_seqs, A.group, BN) * A.kv_heads;
     if (deltas > 0x7fffffffll || keys > 0x7fffffffll || queries > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     A.splits = splits_for(block_numbers(A.tokens_k, A.n_seqs, 1, BN), A.kv_heads, A.group, compute_units);
@@ -517,7 +511,6 @@ size_t parts_bytes(const rb_heads *H, int tokens_k)      // (more sequences are 
     const int splits = splits_for((tokens_k + BN - 1) / BN, H->kv_heads, H->heads / H->kv_heads, rb::mx::device_groups());
     return splits < 2 ? 0 : (size_t)splits * 2 * tokens_k * H->kv_heads * H->dim * 4;
 }
-size_t most_bytes(int tokens, int heads) { return rounded((size_t)((tokens + 63) / 64) * heads * 4); }
 
 }  // namespace
 }  // namespace attn
@@ -528,7 +521,7 @@ using namespace rb::attn;
 extern "C" size_t rb_attn_grad_workspace_bytes(const rb_heads *H, int tokens_q, int tokens_k)
 {
     if (check_heads(H) != RB_OK || tokens_q < 1 || tokens_k < 1) return 0;
-    return delta_bytes(H, tokens_q) + most_bytes(tokens_q, H->heads) + most_bytes(tokens_k, H->kv_heads) + parts_bytes(H, tokens_k);
+    return delta_bytes(H, tokens_q) + parts_bytes(H, tokens_k);
 }
 
 extern "C" int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, const int32_t *first_q,
@@ -550,9 +543,7 @@ extern "C" int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void
     A.o = side(o, (long long)H->heads * H->dim, H->dim);
     A.go = rb::address_of(go), A.lse = rb::address_of(lse), A.first_q = rb::address_of(first_q), A.first_k = rb::address_of(first_k ? first_k : first_q);
     A.delta = rb::address_of(workspace);
-    A.most_o = A.delta + delta_bytes(H, tokens_q);
-    A.most_v = A.most_o + most_bytes(tokens_q, H->heads);
-    A.parts = A.most_v + most_bytes(tokens_k, H->kv_heads);
+    A.parts = A.delta + delta_bytes(H, tokens_q);
     A.dq = rb::address_of(dq), A.dk = rb::address_of(dk), A.dv = rb::address_of(dv);
     A.n_seqs = n_seqs, A.tokens_q = tokens_q, A.tokens_k = tokens_k;
     A.heads = H->heads, A.kv_heads = H->kv_heads, A.group = H->heads / H->kv_heads, A.dim = H->dim, A.causal = causal != 0;
