@@ -409,7 +409,9 @@ int rb_add(const uint16_t *a, const uint16_t *b, uint16_t *y, size_t n, void *st
  *
  * Sequences are packed one after the other: sequence s has the tokens first[s]
  * .. first[s + 1] - 1 (device int32 [n_seqs + 1], first[0] = 0, not decreasing;
- * lengths of zero are allowed; at most 2^24 tokens and 2^20 sequences).  The arrays are read on the
+ * lengths of zero are allowed; at most 2^24 tokens and 2^20 sequences).  Tokens from
+ * first[n_seqs] on (padding, where a call's number of tokens is fixed) belong to no sequence: they are not
+ * read into any, and their rows of every result and gradient are left as they are.  The arrays are read on the
  * device; entries out of order or out of range give unspecified results, but
  * nothing outside the buffers is touched.
  *
@@ -470,7 +472,8 @@ typedef struct rb_cache {
  * where `interleaved`.  rotary is a multiple of 8, at most dim.  cos and sin NULL: nothing is turned.  The
  * turned q goes to q_out, contiguous [tokens][heads][dim] (may be q itself if that is
  * contiguous); q and q_out NULL: no queries.  H: strides of q, k, v, and their heads, which have to be the cache's.
- * Positions outside the page table are not stored.
+ * Positions outside the page table, and those whose table entry is not the number of a page, are not stored.  A position
+ * that has no row of cos and sin is turned by the last row: table_rows has to cover the lengths.
  */
 int rb_cache_append(const rb_cache *C, const rb_heads *H, const void *q, const void *k, const void *v,
                     const float *cos, const float *sin, int table_rows, int rotary, int interleaved,

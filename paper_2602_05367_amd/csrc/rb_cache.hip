@@ -53,14 +53,15 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs A)
     }
     const long long position = (long long)length - end + token;
     const bool inside = position >= 0 && position < (long long)A.width << A.page_shift;
-    if (!there) return;
+    if (!there || token >= end) return;      // behind the last sequence's end (padding): nobody's
     uint8_t *to;
     if (is_q) {
         to = global_at<uint8_t>(A.q_to) + ((long long)token * A.heads + head) * (A.dim * 2);
     } else {
         if (!inside) return;
-        const int p = (int)position, page = min(max(global_at<const int>(A.table)[(long long)s * A.width + (p >> A.page_shift)], 0), A.pages - 1);
-        to = global_at<uint8_t>(is_v ? A.v_to : A.k_to) + page * A.page + (p & ((1 << A.page_shift) - 1)) * A.token_stride + kvh * A.head_stride;
+        const int p = (int)position, page = global_at<const int>(A.table)[(long long)s * A.width + (p >> A.page_shift)];
+        if (page < 0 || page >= A.pages) return;      // (another's page is not written over)
+        to = global_at<uint8_t>(is_v ? A.v_to : A.k_to) + (long long)page * A.page + (p & ((1 << A.page_shift) - 1)) * A.token_stride + kvh * A.head_stride;
     }
     if (!turned) {
         *(v4u *)(to + at_x) = (v4u){a.w.x, a.w.y, b.w.x, b.w.y};
