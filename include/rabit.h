@@ -441,7 +441,8 @@ int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, const void *
  * [tokens_k][kv_heads][dim], contiguous, of the inputs' dtype; dk and dv are summed over the query heads that share a key head.
  * Sums are fp32; weights and score gradients are rounded to dtype before they meet the other operand
  * (fp16: scaled by a power of two first, so small gradients keep their bits).  No atomics: the same
- * inputs give the same bits.  workspace: rb_attn_grad_workspace_bytes bytes, 16-byte aligned.
+ * inputs give the same bits.  workspace: rb_attn_grad_workspace_bytes bytes, 16-byte aligned; so many serve every
+ * call of at most as many queries and keys.
  */
 size_t rb_attn_grad_workspace_bytes(const rb_heads *H, int tokens_q, int tokens_k);
 int rb_attn_prompt_grad(const rb_heads *H, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse,
@@ -485,7 +486,7 @@ int rb_cache_append(const rb_cache *C, const rb_heads *H, const void *q, const v
  * first[s + 1] - 1 of q, which are the last of its lengths[s] positions (their
  * keys and values are in the cache already).  A token sees the positions up to its
  * own.  Any mix of single tokens and chunks.  workspace: rb_attn_paged_workspace_bytes
- * bytes of device memory, 16-byte aligned.
+ * bytes of device memory, 16-byte aligned; so many serve every call of at most as many sequences and tokens.
  */
 size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens);
 int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads,

@@ -316,10 +316,10 @@ int groups_wanted(int tokens, int n_seqs, int kv_heads, int group, long long mos
     if (blocks * kv_heads >= MANY * compute_units || blocks * (most_positions / KEYS + 2) >= 0x7fffffffll) return 0;
     return (int)std::max(GROUPS * compute_units / kv_heads, 1ll);
 }
-// Blocks of more than one part have at most twice the workgroups wanted: a block that x > 1 would do for has less than x + 1
-size_t parts_workspace_bytes(int tokens, int n_seqs, int kv_heads, int group, int dim, int compute_units)
+// Blocks of more than one part have at most twice the workgroups wanted: a block that x > 1 would do for has less than x + 1.  (As much for any number of tokens, if for one.)
+size_t parts_workspace_bytes(int kv_heads, int group, int dim, int compute_units)
 {
-    const size_t slots = (size_t)groups_wanted(tokens, n_seqs, kv_heads, group, 0, compute_units) * 2;
+    const size_t slots = (size_t)groups_wanted(1, 1, kv_heads, group, 0, compute_units) * 2;
     return slots * kv_heads * (dim <= 64 ? PartOfRows<64, BM>::FLOATS : PartOfRows<128, BM>::FLOATS) * 4;
 }
 
@@ -394,9 +394,9 @@ extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, in
 {
     if (check_cache(C) != RB_OK || heads < 1 || heads % C->kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
     const int units = rb::mx::device_groups(), group = heads / C->kv_heads;
-    // whichever kernel the table's width will choose
-    const size_t few = few_applies(tokens, n_seqs, group, 0) ? few_workspace_bytes(C->kv_heads, C->dim, units) : 0;
-    return std::max(few, parts_workspace_bytes(tokens, n_seqs, C->kv_heads, group, C->dim, units));
+    // whichever kernel a call of up to so many tokens and sequences and its table's width will choose
+    const size_t few = few_applies(1, n_seqs, group, 0) ? few_workspace_bytes(C->kv_heads, C->dim, units) : 0;
+    return std::max(few, parts_workspace_bytes(C->kv_heads, group, C->dim, units));
 }
 
 extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,

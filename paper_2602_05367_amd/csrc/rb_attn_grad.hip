@@ -506,10 +506,13 @@ template <class T, int D> int launch(GradArgs A, int compute_units, hipStream_t 
 
 size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
 size_t delta_bytes(const rb_heads *H, int tokens_q) { return rounded((size_t)tokens_q * H->heads * 4); }
-size_t parts_bytes(const rb_heads *H, int tokens_k)      // (more sequences are not fewer blocks)
+// What up to so many keys can need: for each number of splits, the most keys that have it.  (More sequences are not fewer blocks.)
+size_t parts_bytes(const rb_heads *H, int tokens_k)
 {
-    const int splits = splits_for((tokens_k + BN - 1) / BN, H->kv_heads, H->heads / H->kv_heads, rb::mx::device_groups());
-    return splits < 2 ? 0 : (size_t)splits * 2 * tokens_k * H->kv_heads * H->dim * 4;
+    const int units = rb::mx::device_groups(), group = H->heads / H->kv_heads;
+    long long most = 0;
+    for (long long splits = 2; splits <= std::min(group, units / H->kv_heads); ++splits) most = std::max(most, splits * std::min((long long)tokens_k, units / (splits * H->kv_heads) * BN));
+    return (size_t)most * 2 * H->kv_heads * H->dim * 4;
 }
 
 }  // namespace
