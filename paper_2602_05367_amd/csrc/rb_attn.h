@@ -14,6 +14,7 @@
 #include <cstdint>
 
 #include "rabit.h"
+#include "rb_attn_shares.h"
 #include "rb_device.h"
 
 namespace rb {
@@ -392,11 +393,6 @@ struct Args {
 // are rescaled a few times per row instead of at every tile.  2^(8 + BIAS) is within fp16.
 constexpr float SLACK = 8.f;
 
-// positions of a sequence in a cache: what its length says, as far as the page table reaches
-__device__ __forceinline__ int positions(int length, int width, int page_shift)
-{
-    return min(max(length, 0), (int)min((long long)width << page_shift, 0x7fffffc0ll));
-}
 // Work over a cache: that of a key head is a row of pieces (tiles, workgroups), sequence after sequence and job (a block of JOB rows) after job.  Shape says what a sequence has
 // of it: of(A, q0, q1, length), and count() pieces.
 //

@@ -14,51 +14,20 @@
 #include "rabit.h"
 #include "rb_attn.h"
 #include "rb_attn_host.h"
+#include "rb_attn_shares.h"
 
 namespace rb {
 namespace attn {
 namespace {
 
-constexpr int KEYS = 32, ROWS = 32, WAVES = 4;
-
-// Where the work of a sequence lies among all tiles of a key head.  (All of them, as many as rows and positions allow, are counted in 31 bits: see few_applies.)
-struct Shape {
-    static constexpr int JOB = ROWS;
-    int rows, blocks, tiles;
-    __device__ __forceinline__ int count() const { return blocks * tiles; }
-    static __device__ __forceinline__ Shape of(const Args &A, int q0, int q1, int length)
-    {
-        q0 = min(max(q0, 0), A.tokens_q);
-        q1 = min(max(q1, q0), A.tokens_q);
-        const int rows = (q1 - q0) * A.group;
-        // a sequence that has rows but no positions: one tile, of which they see nothing
-        return {rows, (rows + ROWS - 1) / ROWS, rows ? max((positions(length, A.width, A.page_shift) + KEYS - 1) / KEYS, 1) : 0};
-    }
-};
-// All tiles in equal shares, the first ones longer by one; never more shares than tiles: none is empty
-struct Shares {
-    int n, each, longer;
-    __device__ __forceinline__ Shares(int all, int wavefronts) : n(min(wavefronts, max(all, 1))), each((int)((unsigned)all / (unsigned)n)), longer(all - each * n) {}
-    __device__ __forceinline__ int start(int w) const { return w * each + min(w, longer); }
-    __device__ __forceinline__ int of(int tile) const
-    {
-        const unsigned in_longer = (unsigned)(each + 1) * longer;
-        return (unsigned)tile < in_longer ? (int)((unsigned)tile / (unsigned)(each + 1)) : longer + (int)(((unsigned)tile - in_longer) / (unsigned)each);
-    }
-};
+using few::Cursor, few::KEYS, few::ROWS, few::Shape, few::Shares;
+constexpr int WAVES = 4;
 
 // the part that share w has of a job of which it does not have all: its first job (0) or its last (1)
 template <int D> __device__ __forceinline__ PartOfRows<D, ROWS> part_of(Address workspace, int kvh, int wavefronts, int w, int which)
 {
     return PartOfRows<D, ROWS>(workspace, ((size_t)kvh * wavefronts + w) * 2 + which);
 }
-
-// a position in the row of tiles
-struct Cursor {
-    int s, block, t;
-    Shape shape;
-    int q0, n_k;
-};
 
 template <class T, int D>
 __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
@@ -78,35 +47,11 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     const int n = shares.start(w + 1) - begin;
     if (n <= 0) return;
 
-    auto visit = [&](Cursor &c) RB_INLINE {      // sequence c.s, or nothing behind the last
-        if (c.s >= A.n_seqs) {
-            c.shape = {0, 1, 0x7fffffff};
-            c.n_k = 0;
-            return;
-        }
-        int q0, q1, length;
-        sums_of.entries(c.s, q0, q1, length);
-        c.q0 = min(max(q0, 0), A.tokens_q);
-        c.shape = Shape::of(A, q0, q1, length);
-        c.n_k = positions(length, A.width, A.page_shift);
-    };
-    auto advance = [&](Cursor &c) RB_INLINE {
-        if (++c.t < c.shape.tiles) return;
-        c.t = 0;
-        if (++c.block < c.shape.blocks) return;
-        c.block = 0;
-        do {
-            ++c.s;
-            visit(c);
-        } while (c.shape.blocks == 0);
-    };
+    auto entries = [&](int s, int &q0, int &q1, int &length) RB_INLINE { sums_of.entries(s, q0, q1, length); };
     Cursor at = {}, ahead = {};      // the tile at hand, and the next to be asked for
     at.s = __builtin_amdgcn_readfirstlane(sums_of.locate(begin));
-    if (at.s >= A.n_seqs) return;
-    visit(at);
-    if (begin < 0 || at.shape.blocks == 0) return;      // (arrays that are not in order)
-    at.block = min(__builtin_amdgcn_readfirstlane((int)((unsigned)begin / (unsigned)at.shape.tiles)), at.shape.blocks - 1);
-    at.t = min(begin - at.block * at.shape.tiles, at.shape.tiles - 1);
+    if (!at.stand(A, begin, entries)) return;
+    at.block = __builtin_amdgcn_readfirstlane(at.block), at.t = __builtin_amdgcn_readfirstlane(at.t);
     ahead = at;
 
     constexpr int LOADS = Part<D, KEYS, 1>::LOADS;
@@ -137,7 +82,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         }
     };
     auto next_ahead = [&]() RB_INLINE {
-        advance(ahead);
+        ahead.advance(A, entries);
         ask_pages(ahead);
     };
 
@@ -249,7 +194,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         load(i + 2, v_base, values);
         next_ahead();
         if (i == n - 1 || at.t == at.shape.tiles - 1) finish();
-        advance(at);
+        at.advance(A, entries);
     };
 
     uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS), *const kb = keys_b + wave * L::bytes(KEYS), *const vb = values_b + wave * L::bytes(KEYS);
@@ -262,9 +207,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     load(1, v_base, vb);
     next_ahead();
     rows_arrived();
-    for (int i = 0; i < n; i += 2) {
+    for (int i = 0; i < n && at.there(A); i += 2) {      // (past the last sequence only where the arrays are not in order)
         step(i, ka, va);
-        if (i + 1 < n) step(i + 1, kb, vb);
+        if (i + 1 < n && at.there(A)) step(i + 1, kb, vb);
     }
     loads_arrived();
 }
@@ -282,8 +227,9 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
     const int b = block - block_start(q0, s, A.group, ROWS);
     if (b < 0 || b >= shape.blocks || b * ROWS + row0 >= shape.rows) return;
     const Shares shares(sums_of.before(A.n_seqs), wavefronts);
-    const int from = sums_of.before(s) + b * shape.tiles, w0 = shares.of(from), w1 = shares.of(from + shape.tiles - 1);
-    if (w0 == w1) return;      // it has stored the result
+    const int from = sums_of.before(s) + b * shape.tiles;
+    int w0, w1;
+    if (!shares.of_job(from, shape.tiles, w0, w1) || w0 == w1) return;      // (one: it has stored the result)
     const bool starts_inside = shares.start(w0) < from;      // the first part is that share's last, all others are their shares' first
     const int n_q = shape.rows / A.group, n_k = positions(length, A.width, A.page_shift);
     q0 = min(max(q0, 0), A.tokens_q);
