@@ -427,7 +427,7 @@ typedef struct rb_heads {
  * Whole prompts.  Row i of a sequence sees its keys j <= i (causal), or all of
  * them.  first_k / tokens_k: the keys' own packing where it differs from the queries' (NULL:
  * the same, tokens_k = tokens_q); causal rows are then aligned at the end, row i of n sees
- * j <= i + (keys - n).  scores are scale * q.k, scale > 0 (RB_ERR_VALUE).
+ * j <= i + (keys - n).  scores are scale * q.k, 0 < scale <= 2e38 (RB_ERR_VALUE).
  * lse: NULL or fp32 [tokens_q][heads], log sum_j exp(scale * q_i.k_j), which the
  * gradient needs.
  */

@@ -363,7 +363,7 @@ int check_heads(const rb_heads *H)
 
 int check_scale(float scale)
 {
-    return scale > 0.f && scale <= 3e38f ? RB_OK : RB_ERR_VALUE;
+    return scale > 0.f && scale <= 2e38f ? RB_OK : RB_ERR_VALUE;      // (times log2(e) it is a number still)
 }
 
 }  // namespace attn

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     using L = Tile<D>;
     constexpr int W = 8, LOADS = Part<D, ROWS, W>::LOADS, E = D / 32;
     __shared__ __attribute__((aligned(16))) uint8_t queries_a[L::bytes(ROWS)], outs_a[L::bytes(ROWS)], queries_b[L::bytes(ROWS)], outs_b[L::bytes(ROWS)], keys[L::bytes(BN)], values[L::bytes(BN)];
-    // of the rows: -lse in units of the scores, which their sums of products start from, and delta
+    // of the rows: the exponent that their weights are taken relative to, and delta
     __shared__ __attribute__((aligned(16))) float rows_a[2][ROWS], rows_b[2][ROWS];
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     auto step = [&](int n, uint8_t *queries, uint8_t *outs, float (&rows_of)[2][ROWS], uint8_t *next_queries, uint8_t *next_outs) RB_INLINE {
         if (wave == 0) {
             // a row past the end: no weight (do is zero there as well)
-            rows_of[0][lane] = t * ROWS + lane < S.n_q ? T::GRAD_BIAS / A.c - next_lse / A.scale : RB_NEG_INF;
+            rows_of[0][lane] = t * ROWS + lane < S.n_q ? next_lse * LOG2E - T::GRAD_BIAS : -RB_NEG_INF;
             rows_of[1][lane] = next_delta;
         }
         loads_arrived();
@@ -204,10 +204,8 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
         const int row0 = t * ROWS + half * 32;
         if (++t == tile0 + tiles) t = tile0;
         const bool any = !A.causal || wave_first <= ahead + row0 + 31;
-        v16f x, y = {};
+        v16f x = {}, y = {};
         if (any) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = rows_of[0][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
             // both operands come from LDS
             constexpr int AHEAD = 3;
             auto right = [&](int i) RB_INLINE { return rows.read(i % 2 ? values : keys, part, i / 2); };
@@ -232,21 +230,19 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
         if (!any) return;
         const bool masked = A.causal && wave_last > ahead + row0;
         const int least = my_key - ahead - row0 - 4 * h;      // the first row that sees this key
-        float delta[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) delta[i] = rows_of[1][half * 32 + 8 * (i / 4) + 4 * h + i % 4];
+        const int mine = half * 32 + 4 * h;
         uint32_t w[8], z[8];
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            float p[2];
+        for (int i = 0; i < 16; i += 4) {
+            const v4f zero_at = *(const v4f *)&rows_of[0][mine + 2 * i], delta = *(const v4f *)&rows_of[1][mine + 2 * i];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const int r = i + j;
-                p[j] = __builtin_amdgcn_exp2f(x[r] * A.c);
-                y[r] = p[j] * (y[r] - delta[r]) * held.unit;      // ds, from the dp that queries_kernel has, bit for bit
-                if (masked && 8 * (r / 4) + r % 4 < least) p[j] = y[r] = 0.f;
+                x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], A.c, -zero_at[j]));
+                y[r] = x[r] * (y[r] - delta[j]) * held.unit;      // ds, from the dp that queries_kernel has, bit for bit
+                if (masked && 8 * (r / 4) + r % 4 < least) x[r] = y[r] = 0.f;
             }
-            w[i / 2] = T::pack(p[0], p[1]);
+            w[i / 2] = T::pack(x[i], x[i + 1]), w[i / 2 + 1] = T::pack(x[i + 2], x[i + 3]);
         }
         float moved;
         if (held.follow(y, moved))
