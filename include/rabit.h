@@ -427,7 +427,7 @@ typedef struct rb_heads {
  * Whole prompts.  Row i of a sequence sees its keys j <= i (causal), or all of
  * them.  first_k / tokens_k: the keys' own packing where it differs from the queries' (NULL:
  * the same, tokens_k = tokens_q); causal rows are then aligned at the end, row i of n sees
- * j <= i + (keys - n).  scores are scale * q.k, 0 < scale <= 2e38 (RB_ERR_VALUE).
+ * j <= i + (keys - n).  Without any keys (first_k, tokens_k = 0) k and v may be NULL.  scores are scale * q.k, 0 < scale <= 2e38 (RB_ERR_VALUE).
  * lse: NULL or fp32 [tokens_q][heads], log sum_j exp(scale * q_i.k_j), which the
  * gradient needs.
  */
@@ -436,7 +436,7 @@ int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, const void *
                    int causal, float scale, void *o, float *lse, void *stream);
 
 /*
- * Gradients of rb_attn_prompt for the same operands: go, the gradient of o, and o itself are contiguous
+ * Gradients of rb_attn_prompt for the same operands, one key at least (without keys dq is zero): go, the gradient of o, and o itself are contiguous
  * [tokens_q][heads][dim], lse is what the forward call gave.  dq [tokens_q][heads][dim], dk and dv
  * [tokens_k][kv_heads][dim], contiguous, of the inputs' dtype; dk and dv are summed over the query heads that share a key head.
  * Sums are fp32; weights and score gradients are rounded to dtype before they meet the other operand

@@ -555,6 +555,8 @@ def rb_attn_prompt_grad(go: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     for x in (go, o):
         assert x.is_cuda and x.dtype is dtype and x.shape == shape and x.is_contiguous()
     assert lse.is_cuda and lse.dtype is torch.float32 and lse.shape == shape[:2] and lse.is_contiguous()
+    if k.shape[0] == 0:
+        return torch.zeros(shape, dtype=dtype, device=device), torch.empty_like(k), torch.empty_like(v)
     dq, dk, dv = (torch.empty(s, dtype=dtype, device=device) for s in (shape, k.shape, k.shape))
     need = lib.rb_attn_grad_workspace_bytes(ctypes.byref(H), shape[0], k.shape[0])
     ws = torch.empty(max(need, 16), dtype=torch.uint8, device=device)

@@ -376,7 +376,7 @@ extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, c
 {
     const int rc = check_heads(H);
     if (rc != RB_OK) return rc;
-    if (!q || !k || !v || !first_q || !o) return RB_ERR_NULL;
+    if (!q || (tokens_k != 0 && (!k || !v)) || !first_q || !o) return RB_ERR_NULL;
     if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens_q < 1 || tokens_k < 0 || tokens_q > MAX_TOKENS || tokens_k > MAX_TOKENS || (!first_k && tokens_k != tokens_q)) return RB_ERR_SHAPE;
     if (check_scale(scale) != RB_OK) return RB_ERR_VALUE;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) return RB_ERR_ALIGN;
