@@ -640,7 +640,9 @@ def rb_attn_paged(cache: Cache, q: torch.Tensor, first: torch.Tensor, lengths: t
     if workspace is None:
         need = lib.rb_attn_paged_workspace_bytes(C, heads, at[4], tokens)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    at_ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    else:
+        assert workspace.is_cuda and workspace.is_contiguous()
+    at_ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check("rb_attn_paged", lib.rb_attn_paged(
         C, q.data_ptr(), strides[0], strides[1], heads, *at, tokens, dim ** -0.5 if scale is None else scale, o.data_ptr(), at_ws, size, _stream()))
     return o
