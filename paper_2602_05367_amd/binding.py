@@ -512,10 +512,21 @@ _I32 = torch.int32
 def _heads(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> rb_heads:
     """Shapes and strides of q [tokens][heads][dim] and k, v [tokens][kv_heads][dim], elements of a head contiguous."""
     qs, ks, vs, dtype = q.stride(), k.stride(), v.stride(), k.dtype
-    _, heads, dim = q.shape
+    tokens, heads, dim = q.shape
+    tokens_k, kv_heads, dim_k = k.shape
     assert k.is_cuda and v.is_cuda and q.is_cuda and q.dtype is dtype and v.dtype is dtype and k.shape == v.shape
-    assert qs[2] == ks[2] == vs[2] == 1 and k.shape[2] == dim
-    return rb_heads(heads, k.shape[1], dim, _DTYPE_CODE[dtype], qs[0], qs[1], ks[0], ks[1], vs[0], vs[1])
+    assert qs[2] == ks[2] == vs[2] == 1 and dim_k == dim
+    H = rb_heads(heads, kv_heads, dim, _DTYPE_CODE[dtype], qs[0], qs[1], ks[0], ks[1], vs[0], vs[1])
+    # one token or head: torch's stride says nothing and may be anything
+    if tokens == 1:
+        H.q_token = dim
+    if heads == 1:
+        H.q_head = dim
+    if tokens_k <= 1:
+        H.k_token = H.v_token = dim
+    if kv_heads == 1:
+        H.k_head = H.v_head = dim
+    return H
 
 
 def _starts(first: torch.Tensor, first_k: torch.Tensor = None):
@@ -571,11 +582,12 @@ class Cache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype is v.dtype
-        strides = k.stride()
-        assert strides == v.stride() and strides[3] == 1
         self.k, self.v, self.dtype = k, v, k.dtype
         pages, page_tokens, self.kv_heads, self.dim = k.shape
-        self._struct = rb_cache(k.data_ptr(), v.data_ptr(), pages, page_tokens, self.kv_heads, self.dim, _DTYPE_CODE[k.dtype], *strides[:3])
+        strides = [(page if pages > 1 else page_tokens * token, token, head if self.kv_heads > 1 else self.dim, one)      # (of a single page or head torch's says nothing)
+                   for page, token, head, one in (k.stride(), v.stride())]
+        assert strides[0] == strides[1] and strides[0][3] == 1
+        self._struct = rb_cache(k.data_ptr(), v.data_ptr(), pages, page_tokens, self.kv_heads, self.dim, _DTYPE_CODE[k.dtype], *strides[0][:3])
 
     @classmethod
     def zeros(cls, pages: int, page_tokens: int, kv_heads: int, dim: int, dtype=torch.float16, device="cuda:0") -> "Cache":
@@ -644,7 +656,7 @@ def rb_attn_paged(cache: Cache, q: torch.Tensor, first: torch.Tensor, lengths: t
         assert workspace.is_cuda and workspace.is_contiguous()
     at_ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check("rb_attn_paged", lib.rb_attn_paged(
-        C, q.data_ptr(), strides[0], strides[1], heads, *at, tokens, dim ** -0.5 if scale is None else scale, o.data_ptr(), at_ws, size, _stream()))
+        C, q.data_ptr(), strides[0] if tokens > 1 else dim, strides[1] if heads > 1 else dim, heads, *at, tokens, dim ** -0.5 if scale is None else scale, o.data_ptr(), at_ws, size, _stream()))
     return o
 
 
