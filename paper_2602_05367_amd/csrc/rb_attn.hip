@@ -177,6 +177,8 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
         if constexpr (PAGED) ask_pages(t + 1);
     };
 
+    // A tile's rows past the sequence's end are zeros, but where one value stands for all (a stride of zero) they are that value again, which no row sees
+    const int rows_end = !PAGED && A.v.token < A.dim * 2 ? 0x7fffffff : S.n_k;
     const Rows<D> rows(lane);
     const Columns<D> columns(lane);
     constexpr int B = D / 32, H = KEYS / 32 / HALVES;      // 32s of elements, and of keys of a tile
@@ -186,7 +188,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
         loads_arrived();
         __syncthreads();      // tile t is there, everybody has done with tile t - 1
         if (t + 1 < n_tiles) load(t + 1, next_keys, next_values);
-        if (block_least < min(t * KEYS + KEYS, S.n_k) - 1) {      // some row of the workgroup does not see all of the tile's keys
+        if (block_least < min(t * KEYS + KEYS, rows_end) - 1) {      // some row of the workgroup does not see all of the tile's keys
             make_finite<T, D, KEYS, WAVES>(values, &found, tid);
             __syncthreads();
         }
