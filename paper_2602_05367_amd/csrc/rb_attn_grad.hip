@@ -187,8 +187,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
     v16f sums_k[E] = {}, sums_v[E] = {};
     auto step = [&](int n, uint8_t *queries, uint8_t *outs, float (&rows_of)[2][ROWS], uint8_t *next_queries, uint8_t *next_outs) RB_INLINE {
         if (wave == 0) {
-            // a row past the end: no weight (do is zero there as well)
-            rows_of[0][lane] = t * ROWS + lane < S.n_q ? next_lse * LOG2E - T::GRAD_BIAS : -RB_NEG_INF;
+            rows_of[0][lane] = next_lse * LOG2E - T::GRAD_BIAS;
             rows_of[1][lane] = next_delta;
         }
         loads_arrived();
@@ -228,8 +227,8 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
             __syncthreads();
         }
         if (!any) return;
-        const bool masked = A.causal && wave_last > ahead + row0;
-        const int least = my_key - ahead - row0 - 4 * h;      // the first row that sees this key
+        const bool masked = row0 + 32 > S.n_q || (A.causal && wave_last > ahead + row0);
+        const int least = (A.causal ? my_key - ahead : 0) - row0 - 4 * h, beyond = S.n_q - row0 - 4 * h;      // the first row that sees this key; the end of the rows
         const int mine = half * 32 + 4 * h;
         uint32_t w[8], z[8];
 #pragma unroll
@@ -240,7 +239,7 @@ __global__ __launch_bounds__(512, 2) void keys_kernel(const GradArgs A)
                 const int r = i + j;
                 x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], A.c, -zero_at[j]));
                 y[r] = x[r] * (y[r] - delta[j]) * held.unit;      // ds, from the dp that queries_kernel has, bit for bit
-                if (masked && 8 * (r / 4) + r % 4 < least) x[r] = y[r] = 0.f;
+                if (masked && (8 * (r / 4) + r % 4 < least || 8 * (r / 4) + r % 4 >= beyond)) x[r] = y[r] = 0.f;
             }
             w[i / 2] = T::pack(x[i], x[i + 1]), w[i / 2 + 1] = T::pack(x[i + 2], x[i + 3]);
         }
