@@ -405,7 +405,8 @@ int rb_add(const uint16_t *a, const uint16_t *b, uint16_t *y, size_t n, void *st
  * elements, multiples of 8 and at most 2^23; elements of a head are contiguous.  k and v likewise.  o is
  * contiguous [tokens][heads][dim].  q, k, v, o are device memory of one dtype,
  * RB_F16 or RB_BF16, 16-byte aligned.  Scores, softmax and sums are fp32; the
- * softmax weights are rounded to dtype before they meet the values.
+ * softmax weights are rounded to dtype before they meet the values (in rb_attn_paged with few
+ * tokens per sequence in two parts, as good as fp32: there are few weights for roundings to average out over).
  *
  * Sequences are packed one after the other: sequence s has the tokens first[s]
  * .. first[s + 1] - 1 (device int32 [n_seqs + 1], first[0] = 0, not decreasing;
@@ -440,7 +441,8 @@ int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, const void *
  * [tokens_q][heads][dim], lse is what the forward call gave.  dq [tokens_q][heads][dim], dk and dv
  * [tokens_k][kv_heads][dim], contiguous, of the inputs' dtype; dk and dv are summed over the query heads that share a key head.
  * Sums are fp32; weights and score gradients are rounded to dtype before they meet the other operand
- * (fp16: scaled by a power of two first, so small gradients keep their bits).  No atomics: the same
+ * (fp16: in powers of two that follow each row's and each key's own largest, so small gradients keep their
+ * bits, whatever else is in the call).  A row that sees one key has a dq, and a part in dk, of exactly zero.  No atomics: the same
  * inputs give the same bits.  workspace: rb_attn_grad_workspace_bytes bytes, 16-byte aligned; so many serve every
  * call of at most as many queries and keys.
  */

@@ -69,7 +69,7 @@ __device__ __forceinline__ Args with_shares(Args A, const Sums<Tiles> &tiles)
 
 // One workgroup does 128 rows of one key head, 32 per wavefront, over all keys that they see, KEYS at a time; the next tile of keys and values
 // is on its way into LDS while one is used.  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part (one long
-// prompt of 8192 tokens, 64 query and 8 key heads of 128, causal, bf16: 1.00 to 1.07 ms, 1.02 to 1.10 PFLOP/s, on different cards).  What was tried beside it: 32 keys at a time and
+// prompt of 8192 tokens, 64 query and 8 key heads of 128, causal, bf16: 1.00 to 1.14 ms, 0.97 to 1.10 PFLOP/s, by the card and by how long it has been at work).  What was tried beside it: 32 keys at a time and
 // three wavefronts per SIMD, the same on long prompts and a fifth slower on short ones; a pipeline within a wavefront, scores of one half of a tile
 // beside the weights of the other, 1.08 ms; eight wavefronts and three tiles ahead, 1.09 ms; operand reads left to the compiler, 1.11 ms.
 //

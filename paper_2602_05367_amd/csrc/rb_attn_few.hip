@@ -5,8 +5,8 @@
 // compute unit alike.  A wavefront keeps two tiles of keys and values on their way into LDS of its own, across jobs, and meets nobody.  What it has
 // of a job that it does not have all of goes to the workspace, unnormalised, and a second launch joins the parts in a fixed order.
 //
-// Bound: bytes, where there are enough of them (48 sequences of 250000 positions in all, 64 query and 8 key heads of 128, bf16: 178 us and 6 for the join, 5.7 TB/s;
-// six sequences of 3 to 5 drafts on 8500 positions, 40 heads: 34 and 5); else a chain of latencies, the arrays, the table, the keys, their scores, and a launch
+// Bound: bytes, where there are enough of them (48 sequences of 250000 positions in all, 64 query and 8 key heads of 128, bf16: 180 to 184 us and 6 for the join, 5.6 to 5.7 TB/s;
+// six sequences of 3 to 5 drafts on 8500 positions, 40 heads: 35 and 5); else a chain of latencies, the arrays, the table, the keys, their scores, and a launch
 // for the join (one token on 2000 positions, 32 heads, fp16: 11 and 5 us).
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -257,6 +257,10 @@ template <class T, int D> int launch(const Args &A, int compute_units, hipStream
 
 }  // namespace
 
+// Up to 32 rows per sequence and key head on average: few_kernel reads a sequence's positions once per 32 rows, rows_kernel once per 128, with more to start and to join.  (fp16, 32 query and
+// 8 key heads of 128, calls in us by few_kernel and by rows_kernel: sixteen sequences of 1, 4, 8, 12 and 16 tokens on 2000 31 and 35, 34 and 36, 36.6 and 37.1, 43 and 39, 46 and 41; one of 1, 8 and 16 on
+// 8000 18 and 22, 23.3 and 23.0, 28 and 24; 128 tokens on 2000 beside 15, 32, 64 and 256 single ones on 1000 41 and 35, 48 and 56, 65 and 84, 240 and 239.  What an average costs: 512 tokens on 7700 beside
+// 64, 128 and 256 single ones 274 and 166, 314 and 260, 388 and 346, of which the last two are few_kernel's by it.  32 key heads, sixteen of 8, 16 and 32 tokens 107 and 112, 113 and 108, 120 and 111.)
 bool few_applies(int tokens, int n_seqs, int group, long long positions)
 {
     const long long tiles = block_numbers(tokens, n_seqs, group, ROWS) * (std::min(positions, 0x7fffffffll) / KEYS + 1);

@@ -40,7 +40,8 @@ struct GradArgs {
 };
 
 // ------------------------------------------------------------------ delta ---
-// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o.  Bound: bytes.
+// Sixteen lanes per row, four rows per wavefront and step; a workgroup takes 64 tokens of one head of do and o.  Bound: bytes (6092 tokens of 32 heads of 128,
+// bf16: 16.8 us, 6.0 TB/s, o being just written).
 template <class T> __global__ __launch_bounds__(256) void delta_kernel(const GradArgs A)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (lane & 15) * 8;
@@ -122,7 +123,7 @@ template <int E> __device__ __forceinline__ bool add_halves(v16f (&sums)[E], uin
 // time, through LDS.  Eight wavefronts: four times 32 keys, by the upper and the lower 32 rows of a tile, whose sums are added at the end.  All operands come from LDS,
 // since the two sums of 32 keys fill half of the registers (with keys and values in registers they spilled, which costs more than twice the time: what is spilled waits behind
 // the loads).  Bound: matrix and vector instructions, which two wavefronts per SIMD overlap in part, and the power the former may draw (five sequences of 6000 tokens in all,
-// 32 heads of 128, causal, bf16: 265 us, 0.65 PFLOP/s for its four products).  Blocks in the order of the sequences instead of the heaviest first: 289 us.
+// 32 heads of 128, causal, bf16: 274 us, 0.63 PFLOP/s for its four products).  Blocks in the order of the sequences instead of the heaviest first: 289 us against 265.
 constexpr int BN = 128;
 __device__ __forceinline__ float *part_at(const GradArgs &A, int split, int which, long long row)
 {
@@ -333,8 +334,8 @@ int splits_for(long long blocks, int kv_heads, int group, int compute_units) { r
 
 // ---------------------------------------------------------------------- dq ---
 // The same the other way round: 128 rows' q and do of one key head stay in LDS, keys and values go by, 64 at a time.  Eight wavefronts: four times 32 rows,
-// by the first and the second 32 keys of a tile, whose sums are added at the end.  (The same sequences: 240 us, 0.71 PFLOP/s for four products.  Four wavefronts that keep q and do
-// in registers, 32 keys at a time: 205 to 213 us there, but 28 instead of 23.5 where a workgroup has a compute unit to itself, 512 tokens of 32 heads.)
+// by the first and the second 32 keys of a tile, whose sums are added at the end.  (The same sequences: 239 us, 0.72 PFLOP/s for four products.  Four wavefronts that keep q and do
+// in registers, 32 keys at a time: 205 to 213 us there against 240, but 28 against 23.5 where a workgroup has a compute unit to itself, 512 tokens of 32 heads.)
 template <class T, int D>
 __global__ __launch_bounds__(512, 2) void queries_kernel(const GradArgs A)
 {
