@@ -255,7 +255,9 @@ __device__ __forceinline__ void meet()
 __device__ __forceinline__ int block_start(int first, int s, int group, int BM) { return (int)((long long)first * group / BM) + s; }
 inline long long block_numbers(long long tokens, int n_seqs, int group, int BM) { return tokens * group / BM + n_seqs; }
 
-// the last of n places whose start is not beyond `value` (place 0's never is); a wavefront looks at 64 at a time
+// lanes of which something is true, as a number with a sign: one less than none is -1
+__device__ __forceinline__ int lanes_of(unsigned long long mask) { return (int)__popcll(mask); }
+// the last of n places whose start is not beyond `value`, place 0 where all are (arrays that are not in order); a wavefront looks at 64 at a time
 template <class Start> __device__ __forceinline__ int last_not_beyond(int n, int value, int lane, Start start)
 {
     const int last = n - 1;
@@ -263,7 +265,7 @@ template <class Start> __device__ __forceinline__ int last_not_beyond(int n, int
     while (n > 1) {
         const int step = (n + 63) / 64;
         const unsigned long long below = __ballot(lane * step < n && start(min(lo + lane * step, last)) <= value);
-        const int k = max(0, __popcll(below) - 1);
+        const int k = max(0, lanes_of(below) - 1);
         lo += k * step;
         n = min(step, n - k * step);
     }
@@ -433,7 +435,7 @@ template <class Shape> struct Sums {
     __device__ __forceinline__ int of_block(int block) const
     {
         if (A.n_seqs > 64) return sequence_of_block(first, A.n_seqs, A.group, JOB, block, lane);
-        return max(__popcll(__ballot(lane < A.n_seqs && block_start(q0, lane, A.group, JOB) <= block)) - 1, 0);
+        return max(lanes_of(__ballot(lane < A.n_seqs && block_start(q0, lane, A.group, JOB) <= block)) - 1, 0);
     }
     // the tiles before sequence `end`
     __device__ __forceinline__ int before(int end) const

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs A)
     int s, end, length;      // the token's sequence, where it ends, its positions
     if (A.n_seqs < 64) {
         const int starts = first[min(lane, A.n_seqs)], all = lengths[min(lane, A.n_seqs - 1)];
-        s = max(__popcll(__ballot(lane < A.n_seqs && starts <= token)) - 1, 0);
+        s = max(lanes_of(__ballot(lane < A.n_seqs && starts <= token)) - 1, 0);
         end = __builtin_amdgcn_readlane(starts, s + 1), length = __builtin_amdgcn_readlane(all, s);
     } else {
         s = last_not_beyond(A.n_seqs, token, lane, [&](int i) { return first[i]; });
