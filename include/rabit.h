@@ -496,6 +496,66 @@ int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long
                   int n_seqs, int tokens, float scale, void *o,
                   void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * A cache in 8 bits: a paged cache as above, its elements e4m3 (8 bits: 4 of exponent, 3 of mantissa, no infinities) in units of one power of two per
+ * token and key head, 2^(byte - 127), the bytes in k_exp and v_exp, contiguous [pages][kv_heads][page_tokens], 8-byte aligned.  dtype (RB_F16 or
+ * RB_BF16) is that of the tokens that enter it and of the queries.  dim is a multiple of 16 up to 128 (RB_ERR_UNSUPPORTED otherwise);
+ * strides of k and v are in elements, multiples of 16, token_stride dim at least; elements of a head are contiguous, k and v 16-byte aligned.
+ *
+ * How a head x is held: first brought to at most 15/16 of the power of two above dtype's largest finite value (61440 for fp16), so that
+ * what is held is finite in dtype again.  With m 2^n, 1 <= m < 2, the largest |x_i|: the unit is 2^(n - 8) if m <= 1.75, else
+ * 2^(n - 7) (so that all are at most 448 units), but not below 2^-126; elements are x_i / unit, rounded to nearest, ties to even.  Infinities
+ * and NaN are held as NaN, the others of their head as if they were not there.
+ */
+typedef struct rb_cache8 {
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;
+    int pages, page_tokens, kv_heads, dim, dtype;
+    long long page_stride, token_stride, head_stride;
+} rb_cache8;
+
+/* rb_cache_append into it: the same arguments, refusals and results; turned keys are rounded once, from fp32 to what is held. */
+int rb_cache8_append(const rb_cache8 *C, const rb_heads *H, const void *q, const void *k, const void *v,
+                     const float *cos, const float *sin, int table_rows, int rotary, int interleaved,
+                     const int32_t *first, const int32_t *lengths, const int32_t *table, int width,
+                     int n_seqs, int tokens, void *q_out, void *stream);
+
+/*
+ * Tokens come back out of it, as attention sees them: sequence s's last first[s + 1] - first[s] of its lengths[s] positions (all of them, where that is
+ * as many) to rows first[s] .. first[s + 1] - 1 of k and v, contiguous [tokens][kv_heads][dim] of the cache's dtype, 16-byte aligned.  Where a
+ * position lies outside the page table, or its entry there is not the number of a page, the row is zeros.  Rows from first[n_seqs] on are left as they are.
+ */
+int rb_cache8_read(const rb_cache8 *C, const int32_t *first, const int32_t *lengths, const int32_t *table, int width,
+                   int n_seqs, int tokens, void *k, void *v, void *stream);
+
+/* rb_attn_paged over it: the same arguments, refusals and results, of the values that the cache holds. */
+size_t rb_attn_cache8_workspace_bytes(const rb_cache8 *C, int heads, int n_seqs, int tokens);
+int rb_attn_cache8(const rb_cache8 *C, const void *q, long long q_token, long long q_head, int heads,
+                   const int32_t *first, const int32_t *lengths, const int32_t *table, int width,
+                   int n_seqs, int tokens, float scale, void *o,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The next token of each row of logits, drawn with a given random number.  logits: device [rows][vocab] of dtype (RB_F16, RB_BF16 or RB_F32), rows `stride`
+ * elements apart (vocab at least), aligned as their elements are; u, temperature, top_p, min_p: device fp32 [rows], top_k: device int32 [rows];
+ * tokens: device int32 [rows].  temperature, top_k, top_p and min_p may be NULL: 1, all, 1 and 0 for every row.
+ *
+ * With w_j = exp((x_j - max x) / temperature) and the tokens in descending order of x, equal ones the lowest index first:
+ *   the first top_k of them (all, if top_k < 1 or > vocab);
+ *   of these, as few from the front as have a sum of w of top_p times that of these (all, if top_p >= 1; one at least);
+ *   of these, the ones of w_j >= min_p (min_p > 1 counts as 1, the largest stay);
+ *   tokens[row] = the lowest index j of those left such that the sum of w over those left up to j exceeds u times the sum over all of them.
+ * u is in [0, 1); what is below counts as 0, what is not below 1 as the largest number below it.  temperature <= 0: the first in the order above, whatever the
+ * other parameters are.  NaN counts as 0 in u and min_p, as 1 in top_p, as 0 in temperature.
+ *
+ * Logits of minus infinity (masked) and NaN are never drawn; a row that has no others gives -1.  Logits of plus infinity: only these are left, with equal weights.
+ * Weights are fp32, to (1 + |log2 w|) 2^-23 of themselves, held in units of 2^-38 (less is zero), and their sums are exact: they depend on no order, and the same input
+ * gives the same token.  1 <= rows <= 2^20, 1 <= vocab <= 2^22, stride < 2^40.
+ */
+int rb_sample(const void *logits, int dtype, long long stride, int rows, int vocab, const float *u,
+              const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+              int32_t *tokens, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

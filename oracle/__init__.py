@@ -494,3 +494,42 @@ def rotary(x, cos, sin, interleaved: bool):
     u, w = x[..., a].copy(), x[..., b].copy()
     x[..., a], x[..., b] = u * cos - w * sin, w * cos + u * sin
     return x
+
+
+LARGEST_HELD = {"fp16": 1.875 * 2.0 ** 15, "bf16": 1.875 * 2.0 ** 127}
+
+
+def held_in_8_bits(x, dtype: str):
+    """Heads x [..., d] as a cache in 8 bits holds them: (elements [..., d], numbers that e4m3 has, or NaN; bytes [...] of the units 2^(byte - 127))."""
+    x = _f64(x)
+    finite = np.where(np.isfinite(x), np.clip(x, -LARGEST_HELD[dtype], LARGEST_HELD[dtype]), 0.0)
+    most = np.abs(finite).max(-1)
+    m, e = np.frexp(most)                                    # m in [1/2, 1)
+    unit = np.where(most > 0, np.maximum(e - 9 + (m > 0.875), -126), -126)
+    y = np.ldexp(finite, -unit[..., None])
+    step = np.ldexp(1.0, np.maximum(np.frexp(y)[1] - 1, -6) - 3)
+    return np.where(np.isfinite(x), np.rint(y / step) * step, np.nan), unit + 127
+
+
+def next_token(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> int:
+    """The token drawn from one row of logits x by u in [0, 1): see rb_sample."""
+    x = _f64(x)
+    x = np.where(np.isnan(x), -np.inf, x)
+    order = np.argsort(-x, kind="stable")
+    most = x[order[0]]
+    if most == -np.inf:
+        return -1
+    if not temperature > 0:
+        return int(order[0])
+    with np.errstate(over="ignore", invalid="ignore"):
+        w = np.where(x == most, 1.0, np.where(x == -np.inf, 0.0, np.exp((x - most) / temperature)))
+    kept = order[:top_k] if 1 <= top_k < len(x) else order
+    if top_p < 1:
+        upto = np.cumsum(w[kept])
+        kept = kept[:max(int((upto < top_p * upto[-1]).sum()) + 1, 1)]
+    kept = kept[w[kept] >= min(min_p, 1.0)] if min_p > 0 else kept
+    only = np.zeros_like(w)
+    only[kept] = w[kept]
+    upto = np.cumsum(only)
+    u = min(max(u, 0.0), 1.0 - 2.0 ** -24) if u == u else 0.0
+    return int(np.argmax(upto > u * upto[-1]))

@@ -34,6 +34,7 @@ EXPORTS = [
     "rb_block_prepare", "rb_block_workspace_bytes", "rb_rmsnorm", "rb_silu_mul", "rb_add",
     "rb_derive_iterative", "rb_derive_workspace_bytes",
     "rb_attn_prompt", "rb_attn_prompt_grad", "rb_attn_grad_workspace_bytes", "rb_attn_paged", "rb_attn_paged_workspace_bytes", "rb_cache_append",
+    "rb_cache8_append", "rb_cache8_read", "rb_attn_cache8", "rb_attn_cache8_workspace_bytes", "rb_sample",
     "rb_dense_gemv_f16", "rb_stream_read", "rb_stream_read_groups", "rb_version", "rb_last_path",
 ]
 
@@ -65,6 +66,12 @@ class rb_heads(ctypes.Structure):
 
 class rb_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int) for n in ("pages", "page_tokens", "kv_heads", "dim", "dtype")] + \
+               [(n, ctypes.c_longlong) for n in ("page_stride", "token_stride", "head_stride")]
+
+
+class rb_cache8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
                [(n, ctypes.c_int) for n in ("pages", "page_tokens", "kv_heads", "dim", "dtype")] + \
                [(n, ctypes.c_longlong) for n in ("page_stride", "token_stride", "head_stride")]
 
@@ -121,6 +128,12 @@ def _load() -> ctypes.CDLL:
     lib.rb_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(rb_cache), i, i, i]
     lib.rb_attn_paged_workspace_bytes.restype = z
     lib.rb_attn_paged.argtypes = [ctypes.POINTER(rb_cache), p, l, l, i, p, p, p, i, i, i, f, p, p, z, p]
+    lib.rb_cache8_append.argtypes = [ctypes.POINTER(rb_cache8), *lib.rb_cache_append.argtypes[1:]]
+    lib.rb_cache8_read.argtypes = [ctypes.POINTER(rb_cache8), p, p, p, i, i, i, p, p, p]
+    lib.rb_attn_cache8_workspace_bytes.argtypes = [ctypes.POINTER(rb_cache8), i, i, i]
+    lib.rb_attn_cache8_workspace_bytes.restype = z
+    lib.rb_attn_cache8.argtypes = [ctypes.POINTER(rb_cache8), *lib.rb_attn_paged.argtypes[1:]]
+    lib.rb_sample.argtypes = [p, i, l, i, i, p, p, p, p, p, p, p]
     lib.rb_dense_gemv_f16.argtypes = [p, p, p, i, i, p]
     lib.rb_stream_read.argtypes = [p, z, p, p]
     lib.rb_stream_read_groups.argtypes = []
@@ -129,7 +142,7 @@ def _load() -> ctypes.CDLL:
     for name in EXPORTS:
         if name not in ("rb_native_bytes", "rb_workspace_bytes", "rb_noalloc_scratch_bytes",
                         "rb_scale_grads_workspace_bytes", "rb_block_workspace_bytes", "rb_derive_workspace_bytes",
-                        "rb_attn_paged_workspace_bytes", "rb_attn_grad_workspace_bytes"):
+                        "rb_attn_paged_workspace_bytes", "rb_attn_grad_workspace_bytes", "rb_attn_cache8_workspace_bytes"):
             getattr(lib, name).restype = i
     return lib
 
@@ -606,11 +619,47 @@ def _sequences(first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
     return first.data_ptr(), lengths.data_ptr(), table.data_ptr(), width, n
 
 
+class Cache8:
+    """A paged cache in 8 bits: k and v float8_e4m3fn [pages][page_tokens][kv_heads][dim] of equal strides, k_exp and v_exp uint8 [pages][kv_heads][page_tokens],
+    an element being e4m3 * 2^(byte - 127); dtype: fp16 or bf16, of the tokens that enter it and of the queries."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, dtype: torch.dtype = torch.float16):
+        assert k.is_cuda and v.is_cuda and k_exp.is_cuda and v_exp.is_cuda and k.dim() == 4 and k.shape == v.shape
+        assert k.dtype is v.dtype is torch.float8_e4m3fn and k_exp.dtype is v_exp.dtype is torch.uint8
+        self.k, self.v, self.k_exp, self.v_exp, self.dtype = k, v, k_exp, v_exp, dtype
+        pages, page_tokens, self.kv_heads, self.dim = k.shape
+        assert k_exp.shape == v_exp.shape == (pages, self.kv_heads, page_tokens) and k_exp.is_contiguous() and v_exp.is_contiguous()
+        strides = [(page if pages > 1 else page_tokens * token, token, head if self.kv_heads > 1 else self.dim, one) for page, token, head, one in (k.stride(), v.stride())]
+        assert strides[0] == strides[1] and strides[0][3] == 1
+        self._struct = rb_cache8(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, page_tokens, self.kv_heads, self.dim, _DTYPE_CODE[dtype],
+                                 *strides[0][:3])
+
+    @classmethod
+    def zeros(cls, pages: int, page_tokens: int, kv_heads: int, dim: int, dtype=torch.float16, device="cuda:0") -> "Cache8":
+        bytes_of = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)
+        return cls(*(bytes_of(pages, page_tokens, kv_heads, dim).view(torch.float8_e4m3fn) for _ in range(2)), *(bytes_of(pages, kv_heads, page_tokens) for _ in range(2)),
+                   dtype)
+
+    def struct(self) -> rb_cache8:
+        return self._struct
+
+
 def rb_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
                     q: torch.Tensor = None, cos: torch.Tensor = None, sin: torch.Tensor = None, interleaved: bool = False,
                     q_out: torch.Tensor = None):
     """New tokens k, v [tokens][kv_heads][dim] become the last of each sequence's lengths int32 [n_seqs] positions of the
     cache, with the rotary embedding of cos, sin fp32 [rows][rotary / 2] on k and q [tokens][heads][dim]; returns the turned q."""
+    return _append("rb_cache_append", lib.rb_cache_append, cache, k, v, first, lengths, table, q, cos, sin, interleaved, q_out)
+
+
+def rb_cache8_append(cache: Cache8, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
+                     q: torch.Tensor = None, cos: torch.Tensor = None, sin: torch.Tensor = None, interleaved: bool = False,
+                     q_out: torch.Tensor = None):
+    """rb_cache_append into a cache in 8 bits."""
+    return _append("rb_cache8_append", lib.rb_cache8_append, cache, k, v, first, lengths, table, q, cos, sin, interleaved, q_out)
+
+
+def _append(name, entry, cache, k, v, first, lengths, table, q, cos, sin, interleaved, q_out):
     at = _sequences(first, lengths, table)
     H = _heads(k if q is None else q, k, v)
     assert H.kv_heads == cache.kv_heads and H.dim == cache.dim and k.dtype is cache.dtype
@@ -631,15 +680,39 @@ def rb_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, first: torch
         assert cos.is_cuda and sin.is_cuda and cos.dtype is sin.dtype is torch.float32 and sin.shape == cos.shape
         assert cos.is_contiguous() and sin.is_contiguous()
         at_cos, at_sin = cos.data_ptr(), sin.data_ptr()
-    _check("rb_cache_append", lib.rb_cache_append(
-        ctypes.byref(cache._struct), ctypes.byref(H), from_q, k.data_ptr(), v.data_ptr(), at_cos, at_sin, rows, 2 * half, interleaved,
-        *at, tokens, to_q, _stream()))
+    _check(name, entry(ctypes.byref(cache._struct), ctypes.byref(H), from_q, k.data_ptr(), v.data_ptr(), at_cos, at_sin, rows, 2 * half, interleaved,
+                       *at, tokens, to_q, _stream()))
     return q_out
+
+
+def rb_cache8_read(cache: Cache8, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, tokens: int, k: torch.Tensor = None, v: torch.Tensor = None):
+    """The last first[s + 1] - first[s] of each sequence's lengths[s] positions, `tokens` in all (first[n_seqs], or more), as
+    k and v [tokens][kv_heads][dim] of the cache's dtype."""
+    at = _sequences(first, lengths, table)
+    shape = (tokens, cache.kv_heads, cache.dim)
+    if k is None:
+        k = torch.empty(shape, dtype=cache.dtype, device=cache.k.device)
+    if v is None:
+        v = torch.empty(shape, dtype=cache.dtype, device=cache.k.device)
+    for x in (k, v):
+        assert x.is_cuda and x.dtype is cache.dtype and x.shape == shape and x.is_contiguous()
+    _check("rb_cache8_read", lib.rb_cache8_read(ctypes.byref(cache._struct), *at, tokens, k.data_ptr(), v.data_ptr(), _stream()))
+    return k, v
 
 
 def rb_attn_paged(cache: Cache, q: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, scale: float = None,
                   o: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """Attention of new tokens q [tokens][heads][dim], the last of each sequence's lengths positions, over the cache."""
+    return _over_cache("rb_attn_paged", lib.rb_attn_paged, lib.rb_attn_paged_workspace_bytes, cache, q, first, lengths, table, scale, o, workspace)
+
+
+def rb_attn_cache8(cache: Cache8, q: torch.Tensor, first: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, scale: float = None,
+                   o: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
+    """rb_attn_paged over a cache in 8 bits."""
+    return _over_cache("rb_attn_cache8", lib.rb_attn_cache8, lib.rb_attn_cache8_workspace_bytes, cache, q, first, lengths, table, scale, o, workspace)
+
+
+def _over_cache(name, entry, workspace_bytes, cache, q, first, lengths, table, scale, o, workspace):
     at = _sequences(first, lengths, table)
     shape, strides = q.shape, q.stride()
     tokens, heads, dim = shape
@@ -650,14 +723,32 @@ def rb_attn_paged(cache: Cache, q: torch.Tensor, first: torch.Tensor, lengths: t
         assert o.is_cuda and o.dtype is q.dtype and o.shape == shape and o.is_contiguous()
     C = ctypes.byref(cache._struct)
     if workspace is None:
-        need = lib.rb_attn_paged_workspace_bytes(C, heads, at[4], tokens)
+        need = workspace_bytes(C, heads, at[4], tokens)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     else:
         assert workspace.is_cuda and workspace.is_contiguous()
     at_ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check("rb_attn_paged", lib.rb_attn_paged(
-        C, q.data_ptr(), strides[0] if tokens > 1 else dim, strides[1] if heads > 1 else dim, heads, *at, tokens, dim ** -0.5 if scale is None else scale, o.data_ptr(), at_ws, size, _stream()))
+    _check(name, entry(C, q.data_ptr(), strides[0] if tokens > 1 else dim, strides[1] if heads > 1 else dim, heads, *at, tokens,
+                       dim ** -0.5 if scale is None else scale, o.data_ptr(), at_ws, size, _stream()))
     return o
+
+
+# -------------------------------------------------------------- sampling ---
+def rb_sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor = None, top_k: torch.Tensor = None, top_p: torch.Tensor = None,
+              min_p: torch.Tensor = None, tokens: torch.Tensor = None) -> torch.Tensor:
+    """The next token int32 [rows] of logits [rows][vocab] (fp16, bf16 or fp32, any stride of rows), drawn with u fp32 [rows] in [0, 1); temperature, top_p and
+    min_p fp32 [rows], top_k int32 [rows], None: not filtered.  -1: the row has no logit above minus infinity."""
+    rows, vocab = logits.shape
+    stride, one = logits.stride()
+    assert logits.is_cuda and (one == 1 or vocab == 1)
+    if tokens is None:
+        tokens = torch.empty(rows, dtype=_I32, device=logits.device)
+    at = []
+    for x, dtype in ((u, torch.float32), (temperature, torch.float32), (top_k, _I32), (top_p, torch.float32), (min_p, torch.float32), (tokens, _I32)):
+        assert x is None or (x.is_cuda and x.dtype is dtype and x.shape == (rows,) and x.is_contiguous())
+        at.append(None if x is None else x.data_ptr())
+    _check("rb_sample", lib.rb_sample(logits.data_ptr(), _DTYPE_CODE[logits.dtype], stride if rows > 1 else vocab, rows, vocab, *at, _stream()))
+    return tokens
 
 
 def rb_stack_set_option(option: int, value: int) -> None:

@@ -63,6 +63,11 @@ struct BF16 {
     static __device__ __forceinline__ float sum(uint32_t w, float on) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2b, w), (v2b){(__bf16)1.f, (__bf16)1.f}, on, false); }
 };
 
+union Four {      // 16-bit values
+    v2u w;
+    uint16_t h[4];
+};
+
 // an infinity or a NaN among the two 16-bit values of a word
 template <class T> __device__ __forceinline__ bool not_finite(uint32_t w)
 {
@@ -206,22 +211,26 @@ template <class T, int D, int ROWS, int W> __device__ __forceinline__ void make_
         }
     }
 }
-// At the end, where something was found: sums [element][column of the lane] += what is not finite in row `from` (in memory), if the lane's
-// column sees it.  Any weight gives the same.
-template <class T, int D> __device__ __forceinline__ void add_not_finite(v16f (&sums)[D / 32], const uint8_t *from, int dim, int h, bool seen)
+// At the end, where something was found: sums [element][column of the lane] += what is not finite in a row of values (in memory), if the lane's
+// column sees it.  Any weight gives the same.  four(e): elements e + 4 h .. + 3 of the row, in 16 bits each
+template <class T, int D, class Four_> __device__ __forceinline__ void add_not_finite(v16f (&sums)[D / 32], bool seen, Four_ four)
 {
-    const __amdgpu_buffer_rsrc_t row = buffer(from, dim * 2);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const v2u w = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(row, h * 8, (b * 32 + 2 * i) * 2, 0));
+            const v2u w = four(b * 32 + 2 * i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t bits = (j < 2 ? w.x : w.y) >> (j % 2 * 16) & 0xffffu;
                 if (seen && (bits & T::EXPONENT) == T::EXPONENT) sums[b][i + j] += T::widen(bits);
             }
         }
+}
+template <class T, int D> __device__ __forceinline__ void add_not_finite(v16f (&sums)[D / 32], const uint8_t *from, int dim, int h, bool seen)
+{
+    const __amdgpu_buffer_rsrc_t row = buffer(from, dim * 2);
+    add_not_finite<T, D>(sums, seen, [&](int e) RB_INLINE { return __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(row, h * 8, e * 2, 0)); });
 }
 // sums [element][column], element 32 b + 8 (i / 4) + 4 h + i % 4, as a row of 16-bit values per column; `empty`: zeros whatever they are
 template <class T, int D> __device__ __forceinline__ void store_columns(const v16f (&sums)[D / 32], float scale, uint8_t *to, int dim, int h, bool real, bool empty)
@@ -311,6 +320,19 @@ template <class Count> __device__ __forceinline__ bool nth_heaviest(int n_seqs, 
     return true;
 }
 
+// A packed token's sequence, where that ends, and its positions; the same in all lanes
+__device__ __forceinline__ void sequence_of_token(const int *first, const int *lengths, int n_seqs, int token, int lane, int &s, int &end, int &length)
+{
+    if (n_seqs < 64) {
+        const int starts = first[min(lane, n_seqs)], all = lengths[min(lane, n_seqs - 1)];
+        s = max(lanes_of(__ballot(lane < n_seqs && starts <= token)) - 1, 0);
+        end = __builtin_amdgcn_readlane(starts, s + 1), length = __builtin_amdgcn_readlane(all, s);
+    } else {
+        s = last_not_beyond(n_seqs, token, lane, [&](int i) { return first[i]; });
+        end = first[s + 1], length = lengths[s];
+    }
+}
+
 // One sequence's part of the work.  What the arrays say is brought into the range of the buffers: an array that
 // is not in order gives wrong results, but no access outside.
 struct Sequence {
@@ -381,7 +403,7 @@ struct Side {
 struct Args {
     Side q, k, v;
     Address o, lse, first_q, first_k;        // paged: first_k holds the sequences' lengths
-    Address table;
+    Address table, k_exp, v_exp;             // k_exp, v_exp: of a cache in 8 bits
     long long page;
     int n_seqs, tokens_q, tokens_k, heads, kv_heads, group, dim, causal, ordered;
     int page_shift, pages, width;

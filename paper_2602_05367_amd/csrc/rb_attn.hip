@@ -5,6 +5,7 @@
 
 #include "rabit.h"
 #include "rb_attn.h"
+#include "rb_attn8.h"
 #include "rb_attn_host.h"
 #include "rb_internal.h"
 
@@ -78,11 +79,13 @@ __device__ __forceinline__ Args with_shares(Args A, const Sums<Tiles> &tiles)
 // heads of 128: 64 tokens of 8 heads 12.4 -> 9.9 us, 512 of 32 16.3 -> 15.3, 1200 of 32 and 8 28.6 -> 25.3, 8192 of one head 141 -> 111, 6000 of 8 116 -> 96; heads of 64 3 to 10 %).
 // Beyond, two workgroups fill a compute unit as well as one of twice the size, without the join (2600 tokens of 32 and 8 heads, 656 workgroups, 67 and 78 us; eight sequences of 1000
 // tokens in all, 312 workgroups, 11.5 and 16.8).
-template <class T, int D, bool PAGED, int HALVES>
+enum From { PACKED, PAGES, PAGES8 };      // where keys and values are: packed, in a cache, in a cache in 8 bits
+template <class T, int D, From FROM, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 {
     using L = Tile<D>;
     constexpr int WAVES = 4 * HALVES;
+    constexpr bool PAGED = FROM != PACKED, IN8 = FROM == PAGES8;
     // tiles as variables of their own: the compiler then knows that loads into one do not concern reads of another
     __shared__ __attribute__((aligned(16))) uint8_t keys_a[L::bytes(KEYS)], values_a[L::bytes(KEYS)], keys_b[L::bytes(KEYS)], values_b[L::bytes(KEYS)];
     __shared__ int found;
@@ -171,6 +174,24 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
                 part.template load<PART_LOADS, PART_LOADS>(rows_buffer(base + place(pages[1], r + 8) - 8 * stride, stride, S.n_k - r, 16, A.dim), tile, wave);
         }
     };
+    // of 8 bits, by way of registers
+    const uint32_t at8 = Rows8<D, MINE>::at(A.k.token, A.dim, lane);
+    auto exponents_at = [&](Address exponents, int page, int r) RB_INLINE {
+        return global_at<const uint8_t>(exponents) + (((long long)min(max(page, 0), A.pages - 1) * A.kv_heads + kvh) << A.page_shift) + (r & ((1 << A.page_shift) - 1));
+    };
+    [[maybe_unused]] Rows8<D, MINE> raw_k, raw_v;
+    [[maybe_unused]] auto load8 = [&](int t) RB_INLINE {
+        const int r = t * KEYS + wave * MINE;
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) raw_k.load(i, k_base + place(pages[i], r + i * 8), exponents_at(A.k_exp, pages[i], r + i * 8), A.k.token, S.n_k - r - i * 8, A.dim, at8, lane);
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) raw_v.load(i, v_base + place(pages[i], r + i * 8), exponents_at(A.v_exp, pages[i], r + i * 8), A.v.token, S.n_k - r - i * 8, A.dim, at8, lane);
+        ask_pages(t + 1);
+    };
+    auto write8 = [&](uint8_t *keys, uint8_t *values) RB_INLINE {
+        raw_k.template write<T>(keys, wave * MINE, lane);
+        raw_v.template write<T>(values, wave * MINE, lane);
+    };
     auto load = [&](int t, uint8_t *keys, uint8_t *values) RB_INLINE {
         load_one(t, k_base, A.k.token, k_part, keys);
         load_one(t, v_base, A.v.token, v_part, values);
@@ -185,9 +206,15 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
     v16f sums[B] = {};
     float top = RB_NEG_INF, total = 0.f;
     auto step = [&](int t, uint8_t *keys, uint8_t *values, uint8_t *next_keys, uint8_t *next_values) RB_INLINE {
-        loads_arrived();
-        __syncthreads();      // tile t is there, everybody has done with tile t - 1
-        if (t + 1 < n_tiles) load(t + 1, next_keys, next_values);
+        if constexpr (IN8) {
+            meet();
+            if (t + 1 < n_tiles) write8(next_keys, next_values);
+            if (t + 2 < n_tiles) load8(t + 2);
+        } else {
+            loads_arrived();
+            __syncthreads();      // tile t is there, everybody has done with tile t - 1
+            if (t + 1 < n_tiles) load(t + 1, next_keys, next_values);
+        }
         if (block_least < min(t * KEYS + KEYS, rows_end) - 1) {      // some row of the workgroup does not see all of the tile's keys
             make_finite<T, D, KEYS, WAVES>(values, &found, tid);
             __syncthreads();
@@ -235,7 +262,13 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
     if (tid == 0) found = 0;
     if (first_tile < n_tiles) {
         if constexpr (PAGED) ask_pages(first_tile);
-        load(first_tile, keys_a, values_a);
+        if constexpr (IN8) {
+            load8(first_tile);
+            write8(keys_a, values_a);
+            load8(first_tile + 1);
+        } else {
+            load(first_tile, keys_a, values_a);
+        }
     }
     for (int t = first_tile; t < n_tiles; t += 2) {
         step(t, keys_a, values_a, keys_b, values_b);
@@ -266,9 +299,16 @@ __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
 #pragma unroll
             for (int i = 0; i < 16; ++i) sums[b][i] = sums[b][i] * mine + ((const v4f *)(by + (b * 4 + i / 4) * 1024 + lane * 16))[0][i % 4] * theirs;
     }
-    if (__builtin_amdgcn_readfirstlane(found))
-        for (int r = max(max(block_least + 1, 0) / KEYS, first_tile) * KEYS; r <= min(wave_most, n_tiles * KEYS - 1); ++r)
-            add_not_finite<T, D>(sums, v_base + (PAGED ? place(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), r) : r * A.v.token), A.dim, h, r <= limit);
+    if (__builtin_amdgcn_readfirstlane(found)) {
+        for (int r = max(max(block_least + 1, 0) / KEYS, first_tile) * KEYS; r <= min(wave_most, n_tiles * KEYS - 1); ++r) {
+            if constexpr (IN8) {
+                const int page = __builtin_amdgcn_readfirstlane(table[r >> A.page_shift]);
+                add_not_finite8<T, D>(sums, v_base + place(page, r), *exponents_at(A.v_exp, page, r), A.dim, h, r <= limit);
+            } else {
+                add_not_finite<T, D>(sums, v_base + (PAGED ? place(__builtin_amdgcn_readfirstlane(table[r >> A.page_shift]), r) : r * A.v.token), A.dim, h, r <= limit);
+            }
+        }
+    }
 
     total = over_halves_sum(total);
     const bool empty = limit < 0;
@@ -332,13 +372,16 @@ template <class T, int D> int launch_rows(Args A, bool paged, int compute_units,
     A.ordered = ordered_for(A.n_seqs, n, 2ll * compute_units);
     const dim3 grid((unsigned)n);
     if (paged) {
-        hipLaunchKernelGGL((rows_kernel<T, D, true, 1>), grid, dim3(256), 0, stream, A);
+        if (A.k_exp)
+            hipLaunchKernelGGL((rows_kernel<T, D, PAGES8, 1>), grid, dim3(256), 0, stream, A);
+        else
+            hipLaunchKernelGGL((rows_kernel<T, D, PAGES, 1>), grid, dim3(256), 0, stream, A);
         const int joined = rows_joined(blocks, BM);
         if (A.wanted) hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)blocks, (unsigned)std::min((long long)BM / joined, std::max(JOINING / blocks, 1ll))), dim3(256), 0, stream, A, joined);
     } else if (n <= (A.n_seqs == 1 ? 2 : 1) * compute_units) {
-        hipLaunchKernelGGL((rows_kernel<T, D, false, 2>), grid, dim3(512), 0, stream, A);
+        hipLaunchKernelGGL((rows_kernel<T, D, PACKED, 2>), grid, dim3(512), 0, stream, A);
     } else {
-        hipLaunchKernelGGL((rows_kernel<T, D, false, 1>), grid, dim3(256), 0, stream, A);
+        hipLaunchKernelGGL((rows_kernel<T, D, PACKED, 1>), grid, dim3(256), 0, stream, A);
     }
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
@@ -392,41 +435,72 @@ extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, c
     return launch(A, H->dtype, false, rb::mx::device_groups(), static_cast<hipStream_t>(stream));
 }
 
-extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
-{
-    if (check_cache(C) != RB_OK || heads < 1 || heads % C->kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
-    const int units = rb::mx::device_groups(), group = heads / C->kv_heads;
-    // whichever kernel a call of up to so many tokens and sequences and its table's width will choose
-    const size_t few = few_applies(1, n_seqs, group, 0) ? few_workspace_bytes(C->kv_heads, C->dim, units) : 0;
-    return std::max(few, parts_workspace_bytes(C->kv_heads, group, C->dim, units));
-}
+namespace {
 
-extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
-                             const int32_t *table, int width, int n_seqs, int tokens, float scale, void *o, void *workspace, size_t workspace_bytes, void *stream)
+// A call over a cache: `C` as one of 16 bits, its strides in elements of `size` bytes
+size_t paged_workspace_bytes(const rb_cache &C, int heads, int n_seqs, int tokens)
 {
-    int rc = check_cache(C);
-    if (rc != RB_OK) return rc;
-    const rb_heads H = {heads, C->kv_heads, C->dim, C->dtype, q_token, q_head, C->token_stride, C->head_stride, C->token_stride, C->head_stride};
-    rc = check_heads(&H);
+    if (heads < 1 || heads % C.kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
+    const int units = rb::mx::device_groups(), group = heads / C.kv_heads;
+    // whichever kernel a call of up to so many tokens and sequences and its table's width will choose
+    const size_t few = few_applies(1, n_seqs, group, 0) ? few_workspace_bytes(C.kv_heads, C.dim, units) : 0;
+    return std::max(few, parts_workspace_bytes(C.kv_heads, group, C.dim, units));
+}
+int paged(const rb_cache &C, int size, const uint8_t *k_exp, const uint8_t *v_exp, const void *q, long long q_token, long long q_head, int heads, const int32_t *first,
+          const int32_t *lengths, const int32_t *table, int width, int n_seqs, int tokens, float scale, void *o, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const rb_heads H = {heads, C.kv_heads, C.dim, C.dtype, q_token, q_head, C.token_stride, C.head_stride, C.token_stride, C.head_stride};
+    const int rc = check_heads(&H);
     if (rc != RB_OK) return rc;
     if (!q || !first || !lengths || !table || !o) return RB_ERR_NULL;
     if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens < 1 || tokens > MAX_TOKENS || width < 1) return RB_ERR_SHAPE;
     if (check_scale(scale) != RB_OK) return RB_ERR_VALUE;
     if (((uintptr_t)q | (uintptr_t)o) & 15) return RB_ERR_ALIGN;
     if (((uintptr_t)first | (uintptr_t)lengths | (uintptr_t)table) & 3) return RB_ERR_ALIGN;
-    if (workspace_bytes < rb_attn_paged_workspace_bytes(C, heads, n_seqs, tokens) || (workspace_bytes && !workspace)) return RB_ERR_WORKSPACE;
+    if (workspace_bytes < paged_workspace_bytes(C, heads, n_seqs, tokens) || (workspace_bytes && !workspace)) return RB_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15) return RB_ERR_ALIGN;
     Args A = {};
-    A.q = side(q, q_token, q_head), A.k = side(C->k, C->token_stride, C->head_stride), A.v = side(C->v, C->token_stride, C->head_stride);
+    A.q = side(q, q_token, q_head);
+    A.k = {rb::address_of(C.k), C.token_stride * size, C.head_stride * size}, A.v = {rb::address_of(C.v), C.token_stride * size, C.head_stride * size};
+    A.k_exp = rb::address_of(k_exp), A.v_exp = rb::address_of(v_exp);
     A.o = rb::address_of(o), A.first_q = rb::address_of(first), A.first_k = rb::address_of(lengths), A.table = rb::address_of(table);
-    A.page = C->page_stride * 2, A.pages = C->pages, A.width = width, A.page_shift = __builtin_ctz((unsigned)C->page_tokens);
+    A.page = C.page_stride * size, A.pages = C.pages, A.width = width, A.page_shift = __builtin_ctz((unsigned)C.page_tokens);
     A.n_seqs = n_seqs, A.tokens_q = tokens;
-    A.heads = heads, A.kv_heads = C->kv_heads, A.group = heads / C->kv_heads, A.dim = C->dim, A.causal = 1;
+    A.heads = heads, A.kv_heads = C.kv_heads, A.group = heads / C.kv_heads, A.dim = C.dim, A.causal = 1;
     A.c = scale * LOG2E;
     A.parts = rb::address_of(workspace);
     const int units = rb::mx::device_groups();
-    A.wanted = groups_wanted(tokens, n_seqs, A.kv_heads, A.group, std::min((long long)width * C->page_tokens, 0x7fffffffll), units);
+    A.wanted = groups_wanted(tokens, n_seqs, A.kv_heads, A.group, std::min((long long)width * C.page_tokens, 0x7fffffffll), units);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_applies(tokens, n_seqs, A.group, (long long)width * C->page_tokens)) return launch_few(A, C->dtype, units, st);
-    return launch(A, C->dtype, true, units, st);
+    if (few_applies(tokens, n_seqs, A.group, (long long)width * C.page_tokens)) return launch_few(A, C.dtype, units, st);
+    return launch(A, C.dtype, true, units, st);
+}
+rb_cache as16(const rb_cache8 &C) { return {C.k, C.v, C.pages, C.page_tokens, C.kv_heads, C.dim, C.dtype, C.page_stride, C.token_stride, C.head_stride}; }
+
+}  // namespace
+
+extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
+{
+    return check_cache(C) == RB_OK ? paged_workspace_bytes(*C, heads, n_seqs, tokens) : 0;
+}
+
+extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
+                             const int32_t *table, int width, int n_seqs, int tokens, float scale, void *o, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_cache(C);
+    if (rc != RB_OK) return rc;
+    return paged(*C, 2, nullptr, nullptr, q, q_token, q_head, heads, first, lengths, table, width, n_seqs, tokens, scale, o, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t rb_attn_cache8_workspace_bytes(const rb_cache8 *C, int heads, int n_seqs, int tokens)
+{
+    return check_cache8(C) == RB_OK ? paged_workspace_bytes(as16(*C), heads, n_seqs, tokens) : 0;
+}
+
+extern "C" int rb_attn_cache8(const rb_cache8 *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
+                              const int32_t *table, int width, int n_seqs, int tokens, float scale, void *o, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_cache8(C);
+    if (rc != RB_OK) return rc;
+    return paged(as16(*C), 1, C->k_exp, C->v_exp, q, q_token, q_head, heads, first, lengths, table, width, n_seqs, tokens, scale, o, workspace, workspace_bytes, stream);
 }

@@ -13,6 +13,7 @@
 
 #include "rabit.h"
 #include "rb_attn.h"
+#include "rb_attn8.h"
 #include "rb_attn_host.h"
 #include "rb_attn_shares.h"
 
@@ -29,11 +30,12 @@ template <int D> __device__ __forceinline__ PartOfRows<D, ROWS> part_of(Address 
     return PartOfRows<D, ROWS>(workspace, ((size_t)kvh * wavefronts + w) * 2 + which);
 }
 
-template <class T, int D>
+template <class T, int D, bool IN8>
 __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
 {
     using L = Tile<D>;
-    __shared__ __attribute__((aligned(16))) uint8_t keys_a[WAVES * L::bytes(KEYS)], values_a[WAVES * L::bytes(KEYS)], keys_b[WAVES * L::bytes(KEYS)], values_b[WAVES * L::bytes(KEYS)];
+    constexpr int SECOND = IN8 ? 16 : WAVES * L::bytes(KEYS);
+    __shared__ __attribute__((aligned(16))) uint8_t keys_a[WAVES * L::bytes(KEYS)], values_a[WAVES * L::bytes(KEYS)], keys_b[SECOND], values_b[SECOND];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kvh = blockIdx.x % A.kv_heads, wavefronts = (int)(gridDim.x / A.kv_heads) * WAVES, w = (int)(blockIdx.x / A.kv_heads) * WAVES + wave;
@@ -66,6 +68,18 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) pages[i] = row[min((c.t * KEYS + i * 8) >> A.page_shift, A.width - 1)];
+        }
+    };
+    const uint32_t at8 = Rows8<D, KEYS>::at(A.k.token, A.dim, lane);
+    auto exponents_at = [&](Address exponents, int page, int r) RB_INLINE {
+        return global_at<const uint8_t>(exponents) + (((long long)min(max(page, 0), A.pages - 1) * A.kv_heads + kvh) << A.page_shift) + (r & ((1 << A.page_shift) - 1));
+    };
+    [[maybe_unused]] auto load8 = [&](int i, const uint8_t *base, Address exponents, Rows8<D, KEYS> &to) RB_INLINE {
+        const int r = ahead.t * KEYS, len = i < n ? ahead.n_k - r : 0;
+#pragma unroll
+        for (int j = 0; j < KEYS / 8; ++j) {
+            const int page = pages[A.page_shift >= 5 ? 0 : j];
+            to.load(j, base + place(page, r + j * 8), exponents_at(exponents, page, r + j * 8), A.k.token, len - j * 8, A.dim, at8, lane);
         }
     };
     // tile number i of the share, which `ahead` stands at; past the share's end loads count, but fetch nothing
@@ -122,7 +136,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         if (found)
             for (int r = max(max(least + 1, 0) / KEYS, from_t) * KEYS; r < min((at.t + 1) * KEYS, at.n_k); ++r) {
                 const int page = table_u[(long long)at.s * A.width + (r >> A.page_shift)];
-                add_not_finite<T, D>(sums, v_base + place(page, r), A.dim, h, r <= limit);
+                if constexpr (IN8)
+                    add_not_finite8<T, D>(sums, v_base + place(page, r), *exponents_at(A.v_exp, page, r), A.dim, h, r <= limit);
+                else
+                    add_not_finite<T, D>(sums, v_base + place(page, r), A.dim, h, r <= limit);
             }
         total = over_halves_sum(total);
         if (from_t == 0 && at.t == at.shape.tiles - 1) {
@@ -134,15 +151,21 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         first_job = false;
     };
 
-    auto step = [&](int i, uint8_t *keys, uint8_t *values) RB_INLINE {
+    Rows8<D, KEYS> raw_ka, raw_va, raw_kb, raw_vb;
+    auto step = [&](int i, uint8_t *keys, uint8_t *values, [[maybe_unused]] Rows8<D, KEYS> &raw_k, [[maybe_unused]] Rows8<D, KEYS> &raw_v) RB_INLINE {
         if (i > 0 && at.t == 0) {
             start();
             rows_arrived();
         }
-        loads_arrived<3 * LOADS>();
+        if constexpr (IN8) {
+            raw_k.template write<T>(keys, 0, lane);
+            load8(i + 2, k_base, A.k_exp, raw_k);
+        } else {
+            loads_arrived<3 * LOADS>();
+        }
         v16f x = {};
         stream_operands<D / 16, 4>([&](int k) RB_INLINE { return rows.read(keys, 0, k); }, [&](int k, v4u a) RB_INLINE { x = T::mfma(a, q[k], x); });
-        load(i + 2, k_base, keys);
+        if constexpr (!IN8) load(i + 2, k_base, keys);
         const int first_key = at.t * KEYS;
         if (first_key + KEYS - 1 > least) {
             const int seen = limit - first_key - 4 * h;
@@ -173,7 +196,12 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
             rest[e / 2] = T::pack(a - T::widen(wt[e / 2] & 0xffffu), z - T::widen(wt[e / 2] >> 16));
         }
         const v4u p[2] = {{wt[0], wt[1], wt[2], wt[3]}, {wt[4], wt[5], wt[6], wt[7]}}, p_rest[2] = {{rest[0], rest[1], rest[2], rest[3]}, {rest[4], rest[5], rest[6], rest[7]}};
-        loads_arrived<3 * LOADS>();
+        if constexpr (IN8) {
+            raw_v.template write<T>(values, 0, lane);
+            load8(i + 2, v_base, A.v_exp, raw_v);
+        } else {
+            loads_arrived<3 * LOADS>();
+        }
         if (least < min(first_key + KEYS, at.n_k) - 1) {      // some row does not see all of the tile's keys: see make_finite
             bool any = false;
 #pragma unroll
@@ -191,25 +219,35 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
             sums[k % B] = T::mfma(a, p[k / B], sums[k % B]);
             sums[k % B] = T::mfma(a, p_rest[k / B], sums[k % B]);
         });
-        load(i + 2, v_base, values);
+        if constexpr (!IN8) load(i + 2, v_base, values);
         next_ahead();
         if (i == n - 1 || at.t == at.shape.tiles - 1) finish();
         at.advance(A, entries);
     };
 
-    uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS), *const kb = keys_b + wave * L::bytes(KEYS), *const vb = values_b + wave * L::bytes(KEYS);
+    uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS);
+    uint8_t *const kb = IN8 ? ka : keys_b + wave * L::bytes(KEYS), *const vb = IN8 ? va : values_b + wave * L::bytes(KEYS);
     ask_pages(ahead);
     start();
-    load(0, k_base, ka);
-    load(0, v_base, va);
-    next_ahead();
-    load(1, k_base, kb);
-    load(1, v_base, vb);
-    next_ahead();
+    if constexpr (IN8) {
+        load8(0, k_base, A.k_exp, raw_ka);
+        load8(0, v_base, A.v_exp, raw_va);
+        next_ahead();
+        load8(1, k_base, A.k_exp, raw_kb);
+        load8(1, v_base, A.v_exp, raw_vb);
+        next_ahead();
+    } else {
+        load(0, k_base, ka);
+        load(0, v_base, va);
+        next_ahead();
+        load(1, k_base, kb);
+        load(1, v_base, vb);
+        next_ahead();
+    }
     rows_arrived();
     for (int i = 0; i < n && at.there(A); i += 2) {      // (past the last sequence only where the arrays are not in order)
-        step(i, ka, va);
-        if (i + 1 < n && at.there(A)) step(i + 1, kb, vb);
+        step(i, ka, va, raw_ka, raw_va);
+        if (i + 1 < n && at.there(A)) step(i + 1, kb, vb, raw_kb, raw_vb);
     }
     loads_arrived();
 }
@@ -249,7 +287,11 @@ template <class T, int D> int launch(const Args &A, int compute_units, hipStream
     const int groups = groups_per_head(A, compute_units);
     const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, ROWS) * A.kv_heads;
     if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
-    hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES), 0, stream, A);
+    const dim3 grid((unsigned)(groups * A.kv_heads)), threads(64 * WAVES);
+    if (A.k_exp)
+        hipLaunchKernelGGL((few_kernel<T, D, true>), grid, threads, 0, stream, A);
+    else
+        hipLaunchKernelGGL((few_kernel<T, D, false>), grid, threads, 0, stream, A);
     const int rows = (int)std::min((long long)ROWS, (long long)A.tokens_q * A.group), joined = rows_joined(jobs, rows);      // rows of one job, at most
     hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs, (rows + joined - 1) / joined), dim3(256), 0, stream, A, groups * WAVES, joined);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;

@@ -30,6 +30,18 @@ inline int check_cache(const rb_cache *C)
     return RB_OK;
 }
 
+inline int check_cache8(const rb_cache8 *C)
+{
+    if (!C || !C->k || !C->v || !C->k_exp || !C->v_exp) return RB_ERR_NULL;
+    const rb_cache pages = {C->k, C->v, C->pages, C->page_tokens, C->kv_heads, C->dim, C->dtype, C->page_stride, C->token_stride, C->head_stride};
+    const int rc = check_cache(&pages);
+    if (rc != RB_OK) return rc;
+    if (C->token_stride < C->dim) return RB_ERR_SHAPE;      // (rows past a sequence's end are told by where they lie)
+    if (C->dim % 16 != 0) return RB_ERR_UNSUPPORTED;
+    if ((C->page_stride | C->token_stride | C->head_stride) % 16 != 0 || ((uintptr_t)C->k_exp | (uintptr_t)C->v_exp) & 7) return RB_ERR_ALIGN;
+    return RB_OK;
+}
+
 // Rows that a workgroup joins the parts of, where `jobs` have up to `rows` of them: two where that is few workgroups, else eight, since many of the workgroups find
 // no work (130 decoding sequences of 8 heads 61 us with two everywhere and 41 so, 512 new tokens 31 and 23; one sequence of 32 heads 0.5 us less with two).
 inline int rows_joined(long long jobs, long long rows) { return jobs * rows <= 2048 ? 2 : 8; }

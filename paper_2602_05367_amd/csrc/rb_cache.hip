@@ -16,11 +16,6 @@ struct AppendArgs {
     int n_seqs, tokens, heads, kv_heads, dim, rotary, table_rows, pages, page_shift, width, blocks;
 };
 
-union Four {
-    v2u w;
-    uint16_t h[4];
-};
-
 // Element pairs (x, y) of a head become (x cos - y sin, y cos + x sin), products and sum in fp32 and rounded once.  Eight elements per thread, so loads and stores are
 // of eight bytes or sixteen: four of either half of a head, or eight in a row where pairs are neighbours or nothing is turned.  A workgroup has elements of one token and finds its sequence itself.
 // Bound: bytes (sixteen prompts of 6000 tokens in all, 64 and 8 heads of 128, bf16: 42 us, 5.8 TB/s); one token: latencies, 3 us.  The elements are
@@ -42,15 +37,8 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs A)
         b.w = *(const v2u *)(from + at_y);
     }
     const int *first = global_at<const int>(A.first), *lengths = global_at<const int>(A.lengths);
-    int s, end, length;      // the token's sequence, where it ends, its positions
-    if (A.n_seqs < 64) {
-        const int starts = first[min(lane, A.n_seqs)], all = lengths[min(lane, A.n_seqs - 1)];
-        s = max(lanes_of(__ballot(lane < A.n_seqs && starts <= token)) - 1, 0);
-        end = __builtin_amdgcn_readlane(starts, s + 1), length = __builtin_amdgcn_readlane(all, s);
-    } else {
-        s = last_not_beyond(A.n_seqs, token, lane, [&](int i) { return first[i]; });
-        end = first[s + 1], length = lengths[s];
-    }
+    int s, end, length;
+    sequence_of_token(first, lengths, A.n_seqs, token, lane, s, end, length);
     const long long position = (long long)length - end + token;
     const bool inside = position >= 0 && position < (long long)A.width << A.page_shift;
     if (!there || token >= end) return;      // behind the last sequence's end (padding): nobody's

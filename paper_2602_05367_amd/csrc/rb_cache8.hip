@@ -1,0 +1,191 @@
+// Tokens enter a paged cache in 8 bits, their rotary embedding on the way, and come back out of it: bytes in, bytes out.
+#include <hip/hip_runtime.h>
+
+#include "rabit.h"
+#include "rb_attn.h"
+#include "rb_attn8.h"
+#include "rb_attn_host.h"
+
+namespace rb {
+namespace attn {
+namespace {
+
+struct Cache8Args {
+    Address k, v, k_exp, v_exp, first, lengths, table;
+    long long page, token_stride, head_stride;      // of k and v, in bytes
+    int n_seqs, tokens, kv_heads, dim, pages, page_shift, width;
+};
+Cache8Args cache8_args(const rb_cache8 *C, const int32_t *first, const int32_t *lengths, const int32_t *table, int width, int n_seqs, int tokens)
+{
+    return {rb::address_of(C->k), rb::address_of(C->v), rb::address_of(C->k_exp), rb::address_of(C->v_exp), rb::address_of(first), rb::address_of(lengths), rb::address_of(table),
+            C->page_stride, C->token_stride, C->head_stride, n_seqs, tokens, C->kv_heads, C->dim, C->pages, __builtin_ctz((unsigned)C->page_tokens), width};
+}
+struct Append8Args {
+    Cache8Args c;
+    Side q, k_from, v_from;
+    Address q_to, cos, sin;
+    int heads, rotary, table_rows, blocks, lanes_shift;      // lanes of a head: the power of two that holds its pieces
+};
+
+// Where a position lies in the cache, behind the first head's elements and exponents; false: nowhere
+__device__ __forceinline__ bool place_of(const Cache8Args &C, int s, long long position, long long &elements, long long &exponents)
+{
+    if (position < 0 || position >= (long long)C.width << C.page_shift) return false;
+    const int p = (int)position, page = global_at<const int>(C.table)[(long long)s * C.width + (p >> C.page_shift)], row = p & ((1 << C.page_shift) - 1);
+    if (page < 0 || page >= C.pages) return false;
+    elements = page * C.page + row * C.token_stride;
+    exponents = (((long long)page * C.kv_heads) << C.page_shift) + row;
+    return true;
+}
+
+// Element pairs are turned as in append_kernel (rb_cache.hip), eight elements per thread: four of either half of a head, or eight in a row.  Keys and values are then held in
+// units of a power of two of the head's own, so x / unit is exact and the one rounding is that to e4m3: the largest |x| of the head is found
+// among its lanes, a power of two of them.  A workgroup has elements of one token and finds its sequence itself.
+template <class T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
+{
+    const Cache8Args &C = A.c;
+    const int token = blockIdx.x / A.blocks, part = blockIdx.x % A.blocks, lane = threadIdx.x & 63;
+    const int unit = part * 256 + threadIdx.x, head = unit >> A.lanes_shift, piece = unit & ((1 << A.lanes_shift) - 1);
+    const bool there = head < A.heads + 2 * C.kv_heads && piece * 8 < C.dim;
+    const bool is_q = head < A.heads, is_v = head >= A.heads + C.kv_heads, turned = !is_v && piece * 8 < A.rotary;
+    const int kvh = is_q ? head : head - A.heads - (is_v ? C.kv_heads : 0);
+    const int at_x = piece * (INTERLEAVED || !turned ? 8 : 4), at_y = INTERLEAVED || !turned ? at_x + 4 : at_x + A.rotary / 2;      // elements
+    Four a = {}, b = {};
+    if (there) {      // on the way while the place is looked up
+        const Side &from_side = is_q ? A.q : is_v ? A.v_from : A.k_from;
+        const uint8_t *from = global_at<const uint8_t>(from_side.at) + token * from_side.token + kvh * from_side.head;
+        a.w = *(const v2u *)(from + at_x * 2);
+        b.w = *(const v2u *)(from + at_y * 2);
+    }
+    int s, end, length;
+    sequence_of_token(global_at<const int>(C.first), global_at<const int>(C.lengths), C.n_seqs, token, lane, s, end, length);
+    const long long position = (long long)length - end + token;
+    float x[4], y[4];      // the elements from at_x and at_y on
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = T::widen(a.h[i]), y[i] = T::widen(b.h[i]);
+    if (turned && there) {
+        const long long row = min(max(position, 0ll), (long long)A.table_rows - 1) * (A.rotary / 2) + piece * 4;
+        const v4f c = *(const v4f *)(global_at<const float>(A.cos) + row), sn = *(const v4f *)(global_at<const float>(A.sin) + row);
+        auto turn = [&](float &u, float &w, int i) RB_INLINE {
+            const float t = u * c[i] - w * sn[i];
+            w = w * c[i] + u * sn[i];
+            u = t;
+        };
+        if constexpr (INTERLEAVED) {
+            turn(x[0], x[1], 0), turn(x[2], x[3], 1), turn(y[0], y[1], 2), turn(y[2], y[3], 3);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) turn(x[i], y[i], i);
+        }
+    }
+    // the head's exponent, in every lane of it
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bounded8<T>(x[i]), bounded8<T>(y[i])));
+    for (int d = 1; d < 1 << A.lanes_shift; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if (!there || token >= end) return;      // behind the last sequence's end (padding): nobody's
+    if (is_q) {
+        uint8_t *to = global_at<uint8_t>(A.q_to) + ((long long)token * A.heads + head) * (C.dim * 2);
+        *(v2u *)(to + at_x * 2) = turned ? (v2u){T::pack(x[0], x[1]), T::pack(x[2], x[3])} : a.w;
+        *(v2u *)(to + at_y * 2) = turned ? (v2u){T::pack(y[0], y[1]), T::pack(y[2], y[3])} : b.w;
+        return;
+    }
+    long long elements, exponents;
+    if (!place_of(C, s, position, elements, exponents)) return;      // (another's page is not written over)
+    const int exponent = exponent8(most);
+    uint8_t *to = global_at<uint8_t>(is_v ? C.v : C.k) + elements + kvh * C.head_stride;
+    *(uint32_t *)(to + at_x) = narrow8<T>(x, exponent);
+    *(uint32_t *)(to + at_y) = narrow8<T>(y, exponent);
+    if (piece == 0) global_at<uint8_t>(is_v ? C.v_exp : C.k_exp)[exponents + ((long long)kvh << C.page_shift)] = (uint8_t)exponent;
+}
+
+// Sixteen elements per thread: one load, two stores.  A workgroup has `group` tokens, each of its wavefronts elements of one.
+template <class T>
+__global__ __launch_bounds__(256) void read8_kernel(const Cache8Args C, Address k_to, Address v_to, int waves)      // wavefronts of a token
+{
+    const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), token = wave / waves;
+    if (token >= C.tokens) return;
+    const int pieces = C.dim / 16, unit = wave % waves * 64 + lane, head = unit / pieces, piece = unit % pieces;
+    int s, end, length;
+    sequence_of_token(global_at<const int>(C.first), global_at<const int>(C.lengths), C.n_seqs, token, lane, s, end, length);
+    if (token >= end || head >= 2 * C.kv_heads) return;
+    const bool is_v = head >= C.kv_heads;
+    const int kvh = is_v ? head - C.kv_heads : head;
+    long long elements, exponents;
+    v4u lo = {}, hi = {};
+    if (place_of(C, s, (long long)length - end + token, elements, exponents)) {
+        const v4u w = *(const v4u *)(global_at<const uint8_t>(is_v ? C.v : C.k) + elements + kvh * C.head_stride + piece * 16);
+        const uint32_t exponent = global_at<const uint8_t>(is_v ? C.v_exp : C.k_exp)[exponents + ((long long)kvh << C.page_shift)];
+        lo = widen8<T>((v2u){w.x, w.y}, unit8(exponent)), hi = widen8<T>((v2u){w.z, w.w}, unit8(exponent));
+    }
+    uint8_t *to = global_at<uint8_t>(is_v ? v_to : k_to) + (((long long)token * C.kv_heads + kvh) * C.dim + piece * 16) * 2;
+    *(v4u *)to = lo;
+    *(v4u *)(to + 16) = hi;
+}
+
+}  // namespace
+}  // namespace attn
+}  // namespace rb
+
+using namespace rb::attn;
+
+extern "C" int rb_cache8_append(const rb_cache8 *C, const rb_heads *H, const void *q, const void *k, const void *v, const float *cos, const float *sin, int table_rows,
+                                int rotary, int interleaved, const int32_t *first, const int32_t *lengths, const int32_t *table, int width, int n_seqs, int tokens,
+                                void *q_out, void *stream)
+{
+    int rc = check_cache8(C);
+    if (rc != RB_OK) return rc;
+    rc = check_heads(H);
+    if (rc != RB_OK) return rc;
+    if (!k || !v || !first || !lengths || !table || !q != !q_out || !cos != !sin) return RB_ERR_NULL;
+    if (H->kv_heads != C->kv_heads || H->dim != C->dim || H->dtype != C->dtype) return RB_ERR_SHAPE;
+    if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens < 1 || tokens > MAX_TOKENS || width < 1) return RB_ERR_SHAPE;
+    if (cos && (table_rows < 1 || rotary < 8 || rotary % 8 != 0 || rotary > C->dim)) return RB_ERR_SHAPE;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out | (uintptr_t)cos | (uintptr_t)sin) & 15) return RB_ERR_ALIGN;
+    if (((uintptr_t)first | (uintptr_t)lengths | (uintptr_t)table) & 3) return RB_ERR_ALIGN;
+    Append8Args A = {};
+    A.c = cache8_args(C, first, lengths, table, width, n_seqs, tokens);
+    A.q = side(q, H->q_token, H->q_head), A.k_from = side(k, H->k_token, H->k_head), A.v_from = side(v, H->v_token, H->v_head);
+    A.q_to = rb::address_of(q_out), A.cos = rb::address_of(cos), A.sin = rb::address_of(sin);
+    A.heads = q ? H->heads : 0, A.rotary = cos ? rotary : 0, A.table_rows = table_rows;
+    while (8 << A.lanes_shift < C->dim) ++A.lanes_shift;
+    A.blocks = (int)((((long long)(A.heads + 2 * C->kv_heads) << A.lanes_shift) + 255) / 256);
+    const long long n = (long long)tokens * A.blocks;
+    if (n > 0x7fffffffll) return RB_ERR_SHAPE;
+    const dim3 grid((unsigned)n), threads(256);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (H->dtype == RB_F16) {
+        if (interleaved)
+            hipLaunchKernelGGL((append8_kernel<F16, true>), grid, threads, 0, st, A);
+        else
+            hipLaunchKernelGGL((append8_kernel<F16, false>), grid, threads, 0, st, A);
+    } else {
+        if (interleaved)
+            hipLaunchKernelGGL((append8_kernel<BF16, true>), grid, threads, 0, st, A);
+        else
+            hipLaunchKernelGGL((append8_kernel<BF16, false>), grid, threads, 0, st, A);
+    }
+    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
+
+extern "C" int rb_cache8_read(const rb_cache8 *C, const int32_t *first, const int32_t *lengths, const int32_t *table, int width, int n_seqs, int tokens, void *k, void *v,
+                              void *stream)
+{
+    const int rc = check_cache8(C);
+    if (rc != RB_OK) return rc;
+    if (!first || !lengths || !table || !k || !v) return RB_ERR_NULL;
+    if (n_seqs < 1 || n_seqs > MAX_SEQS || tokens < 1 || tokens > MAX_TOKENS || width < 1) return RB_ERR_SHAPE;
+    if (((uintptr_t)k | (uintptr_t)v) & 15) return RB_ERR_ALIGN;
+    if (((uintptr_t)first | (uintptr_t)lengths | (uintptr_t)table) & 3) return RB_ERR_ALIGN;
+    const Cache8Args A = cache8_args(C, first, lengths, table, width, n_seqs, tokens);
+    const int waves = (int)(((long long)2 * C->kv_heads * (C->dim / 16) + 63) / 64);
+    const long long n = ((long long)tokens * waves + 3) / 4;
+    if (n > 0x1fffffffll) return RB_ERR_SHAPE;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (C->dtype == RB_F16)
+        hipLaunchKernelGGL((read8_kernel<F16>), dim3((unsigned)n), dim3(256), 0, st, A, rb::address_of(k), rb::address_of(v), waves);
+    else
+        hipLaunchKernelGGL((read8_kernel<BF16>), dim3((unsigned)n), dim3(256), 0, st, A, rb::address_of(k), rb::address_of(v), waves);
+    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
