@@ -34,7 +34,7 @@ EXPORTS = [
     "rb_block_prepare", "rb_block_workspace_bytes", "rb_rmsnorm", "rb_silu_mul", "rb_add",
     "rb_derive_iterative", "rb_derive_workspace_bytes",
     "rb_attn_prompt", "rb_attn_prompt_grad", "rb_attn_grad_workspace_bytes", "rb_attn_paged", "rb_attn_paged_workspace_bytes", "rb_cache_append",
-    "rb_cache8_append", "rb_cache8_read", "rb_attn_cache8", "rb_attn_cache8_workspace_bytes", "rb_sample",
+    "rb_cache8_append", "rb_cache8_read", "rb_attn_cache8", "rb_attn_cache8_workspace_bytes", "rb_sample", "rb_sample_workspace_bytes",
     "rb_dense_gemv_f16", "rb_stream_read", "rb_stream_read_groups", "rb_version", "rb_last_path",
 ]
 
@@ -133,7 +133,9 @@ def _load() -> ctypes.CDLL:
     lib.rb_attn_cache8_workspace_bytes.argtypes = [ctypes.POINTER(rb_cache8), i, i, i]
     lib.rb_attn_cache8_workspace_bytes.restype = z
     lib.rb_attn_cache8.argtypes = [ctypes.POINTER(rb_cache8), *lib.rb_attn_paged.argtypes[1:]]
-    lib.rb_sample.argtypes = [p, i, l, i, i, p, p, p, p, p, p, p]
+    lib.rb_sample.argtypes = [p, i, l, i, i, p, p, p, p, p, p, p, z, p]
+    lib.rb_sample_workspace_bytes.argtypes = [i, i, i]
+    lib.rb_sample_workspace_bytes.restype = z
     lib.rb_dense_gemv_f16.argtypes = [p, p, p, i, i, p]
     lib.rb_stream_read.argtypes = [p, z, p, p]
     lib.rb_stream_read_groups.argtypes = []
@@ -142,7 +144,7 @@ def _load() -> ctypes.CDLL:
     for name in EXPORTS:
         if name not in ("rb_native_bytes", "rb_workspace_bytes", "rb_noalloc_scratch_bytes",
                         "rb_scale_grads_workspace_bytes", "rb_block_workspace_bytes", "rb_derive_workspace_bytes",
-                        "rb_attn_paged_workspace_bytes", "rb_attn_grad_workspace_bytes", "rb_attn_cache8_workspace_bytes"):
+                        "rb_attn_paged_workspace_bytes", "rb_attn_grad_workspace_bytes", "rb_attn_cache8_workspace_bytes", "rb_sample_workspace_bytes"):
             getattr(lib, name).restype = i
     return lib
 
@@ -735,7 +737,7 @@ def _over_cache(name, entry, workspace_bytes, cache, q, first, lengths, table, s
 
 # -------------------------------------------------------------- sampling ---
 def rb_sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor = None, top_k: torch.Tensor = None, top_p: torch.Tensor = None,
-              min_p: torch.Tensor = None, tokens: torch.Tensor = None) -> torch.Tensor:
+              min_p: torch.Tensor = None, tokens: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """The next token int32 [rows] of logits [rows][vocab] (fp16, bf16 or fp32, any stride of rows), drawn with u fp32 [rows] in [0, 1); temperature, top_p and
     min_p fp32 [rows], top_k int32 [rows], None: not filtered.  -1: the row has no logit above minus infinity."""
     rows, vocab = logits.shape
@@ -747,7 +749,14 @@ def rb_sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor =
     for x, dtype in ((u, torch.float32), (temperature, torch.float32), (top_k, _I32), (top_p, torch.float32), (min_p, torch.float32), (tokens, _I32)):
         assert x is None or (x.is_cuda and x.dtype is dtype and x.shape == (rows,) and x.is_contiguous())
         at.append(None if x is None else x.data_ptr())
-    _check("rb_sample", lib.rb_sample(logits.data_ptr(), _DTYPE_CODE[logits.dtype], stride if rows > 1 else vocab, rows, vocab, *at, _stream()))
+    dtype = _DTYPE_CODE[logits.dtype]
+    if workspace is None:
+        need = lib.rb_sample_workspace_bytes(dtype, rows, vocab)
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+    else:
+        assert workspace.is_cuda and workspace.is_contiguous()
+    at_ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check("rb_sample", lib.rb_sample(logits.data_ptr(), dtype, stride if rows > 1 else vocab, rows, vocab, *at, at_ws, size, _stream()))
     return tokens
 
 

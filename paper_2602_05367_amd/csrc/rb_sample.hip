@@ -1,40 +1,55 @@
 // The next token from logits, with temperature, top-k, top-p and min-p, drawn with a given random number.
 //
-// With w_j = exp((x_j - max) / T): what is left after the filters is a prefix of the tokens in descending order, all above some border t and the first `ties` of those equal to it.  A
-// histogram of the logits below the maximum, counts and weights, says in which of its bins a border lies, what is above it, and the bin's few logits are then ranked
-// among themselves: nothing is sorted.  The token is found in the order of the indexes: sums per piece of the row, then within the one that u falls into.
+// With w_j = exp((x_j - max) / T): what the filters leave is a prefix of the tokens in descending order, equal ones by their index.  Nothing is sorted.  A
+// histogram over -log2 w, counts and weights, says in which of its bins the last token of that prefix lies; what lies in earlier bins is left for sure, and the few tokens of that
+// bin are candidates, which are ranked among themselves.  The token is then found in the order of the indexes: sums over pieces of the row, and within the piece that u falls into.
 //
-// Weights are whole numbers of units of 2^-38, in 64 bits: their sums depend on no order, so histograms may be summed by atomics.
+// Weights are whole numbers of units of 2^-30, their sums are of 64 bits: they depend on no order, so histograms may be summed by atomics.
 #include <hip/hip_runtime.h>
+#include <algorithm>
+#include <type_traits>
 
 #include "rabit.h"
 #include "rb_device.h"
+#include "rb_internal.h"
 
 namespace rb {
 namespace sample {
 namespace {
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2 * THREADS, PIECES = 64, LISTED = THREADS;
-constexpr float RANGE = 39.f;      // -log2 of the weights that round to nothing
+constexpr int THREADS = 1024, WAVES = THREADS / 64, PER_THREAD = 2, BINS = PER_THREAD * THREADS, BIN_BITS = 11, PIECES = 64, LISTED = 2 * THREADS;
+static_assert(BINS == 1 << BIN_BITS);
+constexpr float RANGE = 31.f;      // -log2 of the weights that round to nothing
 typedef unsigned long long Weight;
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-struct Args {
-    Address logits, u, temperature, top_k, top_p, min_p, tokens;
-    long long stride;      // in bytes
-    int rows, vocab;
-};
-
+// word j of a tile's, j differing among lanes
+__device__ __forceinline__ uint32_t word(v4u w, int j)
+{
+    const uint32_t lo = j & 1 ? w[1] : w[0], hi = j & 1 ? w[3] : w[2];
+    return j & 2 ? hi : lo;
+}
 struct F16 {
     static constexpr int N = 8, SIZE = 2;      // elements of 16 bytes
-    static __device__ __forceinline__ float at(const uint32_t *w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i / 2] >> i % 2 * 16)); }
+    static __device__ __forceinline__ float at(v4u w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i / 2] >> i % 2 * 16)); }
+    static __device__ __forceinline__ float any(v4u w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(word(w, i / 2) >> i % 2 * 16)); }
+    static constexpr uint32_t NONE = 0x7e007e00u;      // NaN
+    // 0 for plus infinity, NaN for all else
+    static __device__ __forceinline__ uint32_t infinite(uint32_t w) { return ((w & 0xffffu) == 0x7c00u ? 0u : 0x7e00u) | (w >> 16 == 0x7c00u ? 0u : 0x7e000000u); }
 };
 struct BF16 {
     static constexpr int N = 8, SIZE = 2;
-    static __device__ __forceinline__ float at(const uint32_t *w, int i) { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+    static __device__ __forceinline__ float at(v4u w, int i) { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+    static __device__ __forceinline__ float any(v4u w, int i) { return __uint_as_float(word(w, i / 2) >> i % 2 * 16 << 16); }
+    static constexpr uint32_t NONE = 0x7fc07fc0u;
+    static __device__ __forceinline__ uint32_t infinite(uint32_t w) { return ((w & 0xffffu) == 0x7f80u ? 0u : 0x7fc0u) | (w >> 16 == 0x7f80u ? 0u : 0x7fc00000u); }
 };
 struct F32 {
     static constexpr int N = 4, SIZE = 4;
-    static __device__ __forceinline__ float at(const uint32_t *w, int i) { return __uint_as_float(w[i]); }
+    static __device__ __forceinline__ float at(v4u w, int i) { return __uint_as_float(w[i]); }
+    static __device__ __forceinline__ float any(v4u w, int i) { return __uint_as_float(word(w, i)); }
+    static constexpr uint32_t NONE = 0x7fc00000u;
+    static __device__ __forceinline__ uint32_t infinite(uint32_t w) { return w == 0x7f800000u ? 0u : NONE; }
 };
 
 __device__ __forceinline__ float not_below(double x)
@@ -42,339 +57,911 @@ __device__ __forceinline__ float not_below(double x)
     const float f = (float)x;
     return f < x ? nextafterf(f, __builtin_inff()) : f;
 }
-// Floats in their order as whole numbers (0 and -0 have to be the same already)
-__device__ __forceinline__ uint32_t ordered(float x)
+// A token's place in the descending order as one number: larger comes first (0 and -0 are the same)
+typedef unsigned long long Place;
+constexpr int INDEX_BITS = 22, PLACE_BITS = 32 + INDEX_BITS, MAX_VOCAB = 1 << INDEX_BITS;
+__device__ __forceinline__ Place place(float x, int index)
 {
-    const uint32_t b = __float_as_uint(x);
-    return b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return (Place)(b ^ ((uint32_t)((int)b >> 31) | 0x80000000u)) << INDEX_BITS | (MAX_VOCAB - 1 - index);
 }
-__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o ^ (o & 0x80000000u ? 0x80000000u : 0xffffffffu)); }
+__device__ __forceinline__ int index_of(Place p) { return MAX_VOCAB - 1 - (int)(p & (MAX_VOCAB - 1)); }
 
 // What a row's weights come from.  (x - max) / T is taken from halves, which do not overflow, and times log2(e) / T in two parts: rounded once.
 struct Scale {
-    float half_max, most, hi, lo;
-    // -log2 of x's weight; a larger x never has a larger one
+    float half_max, hi, lo;
+    // -log2 of x's weight; a larger x never has a larger one.  (NaN stays NaN: none)
     __device__ __forceinline__ float below(float x) const
     {
-        const float d = x == most ? 0.f : __builtin_fmaf(x, -0.5f, half_max);
+        const float d = __builtin_fmaf(x, -0.5f, half_max);
         return __builtin_fmaf(d, hi, d * lo);
     }
-    static __device__ __forceinline__ Weight weight(float below)
+    // in units of 2^-30, to the nearest: nothing beyond RANGE, for infinity and NaN
+    static __device__ __forceinline__ uint32_t weight(float below)
     {
-        // 2^14 + w in 64 bits: its last bits are those of w in units of 2^-38
-        constexpr double ONE = 16384.0;
-        return below < RANGE ? __builtin_bit_cast(Weight, (double)__builtin_amdgcn_exp2f(-below) + ONE) - __builtin_bit_cast(Weight, ONE) : 0;
+        int units;
+        const float w = __builtin_amdgcn_exp2f(-below) * 0x1p+30f;
+        asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(units) : "v"(w));
+        return (uint32_t)units;
     }
-    __device__ __forceinline__ Weight of(float x) const { return weight(below(x)); }
 };
 
-__device__ __forceinline__ Weight shuffle_up(Weight v, int d)
+// Sums over the lanes up to each, by data-parallel moves
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ Weight moved(Weight v) { return (Weight)moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v); }
+template <class V> __device__ __forceinline__ V up_to_lane(V v)
 {
-    return (Weight)__shfl_up((uint32_t)(v >> 32), d) << 32 | __shfl_up((uint32_t)v, d);
-}
-template <class V> __device__ __forceinline__ V up_to_lane(V v, int lane)
-{
-    for (int d = 1; d < 64; d <<= 1) {
-        V u;
-        if constexpr (sizeof(V) == 8)
-            u = shuffle_up(v, d);
-        else
-            u = __shfl_up(v, d);
-        if (lane >= d) v += u;
-    }
+    v += moved<0x111, 0xf>(v);      // one, two, four and eight lanes on within sixteen, then the last of the sixteen before, then of the 32
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
     return v;
 }
-__device__ __forceinline__ Weight of_lane(Weight v, int lane)
-{
-    return (Weight)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
-}
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ Weight of_lane(Weight v, int lane) { return (Weight)of_lane((uint32_t)(v >> 32), lane) << 32 | of_lane((uint32_t)v, lane); }
 
-// One border: `target` counts (top-k) or weight (top-p) are reached among the logits equal to x; more of them and of weight lie above
-struct Border {
+struct Candidate {
+    Place place;
+    Weight weight;      // with what it is a candidate for
+};
+struct Found {      // as it is met
     float x;
-    int above, equal;
-    Weight weight_above;
+    int index;
+};
+constexpr Weight FOR_COUNT = 1ull << 62, FOR_WEIGHT = 1ull << 63, ONLY_WEIGHT = FOR_COUNT - 1;
+// What several threads find out for all: each use has a place of its own, so one barrier is enough
+enum Use { BOUND, BORDER, SECOND, FIRST, USES };
+struct Reached {
+    int bin;
+    uint32_t count;      // before the bin, and
+    Weight before, here; // weight before it and in it
+};
+struct Shared {
+    Weight weights[BINS];
+    uint32_t counts[BINS];
+    Weight pieces[PIECES];
+    Found found[LISTED];
+    Candidate listed[LISTED];
+    Weight wave_weights[USES][WAVES];
+    uint32_t wave_counts[USES][WAVES];
+    float wave_max[WAVES];
+    Reached reached[USES];
+    uint32_t n_listed;
+    Place found_place[2];
+    Weight found_weight[2];
+    int differ[2];
+    // (before a list is used)
+    __device__ __forceinline__ void begin_list(uint32_t n)
+    {
+        n_listed = n;
+        for (int i = 0; i < 2; ++i) found_place[i] = 0, found_weight[i] = 0, differ[i] = 0;
+    }
 };
 
-// A workgroup does a row.  Its wavefronts have consecutive parts of it, and 16 bytes per lane at a time.
-template <class E> __global__ __launch_bounds__(THREADS) void sample_kernel(const Args A)
+// Of a workgroup's threads: sums up to each, and over all (there is a barrier inside)
+template <class V> __device__ __forceinline__ V over_waves(V upto, const V *waves, int lane, int wave, V &all)
 {
-    __shared__ uint32_t counts[BINS];
-    __shared__ Weight weights[BINS];
-    __shared__ uint32_t piece_ties[WAVES * PIECES];
-    __shared__ Weight piece_weights[WAVES * PIECES];
-    __shared__ uint32_t listed[LISTED];
-    __shared__ Weight listed_weights[LISTED];
-    __shared__ uint32_t wave_counts[WAVES], n_listed;
-    __shared__ Weight wave_weights[WAVES];
-    __shared__ float wave_max[WAVES];
-    __shared__ Border found;
-    __shared__ int found_bin;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x;
-    const uint8_t *logits = global_at<const uint8_t>(A.logits) + row * A.stride;
-    constexpr int TILE = 64 * E::N;      // elements of a wavefront's step
-    const int tiles = (A.vocab + TILE - 1) / TILE, each = (tiles + WAVES - 1) / WAVES, from_tile = min(wave * each, tiles), to_tile = min(from_tile + each, tiles);
+    const V sums = up_to_lane(lane < WAVES ? waves[lane] : (V)0);
+    all = of_lane(sums, WAVES - 1);
+    return wave ? upto + of_lane(sums, wave - 1) : upto;
+}
+__device__ __forceinline__ void up_to_thread(Shared &S, Use use, uint32_t &count, Weight &weight, uint32_t &all_counts, Weight &all_weights, int lane, int wave)
+{
+    count = up_to_lane(count), weight = up_to_lane(weight);
+    if (lane == 63) S.wave_counts[use][wave] = count, S.wave_weights[use][wave] = weight;
+    __syncthreads();
+    count = over_waves(count, S.wave_counts[use], lane, wave, all_counts);
+    weight = over_waves(weight, S.wave_weights[use], lane, wave, all_weights);
+}
 
-    // a lane's elements of a tile; NaN past the row's end
-    auto load = [&](int tile, float (&x)[E::N]) {
+// A row is cut into `groups` parts, one for a workgroup where there are several, and each of those into PIECES / groups pieces, of whole tiles
+struct Cut {
+    int groups, tiles, of_group, per_piece;
+    __host__ __device__ Cut(int groups_, int vocab, int tile)
+        : groups(groups_), tiles((vocab + tile - 1) / tile), of_group((tiles + groups - 1) / groups), per_piece((of_group + PIECES / groups - 1) / (PIECES / groups))
+    {
+    }
+    __device__ __forceinline__ int piece_of(int tile) const { return groups == 1 ? tile / per_piece : tile / of_group * (PIECES / groups) + tile % of_group / per_piece; }
+    __device__ __forceinline__ void tiles_of(int piece, int &from, int &to) const
+    {
+        const int group = piece / (PIECES / groups);
+        from = group * of_group + piece % (PIECES / groups) * per_piece;
+        to = min(min(from + per_piece, (group + 1) * of_group), tiles);
+    }
+};
+
+struct Args {
+    Address logits, u, temperature, top_k, top_p, min_p, tokens;
+    Address workspace;
+    long long stride;      // in bytes
+    int rows, vocab, groups;
+};
+constexpr float ALL_BINS = __builtin_inff();
+// What a histogram says: tokens of bins before `sure` are left; for those of low .. high (the border of top-p) and of count_bin (that of top-k) it has to be seen
+struct Bins {
+    int sure = BINS, low = BINS, high = -1, count_bin = BINS;
+    uint32_t count_before = 0;                           // tokens before count_bin, and
+    Weight weight_before_count = 0, weight_before_low = 0, all = 0;      // weights; of all
+    // the bins that matter end here
+    __device__ __forceinline__ float end() const { return sure == BINS ? ALL_BINS : (float)(max(max(sure - 1, high), count_bin < BINS ? count_bin : -1) + 1); }
+    __device__ __forceinline__ bool is_candidate(int bin) const { return bin == count_bin || (bin >= low && bin <= high); }
+    __device__ __forceinline__ Weight candidate(int bin) const { return (bin == count_bin ? FOR_COUNT : 0) | (bin >= low && bin <= high ? FOR_WEIGHT : 0); }
+};
+static_assert(sizeof(Bins) <= 64, "a place of a row's");
+// What the workgroups of a row hand on: for each row what they add up, for each part what it found
+struct Parts {
+    Weight *weights, *pieces;
+    uint32_t *counts, *n_listed;
+    Bins *bins;
+    Found *found;
+    float *maxima;
+    static constexpr int LISTED_EACH = 512;
+    static constexpr size_t ROW = BINS * 12 + PIECES * sizeof(Weight) + 64, PART = LISTED_EACH * sizeof(Found) + 8;      // bytes
+    static constexpr size_t bytes(size_t rows, size_t parts) { return rows * ROW + parts * PART; }
+    __device__ __forceinline__ Parts(Address workspace, size_t rows, size_t parts)
+    {
+        weights = global_at<Weight>(workspace);
+        pieces = weights + rows * BINS;
+        found = (Found *)(pieces + rows * PIECES);
+        bins = (Bins *)(found + parts * LISTED_EACH);
+        counts = (uint32_t *)((uint8_t *)bins + rows * 64);
+        maxima = (float *)(counts + rows * BINS);
+        n_listed = (uint32_t *)(maxima + parts);
+    }
+};
+
+// One row's parameters, and what follows from them once its maximum is known
+struct Given {
+    float temperature, min_p, top_p, u;
+    int top_k;
+    __device__ __forceinline__ Given(const Args &A, int row)
+        : temperature(A.temperature ? global_at<const float>(A.temperature)[row] : 1.f), min_p(A.min_p ? global_at<const float>(A.min_p)[row] : 0.f),
+          top_p(A.top_p ? global_at<const float>(A.top_p)[row] : 1.f), u(global_at<const float>(A.u)[row]), top_k(A.top_k ? global_at<const int>(A.top_k)[row] : 0)
+    {
+    }
+};
+struct Row : Given {
+    Scale scale;
+    float least;      // no token below it is left (min-p; greedy: the largest alone)
+    bool by_count, by_weight, infinite;      // filtered by top-k, by top-p; only logits of plus infinity are left, which count as 0 then
+    __device__ __forceinline__ Row(const Given &G, int vocab, float most) : Given(G)
+    {
+        infinite = most == __builtin_inff();
+        if (infinite) most = 0.f;
+        const bool greedy = !(temperature > 0.f);
+        u = u >= 0.f && !greedy ? fminf(u, 0x1.fffffep-1f) : 0.f;
+        by_count = !greedy && top_k >= 1 && top_k < vocab, by_weight = !greedy && top_p < 1.f;
+        least = -0x1.fffffep+127f;
+        if (greedy || min_p >= 1.f)
+            least = most;
+        else if (min_p > 0.f)      // w >= min_p: x >= max + T log(min_p), the smallest float that is
+            least = fmaxf(least, not_below((double)most + (double)temperature * log((double)min_p)));
+        const double c = fmin(2 * 1.4426950408889634 / (greedy ? 1.0 : (double)temperature), 0x1p+127);
+        scale.half_max = 0.5f * most;
+        scale.hi = (float)c;
+        if ((double)scale.hi > c) scale.hi = __uint_as_float(__float_as_uint(scale.hi) - 1u);      // (lo not below zero: where both parts overflow, so does their sum)
+        scale.lo = (float)(c - (double)scale.hi);
+    }
+    // a token's bin is this one's whole part (within RANGE one of them, whatever it is rounded to)
+    static __device__ __forceinline__ float bin_of(float below) { return below * ((BINS - 0.01f) / RANGE); }
+};
+
+// The tiles of a wavefront, 64 lanes times 16 bytes each: a workgroup's wavefronts have consecutive ones
+template <class E> struct Tiles {
+    static constexpr int TILE = 64 * E::N;
+    const uint8_t *row;
+    int vocab, from, to, lane;
+    __device__ __forceinline__ Tiles(const Args &A, int number, int from_, int to_, int lane_)
+        : row(global_at<const uint8_t>(A.logits) + number * A.stride), vocab(A.vocab), from(from_), to(to_), lane(lane_)
+    {
+    }
+    static __device__ __forceinline__ Tiles of_wave(const Args &A, int number, const Cut &C, int group, int wave, int lane)
+    {
+        const int end = min((group + 1) * C.of_group, C.tiles), each = (C.of_group + WAVES - 1) / WAVES, from = min(group * C.of_group + wave * each, end);
+        return Tiles(A, number, from, min(from + each, end), lane);
+    }
+    // A tile that the row fills, whatever lies there of another
+    __device__ __forceinline__ v4u load(int tile) const
+    {
+        v4u w = (v4u)(E::NONE);
+        if (vocab >= E::N) __builtin_memcpy(&w, row + (long long)min(tile * TILE + lane * E::N, vocab - E::N) * E::SIZE, 16);
+        return w;
+    }
+    // The last tile of a row that does not fill it, NaN past its end
+    __device__ __forceinline__ bool is_cut(int tile) const { return (tile + 1) * TILE > vocab; }
+    __device__ __forceinline__ v4u load_cut(int tile) const
+    {
         const int at = tile * TILE + lane * E::N;
-        uint32_t w[4] = {};
-        if (at + E::N <= A.vocab) {
-            __builtin_memcpy(w, logits + (long long)at * E::SIZE, 16);
+        uint32_t e[E::N];
 #pragma unroll
-            for (int i = 0; i < E::N; ++i) x[i] = E::at(w, i) + 0.f;      // (0 for -0)
+        for (int i = 0; i < E::N; ++i) {
+            e[i] = E::NONE & (E::SIZE == 4 ? ~0u : 0xffffu);
+            if (at + i < vocab) {
+                if constexpr (E::SIZE == 4)
+                    e[i] = *(const uint32_t *)(row + (long long)(at + i) * 4);
+                else
+                    e[i] = *(const uint16_t *)(row + (long long)(at + i) * 2);
+            }
+        }
+        v4u w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = E::SIZE == 4 ? e[j] : e[2 * j % E::N] | e[(2 * j + 1) % E::N] << 16;
+        return w;
+    }
+    static __device__ __forceinline__ v4u as_row_says(const Row &R, v4u w)
+    {
+        if (R.infinite) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = E::infinite(w[j]);
+        }
+        return w;
+    }
+};
+template <class E> __device__ __forceinline__ float largest_of(v4u w)      // (NaN is passed over)
+{
+    float t = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) t = fmaxf(t, E::at(w, i));
+    return t;
+}
+
+// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time
+template <class E, int HELD> struct Elements : Tiles<E> {
+    // word j of each tile: one place of a vector, so that a loop over the tiles is one copy of its body (sixteen do not fit the instruction cache)
+    typedef uint32_t Words __attribute__((ext_vector_type(HELD ? HELD : 1)));
+    Words held[4];
+    float top[HELD ? HELD / 2 : 1];      // of a lane's elements, the largest of each two tiles
+    using Tiles<E>::from;
+    using Tiles<E>::to;
+    __device__ __forceinline__ Elements(const Tiles<E> &tiles) : Tiles<E>(tiles)
+    {
+        if constexpr (HELD != 0) {
+            v4u w[HELD];
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+                if (from + i < to) w[i] = this->load(from + i);
+            if (from < to && this->is_cut(to - 1)) {
+                const v4u last = this->load_cut(to - 1);
+#pragma unroll
+                for (int i = 0; i < HELD; ++i)
+                    if (from + i == to - 1) w[i] = last;
+            }
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) held[j][i] = w[i][j];
+#pragma unroll
+            for (int i = 0; i < HELD; i += 2) {
+                top[i / 2] = from + i < to ? largest_of<E>(w[i]) : -__builtin_inff();
+                if (from + i + 1 < to) top[i / 2] = fmaxf(top[i / 2], largest_of<E>(w[i + 1]));
+            }
+        }
+    }
+    template <class Use> __device__ __forceinline__ void each_tile(Use use) const
+    {
+        if constexpr (HELD != 0) {
+#pragma unroll 1
+            for (int i = 0; i < to - from; ++i) use(from + i, (v4u){held[0][i], held[1][i], held[2][i], held[3][i]});
         } else {
+            const int end = from < to && this->is_cut(to - 1) ? to - 1 : to;
+            for (int tile = from; tile < end; tile += 4) {
+                v4u w[4];
 #pragma unroll
-            for (int i = 0; i < E::N; ++i) {
-                x[i] = __builtin_nanf("");
-                if (at + i < A.vocab) {
-                    uint32_t one[4] = {};
-                    __builtin_memcpy(one, logits + (long long)(at + i) * E::SIZE, E::SIZE);
-                    x[i] = E::at(one, 0) + 0.f;
+                for (int i = 0; i < 4; ++i)
+                    if (tile + i < end) w[i] = this->load(tile + i);
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    if (tile + i < end) use(tile + i, w[0]);
+                    w[0] = w[1], w[1] = w[2], w[2] = w[3];
+                }
+            }
+            if (end < to) use(end, this->load_cut(end));
+        }
+    }
+    // use(tile, its elements) for those that may have one in a bin before `end`
+    template <class Use> __device__ __forceinline__ void each(const Row &R, float end, Use use) const
+    {
+        if constexpr (HELD != 0) {
+            uint32_t skipped = 0;      // one bit for each two tiles
+            if (end != ALL_BINS && !R.infinite) {
+#pragma unroll
+                for (int i = 0; i < HELD / 2; ++i) skipped |= __ballot(Row::bin_of(R.scale.below(top[i])) < end) ? 0u : 1u << i;
+            }
+            each_tile([&](int tile, v4u w) {
+                if (!(skipped >> (tile - from) / 2 & 1)) use(tile, Tiles<E>::as_row_says(R, w));
+            });
+        } else {
+            each_tile([&](int tile, v4u w) {
+                w = Tiles<E>::as_row_says(R, w);
+                if (end == ALL_BINS || __ballot(Row::bin_of(R.scale.below(largest_of<E>(w))) < end)) use(tile, w);
+            });
+        }
+    }
+    __device__ __forceinline__ float largest() const
+    {
+        float t = -__builtin_inff();
+        if constexpr (HELD != 0) {
+#pragma unroll
+            for (int i = 0; i < HELD / 2; ++i) t = fmaxf(t, top[i]);
+        } else {
+            each_tile([&](int, v4u w) { t = fmaxf(t, largest_of<E>(w)); });
+        }
+        return t;
+    }
+};
+
+__device__ __forceinline__ float largest_of_workgroup(Shared &S, float t, int lane, int wave)
+{
+    for (int d = 1; d < 64; d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
+    if (lane == 0) S.wave_max[wave] = t;
+    __syncthreads();
+    t = S.wave_max[lane % WAVES];
+    for (int d = 1; d < WAVES; d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
+    return t;
+}
+
+__device__ __forceinline__ void clear_bins(Shared &S, int tid)
+{
+    for (int i = tid; i < BINS; i += THREADS) S.counts[i] = 0, S.weights[i] = 0;
+    __syncthreads();
+}
+// The bins before `end`
+template <class E, class Elements_> __device__ __forceinline__ void histogram(Shared &S, const Row &R, const Elements_ &elements, float end, int tid)
+{
+    clear_bins(S, tid);
+    elements.each(R, end, [&](int, v4u w) {
+#pragma unroll
+        for (int half = 0; half < E::N; half += 4) {
+            float below[4];
+            uint32_t weight[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) below[i] = R.scale.below(E::at(w, half + i));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) weight[i] = Scale::weight(below[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float at = Row::bin_of(below[i]);
+                if (below[i] < RANGE && at < end) {
+                    const int bin = (int)at;
+                    if (R.by_count) atomicAdd(&S.counts[bin], 1u);
+                    if (R.by_weight) atomicAdd(&S.weights[bin], (Weight)weight[i]);
                 }
             }
         }
-    };
-    auto for_all = [&](auto use) {
-        for (int tile = from_tile; tile < to_tile; ++tile) {
-            float x[E::N];
-            load(tile, x);
-#pragma unroll
-            for (int i = 0; i < E::N; ++i) use(x[i]);
-        }
-    };
-
-    float most = -__builtin_inff();
-    for_all([&](float x) { most = fmaxf(most, x); });      // (NaN is passed over)
-    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-    if (lane == 0) wave_max[wave] = most;
+    });
     __syncthreads();
-    most = wave_max[lane % WAVES];
-    for (int d = 1; d < WAVES; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+}
+
+// What a thread knows of the bins: its own, and the sums up to its last
+struct Sums {
+    uint32_t counts[PER_THREAD], upto_count = 0, all_count;
+    Weight weights[PER_THREAD], upto_weight = 0, all_weight;
+    __device__ __forceinline__ void add_up(Shared &S, Use use, int lane, int wave)
+    {
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) upto_count += counts[i], upto_weight += weights[i];
+        up_to_thread(S, use, upto_count, upto_weight, all_count, all_weight, lane, wave);
+    }
+    // The bin in which the counts, or the weights, reach `target`, which all of them do: one thread says so
+    __device__ __forceinline__ void say(Reached &to, bool by_count, Weight target, int tid) const
+    {
+        Reached r = {PER_THREAD * tid, upto_count, upto_weight, 0};
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) r.count -= counts[i], r.before -= weights[i];
+        if ((by_count ? r.count : r.before) >= target || (by_count ? upto_count : upto_weight) < target) return;
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) {
+            r.here = weights[i];
+            if ((by_count ? r.count + counts[i] : r.before + weights[i]) >= target) break;
+            r.count += counts[i], r.before += weights[i], ++r.bin;
+        }
+        to = r;
+    }
+};
+__device__ __forceinline__ Sums sums_of(const Shared &S, int tid)
+{
+    Sums s;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) s.counts[i] = S.counts[PER_THREAD * tid + i], s.weights[i] = S.weights[PER_THREAD * tid + i];
+    return s;
+}
+// the weight at which the shortest prefix that has top_p of `all` ends: one token at least
+__device__ __forceinline__ Weight target_of(float top_p, Weight all)
+{
+    const double wanted = ceil((double)top_p * (double)all);
+    return wanted >= 1.0 ? min((Weight)wanted, all) : 1;
+}
+
+__device__ __forceinline__ Bins borders(Shared &S, const Row &R, Sums sums, int tid, int lane, int wave)
+{
+    Bins B;
+    sums.add_up(S, BORDER, lane, wave);
+    Weight least = B.all = sums.all_weight, most = B.all;      // what top-k leaves, whatever is left of its bin
+    if (R.by_count && (uint32_t)R.top_k <= sums.all_count) {
+        sums.say(S.reached[BORDER], true, (Weight)R.top_k, tid);
+        __syncthreads();
+        const Reached r = S.reached[BORDER];
+        B.sure = B.count_bin = r.bin, B.count_before = r.count;
+        least = B.weight_before_count = r.before, most = r.before + r.here;
+    }
+    if (R.by_weight) {
+        const Weight low = target_of(R.top_p, least), high = target_of(R.top_p, most);
+        sums.say(S.reached[SECOND], false, low, tid);
+        if (high != low) sums.say(S.reached[BOUND], false, high, tid);
+        __syncthreads();
+        const Reached r = S.reached[SECOND];
+        B.sure = B.low = min(r.bin, B.count_bin), B.weight_before_low = r.before;
+        B.high = min(high != low ? S.reached[BOUND].bin : r.bin, B.count_bin);
+    }
+    return B;
+}
+// The first bins that top-k can reach into: every token of the first top_k is in them, since so many threads have one there.
+// largest: of this thread's tokens.
+__device__ __forceinline__ float bins_of_top_k(Shared &S, const Row &R, float largest, int tid, int lane, int wave)
+{
+    if (!R.by_count || R.top_k > THREADS / 2) return ALL_BINS;
+    clear_bins(S, tid);
+    const float below = R.scale.below(!R.infinite ? largest : largest == __builtin_inff() ? 0.f : __builtin_nanf(""));
+    if (below < RANGE) atomicAdd(&S.counts[(int)Row::bin_of(below)], 1u);
+    __syncthreads();
+    Sums sums = sums_of(S, tid);
+    sums.add_up(S, BOUND, lane, wave);
+    if (sums.all_count < (uint32_t)R.top_k) return ALL_BINS;
+    sums.say(S.reached[FIRST], true, (Weight)R.top_k, tid);
+    __syncthreads();
+    const int bin = S.reached[FIRST].bin;
+    return bin < BINS - 1 ? (float)(bin + 1) : ALL_BINS;
+}
+
+// All tokens of bins before `end` into the list, as far as there is room; their histogram.  False: they are more
+template <class E, class Elements_> __device__ __forceinline__ bool gather(Shared &S, const Row &R, const Elements_ &elements, float end, int tid, int lane)
+{
+    if (tid == 0) S.begin_list(0);
+    clear_bins(S, tid);
+    if (tid < PIECES) S.pieces[tid] = 0;
+    elements.each(R, end, [&](int tile, v4u w) {
+        uint32_t found = 0;      // one bit for each
+#pragma unroll
+        for (int i = 0; i < E::N; ++i) found |= Row::bin_of(R.scale.below(E::at(w, i))) < end ? 1u << i : 0u;
+        while (__ballot(found)) {
+            if (found) {
+                const int i = __builtin_ctz(found);
+                found &= found - 1;
+                const uint32_t n = atomicAdd(&S.n_listed, 1u);
+                if (n < LISTED) S.found[n] = {E::any(w, i), (tile * 64 + lane) * E::N + i};
+            }
+        }
+    });
+    __syncthreads();
+    const int n = (int)S.n_listed;
+    if (n > LISTED) return false;
+    for (int i = tid; i < n; i += THREADS) {
+        const float below = R.scale.below(S.found[i].x);
+        const int bin = (int)Row::bin_of(below);
+        atomicAdd(&S.counts[bin], 1u);
+        atomicAdd(&S.weights[bin], (Weight)Scale::weight(below));
+    }
+    __syncthreads();
+    return true;
+}
+
+// A wavefront's sums by pieces, its tiles in their order: the lanes' are added up once a piece
+struct PieceSums {
+    Shared &S;
+    const Cut &C;
+    int lane, piece, next;      // the piece at hand, the tile where it ends
+    Weight sum = 0;
+    __device__ __forceinline__ PieceSums(Shared &S_, const Cut &C_, int from, int lane_) : S(S_), C(C_), lane(lane_), piece(C_.piece_of(from))
+    {
+        int first;
+        C.tiles_of(piece, first, next);
+    }
+    __device__ __forceinline__ void add(int tile, Weight w)
+    {
+        if (tile >= next) {
+            end();
+            piece = C.piece_of(tile);
+            int first;
+            C.tiles_of(piece, first, next);
+        }
+        sum += w;
+    }
+    __device__ __forceinline__ void end()
+    {
+        if (__ballot(sum != 0)) {
+            sum = up_to_lane(sum);
+            if (lane == 63) atomicAdd(&S.pieces[piece], sum);
+        }
+        sum = 0;
+    }
+};
+
+// Weights of the tokens that are left for sure, by pieces of the row; candidates into the list, as far as there is room
+template <class E, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int tid, int lane)
+{
+    if (tid < PIECES) S.pieces[tid] = 0;
+    if (tid == 0) S.begin_list(0);
+    __syncthreads();
+    const float sure = B.sure == BINS ? ALL_BINS : (float)B.sure, below_least = R.scale.below(R.least);
+    // (without candidates, min-p's border ends it as well)
+    const float end = B.sure < BINS ? B.end() : below_least < RANGE ? floorf(Row::bin_of(below_least)) + 1.f : ALL_BINS;
+    // (bins between the two borders, if there are any, have none)
+    const bool all_candidates = B.count_bin == BINS || B.low == BINS || B.count_bin <= B.high + 1;
+    PieceSums sums(S, C, elements.from, lane);
+    if (B.sure == BINS) {      // no filter but min-p's
+        elements.each(R, end, [&](int tile, v4u w) {
+            Weight sum = 0;
+#pragma unroll
+            for (int i = 0; i < E::N; i += 2) {
+                const float x = E::at(w, i), y = E::at(w, i + 1);
+                const uint32_t of_x = Scale::weight(R.scale.below(x)), of_y = Scale::weight(R.scale.below(y));
+                sum += (x >= R.least ? of_x : 0u) + (y >= R.least ? of_y : 0u);      // (two of them fit 32 bits)
+            }
+            sums.add(tile, sum);
+        });
+    } else {
+        elements.each(R, end, [&](int tile, v4u w) {
+            Weight sum = 0;
+            bool any = false;
+#pragma unroll
+            for (int half = 0; half < E::N; half += 4) {
+                uint32_t weight[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = E::at(w, half + i), below = R.scale.below(x), at = Row::bin_of(below);
+                    any |= at < end && !(at < sure);
+                    weight[i] = at < sure && x >= R.least ? Scale::weight(below) : 0u;
+                }
+                sum += weight[0] + weight[1], sum += weight[2] + weight[3];
+            }
+            uint32_t candidates = 0;      // one bit for each
+            if (__ballot(any)) {
+#pragma unroll
+                for (int i = 0; i < E::N; ++i) {
+                    const float at = Row::bin_of(R.scale.below(E::at(w, i)));
+                    candidates |= at >= sure && at < end ? 1u << i : 0u;
+                }
+            }
+            while (__ballot(candidates)) {      // (also those that min-p does not leave: they count for top-k and top-p)
+                if (candidates) {
+                    const int i = __builtin_ctz(candidates);
+                    candidates &= candidates - 1;
+                    const float x = E::any(w, i);
+                    if (all_candidates || B.is_candidate((int)Row::bin_of(R.scale.below(x)))) {
+                        const uint32_t n = atomicAdd(&S.n_listed, 1u);
+                        if (n < LISTED) S.found[n] = {x, (tile * 64 + lane) * E::N + i};
+                    }
+                }
+            }
+            sums.add(tile, sum);
+        });
+    }
+    sums.end();
+    __syncthreads();
+}
+
+// Among the candidates that are `flag`: the first one, in their order, with which `target` is reached, 0 if with none.  `weight`: theirs up to it.  Consecutive lanes share a
+// candidate's comparisons.
+__device__ __forceinline__ Place resolve(Shared &S, int use, Weight flag, bool by_count, Weight target, int n, Weight &weight, int tid, int lane)
+{
+    // (the candidates for top-k and those for top-p may be of different logits)
+    for (int i = tid; i < n; i += THREADS)
+        if (S.listed[i].place >> INDEX_BITS != S.listed[0].place >> INDEX_BITS || !(S.listed[i].weight & flag)) S.differ[use] = 1;
+    __syncthreads();
+    const bool same = !S.differ[use];
+    const int shift = n > 1 ? max(10 - (32 - __builtin_clz(n - 1)), 0) : 6, sharing = 1 << min(shift, 6);
+    for (int i = tid / sharing; i < n; i += THREADS / sharing) {
+        const Candidate mine = S.listed[i];
+        uint32_t rank = 0;
+        Weight before = 0;
+        if (same) {      // of equal logits: by their indexes
+            for (int j = lane & (sharing - 1); j < n; j += sharing) rank += (uint32_t)S.listed[j].place > (uint32_t)mine.place;
+            before = rank * (mine.weight & ONLY_WEIGHT);
+        }
+        for (int j = lane & (sharing - 1); j < n && !same; j += sharing) {
+            const Candidate c = S.listed[j];
+            const bool counts = c.place > mine.place && (c.weight & flag);
+            rank += counts;
+            before += counts ? c.weight & ONLY_WEIGHT : 0;
+        }
+        for (int d = 1; d < sharing; d <<= 1) {
+            rank += __shfl_xor(rank, d);
+            before += (Weight)__shfl_xor((uint32_t)(before >> 32), d) << 32 | (uint32_t)__shfl_xor((uint32_t)before, d);
+        }
+        const Weight own = mine.weight & ONLY_WEIGHT, reached = by_count ? rank : before, with = reached + (by_count ? 1 : own);
+        if ((mine.weight & flag) && reached < target && with >= target) S.found_place[use] = mine.place, S.found_weight[use] = before + own;
+    }
+    __syncthreads();
+    weight = S.found_weight[use];
+    return S.found_place[use];
+}
+
+// The same among all tokens, by their places' bits, a histogram of some at a time: where the candidates are more than the list holds (thousands of equal logits).
+// Behind `least` none counts.
+template <class E, class Elements_>
+__device__ __forceinline__ Place resolve_all(Shared &S, const Row &R, const Elements_ &elements, bool by_count, Weight target, Place least, Weight &weight, int tid, int lane, int wave)
+{
+    Place prefix = 0;
+    weight = 0;
+    Weight count = 0;
+    for (int left = PLACE_BITS; left > 0;) {
+        const int bits = min(left, BIN_BITS);
+        left -= bits;
+        clear_bins(S, tid);
+        elements.each(R, ALL_BINS, [&](int tile, v4u w) {
+#pragma unroll 1
+            for (int i = 0; i < E::N; ++i) {
+                const float x = E::at(w, i), below = R.scale.below(x);
+                const Place p = place(x, (tile * 64 + lane) * E::N + i);
+                if (below < RANGE && p >= least && p >> (left + bits) == prefix) {
+                    const int bin = (int)((1u << bits) - 1 - (uint32_t)(p >> left & ((1u << bits) - 1)));      // from the largest down
+                    atomicAdd(&S.counts[bin], 1u);
+                    atomicAdd(&S.weights[bin], (Weight)Scale::weight(below));
+                }
+            }
+        });
+        __syncthreads();
+        Sums sums = sums_of(S, tid);
+        sums.add_up(S, BORDER, lane, wave);
+        if ((by_count ? sums.all_count : sums.all_weight) < target - (by_count ? count : weight)) return 0;      // (never: top-k's and top-p's are reached)
+        sums.say(S.reached[BORDER], by_count, target - (by_count ? count : weight), tid);
+        __syncthreads();
+        const Reached r = S.reached[BORDER];
+        count += r.count, weight += r.before;
+        prefix = prefix << bits | (Place)((1u << bits) - 1 - r.bin);
+        if (left == 0) weight += r.here;
+    }
+    return prefix;
+}
+
+// The border: the last token that top-k and top-p leave (0: they leave all).  Candidates that are left join the pieces.
+template <class E> __device__ __forceinline__ Place settle(Shared &S, const Args &A, int row, const Row &R, const Bins &B, const Cut &C, int tid, int lane, int wave)
+{
+    if (B.count_bin == BINS && B.low == BINS) return 0;
+    Place border = 0;
+    Weight weight, left = B.all;
+    const int n = (int)S.n_listed;
+    if (n <= LISTED) {
+        for (int i = tid; i < n; i += THREADS) {
+            const Found f = S.found[i];
+            const float below = R.scale.below(f.x);
+            S.listed[i] = {place(f.x, f.index), Scale::weight(below) | B.candidate((int)Row::bin_of(below))};
+        }
+        __syncthreads();
+        if (B.count_bin < BINS) {
+            border = resolve(S, 0, FOR_COUNT, true, (Weight)R.top_k - B.count_before, n, weight, tid, lane);
+            left = B.weight_before_count + weight;
+        }
+        if (R.by_weight) border = max(border, resolve(S, 1, FOR_WEIGHT, false, target_of(R.top_p, left) - B.weight_before_low, n, weight, tid, lane));
+        for (int i = tid; i < n; i += THREADS) {      // (a candidate of top-k alone lies behind top-p's border, or there is none; one that is none, before both or behind)
+            const Candidate c = S.listed[i];
+            if (c.place >= border && c.place >= place(R.least, MAX_VOCAB - 1)) atomicAdd(&S.pieces[C.piece_of(index_of(c.place) / Tiles<E>::TILE)], c.weight & ONLY_WEIGHT);
+        }
+    } else {
+        const Elements<E, 0> elements(Tiles<E>::of_wave(A, row, Cut(1, A.vocab, Tiles<E>::TILE), 0, wave, lane));      // (the whole row)
+        if (B.count_bin < BINS) border = resolve_all<E>(S, R, elements, true, (Weight)R.top_k, 0, left, tid, lane, wave);
+        if (R.by_weight) border = max(border, resolve_all<E>(S, R, elements, false, target_of(R.top_p, left), border, weight, tid, lane, wave));
+        if (tid < PIECES) S.pieces[tid] = 0;
+        __syncthreads();
+        PieceSums sums(S, C, elements.from, lane);
+        elements.each(R, ALL_BINS, [&](int tile, v4u w) {
+            Weight sum = 0;
+#pragma unroll 1
+            for (int i = 0; i < E::N; ++i) {
+                const float x = E::at(w, i), below = R.scale.below(x);
+                if (x >= R.least && place(x, (tile * 64 + lane) * E::N + i) >= border) sum += Scale::weight(below);
+            }
+            sums.add(tile, sum);
+        });
+        sums.end();
+    }
+    __syncthreads();
+    return border;
+}
+
+// The token: the piece that u falls into, a tile of it per wavefront, the elements of the lanes
+template <class E> __device__ __forceinline__ void pick(Shared &S, const Args &A, int row, const Row &R, Place border, const Cut &C, int lane, int wave)
+{
+    static_assert(PIECES == 64, "one per lane");
+    const Weight mine = S.pieces[lane], upto = up_to_lane(mine), total = of_lane(upto, 63);
+    const Weight target = min((Weight)((double)R.u * (double)total), total - 1);
+    const int piece = __builtin_ctzll(__ballot(upto > target));
+    Weight before = of_lane(upto - mine, piece);
+    int from, to;
+    C.tiles_of(piece, from, to);
+    const Tiles<E> tiles(A, row, from, to, lane);
+    for (; from < to; from += WAVES) {
+        const int tile = from + wave, at = (tile * 64 + lane) * E::N;
+        v4u w = (v4u)(E::NONE);
+        if (tile < to) w = Tiles<E>::as_row_says(R, tiles.is_cut(tile) ? tiles.load_cut(tile) : tiles.load(tile));
+        uint32_t own[E::N];
+        Weight sum = 0;
+#pragma unroll
+        for (int i = 0; i < E::N; ++i) {
+            const float x = E::at(w, i);
+            own[i] = x >= R.least && place(x, at + i) >= border ? Scale::weight(R.scale.below(x)) : 0;
+            sum += own[i];
+        }
+        Weight upto_lane = up_to_lane(sum), all;
+        __syncthreads();
+        if (lane == 63) S.wave_weights[FIRST][wave] = upto_lane;
+        __syncthreads();
+        upto_lane = before + over_waves(upto_lane, S.wave_weights[FIRST], lane, wave, all);
+        if (upto_lane > target && upto_lane - sum <= target) {
+            Weight upto_i = upto_lane - sum;
+            int i = 0;
+#pragma unroll
+            for (int j = 0; j < E::N; ++j) {
+                upto_i += own[j];
+                i += upto_i <= target;
+            }
+            global_at<int>(A.tokens)[row] = at + i;
+        }
+        before += all;
+        if (before > target) return;
+    }
+}
+
+// One workgroup does a row
+template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kernel(const Args A)
+{
+    __shared__ Shared S;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x;
+    const Cut C(1, A.vocab, Tiles<E>::TILE);
+    const Given G(A, row);
+    const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, 0, wave, lane));
+    const float largest = elements.largest(), most = largest_of_workgroup(S, largest, lane, wave);
     if (most == -__builtin_inff()) {      // nothing that may be drawn
         if (tid == 0) global_at<int>(A.tokens)[row] = -1;
         return;
     }
-
-    const float temperature = A.temperature ? global_at<const float>(A.temperature)[row] : 1.f, min_p = A.min_p ? global_at<const float>(A.min_p)[row] : 0.f;
-    float top_p = A.top_p ? global_at<const float>(A.top_p)[row] : 1.f, u = global_at<const float>(A.u)[row];
-    int top_k = A.top_k ? global_at<const int>(A.top_k)[row] : 0;
-    const bool greedy = !(temperature > 0.f);
-    if (top_k < 1 || top_k > A.vocab) top_k = A.vocab;
-    if (!(top_p < 1.f)) top_p = 1.f;
-    u = u >= 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-    const double c = 2 * 1.4426950408889634 / (greedy ? 1.0 : (double)temperature);
-    Scale scale;
-    scale.most = most, scale.half_max = 0.5f * most;
-    scale.hi = (float)fmin(c, 0x1p+127), scale.lo = (float)(fmin(c, 0x1p+127) - (double)scale.hi);
-
-    // What is left: above `border`, and the first `ties` of those equal to it
-    float border = -__builtin_inff();
-    int ties = 0;
-    if (greedy) {
-        border = most, ties = 1;
-    } else {
-        if (min_p > 0.f) {      // w >= min_p: x >= max + T log(min_p), the smallest float that is
-            border = min_p < 1.f ? fmaxf(not_below((double)most + (double)temperature * log((double)min_p)), -0x1.fffffep+127f) : most;
-            ties = 0x7fffffff;
-        }
-        if (top_k < A.vocab || top_p < 1.f) {
-            for (int i = tid; i < BINS; i += THREADS) counts[i] = 0, weights[i] = 0;
-            __syncthreads();
-            auto bin_of = [&](float below) { return min((int)(below * (BINS / RANGE)), BINS - 1); };
-            for_all([&](float x) {
-                const float below = scale.below(x);
-                if (x > -__builtin_inff() && below < RANGE) {
-                    atomicAdd(&counts[bin_of(below)], 1u);
-                    atomicAdd(&weights[bin_of(below)], Scale::weight(below));
-                }
-            });
-            __syncthreads();
-            // what lies before each bin: two bins a thread
-            const uint32_t c0 = counts[2 * tid], c1 = counts[2 * tid + 1];
-            const Weight w0 = weights[2 * tid], w1 = weights[2 * tid + 1];
-            uint32_t upto_c = up_to_lane(c0 + c1, lane);
-            Weight upto_w = up_to_lane(w0 + w1, lane);
-            if (lane == 63) wave_counts[wave] = upto_c, wave_weights[wave] = upto_w;
-            __syncthreads();
-            const uint32_t sum_c = up_to_lane(lane < WAVES ? wave_counts[lane] : 0u, lane);
-            const Weight sum_w = up_to_lane(lane < WAVES ? wave_weights[lane] : (Weight)0, lane);
-            if (wave) upto_c += __builtin_amdgcn_readlane(sum_c, wave - 1), upto_w += of_lane(sum_w, wave - 1);
-            const uint32_t all_c = __builtin_amdgcn_readlane(sum_c, WAVES - 1);
-            const Weight all_w = of_lane(sum_w, WAVES - 1);
-
-            // The border at which `target` (counts or weight) is reached; there is one
-            auto find = [&](bool by_count, Weight target) -> Border {
-                auto reached = [&](uint32_t count, Weight weight) { return (by_count ? (Weight)count : weight) >= target; };
-                __syncthreads();
-                if (tid == 0) n_listed = 0;
-                if (reached(upto_c, upto_w) && !reached(upto_c - c1 - c0, upto_w - w1 - w0)) {
-                    const bool second = !reached(upto_c - c1, upto_w - w1);
-                    found_bin = 2 * tid + second;
-                    found.above = upto_c - c1 - (second ? 0 : c0), found.weight_above = upto_w - w1 - (second ? 0 : w0);
-                    found.equal = second ? c1 : c0;
-                }
-                __syncthreads();
-                const int bin = found_bin, n = found.equal;
-                Border b = found;
-                __syncthreads();
-                if (n <= LISTED) {      // the bin's logits, each ranked among them
-                    for_all([&](float x) {
-                        const float below = scale.below(x);
-                        if (x > -__builtin_inff() && below < RANGE && bin_of(below) == bin) {
-                            const uint32_t at = atomicAdd(&n_listed, 1u);
-                            listed[at] = ordered(x);
-                            listed_weights[at] = Scale::weight(below);
-                        }
-                    });
-                    __syncthreads();
-                    if (tid < n) {
-                        const uint32_t mine = listed[tid];
-                        int above = b.above, equal = 0;
-                        Weight weight_above = b.weight_above;
-                        for (int i = 0; i < n; ++i) {
-                            const uint32_t o = listed[i];
-                            above += o > mine, equal += o == mine;
-                            weight_above += o > mine ? listed_weights[i] : 0;
-                        }
-                        if (!reached(above, weight_above) && reached(above + equal, weight_above + equal * listed_weights[tid])) {
-                            found.x = from_ordered(mine);
-                            found.above = above, found.equal = equal, found.weight_above = weight_above;
-                        }
-                    }
-                } else {      // by their bits, eleven at a time: those that have the `prefix` found so far
-                    uint32_t prefix = 0;
-                    for (int shift = 21, bits = 11; shift >= 0; bits = min(shift, 11), shift -= max(bits, 1)) {
-                        for (int i = tid; i < BINS; i += THREADS) counts[i] = 0, weights[i] = 0;
-                        __syncthreads();
-                        for_all([&](float x) {
-                            const float below = scale.below(x);
-                            const uint32_t o = ordered(x);
-                            if (x > -__builtin_inff() && below < RANGE && bin_of(below) == bin && (shift + bits == 32 || o >> (shift + bits) == prefix)) {
-                                atomicAdd(&counts[o >> shift & ((1u << bits) - 1)], 1u);
-                                atomicAdd(&weights[o >> shift & ((1u << bits) - 1)], Scale::weight(below));
-                            }
-                        });
-                        __syncthreads();
-                        if (tid == 0) {
-                            int i = (1 << bits) - 1;      // from the largest down
-                            for (; i > 0 && !reached(b.above + counts[i], b.weight_above + weights[i]); --i) b.above += counts[i], b.weight_above += weights[i];
-                            found = b, found.equal = counts[i], found_bin = i;
-                        }
-                        __syncthreads();
-                        b = found;
-                        prefix = prefix << bits | (uint32_t)found_bin;
-                        __syncthreads();
-                        if (shift == 0) break;
-                    }
-                    if (tid == 0) found.x = from_ordered(prefix);
-                }
-                __syncthreads();
-                b = found;
-                return b;
-            };
-            auto tighten = [&](float x, int n) {
-                if (x > border)
-                    border = x, ties = n;
-                else if (x == border)
-                    ties = min(ties, n);
-            };
-            Weight kept = all_w;
-            if ((uint32_t)top_k < all_c) {
-                const Border b = find(true, (Weight)top_k);
-                tighten(b.x, top_k - b.above);
-                kept = b.weight_above + (Weight)(top_k - b.above) * scale.of(b.x);
-            }
-            if (top_p < 1.f) {
-                const double wanted = ceil((double)top_p * (double)kept);
-                const Weight target = wanted >= 1.0 ? min((Weight)wanted, kept) : 1;
-                const Border b = find(false, target);
-                const Weight one = max(scale.of(b.x), (Weight)1);
-                tighten(b.x, (int)min((target - b.weight_above + one - 1) / one, (Weight)0x7fffffff));
-            }
-        }
+    const Row R(G, A.vocab, most);
+    Bins B;
+    bool listed = false;
+    if (R.by_count || R.by_weight) {
+        // top-k: the tokens that can be among the first are few, and all that follows is done with those
+        const float end = bins_of_top_k(S, R, largest, tid, lane, wave);
+        listed = end != ALL_BINS && gather<E>(S, R, elements, end, tid, lane);
+        if (!listed) histogram<E>(S, R, elements, end, tid);
+        B = borders(S, R, sums_of(S, tid), tid, lane, wave);
     }
-
-    // sums over pieces of the row, in its order
-    const int per_piece = (each + PIECES - 1) / PIECES;      // tiles
-    for (int i = tid; i < WAVES * PIECES; i += THREADS) piece_ties[i] = 0, piece_weights[i] = 0;
-    __syncthreads();
-    for (int tile = from_tile; tile < to_tile; ++tile) {
-        float x[E::N];
-        load(tile, x);
-        Weight sum = 0;
-        uint32_t equal = 0;
-#pragma unroll
-        for (int i = 0; i < E::N; ++i) {
-            if (x[i] > border) sum += scale.of(x[i]);
-            equal += x[i] == border;
-        }
-        const int piece = wave * PIECES + (tile - from_tile) / per_piece;
-        if (sum) atomicAdd(&piece_weights[piece], sum);
-        if (equal) atomicAdd(&piece_ties[piece], equal);
-    }
-    __syncthreads();
-    const Weight tie = border > -__builtin_inff() ? scale.of(border) : 0;
-    // a wavefront's pieces, one per lane; then the wavefronts
-    uint32_t upto_ties = up_to_lane(piece_ties[tid], lane);
-    if (lane == 63) wave_counts[wave] = upto_ties;
-    __syncthreads();
-    const uint32_t ties_of_waves = up_to_lane(lane < WAVES ? wave_counts[lane] : 0u, lane);
-    if (wave) upto_ties += __builtin_amdgcn_readlane(ties_of_waves, wave - 1);
-    auto kept_ties = [&](uint32_t before, uint32_t n) { return (Weight)(min(before + n, (uint32_t)ties) - min(before, (uint32_t)ties)); };
-    const uint32_t ties_before = upto_ties - piece_ties[tid];
-    const Weight mine = piece_weights[tid] + kept_ties(ties_before, piece_ties[tid]) * tie;
-    Weight upto = up_to_lane(mine, lane);
-    if (lane == 63) wave_weights[wave] = upto;
-    __syncthreads();
-    const Weight sum_of_waves = up_to_lane(lane < WAVES ? wave_weights[lane] : (Weight)0, lane);
-    if (wave) upto += of_lane(sum_of_waves, wave - 1);
-    const Weight total = of_lane(sum_of_waves, WAVES - 1);
-    const Weight target = min((Weight)((double)u * (double)total), total - 1);
-    const unsigned long long here = __ballot(upto > target && upto - mine <= target);
-    if (!here) return;
-
-    // this wavefront has the piece: its tiles, then the lanes' elements
-    const int piece = __builtin_ctzll(here);
-    Weight before = of_lane(upto - mine, piece);
-    uint32_t equal_before = __builtin_amdgcn_readlane(ties_before, piece);
-    for (int tile = from_tile + piece * per_piece; tile < min(from_tile + (piece + 1) * per_piece, to_tile); ++tile) {
-        float x[E::N];
-        load(tile, x);
-        uint32_t equal = 0;
-#pragma unroll
-        for (int i = 0; i < E::N; ++i) equal += x[i] == border;
-        const uint32_t upto_equal = up_to_lane(equal, lane);
-        uint32_t rank = equal_before + upto_equal - equal;
-        Weight w[E::N], sum = 0;
-#pragma unroll
-        for (int i = 0; i < E::N; ++i) {
-            w[i] = x[i] > border ? scale.of(x[i]) : x[i] == border && rank < (uint32_t)ties ? tie : 0;
-            rank += x[i] == border;
-            sum += w[i];
-        }
-        const Weight upto_lane = before + up_to_lane(sum, lane);
-        const unsigned long long lanes = __ballot(upto_lane > target);
-        if (lanes) {
-            if (lane == __builtin_ctzll(lanes)) {
-                Weight at = upto_lane - sum;
-                int i = 0;
-#pragma unroll
-                for (int j = 0; j < E::N; ++j) {
-                    at += w[j];
-                    i += at <= target;
-                }
-                global_at<int>(A.tokens)[row] = tile * TILE + lane * E::N + i;
-            }
-            return;
-        }
-        before = of_lane(upto_lane, 63);
-        equal_before += __builtin_amdgcn_readlane(upto_equal, 63);
-    }
+    if (!listed) collect<E>(S, R, B, C, elements, tid, lane);
+    const Place border = settle<E>(S, A, row, R, B, C, tid, lane, wave);
+    pick<E>(S, A, row, R, border, C, lane, wave);
 }
 
-constexpr int MAX_ROWS = 1 << 20, MAX_VOCAB = 1 << 22;
+// Several workgroups do a row, in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
+// token.  What they hand on lies in the workspace.
+enum Step { MAXIMUM, HISTOGRAM, COLLECT };
+__device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
+{
+    float t = lane < groups ? P.maxima[first + lane] : -__builtin_inff();
+    for (int d = 1; d < 64; d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
+    return t;
+}
+template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) void part_kernel(const Args A)
+{
+    __shared__ Shared S;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x / A.groups, group = blockIdx.x % A.groups;
+    const Cut C(A.groups, A.vocab, Tiles<E>::TILE);
+    const Given G(A, row);
+    const Parts P(A.workspace, (size_t)A.rows, (size_t)A.rows * A.groups);
+    const size_t first = (size_t)row * A.groups, mine = first + group, bins = (size_t)row * BINS;
+    const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, group, wave, lane));
+    if constexpr (STEP == MAXIMUM) {
+        for (int i = group * THREADS + tid; i < BINS; i += A.groups * THREADS) P.counts[bins + i] = 0, P.weights[bins + i] = 0;
+        const float most = largest_of_workgroup(S, elements.largest(), lane, wave);
+        if (tid == 0) P.maxima[mine] = most;
+    } else {
+        const float most = largest_of_row(P, first, A.groups, lane);
+        if (most == -__builtin_inff()) return;
+        const Row R(G, A.vocab, most);
+        const bool filtered = R.by_count || R.by_weight;
+        if constexpr (STEP == HISTOGRAM) {
+            if (!filtered) return;
+            histogram<E>(S, R, elements, ALL_BINS, tid);
+            for (int i = tid; i < BINS; i += THREADS) {
+                if (S.counts[i]) atomicAdd(&P.counts[bins + i], S.counts[i]);
+                if (S.weights[i]) atomicAdd(&P.weights[bins + i], S.weights[i]);
+            }
+        } else {
+            Bins B;
+            if (filtered) {
+                Sums sums;
+#pragma unroll
+                for (int i = 0; i < PER_THREAD; ++i) sums.counts[i] = P.counts[bins + PER_THREAD * tid + i], sums.weights[i] = P.weights[bins + PER_THREAD * tid + i];
+                B = borders(S, R, sums, tid, lane, wave);
+                if (group == 0 && tid == 0) P.bins[row] = B;
+            }
+            collect<E>(S, R, B, C, elements, tid, lane);
+            const int pieces = PIECES / A.groups, n = (int)S.n_listed;
+            if (tid < pieces) P.pieces[(size_t)row * PIECES + group * pieces + tid] = S.pieces[group * pieces + tid];
+            for (int i = tid; i < min(n, Parts::LISTED_EACH); i += THREADS) P.found[mine * Parts::LISTED_EACH + i] = S.found[i];
+            if (tid == 0) P.n_listed[mine] = n;
+        }
+    }
+}
+template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const Args A)
+{
+    __shared__ Shared S;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x;
+    const Given G(A, row);
+    const Parts P(A.workspace, (size_t)A.rows, (size_t)A.rows * A.groups);
+    const size_t first = (size_t)row * A.groups;
+    if (tid < PIECES) S.pieces[tid] = P.pieces[(size_t)row * PIECES + tid];
+    Bins B = P.bins[row];
+    const float most = largest_of_row(P, first, A.groups, lane);
+    if (most == -__builtin_inff()) {      // nothing that may be drawn
+        if (tid == 0) global_at<int>(A.tokens)[row] = -1;
+        return;
+    }
+    const Row R(G, A.vocab, most);
+    const Cut C(A.groups, A.vocab, Tiles<E>::TILE);
+    if (R.by_count || R.by_weight) {
+        // the parts' candidates one after the other; one that has more than its room: as if they were too many
+        const uint32_t has = lane < A.groups ? P.n_listed[first + lane] : 0, upto = up_to_lane(has > Parts::LISTED_EACH ? (uint32_t)LISTED + 1 : has), n = of_lane(upto, 63);
+        if (tid == 0) S.begin_list(n);
+        if (n <= LISTED) {
+            for (int g = wave; g < A.groups; g += WAVES) {
+                const int count = of_lane(has, g), to = of_lane(upto, g) - count;
+                for (int i = lane; i < count; i += 64) S.found[to + i] = P.found[(first + g) * Parts::LISTED_EACH + i];
+            }
+        }
+    } else {
+        B = Bins();
+    }
+    __syncthreads();
+    const Place border = settle<E>(S, A, row, R, B, C, tid, lane, wave);
+    pick<E>(S, A, row, R, border, C, lane, wave);
+}
+
+constexpr int MAX_ROWS = 1 << 20;
 constexpr long long MAX_STRIDE = 1ll << 40;
+
+// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE tiles at least
+constexpr int SHARE = 16, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
+int compute_units() { return std::max(mx::device_groups(), 2); }
+int groups_of(int rows, int tiles, int compute_units)
+{
+    int groups = 1;
+    if (tiles <= SINGLE) return 1;
+    while (groups < MOST_GROUPS && 2ll * groups * rows <= compute_units && tiles >= 2 * groups * SHARE) groups *= 2;
+    return groups;
+}
+
+template <class E, int HELD> void launch_parts(const Args &A, hipStream_t stream)
+{
+    const dim3 parts((unsigned)(A.rows * A.groups)), threads(THREADS);
+    hipLaunchKernelGGL((part_kernel<E, MAXIMUM, HELD>), parts, threads, 0, stream, A);
+    if (A.top_k || A.top_p) hipLaunchKernelGGL((part_kernel<E, HISTOGRAM, HELD>), parts, threads, 0, stream, A);
+    hipLaunchKernelGGL((part_kernel<E, COLLECT, HELD>), parts, threads, 0, stream, A);
+}
+template <class E> int launch(Args A, hipStream_t stream)
+{
+    const int tiles = (A.vocab + Tiles<E>::TILE - 1) / Tiles<E>::TILE;
+    const dim3 rows((unsigned)A.rows), threads(THREADS);
+    // with top-k alone, a row's few tokens are found by one workgroup before several have met
+    A.groups = A.top_k && !A.top_p && tiles <= 16 * WAVES ? 1 : groups_of(A.rows, tiles, compute_units());
+    if (A.groups > 1) {
+        const int of_group = (tiles + A.groups - 1) / A.groups;
+        if (of_group <= 4 * WAVES)
+            launch_parts<E, 4>(A, stream);
+        else if (of_group <= 16 * WAVES)
+            launch_parts<E, 16>(A, stream);
+        else
+            launch_parts<E, 0>(A, stream);
+        hipLaunchKernelGGL((token_kernel<E>), rows, threads, 0, stream, A);
+    } else if (tiles <= 4 * WAVES) {
+        hipLaunchKernelGGL((row_kernel<E, 4>), rows, threads, 0, stream, A);
+    } else if (tiles <= 16 * WAVES) {
+        hipLaunchKernelGGL((row_kernel<E, 16>), rows, threads, 0, stream, A);
+    } else {
+        hipLaunchKernelGGL((row_kernel<E, 0>), rows, threads, 0, stream, A);
+    }
+    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+}
 
 }  // namespace
 }  // namespace sample
@@ -382,23 +969,28 @@ constexpr long long MAX_STRIDE = 1ll << 40;
 
 using namespace rb::sample;
 
+extern "C" size_t rb_sample_workspace_bytes(int dtype, int rows, int vocab)
+{
+    if ((dtype != RB_F16 && dtype != RB_BF16 && dtype != RB_F32) || rows < 1 || rows > MAX_ROWS || vocab < 1 || vocab > MAX_VOCAB) return 0;
+    const int tile = 64 * (dtype == RB_F32 ? F32::N : F16::N), tiles = (vocab + tile - 1) / tile, units = compute_units();
+    // whatever fewer rows take: no more parts than compute units, of rows that have two at least
+    return groups_of(1, tiles, units) > 1 ? Parts::bytes(units / 2, units) : 0;
+}
+
 extern "C" int rb_sample(const void *logits, int dtype, long long stride, int rows, int vocab, const float *u, const float *temperature, const int32_t *top_k,
-                         const float *top_p, const float *min_p, int32_t *tokens, void *stream)
+                         const float *top_p, const float *min_p, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!logits || !u || !tokens) return RB_ERR_NULL;
     if (dtype != RB_F16 && dtype != RB_BF16 && dtype != RB_F32) return RB_ERR_UNSUPPORTED;
     if (rows < 1 || rows > MAX_ROWS || vocab < 1 || vocab > MAX_VOCAB || stride < vocab || stride >= MAX_STRIDE) return RB_ERR_SHAPE;
     const int size = dtype == RB_F32 ? 4 : 2;
     if ((uintptr_t)logits % size != 0 || (((uintptr_t)u | (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)tokens) & 3)) return RB_ERR_ALIGN;
-    const Args A = {rb::address_of(logits), rb::address_of(u), rb::address_of(temperature), rb::address_of(top_k), rb::address_of(top_p), rb::address_of(min_p),
-                    rb::address_of(tokens), stride * size, rows, vocab};
-    const dim3 grid((unsigned)rows), threads(THREADS);
+    if (workspace_bytes < rb_sample_workspace_bytes(dtype, rows, vocab) || (workspace_bytes && !workspace)) return RB_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15) return RB_ERR_ALIGN;
+    Args A = {};
+    A.logits = rb::address_of(logits), A.u = rb::address_of(u), A.temperature = rb::address_of(temperature), A.top_k = rb::address_of(top_k);
+    A.top_p = rb::address_of(top_p), A.min_p = rb::address_of(min_p), A.tokens = rb::address_of(tokens), A.workspace = rb::address_of(workspace);
+    A.stride = stride * size, A.rows = rows, A.vocab = vocab;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == RB_F16)
-        hipLaunchKernelGGL((sample_kernel<F16>), grid, threads, 0, st, A);
-    else if (dtype == RB_BF16)
-        hipLaunchKernelGGL((sample_kernel<BF16>), grid, threads, 0, st, A);
-    else
-        hipLaunchKernelGGL((sample_kernel<F32>), grid, threads, 0, st, A);
-    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+    return dtype == RB_F16 ? launch<F16>(A, st) : dtype == RB_BF16 ? launch<BF16>(A, st) : launch<F32>(A, st);
 }

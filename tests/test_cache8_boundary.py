@@ -86,8 +86,8 @@ def test_attention_refusals():
     assert rb.lib.rb_attn_cache8_workspace_bytes(_C(dim=72), 4, 2, 5) == 0
 
 
-def _sample(logits=0x100, dtype=rb.RB_F16, stride=50, rows=3, vocab=50, u=0x200, temperature=0x300, top_k=0x400, top_p=0x500, min_p=0x600, tokens=0x700):
-    return rb.lib.rb_sample(logits, dtype, stride, rows, vocab, u, temperature, top_k, top_p, min_p, tokens, None)
+def _sample(logits=0x100, dtype=rb.RB_F16, stride=50, rows=3, vocab=50, u=0x200, temperature=0x300, top_k=0x400, top_p=0x500, min_p=0x600, tokens=0x700, ws=0x1000, size=1 << 30):
+    return rb.lib.rb_sample(logits, dtype, stride, rows, vocab, u, temperature, top_k, top_p, min_p, tokens, ws, size, None)
 
 
 def test_sample_refusals():
@@ -99,6 +99,15 @@ def test_sample_refusals():
     assert _sample(logits=0x101) == rb.RB_ERR_ALIGN and _sample(logits=0x102, dtype=rb.RB_F32) == rb.RB_ERR_ALIGN
     for name in ("u", "temperature", "top_k", "top_p", "min_p", "tokens"):
         assert _sample(**{name: 0x202}) == rb.RB_ERR_ALIGN, name
+    need = rb.lib.rb_sample_workspace_bytes(rb.RB_F16, 3, 400000)
+    large = dict(vocab=400000, stride=400000)
+    assert need > 0 and _sample(size=need - 1, **large) == rb.RB_ERR_WORKSPACE and _sample(ws=None, **large) == rb.RB_ERR_WORKSPACE and _sample(ws=0x1008, **large) == rb.RB_ERR_ALIGN
+    # so many serve every smaller call
+    sizes = [(dtype, rows, vocab) for dtype in (rb.RB_F16, rb.RB_F32) for rows in (1, 3, 40, 300, 1 << 20) for vocab in (1, 5000, 40000, 400000, 1 << 22)]
+    for dtype, rows, vocab in sizes:
+        most = rb.lib.rb_sample_workspace_bytes(dtype, rows, vocab)
+        assert all(rb.lib.rb_sample_workspace_bytes(d, r, v) <= most for d, r, v in sizes if d == dtype and r <= rows and v <= vocab)
+    assert rb.lib.rb_sample_workspace_bytes(rb.RB_F16, 0, 5) == rb.lib.rb_sample_workspace_bytes(5, 1, 400000) == 0
 
 
 def test_binding_refuses_host_tensors_and_wrong_types():

@@ -152,6 +152,12 @@ def test_temperatures_from_tiny_to_infinite():
     torch.cuda.synchronize()
     X, got = x.double().cpu().numpy(), got.tolist()
     assert got[:2] == [int(X[0].argmax()), int(X[1].argmax())] and got[2] == oracle.next_token(X[2], float(np.float32(u[2])), 1e-3)
+    low = x[:4].clone()      # logits of the type's lowest value beside others, at temperatures where what lies between overflows in every way
+    low[:, ::2] = torch.finfo(F32).min
+    cold = [1e-45, 1e-30, 1e-20, 1.0]
+    got_low = rb.rb_sample(low, _f32(u[:4]), temperature=_f32(cold))
+    torch.cuda.synchronize()
+    assert got_low.tolist()[:3] == [int(r.argmax()) for r in low[:3].cpu()] and got_low.tolist()[3] == oracle.next_token(low[3].cpu().numpy(), float(np.float32(u[3])))
     for i in (3, 4, 5):      # all alike, to 1e-3: the token's number is u's share of them
         assert abs(got[i] - u[i] * 2000) < 3
     assert got[6] == oracle.next_token(X[6], float(np.float32(u[6])), float(np.float32(1e38)))
