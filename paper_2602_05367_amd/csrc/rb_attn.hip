@@ -437,13 +437,13 @@ extern "C" int rb_attn_prompt(const rb_heads *H, const void *q, const void *k, c
 
 namespace {
 
-// A call over a cache: `C` as one of 16 bits, its strides in elements of `size` bytes
-size_t paged_workspace_bytes(const rb_cache &C, int heads, int n_seqs, int tokens)
+// Calls over a cache: `C` as one of 16 bits, its strides in elements of `size` bytes
+size_t paged_workspace_bytes(const rb_cache &C, bool in8, int heads, int n_seqs, int tokens)
 {
     if (heads < 1 || heads % C.kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
     const int units = rb::mx::device_groups(), group = heads / C.kv_heads;
     // whichever kernel a call of up to so many tokens and sequences and its table's width will choose
-    const size_t few = few_applies(1, n_seqs, group, 0) ? few_workspace_bytes(C.kv_heads, C.dim, units) : 0;
+    const size_t few = few_applies(1, n_seqs, group, 0) ? few_workspace_bytes(C.kv_heads, C.dim, in8, units) : 0;
     return std::max(few, parts_workspace_bytes(C.kv_heads, group, C.dim, units));
 }
 int paged(const rb_cache &C, int size, const uint8_t *k_exp, const uint8_t *v_exp, const void *q, long long q_token, long long q_head, int heads, const int32_t *first,
@@ -457,7 +457,7 @@ int paged(const rb_cache &C, int size, const uint8_t *k_exp, const uint8_t *v_ex
     if (check_scale(scale) != RB_OK) return RB_ERR_VALUE;
     if (((uintptr_t)q | (uintptr_t)o) & 15) return RB_ERR_ALIGN;
     if (((uintptr_t)first | (uintptr_t)lengths | (uintptr_t)table) & 3) return RB_ERR_ALIGN;
-    if (workspace_bytes < paged_workspace_bytes(C, heads, n_seqs, tokens) || (workspace_bytes && !workspace)) return RB_ERR_WORKSPACE;
+    if (workspace_bytes < paged_workspace_bytes(C, size == 1, heads, n_seqs, tokens) || (workspace_bytes && !workspace)) return RB_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15) return RB_ERR_ALIGN;
     Args A = {};
     A.q = side(q, q_token, q_head);
@@ -481,7 +481,7 @@ rb_cache as16(const rb_cache8 &C) { return {C.k, C.v, C.pages, C.page_tokens, C.
 
 extern "C" size_t rb_attn_paged_workspace_bytes(const rb_cache *C, int heads, int n_seqs, int tokens)
 {
-    return check_cache(C) == RB_OK ? paged_workspace_bytes(*C, heads, n_seqs, tokens) : 0;
+    return check_cache(C) == RB_OK ? paged_workspace_bytes(*C, false, heads, n_seqs, tokens) : 0;
 }
 
 extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,
@@ -494,7 +494,7 @@ extern "C" int rb_attn_paged(const rb_cache *C, const void *q, long long q_token
 
 extern "C" size_t rb_attn_cache8_workspace_bytes(const rb_cache8 *C, int heads, int n_seqs, int tokens)
 {
-    return check_cache8(C) == RB_OK ? paged_workspace_bytes(as16(*C), heads, n_seqs, tokens) : 0;
+    return check_cache8(C) == RB_OK ? paged_workspace_bytes(as16(*C), true, heads, n_seqs, tokens) : 0;
 }
 
 extern "C" int rb_attn_cache8(const rb_cache8 *C, const void *q, long long q_token, long long q_head, int heads, const int32_t *first, const int32_t *lengths,

@@ -31,7 +31,7 @@ template <int D> __device__ __forceinline__ PartOfRows<D, ROWS> part_of(Address 
 }
 
 template <class T, int D, bool IN8>
-__global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
+__global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args A)
 {
     using L = Tile<D>;
     constexpr int SECOND = IN8 ? 16 : WAVES * L::bytes(KEYS);
@@ -151,15 +151,15 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         first_job = false;
     };
 
-    Rows8<D, KEYS> raw_ka, raw_va, raw_kb, raw_vb;
-    auto step = [&](int i, uint8_t *keys, uint8_t *values, [[maybe_unused]] Rows8<D, KEYS> &raw_k, [[maybe_unused]] Rows8<D, KEYS> &raw_v) RB_INLINE {
+    [[maybe_unused]] Rows8<D, KEYS> raw_k, raw_v;
+    auto step = [&](int i, uint8_t *keys, uint8_t *values) RB_INLINE {
         if (i > 0 && at.t == 0) {
             start();
             rows_arrived();
         }
         if constexpr (IN8) {
             raw_k.template write<T>(keys, 0, lane);
-            load8(i + 2, k_base, A.k_exp, raw_k);
+            load8(i + 1, k_base, A.k_exp, raw_k);
         } else {
             loads_arrived<3 * LOADS>();
         }
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         const v4u p[2] = {{wt[0], wt[1], wt[2], wt[3]}, {wt[4], wt[5], wt[6], wt[7]}}, p_rest[2] = {{rest[0], rest[1], rest[2], rest[3]}, {rest[4], rest[5], rest[6], rest[7]}};
         if constexpr (IN8) {
             raw_v.template write<T>(values, 0, lane);
-            load8(i + 2, v_base, A.v_exp, raw_v);
+            load8(i + 1, v_base, A.v_exp, raw_v);
         } else {
             loads_arrived<3 * LOADS>();
         }
@@ -230,11 +230,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
     ask_pages(ahead);
     start();
     if constexpr (IN8) {
-        load8(0, k_base, A.k_exp, raw_ka);
-        load8(0, v_base, A.v_exp, raw_va);
-        next_ahead();
-        load8(1, k_base, A.k_exp, raw_kb);
-        load8(1, v_base, A.v_exp, raw_vb);
+        load8(0, k_base, A.k_exp, raw_k);
+        load8(0, v_base, A.v_exp, raw_v);
         next_ahead();
     } else {
         load(0, k_base, ka);
@@ -245,9 +242,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
         next_ahead();
     }
     rows_arrived();
-    for (int i = 0; i < n && at.there(A); i += 2) {      // (past the last sequence only where the arrays are not in order)
-        step(i, ka, va, raw_ka, raw_va);
-        if (i + 1 < n && at.there(A)) step(i + 1, kb, vb, raw_kb, raw_vb);
+    for (int i = 0; i < n && at.there(A); i += IN8 ? 1 : 2) {      // (past the last sequence only where the arrays are not in order)
+        step(i, ka, va);
+        if constexpr (!IN8)
+            if (i + 1 < n && at.there(A)) step(i + 1, kb, vb);
     }
     loads_arrived();
 }
@@ -279,12 +277,12 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
         [&](int r) { return n_k - n_q + token(r) < 0; });
 }
 
-// one workgroup per compute unit, shared out over the key heads
-int groups_per_head(const Args &A, int compute_units) { return compute_units > A.kv_heads ? compute_units / A.kv_heads : 1; }
+// one workgroup per compute unit, two for a cache in 8 bits, shared out over the key heads
+int groups_per_head(int kv_heads, bool in8, int compute_units) { return std::max((in8 ? 2 : 1) * compute_units / kv_heads, 1); }
 
 template <class T, int D> int launch(const Args &A, int compute_units, hipStream_t stream)
 {
-    const int groups = groups_per_head(A, compute_units);
+    const int groups = groups_per_head(A.kv_heads, A.k_exp != 0, compute_units);
     const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, ROWS) * A.kv_heads;
     if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
     const dim3 grid((unsigned)(groups * A.kv_heads)), threads(64 * WAVES);
@@ -309,11 +307,9 @@ bool few_applies(int tokens, int n_seqs, int group, long long positions)
     return (long long)tokens * group <= (long long)ROWS * n_seqs && tiles < 0x7fffffffll;
 }
 
-size_t few_workspace_bytes(int kv_heads, int dim, int compute_units)
+size_t few_workspace_bytes(int kv_heads, int dim, bool in8, int compute_units)
 {
-    Args A = {};
-    A.kv_heads = kv_heads;
-    return (size_t)kv_heads * groups_per_head(A, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfRows<64, ROWS>::FLOATS : PartOfRows<128, ROWS>::FLOATS) * 4;
+    return (size_t)kv_heads * groups_per_head(kv_heads, in8, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfRows<64, ROWS>::FLOATS : PartOfRows<128, ROWS>::FLOATS) * 4;
 }
 
 int launch_few(const Args &A, int dtype, int compute_units, hipStream_t stream)

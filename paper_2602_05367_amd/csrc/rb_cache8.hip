@@ -79,11 +79,13 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
             for (int i = 0; i < 4; ++i) turn(x[i], y[i], i);
         }
     }
-    // the head's exponent, in every lane of it
+    // the head's exponent, in every lane of it (a wavefront with queries alone has none)
     float most = 0.f;
+    if (__ballot(there && !is_q)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bounded8<T>(x[i]), bounded8<T>(y[i])));
-    for (int d = 1; d < 1 << A.lanes_shift; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bounded8<T>(x[i]), bounded8<T>(y[i])));
+        for (int d = 1; d < 1 << A.lanes_shift; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    }
     if (!there || token >= end) return;      // behind the last sequence's end (padding): nobody's
     if (is_q) {
         uint8_t *to = global_at<uint8_t>(A.q_to) + ((long long)token * A.heads + head) * (C.dim * 2);
@@ -100,28 +102,31 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
     if (piece == 0) global_at<uint8_t>(is_v ? C.v_exp : C.k_exp)[exponents + ((long long)kvh << C.page_shift)] = (uint8_t)exponent;
 }
 
-// Sixteen elements per thread: one load, two stores.  A workgroup has `group` tokens, each of its wavefronts elements of one.
+// Sixteen elements of a key and of its value per thread: two loads, four stores.  A wavefront has elements of one token.
 template <class T>
 __global__ __launch_bounds__(256) void read8_kernel(const Cache8Args C, Address k_to, Address v_to, int waves)      // wavefronts of a token
 {
-    const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6), token = wave / waves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), token = wave / waves;
     if (token >= C.tokens) return;
     const int pieces = C.dim / 16, unit = wave % waves * 64 + lane, head = unit / pieces, piece = unit % pieces;
     int s, end, length;
     sequence_of_token(global_at<const int>(C.first), global_at<const int>(C.lengths), C.n_seqs, token, lane, s, end, length);
-    if (token >= end || head >= 2 * C.kv_heads) return;
-    const bool is_v = head >= C.kv_heads;
-    const int kvh = is_v ? head - C.kv_heads : head;
+    if (token >= end || head >= C.kv_heads) return;
     long long elements, exponents;
-    v4u lo = {}, hi = {};
+    v4u w[2] = {};
+    uint32_t exponent[2] = {};
     if (place_of(C, s, (long long)length - end + token, elements, exponents)) {
-        const v4u w = *(const v4u *)(global_at<const uint8_t>(is_v ? C.v : C.k) + elements + kvh * C.head_stride + piece * 16);
-        const uint32_t exponent = global_at<const uint8_t>(is_v ? C.v_exp : C.k_exp)[exponents + ((long long)kvh << C.page_shift)];
-        lo = widen8<T>((v2u){w.x, w.y}, unit8(exponent)), hi = widen8<T>((v2u){w.z, w.w}, unit8(exponent));
+        elements += head * C.head_stride + piece * 16, exponents += (long long)head << C.page_shift;
+        w[0] = *(const v4u *)(global_at<const uint8_t>(C.k) + elements), w[1] = *(const v4u *)(global_at<const uint8_t>(C.v) + elements);
+        exponent[0] = global_at<const uint8_t>(C.k_exp)[exponents], exponent[1] = global_at<const uint8_t>(C.v_exp)[exponents];
     }
-    uint8_t *to = global_at<uint8_t>(is_v ? v_to : k_to) + (((long long)token * C.kv_heads + kvh) * C.dim + piece * 16) * 2;
-    *(v4u *)to = lo;
-    *(v4u *)(to + 16) = hi;
+    const long long at = (((long long)token * C.kv_heads + head) * C.dim + piece * 16) * 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint8_t *to = global_at<uint8_t>(i ? v_to : k_to) + at;
+        *(v4u *)to = widen8<T>((v2u){w[i].x, w[i].y}, unit8(exponent[i]));
+        *(v4u *)(to + 16) = widen8<T>((v2u){w[i].z, w[i].w}, unit8(exponent[i]));
+    }
 }
 
 }  // namespace
@@ -179,7 +184,7 @@ extern "C" int rb_cache8_read(const rb_cache8 *C, const int32_t *first, const in
     if (((uintptr_t)k | (uintptr_t)v) & 15) return RB_ERR_ALIGN;
     if (((uintptr_t)first | (uintptr_t)lengths | (uintptr_t)table) & 3) return RB_ERR_ALIGN;
     const Cache8Args A = cache8_args(C, first, lengths, table, width, n_seqs, tokens);
-    const int waves = (int)(((long long)2 * C->kv_heads * (C->dim / 16) + 63) / 64);
+    const int waves = (int)(((long long)C->kv_heads * (C->dim / 16) + 63) / 64);
     const long long n = ((long long)tokens * waves + 3) / 4;
     if (n > 0x1fffffffll) return RB_ERR_SHAPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
