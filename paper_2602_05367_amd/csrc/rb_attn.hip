@@ -443,7 +443,7 @@ size_t paged_workspace_bytes(const rb_cache &C, bool in8, int heads, int n_seqs,
     if (heads < 1 || heads % C.kv_heads != 0 || n_seqs < 1 || tokens < 1) return 0;
     const int units = rb::mx::device_groups(), group = heads / C.kv_heads;
     // whichever kernel a call of up to so many tokens and sequences and its table's width will choose
-    const size_t few = few_applies(1, n_seqs, group, 0) ? few_workspace_bytes(C.kv_heads, C.dim, in8, units) : 0;
+    const size_t few = few_applies(1, n_seqs, group, 0) ? (in8 ? few8_workspace_bytes : few_workspace_bytes)(C.kv_heads, C.dim, units) : 0;
     return std::max(few, parts_workspace_bytes(C.kv_heads, group, C.dim, units));
 }
 int paged(const rb_cache &C, int size, const uint8_t *k_exp, const uint8_t *v_exp, const void *q, long long q_token, long long q_head, int heads, const int32_t *first,
@@ -472,7 +472,7 @@ int paged(const rb_cache &C, int size, const uint8_t *k_exp, const uint8_t *v_ex
     const int units = rb::mx::device_groups();
     A.wanted = groups_wanted(tokens, n_seqs, A.kv_heads, A.group, std::min((long long)width * C.page_tokens, 0x7fffffffll), units);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_applies(tokens, n_seqs, A.group, (long long)width * C.page_tokens)) return launch_few(A, C.dtype, units, st);
+    if (few_applies(tokens, n_seqs, A.group, (long long)width * C.page_tokens)) return (size == 1 ? launch_few8 : launch_few)(A, C.dtype, units, st);
     return launch(A, C.dtype, true, units, st);
 }
 rb_cache as16(const rb_cache8 &C) { return {C.k, C.v, C.pages, C.page_tokens, C.kv_heads, C.dim, C.dtype, C.page_stride, C.token_stride, C.head_stride}; }

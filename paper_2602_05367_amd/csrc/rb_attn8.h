@@ -48,6 +48,12 @@ template <class T> __device__ __forceinline__ uint32_t narrow8(const float (&x)[
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
 }
 
+// 16 bytes per lane from a buffer to LDS, one lane's after the other's (a function of its own: inside of another, the host's compiler does not take the size)
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 0);
+}
+
 // ROWS rows of a head on their way from a cache into a tile of T's, in registers: eight a load, which lie in one page.  Rows past the end of a buffer, and
 // elements past a head's last, are zeros.
 template <int D, int ROWS> struct Rows8 {
@@ -82,6 +88,13 @@ template <int D, int ROWS> struct Rows8 {
         }
     }
 };
+
+// four elements without the NaN among them
+__device__ __forceinline__ uint32_t without_nan8(uint32_t w)
+{
+    const uint32_t sevens = (w & 0x7f7f7f7fu) + 0x01010101u;      // 0x80 in the bytes that are NaN
+    return w & ~((sevens >> 7 & 0x01010101u) * 0xffu);
+}
 
 template <class T, int D>
 __device__ __forceinline__ void add_not_finite8(v16f (&sums)[D / 32], const uint8_t *from, uint32_t exponent, int dim, int h, bool seen)

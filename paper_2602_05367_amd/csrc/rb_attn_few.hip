@@ -13,29 +13,20 @@
 
 #include "rabit.h"
 #include "rb_attn.h"
-#include "rb_attn8.h"
+#include "rb_attn_few.h"
 #include "rb_attn_host.h"
-#include "rb_attn_shares.h"
 
 namespace rb {
 namespace attn {
 namespace {
 
-using few::Cursor, few::KEYS, few::ROWS, few::Shape, few::Shares;
-constexpr int WAVES = 4;
+using few::Cursor, few::KEYS, few::part_of, few::ROWS, few::Shape, few::Shares, few::WAVES;
 
-// the part that share w has of a job of which it does not have all: its first job (0) or its last (1)
-template <int D> __device__ __forceinline__ PartOfRows<D, ROWS> part_of(Address workspace, int kvh, int wavefronts, int w, int which)
-{
-    return PartOfRows<D, ROWS>(workspace, ((size_t)kvh * wavefronts + w) * 2 + which);
-}
-
-template <class T, int D, bool IN8>
-__global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args A)
+template <class T, int D>
+__global__ __launch_bounds__(64 * WAVES, 1) void few_kernel(const Args A)
 {
     using L = Tile<D>;
-    constexpr int SECOND = IN8 ? 16 : WAVES * L::bytes(KEYS);
-    __shared__ __attribute__((aligned(16))) uint8_t keys_a[WAVES * L::bytes(KEYS)], values_a[WAVES * L::bytes(KEYS)], keys_b[SECOND], values_b[SECOND];
+    __shared__ __attribute__((aligned(16))) uint8_t keys_a[WAVES * L::bytes(KEYS)], values_a[WAVES * L::bytes(KEYS)], keys_b[WAVES * L::bytes(KEYS)], values_b[WAVES * L::bytes(KEYS)];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kvh = blockIdx.x % A.kv_heads, wavefronts = (int)(gridDim.x / A.kv_heads) * WAVES, w = (int)(blockIdx.x / A.kv_heads) * WAVES + wave;
@@ -68,18 +59,6 @@ __global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) pages[i] = row[min((c.t * KEYS + i * 8) >> A.page_shift, A.width - 1)];
-        }
-    };
-    const uint32_t at8 = Rows8<D, KEYS>::at(A.k.token, A.dim, lane);
-    auto exponents_at = [&](Address exponents, int page, int r) RB_INLINE {
-        return global_at<const uint8_t>(exponents) + (((long long)min(max(page, 0), A.pages - 1) * A.kv_heads + kvh) << A.page_shift) + (r & ((1 << A.page_shift) - 1));
-    };
-    [[maybe_unused]] auto load8 = [&](int i, const uint8_t *base, Address exponents, Rows8<D, KEYS> &to) RB_INLINE {
-        const int r = ahead.t * KEYS, len = i < n ? ahead.n_k - r : 0;
-#pragma unroll
-        for (int j = 0; j < KEYS / 8; ++j) {
-            const int page = pages[A.page_shift >= 5 ? 0 : j];
-            to.load(j, base + place(page, r + j * 8), exponents_at(exponents, page, r + j * 8), A.k.token, len - j * 8, A.dim, at8, lane);
         }
     };
     // tile number i of the share, which `ahead` stands at; past the share's end loads count, but fetch nothing
@@ -136,10 +115,7 @@ __global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args
         if (found)
             for (int r = max(max(least + 1, 0) / KEYS, from_t) * KEYS; r < min((at.t + 1) * KEYS, at.n_k); ++r) {
                 const int page = table_u[(long long)at.s * A.width + (r >> A.page_shift)];
-                if constexpr (IN8)
-                    add_not_finite8<T, D>(sums, v_base + place(page, r), *exponents_at(A.v_exp, page, r), A.dim, h, r <= limit);
-                else
-                    add_not_finite<T, D>(sums, v_base + place(page, r), A.dim, h, r <= limit);
+                add_not_finite<T, D>(sums, v_base + place(page, r), A.dim, h, r <= limit);
             }
         total = over_halves_sum(total);
         if (from_t == 0 && at.t == at.shape.tiles - 1) {
@@ -151,21 +127,15 @@ __global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args
         first_job = false;
     };
 
-    [[maybe_unused]] Rows8<D, KEYS> raw_k, raw_v;
     auto step = [&](int i, uint8_t *keys, uint8_t *values) RB_INLINE {
         if (i > 0 && at.t == 0) {
             start();
             rows_arrived();
         }
-        if constexpr (IN8) {
-            raw_k.template write<T>(keys, 0, lane);
-            load8(i + 1, k_base, A.k_exp, raw_k);
-        } else {
-            loads_arrived<3 * LOADS>();
-        }
+        loads_arrived<3 * LOADS>();
         v16f x = {};
         stream_operands<D / 16, 4>([&](int k) RB_INLINE { return rows.read(keys, 0, k); }, [&](int k, v4u a) RB_INLINE { x = T::mfma(a, q[k], x); });
-        if constexpr (!IN8) load(i + 2, k_base, keys);
+        load(i + 2, k_base, keys);
         const int first_key = at.t * KEYS;
         if (first_key + KEYS - 1 > least) {
             const int seen = limit - first_key - 4 * h;
@@ -196,12 +166,7 @@ __global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args
             rest[e / 2] = T::pack(a - T::widen(wt[e / 2] & 0xffffu), z - T::widen(wt[e / 2] >> 16));
         }
         const v4u p[2] = {{wt[0], wt[1], wt[2], wt[3]}, {wt[4], wt[5], wt[6], wt[7]}}, p_rest[2] = {{rest[0], rest[1], rest[2], rest[3]}, {rest[4], rest[5], rest[6], rest[7]}};
-        if constexpr (IN8) {
-            raw_v.template write<T>(values, 0, lane);
-            load8(i + 1, v_base, A.v_exp, raw_v);
-        } else {
-            loads_arrived<3 * LOADS>();
-        }
+        loads_arrived<3 * LOADS>();
         if (least < min(first_key + KEYS, at.n_k) - 1) {      // some row does not see all of the tile's keys: see make_finite
             bool any = false;
 #pragma unroll
@@ -219,80 +184,35 @@ __global__ __launch_bounds__(64 * WAVES, IN8 ? 2 : 1) void few_kernel(const Args
             sums[k % B] = T::mfma(a, p[k / B], sums[k % B]);
             sums[k % B] = T::mfma(a, p_rest[k / B], sums[k % B]);
         });
-        if constexpr (!IN8) load(i + 2, v_base, values);
+        load(i + 2, v_base, values);
         next_ahead();
         if (i == n - 1 || at.t == at.shape.tiles - 1) finish();
         at.advance(A, entries);
     };
 
-    uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS);
-    uint8_t *const kb = IN8 ? ka : keys_b + wave * L::bytes(KEYS), *const vb = IN8 ? va : values_b + wave * L::bytes(KEYS);
+    uint8_t *const ka = keys_a + wave * L::bytes(KEYS), *const va = values_a + wave * L::bytes(KEYS), *const kb = keys_b + wave * L::bytes(KEYS), *const vb = values_b + wave * L::bytes(KEYS);
     ask_pages(ahead);
     start();
-    if constexpr (IN8) {
-        load8(0, k_base, A.k_exp, raw_k);
-        load8(0, v_base, A.v_exp, raw_v);
-        next_ahead();
-    } else {
-        load(0, k_base, ka);
-        load(0, v_base, va);
-        next_ahead();
-        load(1, k_base, kb);
-        load(1, v_base, vb);
-        next_ahead();
-    }
+    load(0, k_base, ka);
+    load(0, v_base, va);
+    next_ahead();
+    load(1, k_base, kb);
+    load(1, v_base, vb);
+    next_ahead();
     rows_arrived();
-    for (int i = 0; i < n && at.there(A); i += IN8 ? 1 : 2) {      // (past the last sequence only where the arrays are not in order)
+    for (int i = 0; i < n && at.there(A); i += 2) {      // (past the last sequence only where the arrays are not in order)
         step(i, ka, va);
-        if constexpr (!IN8)
-            if (i + 1 < n && at.there(A)) step(i + 1, kb, vb);
+        if (i + 1 < n && at.there(A)) step(i + 1, kb, vb);
     }
     loads_arrived();
 }
 
-// A job that several wavefronts had parts of
-template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(const Args A, int wavefronts, int joined)
-{
-    const int lane = threadIdx.x & 63, kvh = blockIdx.x % A.kv_heads, block = blockIdx.x / A.kv_heads, row0 = blockIdx.y * joined;
-    const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
-    const Sums<Shape> sums_of(A, first, lengths, lane);
-    const int s = __builtin_amdgcn_readfirstlane(sums_of.of_block(block));
-    int q0, q1, length;
-    sums_of.entries(s, q0, q1, length);
-    const Shape shape = Shape::of(A, q0, q1, length);
-    const int b = block - block_start(q0, s, A.group, ROWS);
-    if (b < 0 || b >= shape.blocks || b * ROWS + row0 >= shape.rows) return;
-    const Shares shares(sums_of.before(A.n_seqs), wavefronts);
-    const int from = sums_of.before(s) + b * shape.tiles;
-    int w0, w1;
-    if (!shares.of_job(from, shape.tiles, w0, w1) || w0 == w1) return;      // (one: it has stored the result)
-    const bool starts_inside = shares.start(w0) < from;      // the first part is that share's last, all others are their shares' first
-    const int n_q = shape.rows / A.group, n_k = positions(length, A.width, A.page_shift);
-    q0 = min(max(q0, 0), A.tokens_q);
-    auto token = [&](int r) { return (b * ROWS + r) / A.group; };
-    join_rows<T, D>(
-        joined, w1 - w0 + 1, row0, min(shape.rows - b * ROWS - row0, joined), A.dim,
-        [&](int i) { return part_of<D>(A.parts, kvh, wavefronts, w0 + i, i == 0 && starts_inside ? 1 : 0); },
-        [&](int r) { return global_at<uint8_t>(A.o) + ((long long)(q0 + token(r)) * A.heads + kvh * A.group + (b * ROWS + r) % A.group) * (A.dim * 2); },
-        [&](int r) { return n_k - n_q + token(r) < 0; });
-}
-
-// one workgroup per compute unit, two for a cache in 8 bits, shared out over the key heads
-int groups_per_head(int kv_heads, bool in8, int compute_units) { return std::max((in8 ? 2 : 1) * compute_units / kv_heads, 1); }
+// one workgroup per compute unit, shared out over the key heads
+int groups_per_head(int kv_heads, int compute_units) { return std::max(compute_units / kv_heads, 1); }
 
 template <class T, int D> int launch(const Args &A, int compute_units, hipStream_t stream)
 {
-    const int groups = groups_per_head(A.kv_heads, A.k_exp != 0, compute_units);
-    const long long jobs = block_numbers(A.tokens_q, A.n_seqs, A.group, ROWS) * A.kv_heads;
-    if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
-    const dim3 grid((unsigned)(groups * A.kv_heads)), threads(64 * WAVES);
-    if (A.k_exp)
-        hipLaunchKernelGGL((few_kernel<T, D, true>), grid, threads, 0, stream, A);
-    else
-        hipLaunchKernelGGL((few_kernel<T, D, false>), grid, threads, 0, stream, A);
-    const int rows = (int)std::min((long long)ROWS, (long long)A.tokens_q * A.group), joined = rows_joined(jobs, rows);      // rows of one job, at most
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs, (rows + joined - 1) / joined), dim3(256), 0, stream, A, groups * WAVES, joined);
-    return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
+    return few::launch<T, D>(A, groups_per_head(A.kv_heads, compute_units), stream, [&](dim3 grid, dim3 threads) { hipLaunchKernelGGL((few_kernel<T, D>), grid, threads, 0, stream, A); });
 }
 
 }  // namespace
@@ -307,10 +227,7 @@ bool few_applies(int tokens, int n_seqs, int group, long long positions)
     return (long long)tokens * group <= (long long)ROWS * n_seqs && tiles < 0x7fffffffll;
 }
 
-size_t few_workspace_bytes(int kv_heads, int dim, bool in8, int compute_units)
-{
-    return (size_t)kv_heads * groups_per_head(kv_heads, in8, compute_units) * WAVES * 2 * (dim <= 64 ? PartOfRows<64, ROWS>::FLOATS : PartOfRows<128, ROWS>::FLOATS) * 4;
-}
+size_t few_workspace_bytes(int kv_heads, int dim, int compute_units) { return few::workspace_bytes(kv_heads, dim, groups_per_head(kv_heads, compute_units)); }
 
 int launch_few(const Args &A, int dtype, int compute_units, hipStream_t stream)
 {

@@ -48,8 +48,11 @@ inline int rows_joined(long long jobs, long long rows) { return jobs * rows <= 2
 
 // paged calls with few rows per sequence (rb_attn_few.hip), of sequences of up to `positions` positions
 bool few_applies(int tokens, int n_seqs, int group, long long positions);
-size_t few_workspace_bytes(int kv_heads, int dim, bool in8, int compute_units);
+size_t few_workspace_bytes(int kv_heads, int dim, int compute_units);
 int launch_few(const Args &A, int dtype, int compute_units, hipStream_t stream);
+// the same over a cache in 8 bits (rb_attn_few8.hip)
+size_t few8_workspace_bytes(int kv_heads, int dim, int compute_units);
+int launch_few8(const Args &A, int dtype, int compute_units, hipStream_t stream);
 
 inline Side side(const void *p, long long token, long long head) { return {rb::address_of(p), token * 2, head * 2}; }
 
