@@ -51,7 +51,7 @@ template <class T> __device__ __forceinline__ uint32_t narrow8(const float (&x)[
 // 16 bytes per lane from a buffer to LDS, one lane's after the other's (a function of its own: inside of another, the host's compiler does not take the size)
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t offset)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 2);
 }
 
 // ROWS rows of a head on their way from a cache into a tile of T's, in registers: eight a load, which lie in one page.  Rows past the end of a buffer, and

@@ -25,6 +25,9 @@ template <int D> struct Tile8 {
     static __device__ __forceinline__ int spread(int r) { return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3; }
 };
 
+constexpr int XCDS = 8;
+__host__ __device__ __forceinline__ int heads_together(int kv_heads) { return kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1; }
+
 template <class T, int D>
 __global__ __launch_bounds__(64 * WAVES, 2) void few8_kernel(const Args A)
 {
@@ -34,7 +37,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void few8_kernel(const Args A)
     __shared__ __attribute__((aligned(16))) float units[WAVES * KEYS];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kvh = blockIdx.x % A.kv_heads, wavefronts = (int)(gridDim.x / A.kv_heads) * WAVES, w = (int)(blockIdx.x / A.kv_heads) * WAVES + wave;
+    // A workgroup's wavefronts have the same share of up to four heads: rows of these lie next to each other.  Those that have the same of the others are on the same XCD.
+    const int wavefronts = A.wanted, together = heads_together(A.kv_heads), others = A.kv_heads / together;
+    const int turn = (int)blockIdx.x / XCDS, kvh = turn % others * together + wave % together, w = (turn / others * XCDS + (int)blockIdx.x % XCDS) * (WAVES / together) + wave / together;
     const int *first = global_at<const int>(A.first_q), *lengths = global_at<const int>(A.first_k);
     typedef const __attribute__((address_space(4))) int *Uniform;
     const Uniform table_u = (Uniform)global_at<const int>(A.table);
@@ -283,9 +288,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void few8_kernel(const Args A)
 // two workgroups per compute unit, shared out over the key heads
 int groups_per_head(int kv_heads, int compute_units) { return std::max(2 * compute_units / kv_heads, 1); }
 
-template <class T, int D> int launch(const Args &A, int compute_units, hipStream_t stream)
+template <class T, int D> int launch(Args A, int compute_units, hipStream_t stream)
 {
-    return few::launch<T, D>(A, groups_per_head(A.kv_heads, compute_units), stream, [&](dim3 grid, dim3 threads) { hipLaunchKernelGGL((few8_kernel<T, D>), grid, threads, 0, stream, A); });
+    const int groups = groups_per_head(A.kv_heads, compute_units), together = heads_together(A.kv_heads);
+    A.wanted = groups * WAVES;
+    const int shares = A.wanted / (WAVES / together), turns = (shares + XCDS - 1) / XCDS;      // workgroups of as many heads; those past the last share find no work
+    return few::launch<T, D>(A, groups, stream, [&](dim3, dim3 threads) { hipLaunchKernelGGL((few8_kernel<T, D>), dim3((unsigned)(turns * XCDS * (A.kv_heads / together))), threads, 0, stream, A); });
 }
 
 }  // namespace

@@ -24,7 +24,7 @@ struct Append8Args {
     Cache8Args c;
     Side q, k_from, v_from;
     Address q_to, cos, sin;
-    int heads, rotary, table_rows, blocks, lanes_shift;      // lanes of a head: the power of two that holds its pieces
+    int heads, rotary, table_rows, blocks, lanes_shift, query_units;      // lanes of a head: the power of two that holds its pieces; threads of a token for its queries
 };
 
 // Where a position lies in the cache, behind the first head's elements and exponents; false: nowhere
@@ -40,61 +40,76 @@ __device__ __forceinline__ bool place_of(const Cache8Args &C, int s, long long p
 
 // Element pairs are turned as in append_kernel (rb_cache.hip), eight elements per thread: four of either half of a head, or eight in a row.  Keys and values are then held in
 // units of a power of two of the head's own, so x / unit is exact and the one rounding is that to e4m3: the largest |x| of the head is found
-// among its lanes, a power of two of them.  A workgroup has elements of one token and finds its sequence itself.
+// among its lanes, a power of two of them.  A workgroup has elements of one token and finds its sequence itself; a wavefront has queries, four heads to a thread, or keys and values.
+constexpr int QUERIES = 4;
 template <class T, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
 {
     const Cache8Args &C = A.c;
     const int token = blockIdx.x / A.blocks, part = blockIdx.x % A.blocks, lane = threadIdx.x & 63;
-    const int unit = part * 256 + threadIdx.x, head = unit >> A.lanes_shift, piece = unit & ((1 << A.lanes_shift) - 1);
-    const bool there = head < A.heads + 2 * C.kv_heads && piece * 8 < C.dim;
-    const bool is_q = head < A.heads, is_v = head >= A.heads + C.kv_heads, turned = !is_v && piece * 8 < A.rotary;
-    const int kvh = is_q ? head : head - A.heads - (is_v ? C.kv_heads : 0);
+    const int first_unit = __builtin_amdgcn_readfirstlane(part * 256 + (threadIdx.x & 192)), unit = first_unit + lane;
+    const bool queries = first_unit < A.query_units;      // (whole wavefronts)
+    const int piece = unit & ((1 << A.lanes_shift) - 1), head = queries ? (unit >> A.lanes_shift) * QUERIES : (unit - A.query_units) >> A.lanes_shift;
+    const bool is_v = !queries && head >= C.kv_heads, turned = !is_v && piece * 8 < A.rotary;
+    const int heads = queries ? A.heads : 2 * C.kv_heads, mine = piece * 8 < C.dim ? min(heads - head, queries ? QUERIES : 1) : 0, kvh = is_v ? head - C.kv_heads : head;
     const int at_x = piece * (INTERLEAVED || !turned ? 8 : 4), at_y = INTERLEAVED || !turned ? at_x + 4 : at_x + A.rotary / 2;      // elements
-    Four a = {}, b = {};
-    if (there) {      // on the way while the place is looked up
-        const Side &from_side = is_q ? A.q : is_v ? A.v_from : A.k_from;
+    Four a[QUERIES] = {}, b[QUERIES] = {};
+    {      // on the way while the place is looked up
+        const Side &from_side = queries ? A.q : is_v ? A.v_from : A.k_from;
         const uint8_t *from = global_at<const uint8_t>(from_side.at) + token * from_side.token + kvh * from_side.head;
-        a.w = *(const v2u *)(from + at_x * 2);
-        b.w = *(const v2u *)(from + at_y * 2);
+#pragma unroll
+        for (int i = 0; i < QUERIES; ++i)
+            if (i < mine) {
+                a[i].w = *(const v2u *)(from + i * from_side.head + at_x * 2);
+                b[i].w = *(const v2u *)(from + i * from_side.head + at_y * 2);
+            }
     }
     int s, end, length;
     sequence_of_token(global_at<const int>(C.first), global_at<const int>(C.lengths), C.n_seqs, token, lane, s, end, length);
+    if (token >= end) return;      // behind the last sequence's end (padding): nobody's
     const long long position = (long long)length - end + token;
-    float x[4], y[4];      // the elements from at_x and at_y on
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = T::widen(a.h[i]), y[i] = T::widen(b.h[i]);
-    if (turned && there) {
+    v4f c = {}, sn = {};
+    if (turned && mine > 0) {
         const long long row = min(max(position, 0ll), (long long)A.table_rows - 1) * (A.rotary / 2) + piece * 4;
-        const v4f c = *(const v4f *)(global_at<const float>(A.cos) + row), sn = *(const v4f *)(global_at<const float>(A.sin) + row);
-        auto turn = [&](float &u, float &w, int i) RB_INLINE {
-            const float t = u * c[i] - w * sn[i];
-            w = w * c[i] + u * sn[i];
-            u = t;
+        c = *(const v4f *)(global_at<const float>(A.cos) + row), sn = *(const v4f *)(global_at<const float>(A.sin) + row);
+    }
+    float x[4], y[4];      // the elements from at_x and at_y on
+    auto turn = [&](const Four &u, const Four &w) RB_INLINE {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = T::widen(u.h[i]), y[i] = T::widen(w.h[i]);
+        if (!turned) return;
+        auto pair = [&](float &f, float &g, int i) RB_INLINE {
+            const float t = f * c[i] - g * sn[i];
+            g = g * c[i] + f * sn[i];
+            f = t;
         };
         if constexpr (INTERLEAVED) {
-            turn(x[0], x[1], 0), turn(x[2], x[3], 1), turn(y[0], y[1], 2), turn(y[2], y[3], 3);
+            pair(x[0], x[1], 0), pair(x[2], x[3], 1), pair(y[0], y[1], 2), pair(y[2], y[3], 3);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) turn(x[i], y[i], i);
+            for (int i = 0; i < 4; ++i) pair(x[i], y[i], i);
         }
-    }
-    // the head's exponent, in every lane of it (a wavefront with queries alone has none)
-    float most = 0.f;
-    if (__ballot(there && !is_q)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bounded8<T>(x[i]), bounded8<T>(y[i])));
-        for (int d = 1; d < 1 << A.lanes_shift; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-    }
-    if (!there || token >= end) return;      // behind the last sequence's end (padding): nobody's
-    if (is_q) {
+    };
+    if (queries) {
         uint8_t *to = global_at<uint8_t>(A.q_to) + ((long long)token * A.heads + head) * (C.dim * 2);
-        *(v2u *)(to + at_x * 2) = turned ? (v2u){T::pack(x[0], x[1]), T::pack(x[2], x[3])} : a.w;
-        *(v2u *)(to + at_y * 2) = turned ? (v2u){T::pack(y[0], y[1]), T::pack(y[2], y[3])} : b.w;
+#pragma unroll
+        for (int i = 0; i < QUERIES; ++i)
+            if (i < mine) {
+                turn(a[i], b[i]);
+                *(v2u *)(to + i * C.dim * 2 + at_x * 2) = turned ? (v2u){T::pack(x[0], x[1]), T::pack(x[2], x[3])} : a[i].w;
+                *(v2u *)(to + i * C.dim * 2 + at_y * 2) = turned ? (v2u){T::pack(y[0], y[1]), T::pack(y[2], y[3])} : b[i].w;
+            }
         return;
     }
     long long elements, exponents;
     if (!place_of(C, s, position, elements, exponents)) return;      // (another's page is not written over)
+    turn(a[0], b[0]);
+    // the head's exponent, in every lane of it
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bounded8<T>(x[i]), bounded8<T>(y[i])));
+    for (int d = 1; d < 1 << A.lanes_shift; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if (mine <= 0) return;
     const int exponent = exponent8(most);
     uint8_t *to = global_at<uint8_t>(is_v ? C.v : C.k) + elements + kvh * C.head_stride;
     *(uint32_t *)(to + at_x) = narrow8<T>(x, exponent);
@@ -155,7 +170,9 @@ extern "C" int rb_cache8_append(const rb_cache8 *C, const rb_heads *H, const voi
     A.q_to = rb::address_of(q_out), A.cos = rb::address_of(cos), A.sin = rb::address_of(sin);
     A.heads = q ? H->heads : 0, A.rotary = cos ? rotary : 0, A.table_rows = table_rows;
     while (8 << A.lanes_shift < C->dim) ++A.lanes_shift;
-    A.blocks = (int)((((long long)(A.heads + 2 * C->kv_heads) << A.lanes_shift) + 255) / 256);
+    const long long query_units = (((long long)((A.heads + QUERIES - 1) / QUERIES) << A.lanes_shift) + 63) / 64 * 64;
+    A.query_units = (int)query_units;
+    A.blocks = (int)((query_units + ((long long)2 * C->kv_heads << A.lanes_shift) + 255) / 256);
     const long long n = (long long)tokens * A.blocks;
     if (n > 0x7fffffffll) return RB_ERR_SHAPE;
     const dim3 grid((unsigned)n), threads(256);
