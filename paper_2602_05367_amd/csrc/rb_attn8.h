@@ -48,7 +48,8 @@ template <class T> __device__ __forceinline__ uint32_t narrow8(const float (&x)[
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
 }
 
-// 16 bytes per lane from a buffer to LDS, one lane's after the other's (a function of its own: inside of another, the host's compiler does not take the size)
+// 16 bytes per lane from a buffer to LDS, one lane's after the other's (a function of its own: inside of another, the host's compiler does not take the size).  Not kept by the caches: each
+// byte is used once (48 sequences of 250000 positions together: 110 us, kept 119)
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t offset)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 2);

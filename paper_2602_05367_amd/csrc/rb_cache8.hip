@@ -40,8 +40,11 @@ __device__ __forceinline__ bool place_of(const Cache8Args &C, int s, long long p
 
 // Element pairs are turned as in append_kernel (rb_cache.hip), eight elements per thread: four of either half of a head, or eight in a row.  Keys and values are then held in
 // units of a power of two of the head's own, so x / unit is exact and the one rounding is that to e4m3: the largest |x| of the head is found
-// among its lanes, a power of two of them.  A workgroup has elements of one token and finds its sequence itself; a wavefront has queries, four heads to a thread, or keys and values.
-constexpr int QUERIES = 4;
+// among its lanes, a power of two of them.  A workgroup has elements of one token and finds its sequence itself; a wavefront has queries, two heads to a thread, or keys and values.
+//
+// Bound: bytes, and for a single token the launch (one token, 40 heads of 128: 3.8 us).  16 prompts of 5992 tokens together, 64 heads of 128 over 8 of keys, interleaved (233 MB): 41 us,
+// 5.6 TB/s, a copy of as many bytes 36; 47 with one head of queries to a thread or four, 57 with these in pieces of 8 bytes and loads that lanes without a head branch around.
+constexpr int QUERIES = 2;
 template <class T, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
 {
@@ -54,14 +57,23 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
     const int heads = queries ? A.heads : 2 * C.kv_heads, mine = piece * 8 < C.dim ? min(heads - head, queries ? QUERIES : 1) : 0, kvh = is_v ? head - C.kv_heads : head;
     const int at_x = piece * (INTERLEAVED || !turned ? 8 : 4), at_y = INTERLEAVED || !turned ? at_x + 4 : at_x + A.rotary / 2;      // elements
     Four a[QUERIES] = {}, b[QUERIES] = {};
-    {      // on the way while the place is looked up
-        const Side &from_side = queries ? A.q : is_v ? A.v_from : A.k_from;
-        const uint8_t *from = global_at<const uint8_t>(from_side.at) + token * from_side.token + kvh * from_side.head;
+    {      // on the way while the place is looked up; lanes without a head, or with fewer, load others again
+        const bool there = mine > 0;
+        const Address side_at = queries ? A.q.at : is_v ? A.v_from.at : A.k_from.at;
+        const long long token_step = queries ? A.q.token : is_v ? A.v_from.token : A.k_from.token, head_step = queries ? A.q.head : is_v ? A.v_from.head : A.k_from.head;
+        const uint8_t *from = global_at<const uint8_t>(side_at) + token * token_step + (there ? kvh * head_step : 0);
+        const int x = there ? at_x * 2 : 0;
+        [[maybe_unused]] const int y = there ? at_y * 2 : 0;
 #pragma unroll
         for (int i = 0; i < QUERIES; ++i)
-            if (i < mine) {
-                a[i].w = *(const v2u *)(from + i * from_side.head + at_x * 2);
-                b[i].w = *(const v2u *)(from + i * from_side.head + at_y * 2);
+            if (i == 0 || queries) {
+                const uint8_t *head_from = from + min(i, max(mine - 1, 0)) * head_step;
+                if constexpr (INTERLEAVED) {
+                    const v4u w = *(const v4u *)(head_from + x);
+                    a[i].w = (v2u){w.x, w.y}, b[i].w = (v2u){w.z, w.w};
+                } else {
+                    a[i].w = *(const v2u *)(head_from + x), b[i].w = *(const v2u *)(head_from + y);
+                }
             }
     }
     int s, end, length;
@@ -96,8 +108,14 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
         for (int i = 0; i < QUERIES; ++i)
             if (i < mine) {
                 turn(a[i], b[i]);
-                *(v2u *)(to + i * C.dim * 2 + at_x * 2) = turned ? (v2u){T::pack(x[0], x[1]), T::pack(x[2], x[3])} : a[i].w;
-                *(v2u *)(to + i * C.dim * 2 + at_y * 2) = turned ? (v2u){T::pack(y[0], y[1]), T::pack(y[2], y[3])} : b[i].w;
+                const v4u w = turned ? (v4u){T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(y[0], y[1]), T::pack(y[2], y[3])} : (v4u){a[i].w.x, a[i].w.y, b[i].w.x, b[i].w.y};
+                uint8_t *const head_to = to + i * C.dim * 2;
+                if (INTERLEAVED || !turned) {      // 16 bytes in a row
+                    *(v4u *)(head_to + at_x * 2) = w;
+                } else {
+                    *(v2u *)(head_to + at_x * 2) = (v2u){w.x, w.y};
+                    *(v2u *)(head_to + at_y * 2) = (v2u){w.z, w.w};
+                }
             }
         return;
     }
@@ -108,16 +126,19 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bounded8<T>(x[i]), bounded8<T>(y[i])));
+    if (mine <= 0) most = 0.f;
     for (int d = 1; d < 1 << A.lanes_shift; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
     if (mine <= 0) return;
     const int exponent = exponent8(most);
-    uint8_t *to = global_at<uint8_t>(is_v ? C.v : C.k) + elements + kvh * C.head_stride;
+    const Address to_at = is_v ? C.v : C.k, exponents_at = is_v ? C.v_exp : C.k_exp;
+    uint8_t *to = global_at<uint8_t>(to_at) + elements + kvh * C.head_stride;
     *(uint32_t *)(to + at_x) = narrow8<T>(x, exponent);
     *(uint32_t *)(to + at_y) = narrow8<T>(y, exponent);
-    if (piece == 0) global_at<uint8_t>(is_v ? C.v_exp : C.k_exp)[exponents + ((long long)kvh << C.page_shift)] = (uint8_t)exponent;
+    if (piece == 0) global_at<uint8_t>(exponents_at)[exponents + ((long long)kvh << C.page_shift)] = (uint8_t)exponent;
 }
 
 // Sixteen elements of a key and of its value per thread: two loads, four stores.  A wavefront has elements of one token.
+// Bound: bytes.  16 sequences of 8 heads of 128, 100000 positions together (616 MB): 108 to 120 us, a copy of as many bytes 114; 333 tokens of 12 heads of 80: 3.4 us, the launch.
 template <class T>
 __global__ __launch_bounds__(256) void read8_kernel(const Cache8Args C, Address k_to, Address v_to, int waves)      // wavefronts of a token
 {

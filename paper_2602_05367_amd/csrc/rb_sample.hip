@@ -5,6 +5,12 @@
 // bin are candidates, which are ranked among themselves.  The token is then found in the order of the indexes: sums over pieces of the row, and within the piece that u falls into.
 //
 // Weights are whole numbers of units of 2^-30, their sums are of 64 bits: they depend on no order, so histograms may be summed by atomics.
+//
+// Bound: not by the row's bytes (256 rows of 128000 bf16 are 65 MB, 10 us), but by instructions and, with few rows, by the steps that follow each other.  A logit costs
+// a subtraction, two products, an exponential and its rounding to a whole number in the histogram and again in the sums: some 70 and 55 to 95 cycles per wavefront and element, 14 and 19 us of the 54
+// that those rows take with top-p; reading them and their maximum are 8, the borders, the candidates and the choice 6.  (Weights do not fit the registers beside the logits, to be computed once.)
+// Measured there: no filter 27 us, top-k of 50 24, top-p 54, all filters mixed 59, greedy 16.  One row of 32000 fp16: 14 us with top-k and top-p, 10 without, one launch, of which nine steps with
+// barriers between them are all but 2 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <type_traits>
@@ -19,6 +25,7 @@ namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64, PER_THREAD = 2, BINS = PER_THREAD * THREADS, BIN_BITS = 11, PIECES = 64, LISTED = 2 * THREADS;
 static_assert(BINS == 1 << BIN_BITS);
+// (2048 bins of -log2 w are 0.015 wide; twice as many took the same time: what is saved among the candidates is spent on clearing and adding up)
 constexpr float RANGE = 31.f;      // -log2 of the weights that round to nothing
 typedef unsigned long long Weight;
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -128,14 +135,14 @@ struct Shared {
     uint32_t wave_counts[USES][WAVES];
     float wave_max[WAVES];
     Reached reached[USES];
-    uint32_t n_listed;
+    uint32_t n_listed, n_candidates;
     Place found_place[2];
     Weight found_weight[2];
     int differ[2];
     // (before a list is used)
     __device__ __forceinline__ void begin_list(uint32_t n)
     {
-        n_listed = n;
+        n_listed = n, n_candidates = 0;
         for (int i = 0; i < 2; ++i) found_place[i] = 0, found_weight[i] = 0, differ[i] = 0;
     }
 };
@@ -307,7 +314,8 @@ template <class E> __device__ __forceinline__ float largest_of(v4u w)      // (N
     return t;
 }
 
-// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time
+// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 24 and
+// 30 us, top-p 54 and 60, greedy 16 and 25).  Sixteen tiles are what a wavefront of 128 registers has room for.
 template <class E, int HELD> struct Elements : Tiles<E> {
     // word j of each tile: one place of a vector, so that a loop over the tiles is one copy of its body (sixteen do not fit the instruction cache)
     typedef uint32_t Words __attribute__((ext_vector_type(HELD ? HELD : 1)));
@@ -722,20 +730,26 @@ template <class E> __device__ __forceinline__ Place settle(Shared &S, const Args
     if (B.count_bin == BINS && B.low == BINS) return 0;
     Place border = 0;
     Weight weight, left = B.all;
-    const int n = (int)S.n_listed;
-    if (n <= LISTED) {
-        for (int i = tid; i < n; i += THREADS) {
+    if (S.n_listed <= LISTED) {
+        // candidates into a list of their own; of the rest, which only a list of all that top-k can leave has, what lies before both borders is left
+        for (int i = tid; i < (int)S.n_listed; i += THREADS) {
             const Found f = S.found[i];
             const float below = R.scale.below(f.x);
-            S.listed[i] = {place(f.x, f.index), Scale::weight(below) | B.candidate((int)Row::bin_of(below))};
+            const int bin = (int)Row::bin_of(below);
+            const Weight what_for = B.candidate(bin);
+            if (what_for)
+                S.listed[atomicAdd(&S.n_candidates, 1u)] = {place(f.x, f.index), Scale::weight(below) | what_for};
+            else if (bin < B.sure && f.x >= R.least)
+                atomicAdd(&S.pieces[C.piece_of(f.index / Tiles<E>::TILE)], (Weight)Scale::weight(below));
         }
         __syncthreads();
+        const int n = (int)S.n_candidates;
         if (B.count_bin < BINS) {
             border = resolve(S, 0, FOR_COUNT, true, (Weight)R.top_k - B.count_before, n, weight, tid, lane);
             left = B.weight_before_count + weight;
         }
         if (R.by_weight) border = max(border, resolve(S, 1, FOR_WEIGHT, false, target_of(R.top_p, left) - B.weight_before_low, n, weight, tid, lane));
-        for (int i = tid; i < n; i += THREADS) {      // (a candidate of top-k alone lies behind top-p's border, or there is none; one that is none, before both or behind)
+        for (int i = tid; i < n; i += THREADS) {      // (a candidate of top-k alone lies behind top-p's border, or there is none)
             const Candidate c = S.listed[i];
             if (c.place >= border && c.place >= place(R.least, MAX_VOCAB - 1)) atomicAdd(&S.pieces[C.piece_of(index_of(c.place) / Tiles<E>::TILE)], c.weight & ONLY_WEIGHT);
         }
@@ -832,7 +846,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     pick<E>(S, A, row, R, border, C, lane, wave);
 }
 
-// Several workgroups do a row, in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
+// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 41 us, one workgroup each 60; one row 25 and 55), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
 // token.  What they hand on lies in the workspace.
 enum Step { MAXIMUM, HISTOGRAM, COLLECT };
 __device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
@@ -920,14 +934,16 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
 constexpr int MAX_ROWS = 1 << 20;
 constexpr long long MAX_STRIDE = 1ll << 40;
 
-// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE tiles at least
-constexpr int SHARE = 16, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
+// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 25.6 us with 4096, 25.2 with 2048, 27.6 with 8192; four of 151936
+// fp32 27.2 with 2048, 26.4 with 4096); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 15 us, four launches 30; 7 rows
+// of 50001 bf16, no filter: 13.6 and 14.6.  From there on several are faster: 128000 bf16 with top-p 25.6 us, one workgroup 45)
+constexpr int SHARE = 4096, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
 int compute_units() { return std::max(mx::device_groups(), 2); }
-int groups_of(int rows, int tiles, int compute_units)
+int groups_of(int rows, int tiles, int tile, int compute_units)
 {
     int groups = 1;
     if (tiles <= SINGLE) return 1;
-    while (groups < MOST_GROUPS && 2ll * groups * rows <= compute_units && tiles >= 2 * groups * SHARE) groups *= 2;
+    while (groups < MOST_GROUPS && 2ll * groups * rows <= compute_units && (long long)tiles * tile >= 2ll * groups * SHARE) groups *= 2;
     return groups;
 }
 
@@ -942,8 +958,9 @@ template <class E> int launch(Args A, hipStream_t stream)
 {
     const int tiles = (A.vocab + Tiles<E>::TILE - 1) / Tiles<E>::TILE;
     const dim3 rows((unsigned)A.rows), threads(THREADS);
-    // with top-k alone, a row's few tokens are found by one workgroup before several have met
-    A.groups = A.top_k && !A.top_p && tiles <= 16 * WAVES ? 1 : groups_of(A.rows, tiles, compute_units());
+    // with top-k alone, a row's few tokens are found by one workgroup before several have met (one row of 128000 bf16: the first 50 15.7 us, with
+    // sixteen workgroups 21.7; 300 20.6 and 22.7; more than 512, for which every bin counts, 39 and 22.7)
+    A.groups = A.top_k && !A.top_p && tiles <= 16 * WAVES ? 1 : groups_of(A.rows, tiles, Tiles<E>::TILE, compute_units());
     if (A.groups > 1) {
         const int of_group = (tiles + A.groups - 1) / A.groups;
         if (of_group <= 4 * WAVES)
@@ -974,7 +991,7 @@ extern "C" size_t rb_sample_workspace_bytes(int dtype, int rows, int vocab)
     if ((dtype != RB_F16 && dtype != RB_BF16 && dtype != RB_F32) || rows < 1 || rows > MAX_ROWS || vocab < 1 || vocab > MAX_VOCAB) return 0;
     const int tile = 64 * (dtype == RB_F32 ? F32::N : F16::N), tiles = (vocab + tile - 1) / tile, units = compute_units();
     // whatever fewer rows take: no more parts than compute units, of rows that have two at least
-    return groups_of(1, tiles, units) > 1 ? Parts::bytes(units / 2, units) : 0;
+    return groups_of(1, tiles, tile, units) > 1 ? Parts::bytes(units / 2, units) : 0;
 }
 
 extern "C" int rb_sample(const void *logits, int dtype, long long stride, int rows, int vocab, const float *u, const float *temperature, const int32_t *top_k,
