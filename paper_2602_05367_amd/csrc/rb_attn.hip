@@ -79,6 +79,9 @@ __device__ __forceinline__ Args with_shares(Args A, const Sums<Tiles> &tiles)
 // heads of 128: 64 tokens of 8 heads 12.4 -> 9.9 us, 512 of 32 16.3 -> 15.3, 1200 of 32 and 8 28.6 -> 25.3, 8192 of one head 141 -> 111, 6000 of 8 116 -> 96; heads of 64 3 to 10 %).
 // Beyond, two workgroups fill a compute unit as well as one of twice the size, without the join (2600 tokens of 32 and 8 heads, 656 workgroups, 67 and 78 us; eight sequences of 1000
 // tokens in all, 312 workgroups, 11.5 and 16.8).
+//
+// Of a cache in 8 bits, elements come into registers, are widened to T in their units there, and stored into the tile that the rest of the kernel knows (512 and seven new tokens on 21513 positions,
+// 32 and 8 heads: 114 us and 14 for the join; of 16 bits, where tiles go into LDS past the registers, 90 to 100 and 14).
 enum From { PACKED, PAGES, PAGES8 };      // where keys and values are: packed, in a cache, in a cache in 8 bits
 template <class T, int D, From FROM, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)
