@@ -219,7 +219,8 @@ def check(q, cache, table, hold, new, lengths, scale=None, label=""):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
-@pytest.mark.parametrize("heads,kv,dim,page", [(4, 4, 128, 16), (16, 2, 128, 64), (6, 2, 64, 8), (12, 1, 96, 32), (10, 1, 48, 256), (2, 2, 16, 16)])
+@pytest.mark.parametrize("heads,kv,dim,page", [(4, 4, 128, 16), (16, 2, 128, 64), (6, 2, 64, 8), (12, 1, 96, 32), (10, 1, 48, 256), (2, 2, 16, 16), (3, 3, 80, 64), (12, 6, 112, 16), (5, 5, 32, 8),
+                                                (16, 8, 128, 32), (40, 1, 64, 16), (7, 7, 128, 128)])
 def test_attention(heads, kv, dim, page, dtype):
     for n, (new, lengths) in enumerate(PAGED):
         rng = synth.child_rng(620, heads, dim, n)

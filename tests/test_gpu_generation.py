@@ -204,6 +204,21 @@ def test_shared_rows_with_masks_infinities_and_ties():
         check(x, u, **given, label=sorted(given))
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, torch.float32])
+def test_a_row_gives_the_same_token_alone_and_among_others(dtype):
+    """Alone many workgroups share it, among 300 it has one; sums do not depend on who adds them."""
+    rng = synth.child_rng(657)
+    vocab, n = 100003, 300
+    rows = _logits(rng, 4, vocab, dtype)
+    for i, given in enumerate((dict(), dict(top_k=700), dict(top_k=5), dict(top_p=0.93), dict(top_k=2000, top_p=0.97, min_p=1e-4))):
+        each = {name: torch.full((n,), value, dtype=torch.int32 if name == "top_k" else torch.float32, device="cuda") for name, value in given.items()}
+        u = _f32(rng.random(n))
+        many = rb.rb_sample(rows.repeat(n // 4, 1), u, **each)
+        for j in (0, 1, 2, 3, 130, 299):
+            alone = rb.rb_sample(rows[j % 4:j % 4 + 1], u[j:j + 1].clone(), **{name: x[:1].clone() for name, x in each.items()})
+            assert int(alone) == int(many[j]), (dtype, i, j)
+
+
 def test_two_streams_at_once():
     """Calls on two streams, each with a workspace and a cache of its own, interleaved."""
     rng = synth.child_rng(656)
