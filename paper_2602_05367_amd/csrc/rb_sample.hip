@@ -106,6 +106,13 @@ template <class V> __device__ __forceinline__ V up_to_lane(V v)
     v += moved<0x143, 0xc>(v);
     return v;
 }
+// The largest of a wavefront's lanes, or of its sixteens, whose last lanes then have it
+template <int CTRL, int ROWS> __device__ __forceinline__ float larger(float v)
+{
+    return fmaxf(v, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(v), (int)__float_as_uint(v), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float largest_of_sixteen(float v) { return larger<0x118, 0xf>(larger<0x114, 0xf>(larger<0x112, 0xf>(larger<0x111, 0xf>(v)))); }
+__device__ __forceinline__ float largest_of_lanes(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(larger<0x143, 0xc>(larger<0x142, 0xa>(largest_of_sixteen(v)))), 63)); }
 __device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 __device__ __forceinline__ Weight of_lane(Weight v, int lane) { return (Weight)of_lane((uint32_t)(v >> 32), lane) << 32 | of_lane((uint32_t)v, lane); }
 
@@ -134,16 +141,20 @@ struct Shared {
     Weight wave_weights[USES][WAVES];
     uint32_t wave_counts[USES][WAVES];
     float wave_max[WAVES];
+    double rate, cut;      // of the row: see Given
     Reached reached[USES];
     uint32_t n_listed, n_candidates;
     Place found_place[2];
     Weight found_weight[2];
-    int differ[2];
+    bool differ;
+    // what the threads' largest are counted in, where the list is to be
+    __device__ __forceinline__ uint32_t *tops() { return (uint32_t *)listed; }
     // (before a list is used)
     __device__ __forceinline__ void begin_list(uint32_t n)
     {
         n_listed = n, n_candidates = 0;
-        for (int i = 0; i < 2; ++i) found_place[i] = 0, found_weight[i] = 0, differ[i] = 0;
+        for (int i = 0; i < 2; ++i) found_place[i] = 0, found_weight[i] = 0;
+        differ = false;
     }
 };
 
@@ -228,24 +239,31 @@ struct Given {
           top_p(A.top_p ? global_at<const float>(A.top_p)[row] : 1.f), u(global_at<const float>(A.u)[row]), top_k(A.top_k ? global_at<const int>(A.top_k)[row] : 0)
     {
     }
+    __device__ __forceinline__ bool greedy() const { return !(temperature > 0.f); }
+    // What takes a quotient and a logarithm in 64 bits, by one wavefront each while the row is on its way: 2 log2(e) / T, and T log(min_p), which is how far below the largest min_p's border lies
+    __device__ __forceinline__ void derive(Shared &S, int wave) const
+    {
+        if (wave == WAVES - 1) S.rate = fmin(2 * 1.4426950408889634 / (greedy() ? 1.0 : (double)temperature), 0x1p+127);
+        if (wave == WAVES - 2 && min_p > 0.f && min_p < 1.f) S.cut = (double)temperature * log((double)min_p);
+    }
 };
 struct Row : Given {
     Scale scale;
     float least;      // no token below it is left (min-p; greedy: the largest alone)
     bool by_count, by_weight, infinite;      // filtered by top-k, by top-p; only logits of plus infinity are left, which count as 0 then
-    __device__ __forceinline__ Row(const Given &G, int vocab, float most) : Given(G)
+    __device__ __forceinline__ Row(const Given &G, const Shared &S, int vocab, float most) : Given(G)      // (after a barrier behind derive)
     {
         infinite = most == __builtin_inff();
         if (infinite) most = 0.f;
-        const bool greedy = !(temperature > 0.f);
+        const bool greedy = this->greedy();
         u = u >= 0.f && !greedy ? fminf(u, 0x1.fffffep-1f) : 0.f;
         by_count = !greedy && top_k >= 1 && top_k < vocab, by_weight = !greedy && top_p < 1.f;
         least = -0x1.fffffep+127f;
         if (greedy || min_p >= 1.f)
             least = most;
         else if (min_p > 0.f)      // w >= min_p: x >= max + T log(min_p), the smallest float that is
-            least = fmaxf(least, not_below((double)most + (double)temperature * log((double)min_p)));
-        const double c = fmin(2 * 1.4426950408889634 / (greedy ? 1.0 : (double)temperature), 0x1p+127);
+            least = fmaxf(least, not_below((double)most + S.cut));
+        const double c = S.rate;
         scale.half_max = 0.5f * most;
         scale.hi = (float)c;
         if ((double)scale.hi > c) scale.hi = __uint_as_float(__float_as_uint(scale.hi) - 1u);      // (lo not below zero: where both parts overflow, so does their sum)
@@ -323,13 +341,14 @@ template <class E, int HELD> struct Elements : Tiles<E> {
     float top[HELD ? HELD / 2 : 1];      // of a lane's elements, the largest of each two tiles
     using Tiles<E>::from;
     using Tiles<E>::to;
-    __device__ __forceinline__ Elements(const Tiles<E> &tiles) : Tiles<E>(tiles)
+    template <class Meanwhile> __device__ __forceinline__ Elements(const Tiles<E> &tiles, Meanwhile meanwhile) : Tiles<E>(tiles)
     {
         if constexpr (HELD != 0) {
             v4u w[HELD];
 #pragma unroll
             for (int i = 0; i < HELD; ++i)
                 if (from + i < to) w[i] = this->load(from + i);
+            meanwhile();
             if (from < to && this->is_cut(to - 1)) {
                 const v4u last = this->load_cut(to - 1);
 #pragma unroll
@@ -345,6 +364,8 @@ template <class E, int HELD> struct Elements : Tiles<E> {
                 top[i / 2] = from + i < to ? largest_of<E>(w[i]) : -__builtin_inff();
                 if (from + i + 1 < to) top[i / 2] = fmaxf(top[i / 2], largest_of<E>(w[i + 1]));
             }
+        } else {
+            meanwhile();
         }
     }
     template <class Use> __device__ __forceinline__ void each_tile(Use use) const
@@ -400,14 +421,14 @@ template <class E, int HELD> struct Elements : Tiles<E> {
     }
 };
 
+__device__ __forceinline__ Weight shuffled(Weight w, int d) { return (Weight)__shfl_xor((uint32_t)(w >> 32), d) << 32 | (uint32_t)__shfl_xor((uint32_t)w, d); }
 __device__ __forceinline__ float largest_of_workgroup(Shared &S, float t, int lane, int wave)
 {
-    for (int d = 1; d < 64; d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
+    static_assert(WAVES == 16);
+    t = largest_of_lanes(t);
     if (lane == 0) S.wave_max[wave] = t;
     __syncthreads();
-    t = S.wave_max[lane % WAVES];
-    for (int d = 1; d < WAVES; d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
-    return t;
+    return __uint_as_float(of_lane(__float_as_uint(largest_of_sixteen(S.wave_max[lane % WAVES])), 63));
 }
 
 __device__ __forceinline__ void clear_bins(Shared &S, int tid)
@@ -415,10 +436,16 @@ __device__ __forceinline__ void clear_bins(Shared &S, int tid)
     for (int i = tid; i < BINS; i += THREADS) S.counts[i] = 0, S.weights[i] = 0;
     __syncthreads();
 }
-// The bins before `end`
-template <class E, class Elements_> __device__ __forceinline__ void histogram(Shared &S, const Row &R, const Elements_ &elements, float end, int tid)
+// What is counted and listed from zero on (a barrier has to follow)
+__device__ __forceinline__ void clear_all(Shared &S, int tid)
 {
-    clear_bins(S, tid);
+    for (int i = tid; i < BINS; i += THREADS) S.counts[i] = 0, S.weights[i] = 0, S.tops()[i] = 0;
+    if (tid < PIECES) S.pieces[tid] = 0;
+    if (tid == 0) S.begin_list(0);
+}
+// The bins before `end`
+template <class E, class Elements_> __device__ __forceinline__ void histogram(Shared &S, const Row &R, const Elements_ &elements, float end)
+{
     elements.each(R, end, [&](int, v4u w) {
 #pragma unroll
         for (int half = 0; half < E::N; half += 4) {
@@ -510,25 +537,26 @@ __device__ __forceinline__ Bins borders(Shared &S, const Row &R, Sums sums, int 
 __device__ __forceinline__ float bins_of_top_k(Shared &S, const Row &R, float largest, int tid, int lane, int wave)
 {
     if (!R.by_count || R.top_k > THREADS / 2) return ALL_BINS;
-    clear_bins(S, tid);
     const float below = R.scale.below(!R.infinite ? largest : largest == __builtin_inff() ? 0.f : __builtin_nanf(""));
-    if (below < RANGE) atomicAdd(&S.counts[(int)Row::bin_of(below)], 1u);
+    uint32_t *const tops = S.tops(), k = (uint32_t)R.top_k;
+    if (below < RANGE) atomicAdd(&tops[(int)Row::bin_of(below)], 1u);
     __syncthreads();
-    Sums sums = sums_of(S, tid);
-    sums.add_up(S, BOUND, lane, wave);
-    if (sums.all_count < (uint32_t)R.top_k) return ALL_BINS;
-    sums.say(S.reached[FIRST], true, (Weight)R.top_k, tid);
+    static_assert(PER_THREAD == 2);
+    const uint32_t even = tops[2 * tid], odd = tops[2 * tid + 1], upto_lane = up_to_lane(even + odd);
+    if (lane == 63) S.wave_counts[BOUND][wave] = upto_lane;
+    __syncthreads();
+    uint32_t all;
+    const uint32_t upto = over_waves(upto_lane, S.wave_counts[BOUND], lane, wave, all), before = upto - even - odd;
+    if (all < k) return ALL_BINS;
+    if (before < k && upto >= k) S.reached[FIRST].bin = 2 * tid + (before + even < k);
     __syncthreads();
     const int bin = S.reached[FIRST].bin;
     return bin < BINS - 1 ? (float)(bin + 1) : ALL_BINS;
 }
 
 // All tokens of bins before `end` into the list, as far as there is room; their histogram.  False: they are more
-template <class E, class Elements_> __device__ __forceinline__ bool gather(Shared &S, const Row &R, const Elements_ &elements, float end, int tid, int lane)
+template <class E, class Elements_> __device__ __forceinline__ bool gather(Shared &S, const Row &R, const Elements_ &elements, float end, int lane)
 {
-    if (tid == 0) S.begin_list(0);
-    clear_bins(S, tid);
-    if (tid < PIECES) S.pieces[tid] = 0;
     elements.each(R, end, [&](int tile, v4u w) {
         uint32_t found = 0;      // one bit for each
 #pragma unroll
@@ -537,22 +565,17 @@ template <class E, class Elements_> __device__ __forceinline__ bool gather(Share
             if (found) {
                 const int i = __builtin_ctz(found);
                 found &= found - 1;
+                const float x = E::any(w, i), below = R.scale.below(x);
+                const int bin = (int)Row::bin_of(below);
                 const uint32_t n = atomicAdd(&S.n_listed, 1u);
-                if (n < LISTED) S.found[n] = {E::any(w, i), (tile * 64 + lane) * E::N + i};
+                if (n < LISTED) S.found[n] = {x, (tile * 64 + lane) * E::N + i};
+                atomicAdd(&S.counts[bin], 1u);
+                atomicAdd(&S.weights[bin], (Weight)Scale::weight(below));
             }
         }
     });
     __syncthreads();
-    const int n = (int)S.n_listed;
-    if (n > LISTED) return false;
-    for (int i = tid; i < n; i += THREADS) {
-        const float below = R.scale.below(S.found[i].x);
-        const int bin = (int)Row::bin_of(below);
-        atomicAdd(&S.counts[bin], 1u);
-        atomicAdd(&S.weights[bin], (Weight)Scale::weight(below));
-    }
-    __syncthreads();
-    return true;
+    return S.n_listed <= LISTED;
 }
 
 // A wavefront's sums by pieces, its tiles in their order: the lanes' are added up once a piece
@@ -587,11 +610,8 @@ struct PieceSums {
 };
 
 // Weights of the tokens that are left for sure, by pieces of the row; candidates into the list, as far as there is room
-template <class E, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int tid, int lane)
+template <class E, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int lane)
 {
-    if (tid < PIECES) S.pieces[tid] = 0;
-    if (tid == 0) S.begin_list(0);
-    __syncthreads();
     const float sure = B.sure == BINS ? ALL_BINS : (float)B.sure, below_least = R.scale.below(R.least);
     // (without candidates, min-p's border ends it as well)
     const float end = B.sure < BINS ? B.end() : below_least < RANGE ? floorf(Row::bin_of(below_least)) + 1.f : ALL_BINS;
@@ -650,40 +670,74 @@ template <class E, class Elements_> __device__ __forceinline__ void collect(Shar
     __syncthreads();
 }
 
-// Among the candidates that are `flag`: the first one, in their order, with which `target` is reached, 0 if with none.  `weight`: theirs up to it.  Consecutive lanes share a
-// candidate's comparisons.
-__device__ __forceinline__ Place resolve(Shared &S, int use, Weight flag, bool by_count, Weight target, int n, Weight &weight, int tid, int lane)
+// Among the candidates: the first one, in their order, with which top-k, and of those before it, with which top-p is reached.  How many are before a candidate, and their weights, need
+// neither border; consecutive lanes share a candidate's comparisons.
+__device__ __forceinline__ Place resolve(Shared &S, const Row &R, const Bins &B, int n, int tid, int lane)
 {
-    // (the candidates for top-k and those for top-p may be of different logits)
-    for (int i = tid; i < n; i += THREADS)
-        if (S.listed[i].place >> INDEX_BITS != S.listed[0].place >> INDEX_BITS || !(S.listed[i].weight & flag)) S.differ[use] = 1;
-    __syncthreads();
-    const bool same = !S.differ[use];
-    const int shift = n > 1 ? max(10 - (32 - __builtin_clz(n - 1)), 0) : 6, sharing = 1 << min(shift, 6);
-    for (int i = tid / sharing; i < n; i += THREADS / sharing) {
-        const Candidate mine = S.listed[i];
-        uint32_t rank = 0;
-        Weight before = 0;
-        if (same) {      // of equal logits: by their indexes
-            for (int j = lane & (sharing - 1); j < n; j += sharing) rank += (uint32_t)S.listed[j].place > (uint32_t)mine.place;
-            before = rank * (mine.weight & ONLY_WEIGHT);
-        }
-        for (int j = lane & (sharing - 1); j < n && !same; j += sharing) {
-            const Candidate c = S.listed[j];
-            const bool counts = c.place > mine.place && (c.weight & flag);
-            rank += counts;
-            before += counts ? c.weight & ONLY_WEIGHT : 0;
+    const bool by_count = B.count_bin < BINS, by_weight = R.by_weight, both = by_count && by_weight;
+    bool same = false;      // equal logits, which only the index orders, and of one bin, so candidates for the same: worth looking where they are many
+    if (n > 64) {
+        const Candidate first = S.listed[0];
+        for (int i = tid; i < n; i += THREADS)
+            if (S.listed[i].place >> INDEX_BITS != first.place >> INDEX_BITS) S.differ = true;
+        __syncthreads();
+        same = !S.differ;
+    }
+    const int shift = n > 1 ? max(10 - (32 - __builtin_clz(n - 1)), 0) : 4, sharing = 1 << min(shift, 4);
+    static_assert(LISTED == 2 * THREADS && THREADS == 1 << 10);
+    Candidate mine[2] = {};
+    uint32_t rank[2] = {};
+    Weight before_count[2] = {}, before_weight[2] = {};      // weights of those before it: candidates for top-k, for top-p
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int i = tid / sharing + r * (THREADS / sharing);
+        if (i >= n) break;
+        mine[r] = S.listed[i];
+        if (same) {
+            for (int j = lane & (sharing - 1); j < n; j += sharing) rank[r] += (uint32_t)S.listed[j].place > (uint32_t)mine[r].place;
+        } else if (both) {
+            for (int j = lane & (sharing - 1); j < n; j += sharing) {
+                const Candidate c = S.listed[j];
+                const bool ahead = c.place > mine[r].place, counts = ahead && (c.weight & FOR_COUNT), weighs = ahead && (c.weight & FOR_WEIGHT);
+                rank[r] += counts;
+                before_count[r] += counts ? c.weight & ONLY_WEIGHT : 0;
+                before_weight[r] += weighs ? c.weight & ONLY_WEIGHT : 0;
+            }
+        } else {
+            for (int j = lane & (sharing - 1); j < n; j += sharing) {
+                const Candidate c = S.listed[j];
+                const bool ahead = c.place > mine[r].place;
+                rank[r] += ahead;
+                before_weight[r] += ahead ? c.weight & ONLY_WEIGHT : 0;
+            }
         }
         for (int d = 1; d < sharing; d <<= 1) {
-            rank += __shfl_xor(rank, d);
-            before += (Weight)__shfl_xor((uint32_t)(before >> 32), d) << 32 | (uint32_t)__shfl_xor((uint32_t)before, d);
+            rank[r] += __shfl_xor(rank[r], d);
+            if (!same) before_weight[r] += shuffled(before_weight[r], d);
+            if (both && !same) before_count[r] += shuffled(before_count[r], d);
         }
-        const Weight own = mine.weight & ONLY_WEIGHT, reached = by_count ? rank : before, with = reached + (by_count ? 1 : own);
-        if ((mine.weight & flag) && reached < target && with >= target) S.found_place[use] = mine.place, S.found_weight[use] = before + own;
+        if (same) before_weight[r] = rank[r] * (mine[r].weight & ONLY_WEIGHT);
+        if (!both || same) before_count[r] = before_weight[r];
     }
-    __syncthreads();
-    weight = S.found_weight[use];
-    return S.found_place[use];
+    Place border = 0;
+    Weight left = B.all;
+    if (by_count) {
+        const uint32_t last = (uint32_t)R.top_k - B.count_before - 1;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if ((mine[r].weight & FOR_COUNT) && rank[r] == last) S.found_place[0] = mine[r].place, S.found_weight[0] = before_count[r] + (mine[r].weight & ONLY_WEIGHT);
+        __syncthreads();
+        border = S.found_place[0], left = B.weight_before_count + S.found_weight[0];
+    }
+    if (by_weight) {
+        const Weight target = target_of(R.top_p, left) - B.weight_before_low;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if ((mine[r].weight & FOR_WEIGHT) && before_weight[r] < target && before_weight[r] + (mine[r].weight & ONLY_WEIGHT) >= target) S.found_place[1] = mine[r].place;
+        __syncthreads();
+        border = max(border, S.found_place[1]);
+    }
+    return border;
 }
 
 // The same among all tokens, by their places' bits, a histogram of some at a time: where the candidates are more than the list holds (thousands of equal logits).
@@ -729,7 +783,6 @@ template <class E> __device__ __forceinline__ Place settle(Shared &S, const Args
 {
     if (B.count_bin == BINS && B.low == BINS) return 0;
     Place border = 0;
-    Weight weight, left = B.all;
     if (S.n_listed <= LISTED) {
         // candidates into a list of their own; of the rest, which only a list of all that top-k can leave has, what lies before both borders is left
         for (int i = tid; i < (int)S.n_listed; i += THREADS) {
@@ -744,17 +797,14 @@ template <class E> __device__ __forceinline__ Place settle(Shared &S, const Args
         }
         __syncthreads();
         const int n = (int)S.n_candidates;
-        if (B.count_bin < BINS) {
-            border = resolve(S, 0, FOR_COUNT, true, (Weight)R.top_k - B.count_before, n, weight, tid, lane);
-            left = B.weight_before_count + weight;
-        }
-        if (R.by_weight) border = max(border, resolve(S, 1, FOR_WEIGHT, false, target_of(R.top_p, left) - B.weight_before_low, n, weight, tid, lane));
+        border = resolve(S, R, B, n, tid, lane);
         for (int i = tid; i < n; i += THREADS) {      // (a candidate of top-k alone lies behind top-p's border, or there is none)
             const Candidate c = S.listed[i];
             if (c.place >= border && c.place >= place(R.least, MAX_VOCAB - 1)) atomicAdd(&S.pieces[C.piece_of(index_of(c.place) / Tiles<E>::TILE)], c.weight & ONLY_WEIGHT);
         }
     } else {
-        const Elements<E, 0> elements(Tiles<E>::of_wave(A, row, Cut(1, A.vocab, Tiles<E>::TILE), 0, wave, lane));      // (the whole row)
+        const Elements<E, 0> elements(Tiles<E>::of_wave(A, row, Cut(1, A.vocab, Tiles<E>::TILE), 0, wave, lane), [] {});      // (the whole row)
+        Weight weight, left = B.all;
         if (B.count_bin < BINS) border = resolve_all<E>(S, R, elements, true, (Weight)R.top_k, 0, left, tid, lane, wave);
         if (R.by_weight) border = max(border, resolve_all<E>(S, R, elements, false, target_of(R.top_p, left), border, weight, tid, lane, wave));
         if (tid < PIECES) S.pieces[tid] = 0;
@@ -825,23 +875,33 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x;
     const Cut C(1, A.vocab, Tiles<E>::TILE);
     const Given G(A, row);
-    const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, 0, wave, lane));
+    const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, 0, wave, lane), [&] {
+        G.derive(S, wave);
+        clear_all(S, tid);
+    });
     const float largest = elements.largest(), most = largest_of_workgroup(S, largest, lane, wave);
     if (most == -__builtin_inff()) {      // nothing that may be drawn
         if (tid == 0) global_at<int>(A.tokens)[row] = -1;
         return;
     }
-    const Row R(G, A.vocab, most);
+    const Row R(G, S, A.vocab, most);
     Bins B;
     bool listed = false;
     if (R.by_count || R.by_weight) {
         // top-k: the tokens that can be among the first are few, and all that follows is done with those
         const float end = bins_of_top_k(S, R, largest, tid, lane, wave);
-        listed = end != ALL_BINS && gather<E>(S, R, elements, end, tid, lane);
-        if (!listed) histogram<E>(S, R, elements, end, tid);
+        if (end != ALL_BINS) {
+            listed = gather<E>(S, R, elements, end, lane);
+            if (!listed) {      // more than are listed
+                __syncthreads();
+                clear_all(S, tid);
+                __syncthreads();
+            }
+        }
+        if (!listed) histogram<E>(S, R, elements, end);
         B = borders(S, R, sums_of(S, tid), tid, lane, wave);
     }
-    if (!listed) collect<E>(S, R, B, C, elements, tid, lane);
+    if (!listed) collect<E>(S, R, B, C, elements, lane);
     const Place border = settle<E>(S, A, row, R, B, C, tid, lane, wave);
     pick<E>(S, A, row, R, border, C, lane, wave);
 }
@@ -852,8 +912,7 @@ enum Step { MAXIMUM, HISTOGRAM, COLLECT };
 __device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
 {
     float t = lane < groups ? P.maxima[first + lane] : -__builtin_inff();
-    for (int d = 1; d < 64; d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
-    return t;
+    return largest_of_lanes(t);
 }
 template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) void part_kernel(const Args A)
 {
@@ -863,7 +922,12 @@ template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) vo
     const Given G(A, row);
     const Parts P(A.workspace, (size_t)A.rows, (size_t)A.rows * A.groups);
     const size_t first = (size_t)row * A.groups, mine = first + group, bins = (size_t)row * BINS;
-    const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, group, wave, lane));
+    const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, group, wave, lane), [&] {
+        if constexpr (STEP != MAXIMUM) {
+            G.derive(S, wave);
+            clear_all(S, tid);
+        }
+    });
     if constexpr (STEP == MAXIMUM) {
         for (int i = group * THREADS + tid; i < BINS; i += A.groups * THREADS) P.counts[bins + i] = 0, P.weights[bins + i] = 0;
         const float most = largest_of_workgroup(S, elements.largest(), lane, wave);
@@ -871,11 +935,12 @@ template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) vo
     } else {
         const float most = largest_of_row(P, first, A.groups, lane);
         if (most == -__builtin_inff()) return;
-        const Row R(G, A.vocab, most);
+        __syncthreads();
+        const Row R(G, S, A.vocab, most);
         const bool filtered = R.by_count || R.by_weight;
         if constexpr (STEP == HISTOGRAM) {
             if (!filtered) return;
-            histogram<E>(S, R, elements, ALL_BINS, tid);
+            histogram<E>(S, R, elements, ALL_BINS);
             for (int i = tid; i < BINS; i += THREADS) {
                 if (S.counts[i]) atomicAdd(&P.counts[bins + i], S.counts[i]);
                 if (S.weights[i]) atomicAdd(&P.weights[bins + i], S.weights[i]);
@@ -889,7 +954,7 @@ template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) vo
                 B = borders(S, R, sums, tid, lane, wave);
                 if (group == 0 && tid == 0) P.bins[row] = B;
             }
-            collect<E>(S, R, B, C, elements, tid, lane);
+            collect<E>(S, R, B, C, elements, lane);
             const int pieces = PIECES / A.groups, n = (int)S.n_listed;
             if (tid < pieces) P.pieces[(size_t)row * PIECES + group * pieces + tid] = S.pieces[group * pieces + tid];
             for (int i = tid; i < min(n, Parts::LISTED_EACH); i += THREADS) P.found[mine * Parts::LISTED_EACH + i] = S.found[i];
@@ -904,6 +969,7 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
     const Given G(A, row);
     const Parts P(A.workspace, (size_t)A.rows, (size_t)A.rows * A.groups);
     const size_t first = (size_t)row * A.groups;
+    G.derive(S, wave);
     if (tid < PIECES) S.pieces[tid] = P.pieces[(size_t)row * PIECES + tid];
     Bins B = P.bins[row];
     const float most = largest_of_row(P, first, A.groups, lane);
@@ -911,7 +977,8 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
         if (tid == 0) global_at<int>(A.tokens)[row] = -1;
         return;
     }
-    const Row R(G, A.vocab, most);
+    __syncthreads();
+    const Row R(G, S, A.vocab, most);
     const Cut C(A.groups, A.vocab, Tiles<E>::TILE);
     if (R.by_count || R.by_weight) {
         // the parts' candidates one after the other; one that has more than its room: as if they were too many
