@@ -141,7 +141,7 @@ struct Shared {
     Weight wave_weights[USES][WAVES];
     uint32_t wave_counts[USES][WAVES];
     float wave_max[WAVES];
-    double rate, cut;      // of the row: see Given
+    double derived[2];      // see Given
     Reached reached[USES];
     uint32_t n_listed, n_candidates;
     Place found_place[2];
@@ -215,14 +215,16 @@ struct Parts {
     Bins *bins;
     Found *found;
     float *maxima;
+    double *derived;      // see Given
     static constexpr int LISTED_EACH = 512;
-    static constexpr size_t ROW = BINS * 12 + PIECES * sizeof(Weight) + 64, PART = LISTED_EACH * sizeof(Found) + 8;      // bytes
+    static constexpr size_t ROW = BINS * 12 + PIECES * sizeof(Weight) + 64 + 16, PART = LISTED_EACH * sizeof(Found) + 8;      // bytes
     static constexpr size_t bytes(size_t rows, size_t parts) { return rows * ROW + parts * PART; }
     __device__ __forceinline__ Parts(Address workspace, size_t rows, size_t parts)
     {
         weights = global_at<Weight>(workspace);
         pieces = weights + rows * BINS;
-        found = (Found *)(pieces + rows * PIECES);
+        derived = (double *)(pieces + rows * PIECES);
+        found = (Found *)(derived + 2 * rows);
         bins = (Bins *)(found + parts * LISTED_EACH);
         counts = (uint32_t *)((uint8_t *)bins + rows * 64);
         maxima = (float *)(counts + rows * BINS);
@@ -241,17 +243,17 @@ struct Given {
     }
     __device__ __forceinline__ bool greedy() const { return !(temperature > 0.f); }
     // What takes a quotient and a logarithm in 64 bits, by one wavefront each while the row is on its way: 2 log2(e) / T, and T log(min_p), which is how far below the largest min_p's border lies
-    __device__ __forceinline__ void derive(Shared &S, int wave) const
+    __device__ __forceinline__ void derive(double *to, int wave) const
     {
-        if (wave == WAVES - 1) S.rate = fmin(2 * 1.4426950408889634 / (greedy() ? 1.0 : (double)temperature), 0x1p+127);
-        if (wave == WAVES - 2 && min_p > 0.f && min_p < 1.f) S.cut = (double)temperature * log((double)min_p);
+        if (wave == WAVES - 1) to[0] = fmin(2 * 1.4426950408889634 / (greedy() ? 1.0 : (double)temperature), 0x1p+127);
+        if (wave == WAVES - 2 && min_p > 0.f && min_p < 1.f) to[1] = (double)temperature * log((double)min_p);
     }
 };
 struct Row : Given {
     Scale scale;
     float least;      // no token below it is left (min-p; greedy: the largest alone)
     bool by_count, by_weight, infinite;      // filtered by top-k, by top-p; only logits of plus infinity are left, which count as 0 then
-    __device__ __forceinline__ Row(const Given &G, const Shared &S, int vocab, float most) : Given(G)      // (after a barrier behind derive)
+    __device__ __forceinline__ Row(const Given &G, const double *derived, int vocab, float most) : Given(G)
     {
         infinite = most == __builtin_inff();
         if (infinite) most = 0.f;
@@ -262,8 +264,8 @@ struct Row : Given {
         if (greedy || min_p >= 1.f)
             least = most;
         else if (min_p > 0.f)      // w >= min_p: x >= max + T log(min_p), the smallest float that is
-            least = fmaxf(least, not_below((double)most + S.cut));
-        const double c = S.rate;
+            least = fmaxf(least, not_below((double)most + derived[1]));
+        const double c = derived[0];
         scale.half_max = 0.5f * most;
         scale.hi = (float)c;
         if ((double)scale.hi > c) scale.hi = __uint_as_float(__float_as_uint(scale.hi) - 1u);      // (lo not below zero: where both parts overflow, so does their sum)
@@ -694,8 +696,10 @@ __device__ __forceinline__ Place resolve(Shared &S, const Row &R, const Bins &B,
         if (i >= n) break;
         mine[r] = S.listed[i];
         if (same) {
+#pragma unroll 4
             for (int j = lane & (sharing - 1); j < n; j += sharing) rank[r] += (uint32_t)S.listed[j].place > (uint32_t)mine[r].place;
         } else if (both) {
+#pragma unroll 4
             for (int j = lane & (sharing - 1); j < n; j += sharing) {
                 const Candidate c = S.listed[j];
                 const bool ahead = c.place > mine[r].place, counts = ahead && (c.weight & FOR_COUNT), weighs = ahead && (c.weight & FOR_WEIGHT);
@@ -704,6 +708,7 @@ __device__ __forceinline__ Place resolve(Shared &S, const Row &R, const Bins &B,
                 before_weight[r] += weighs ? c.weight & ONLY_WEIGHT : 0;
             }
         } else {
+#pragma unroll 4
             for (int j = lane & (sharing - 1); j < n; j += sharing) {
                 const Candidate c = S.listed[j];
                 const bool ahead = c.place > mine[r].place;
@@ -876,7 +881,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     const Cut C(1, A.vocab, Tiles<E>::TILE);
     const Given G(A, row);
     const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, 0, wave, lane), [&] {
-        G.derive(S, wave);
+        G.derive(S.derived, wave);
         clear_all(S, tid);
     });
     const float largest = elements.largest(), most = largest_of_workgroup(S, largest, lane, wave);
@@ -884,7 +889,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
         if (tid == 0) global_at<int>(A.tokens)[row] = -1;
         return;
     }
-    const Row R(G, S, A.vocab, most);
+    const Row R(G, S.derived, A.vocab, most);
     Bins B;
     bool listed = false;
     if (R.by_count || R.by_weight) {
@@ -923,8 +928,9 @@ template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) vo
     const Parts P(A.workspace, (size_t)A.rows, (size_t)A.rows * A.groups);
     const size_t first = (size_t)row * A.groups, mine = first + group, bins = (size_t)row * BINS;
     const Elements<E, HELD> elements(Tiles<E>::of_wave(A, row, C, group, wave, lane), [&] {
-        if constexpr (STEP != MAXIMUM) {
-            G.derive(S, wave);
+        if constexpr (STEP == MAXIMUM) {
+            if (group == 0) G.derive(P.derived + 2 * row, wave);
+        } else {
             clear_all(S, tid);
         }
     });
@@ -936,7 +942,7 @@ template <class E, Step STEP, int HELD> __global__ __launch_bounds__(THREADS) vo
         const float most = largest_of_row(P, first, A.groups, lane);
         if (most == -__builtin_inff()) return;
         __syncthreads();
-        const Row R(G, S, A.vocab, most);
+        const Row R(G, P.derived + 2 * row, A.vocab, most);
         const bool filtered = R.by_count || R.by_weight;
         if constexpr (STEP == HISTOGRAM) {
             if (!filtered) return;
@@ -969,7 +975,6 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
     const Given G(A, row);
     const Parts P(A.workspace, (size_t)A.rows, (size_t)A.rows * A.groups);
     const size_t first = (size_t)row * A.groups;
-    G.derive(S, wave);
     if (tid < PIECES) S.pieces[tid] = P.pieces[(size_t)row * PIECES + tid];
     Bins B = P.bins[row];
     const float most = largest_of_row(P, first, A.groups, lane);
@@ -977,8 +982,7 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
         if (tid == 0) global_at<int>(A.tokens)[row] = -1;
         return;
     }
-    __syncthreads();
-    const Row R(G, S, A.vocab, most);
+    const Row R(G, P.derived + 2 * row, A.vocab, most);
     const Cut C(A.groups, A.vocab, Tiles<E>::TILE);
     if (R.by_count || R.by_weight) {
         // the parts' candidates one after the other; one that has more than its room: as if they were too many
