@@ -695,7 +695,7 @@ def rb_cache8_read(cache: Cache8, first: torch.Tensor, lengths: torch.Tensor, ta
     if k is None:
         k = torch.empty(shape, dtype=cache.dtype, device=cache.k.device)
     if v is None:
-        v = torch.empty(shape, dtype=cache.dtype, device=cache.k.device)
+        v = torch.empty_like(k)
     for x in (k, v):
         assert x.is_cuda and x.dtype is cache.dtype and x.shape == shape and x.is_contiguous()
     _check("rb_cache8_read", lib.rb_cache8_read(ctypes.byref(cache._struct), *at, tokens, k.data_ptr(), v.data_ptr(), _stream()))

@@ -7,10 +7,10 @@
 // Weights are whole numbers of units of 2^-30, their sums are of 64 bits: they depend on no order, so histograms may be summed by atomics.
 //
 // Bound: not by the row's bytes (256 rows of 128000 bf16 are 65 MB, 10 us), but by instructions and, with few rows, by the steps that follow each other.  A logit costs
-// a subtraction, two products, an exponential and its rounding to a whole number in the histogram and again in the sums: some 70 and 55 to 95 cycles per wavefront and element, 14 and 19 us of the 54
-// that those rows take with top-p; reading them and their maximum are 8, the borders, the candidates and the choice 6.  (Weights do not fit the registers beside the logits, to be computed once.)
-// Measured there: no filter 27 us, top-k of 50 24, top-p 54, all filters mixed 59, greedy 16.  One row of 32000 fp16: 14 us with top-k and top-p, 10 without, one launch, of which nine steps with
-// barriers between them are all but 2 us.
+// a subtraction, two products, an exponential and its rounding to a whole number in the histogram and again in the sums: some 65 and 55 to 90 cycles per wavefront and element, 14 and 19 us of the 53
+// that those rows take with top-p; reading them and their maximum are 9, the borders, the candidates and the choice 6.  (Weights do not fit the registers beside the logits, to be computed once.)
+// Measured there: no filter 26 us, top-k of 50 22, top-p 53, all filters mixed 58, greedy 16.  One row of 32000 fp16: 11.5 us with top-k and top-p, 9.8 without, one launch: eight steps with
+// barriers between them are all but 1.3 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <type_traits>
@@ -335,7 +335,7 @@ template <class E> __device__ __forceinline__ float largest_of(v4u w)      // (N
 }
 
 // Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 24 and
-// 30 us, top-p 54 and 60, greedy 16 and 25).  Sixteen tiles are what a wavefront of 128 registers has room for.
+// 30 us, top-p 54 and 60, greedy 16 and 25, before the last steps).  Sixteen tiles are what a wavefront of 128 registers has room for.
 template <class E, int HELD> struct Elements : Tiles<E> {
     // word j of each tile: one place of a vector, so that a loop over the tiles is one copy of its body (sixteen do not fit the instruction cache)
     typedef uint32_t Words __attribute__((ext_vector_type(HELD ? HELD : 1)));
@@ -911,7 +911,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     pick<E>(S, A, row, R, border, C, lane, wave);
 }
 
-// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 41 us, one workgroup each 60; one row 25 and 55), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
+// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 40 us, one workgroup each 60; one row 24.5 and 55), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
 // token.  What they hand on lies in the workspace.
 enum Step { MAXIMUM, HISTOGRAM, COLLECT };
 __device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
@@ -1006,8 +1006,8 @@ constexpr int MAX_ROWS = 1 << 20;
 constexpr long long MAX_STRIDE = 1ll << 40;
 
 // Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 25.6 us with 4096, 25.2 with 2048, 27.6 with 8192; four of 151936
-// fp32 27.2 with 2048, 26.4 with 4096); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 15 us, four launches 30; 7 rows
-// of 50001 bf16, no filter: 13.6 and 14.6.  From there on several are faster: 128000 bf16 with top-p 25.6 us, one workgroup 45)
+// fp32 27.2 with 2048, 26.4 with 4096; since then a microsecond less); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 15 us, now 12.7, four launches 30; 7 rows
+// of 50001 bf16, no filter: 13.6 and 14.6.  From there on several are faster: 128000 bf16 with top-p 25.6 us, now 24.4, one workgroup 45)
 constexpr int SHARE = 4096, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
 int compute_units() { return std::max(mx::device_groups(), 2); }
 int groups_of(int rows, int tiles, int tile, int compute_units)
@@ -1029,8 +1029,8 @@ template <class E> int launch(Args A, hipStream_t stream)
 {
     const int tiles = (A.vocab + Tiles<E>::TILE - 1) / Tiles<E>::TILE;
     const dim3 rows((unsigned)A.rows), threads(THREADS);
-    // with top-k alone, a row's few tokens are found by one workgroup before several have met (one row of 128000 bf16: the first 50 15.7 us, with
-    // sixteen workgroups 21.7; 300 20.6 and 22.7; more than 512, for which every bin counts, 39 and 22.7)
+    // with top-k alone, a row's few tokens are found by one workgroup before several have met (one row of 128000 bf16: the first 50 14.2 us, with
+    // sixteen workgroups 21.7; 300 19.1 and 22.7; more than 512, for which every bin counts, 38 and 22.7)
     A.groups = A.top_k && !A.top_p && tiles <= 16 * WAVES ? 1 : groups_of(A.rows, tiles, Tiles<E>::TILE, compute_units());
     if (A.groups > 1) {
         const int of_group = (tiles + A.groups - 1) / A.groups;
