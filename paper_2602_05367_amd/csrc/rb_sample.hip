@@ -334,8 +334,8 @@ template <class E> __device__ __forceinline__ float largest_of(v4u w)      // (N
     return t;
 }
 
-// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 24 and
-// 30 us, top-p 54 and 60, greedy 16 and 25, before the last steps).  Sixteen tiles are what a wavefront of 128 registers has room for.
+// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 22 and
+// 28 us, top-p 53 and 59, greedy 16 and 24).  Sixteen tiles are what a wavefront of 128 registers has room for.
 template <class E, int HELD> struct Elements : Tiles<E> {
     // word j of each tile: one place of a vector, so that a loop over the tiles is one copy of its body (sixteen do not fit the instruction cache)
     typedef uint32_t Words __attribute__((ext_vector_type(HELD ? HELD : 1)));
@@ -911,7 +911,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     pick<E>(S, A, row, R, border, C, lane, wave);
 }
 
-// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 40 us, one workgroup each 60; one row 24.5 and 55), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
+// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 39 us, one workgroup each 58; one row 24.6 and 53), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
 // token.  What they hand on lies in the workspace.
 enum Step { MAXIMUM, HISTOGRAM, COLLECT };
 __device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
@@ -1005,9 +1005,9 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
 constexpr int MAX_ROWS = 1 << 20;
 constexpr long long MAX_STRIDE = 1ll << 40;
 
-// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 25.6 us with 4096, 25.2 with 2048, 27.6 with 8192; four of 151936
-// fp32 27.2 with 2048, 26.4 with 4096; since then a microsecond less); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 15 us, now 12.7, four launches 30; 7 rows
-// of 50001 bf16, no filter: 13.6 and 14.6.  From there on several are faster: 128000 bf16 with top-p 25.6 us, now 24.4, one workgroup 45)
+// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 24.6 us with 4096, 23.8 with 2048, 26.5 with 8192; four of 151936
+// fp32 26.0, 27.0 and 26.3); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 12.8 us, four launches 29; 7 rows
+// of 50001 bf16, no filter: 13.4 and 14.7.  From there on several are faster: 128000 bf16 with top-p 24.6 us, one workgroup 45, no filter 13.8 and 18.3)
 constexpr int SHARE = 4096, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
 int compute_units() { return std::max(mx::device_groups(), 2); }
 int groups_of(int rows, int tiles, int tile, int compute_units)
@@ -1029,9 +1029,9 @@ template <class E> int launch(Args A, hipStream_t stream)
 {
     const int tiles = (A.vocab + Tiles<E>::TILE - 1) / Tiles<E>::TILE;
     const dim3 rows((unsigned)A.rows), threads(THREADS);
-    // with top-k alone, a row's few tokens are found by one workgroup before several have met (one row of 128000 bf16: the first 50 14.2 us, with
-    // sixteen workgroups 21.7; 300 19.1 and 22.7; more than 512, for which every bin counts, 38 and 22.7)
-    A.groups = A.top_k && !A.top_p && tiles <= 16 * WAVES ? 1 : groups_of(A.rows, tiles, Tiles<E>::TILE, compute_units());
+    // With top-k alone a row's few tokens are found by one workgroup before several have met, if no row has more than 512 of them: one row of 128000 bf16, the first 50: 14.3 us, with sixteen
+    // workgroups 22.1; 300: 19.1 and 22.4; 1000, for which every bin counts, 38.5 and 22.8.  48 rows of 131071 fp32: 22.2 and 33.6; 27.3 and 34.8; 49.8 and 35.4.  One row of 200000 fp32: 24.6 and 21.4
+    A.groups = A.top_k && !A.top_p && tiles <= 32 * WAVES ? 1 : groups_of(A.rows, tiles, Tiles<E>::TILE, compute_units());
     if (A.groups > 1) {
         const int of_group = (tiles + A.groups - 1) / A.groups;
         if (of_group <= 4 * WAVES)
