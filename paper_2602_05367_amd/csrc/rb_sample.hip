@@ -7,9 +7,9 @@
 // Weights are whole numbers of units of 2^-30, their sums are of 64 bits: they depend on no order, so histograms may be summed by atomics.
 //
 // Bound: not by the row's bytes (256 rows of 128000 bf16 are 65 MB, 10 us), but by instructions and, with few rows, by the steps that follow each other.  A logit costs
-// a subtraction, two products, an exponential and its rounding to a whole number in the histogram and again in the sums: some 65 and 55 to 90 cycles per wavefront and element, 14 and 19 us of the 53
+// a subtraction, two products, an exponential and its rounding to a whole number in the histogram and again in the sums: some 65 and 47 to 85 cycles per wavefront and element, 14 and 18 us of the 51.5
 // that those rows take with top-p; reading them and their maximum are 9, the borders, the candidates and the choice 6.  (Weights do not fit the registers beside the logits, to be computed once.)
-// Measured there: no filter 26 us, top-k of 50 22, top-p 53, all filters mixed 58, greedy 16.  One row of 32000 fp16: 11.5 us with top-k and top-p, 9.8 without, one launch: eight steps with
+// Measured there: no filter 25 us, top-k of 50 22, top-p 51.5, all filters mixed 58, greedy 16.  One row of 32000 fp16: 11.5 us with top-k and top-p, 9.1 without, one launch: eight steps with
 // barriers between them are all but 1.3 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -86,10 +86,9 @@ struct Scale {
     // in units of 2^-30, to the nearest: nothing beyond RANGE, for infinity and NaN
     static __device__ __forceinline__ uint32_t weight(float below)
     {
-        int units;
-        const float w = __builtin_amdgcn_exp2f(-below) * 0x1p+30f;
-        asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(units) : "v"(w));
-        return (uint32_t)units;
+        uint32_t units;      // (the instruction gives 0 for NaN, where C++ says nothing)
+        asm("v_cvt_u32_f32 %0, %1" : "=v"(units) : "v"(__builtin_fmaf(__builtin_amdgcn_exp2f(-below), 0x1p+30f, 0.5f)));
+        return units;
     }
 };
 
@@ -335,7 +334,7 @@ template <class E> __device__ __forceinline__ float largest_of(v4u w)      // (N
 }
 
 // Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 22 and
-// 28 us, top-p 53 and 59, greedy 16 and 24).  Sixteen tiles are what a wavefront of 128 registers has room for.
+// 28 us, top-p 51.5 and 57, no filter 25 and 28, greedy 16 and 24).  Sixteen tiles are what a wavefront of 128 registers has room for.
 template <class E, int HELD> struct Elements : Tiles<E> {
     // word j of each tile: one place of a vector, so that a loop over the tiles is one copy of its body (sixteen do not fit the instruction cache)
     typedef uint32_t Words __attribute__((ext_vector_type(HELD ? HELD : 1)));
@@ -611,8 +610,8 @@ struct PieceSums {
     }
 };
 
-// Weights of the tokens that are left for sure, by pieces of the row; candidates into the list, as far as there is room
-template <class E, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int lane)
+// Weights of the tokens that are left for sure, by pieces of the row; candidates into the list, as far as there is room.  Without min-p (!MIN_P) no logit is compared with its border (no filter 25 us for 26.5)
+template <class E, bool MIN_P, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int lane)
 {
     const float sure = B.sure == BINS ? ALL_BINS : (float)B.sure, below_least = R.scale.below(R.least);
     // (without candidates, min-p's border ends it as well)
@@ -627,7 +626,7 @@ template <class E, class Elements_> __device__ __forceinline__ void collect(Shar
             for (int i = 0; i < E::N; i += 2) {
                 const float x = E::at(w, i), y = E::at(w, i + 1);
                 const uint32_t of_x = Scale::weight(R.scale.below(x)), of_y = Scale::weight(R.scale.below(y));
-                sum += (x >= R.least ? of_x : 0u) + (y >= R.least ? of_y : 0u);      // (two of them fit 32 bits)
+                sum += (!MIN_P || x >= R.least ? of_x : 0u) + (!MIN_P || y >= R.least ? of_y : 0u);      // (two of them fit 32 bits)
             }
             sums.add(tile, sum);
         });
@@ -642,7 +641,7 @@ template <class E, class Elements_> __device__ __forceinline__ void collect(Shar
                 for (int i = 0; i < 4; ++i) {
                     const float x = E::at(w, half + i), below = R.scale.below(x), at = Row::bin_of(below);
                     any |= at < end && !(at < sure);
-                    weight[i] = at < sure && x >= R.least ? Scale::weight(below) : 0u;
+                    weight[i] = at < sure && (!MIN_P || x >= R.least) ? Scale::weight(below) : 0u;
                 }
                 sum += weight[0] + weight[1], sum += weight[2] + weight[3];
             }
@@ -670,6 +669,14 @@ template <class E, class Elements_> __device__ __forceinline__ void collect(Shar
     }
     sums.end();
     __syncthreads();
+}
+
+template <class E, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int lane)
+{
+    if (R.least > -0x1.fffffep+127f)
+        collect<E, true>(S, R, B, C, elements, lane);
+    else
+        collect<E, false>(S, R, B, C, elements, lane);
 }
 
 // Among the candidates: the first one, in their order, with which top-k, and of those before it, with which top-p is reached.  How many are before a candidate, and their weights, need
@@ -911,7 +918,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     pick<E>(S, A, row, R, border, C, lane, wave);
 }
 
-// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 39 us, one workgroup each 58; one row 24.6 and 53), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
+// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 39 us, one workgroup each 56; one row 24.5 and 52), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
 // token.  What they hand on lies in the workspace.
 enum Step { MAXIMUM, HISTOGRAM, COLLECT };
 __device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
@@ -1007,7 +1014,7 @@ constexpr long long MAX_STRIDE = 1ll << 40;
 
 // Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 24.6 us with 4096, 23.8 with 2048, 26.5 with 8192; four of 151936
 // fp32 26.0, 27.0 and 26.3); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 12.8 us, four launches 29; 7 rows
-// of 50001 bf16, no filter: 13.4 and 14.7.  From there on several are faster: 128000 bf16 with top-p 24.6 us, one workgroup 45, no filter 13.8 and 18.3)
+// of 50001 bf16, no filter: 12.9 and 14.0.  From there on several are faster: 128000 bf16 with top-p 24.5 us, one workgroup 43.5, no filter 14.4 and 17.0)
 constexpr int SHARE = 4096, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
 int compute_units() { return std::max(mx::device_groups(), 2); }
 int groups_of(int rows, int tiles, int tile, int compute_units)
@@ -1030,7 +1037,7 @@ template <class E> int launch(Args A, hipStream_t stream)
     const int tiles = (A.vocab + Tiles<E>::TILE - 1) / Tiles<E>::TILE;
     const dim3 rows((unsigned)A.rows), threads(THREADS);
     // With top-k alone a row's few tokens are found by one workgroup before several have met, if no row has more than 512 of them: one row of 128000 bf16, the first 50: 14.3 us, with sixteen
-    // workgroups 22.1; 300: 19.1 and 22.4; 1000, for which every bin counts, 38.5 and 22.8.  48 rows of 131071 fp32: 22.2 and 33.6; 27.3 and 34.8; 49.8 and 35.4.  One row of 200000 fp32: 24.6 and 21.4
+    // workgroups 22.1; 300: 19.1 and 22.4; 1000, for which every bin counts, 37.4 and 22.8.  48 rows of 131071 fp32: 22.2 and 33.6; 27.5 and 34.8; 49.1 and 35.5.  One row of 200000 fp32: 24.7 and 21.4
     A.groups = A.top_k && !A.top_p && tiles <= 32 * WAVES ? 1 : groups_of(A.rows, tiles, Tiles<E>::TILE, compute_units());
     if (A.groups > 1) {
         const int of_group = (tiles + A.groups - 1) / A.groups;
