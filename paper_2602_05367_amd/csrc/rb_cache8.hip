@@ -138,7 +138,7 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
 }
 
 // Sixteen elements of a key and of its value per thread: two loads, four stores.  A wavefront has elements of one token.
-// Bound: bytes.  16 sequences of 8 heads of 128, 100000 positions together (616 MB): 108 to 120 us, a copy of as many bytes 114; 333 tokens of 12 heads of 80: 3.4 us, the launch.
+// Bound: bytes.  16 sequences of 8 heads of 128, 100000 positions together (616 MB): 116 us, a copy of as many bytes 114; with loads that the caches keep 120, with stores that they do not 187; 333 tokens of 12 heads of 80: 3.4 us, the launch.
 template <class T>
 __global__ __launch_bounds__(256) void read8_kernel(const Cache8Args C, Address k_to, Address v_to, int waves)      // wavefronts of a token
 {
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256) void read8_kernel(const Cache8Args C, Address 
     uint32_t exponent[2] = {};
     if (place_of(C, s, (long long)length - end + token, elements, exponents)) {
         elements += head * C.head_stride + piece * 16, exponents += (long long)head << C.page_shift;
-        w[0] = *(const v4u *)(global_at<const uint8_t>(C.k) + elements), w[1] = *(const v4u *)(global_at<const uint8_t>(C.v) + elements);
+        w[0] = __builtin_nontemporal_load((const v4u *)(global_at<const uint8_t>(C.k) + elements)), w[1] = __builtin_nontemporal_load((const v4u *)(global_at<const uint8_t>(C.v) + elements));
         exponent[0] = global_at<const uint8_t>(C.k_exp)[exponents], exponent[1] = global_at<const uint8_t>(C.v_exp)[exponents];
     }
     const long long at = (((long long)token * C.kv_heads + head) * C.dim + piece * 16) * 2;
