@@ -549,8 +549,9 @@ int rb_attn_cache8(const rb_cache8 *C, const void *q, long long q_token, long lo
  * other parameters are.  NaN counts as 0 in u and min_p, as 1 in top_p, as 0 in temperature.
  *
  * Logits of minus infinity (masked) and NaN are never drawn; a row that has no others gives -1.  Logits of plus infinity: only these are left, with equal weights.
- * Weights are fp32, to (1 + |log2 w|) 2^-23 of themselves, held in units of 2^-30 (less than half of one is zero), and their sums are exact: they depend on no order, and
- * the same input gives the same token.  1 <= rows <= 2^20, 1 <= vocab <= 2^22, stride < 2^40.  workspace: rb_sample_workspace_bytes bytes of device memory,
+ * Weights are fp32, to (1 + |log2 w|) 2^-23 of themselves, held in units of 2^-45, of 2^-(63 - floor(log2 vocab)) from 2^19 tokens on (less than half of one is zero): these roundings
+ * add up to at most 2^-28 of the whole for 2^18 tokens, 2^-24 for 2^20, 2^-20 for 2^22.  Sums are exact: they depend on no order, and the same input gives the same token.
+ * 1 <= rows <= 2^20, 1 <= vocab <= 2^22, stride < 2^40.  workspace: rb_sample_workspace_bytes bytes of device memory,
  * 16-byte aligned; so many serve every call of at most as many rows and tokens.
  */
 size_t rb_sample_workspace_bytes(int dtype, int rows, int vocab);

@@ -4,12 +4,14 @@
 // histogram over -log2 w, counts and weights, says in which of its bins the last token of that prefix lies; what lies in earlier bins is left for sure, and the few tokens of that
 // bin are candidates, which are ranked among themselves.  The token is then found in the order of the indexes: sums over pieces of the row, and within the piece that u falls into.
 //
-// Weights are whole numbers of units of 2^-30, their sums are of 64 bits: they depend on no order, so histograms may be summed by atomics.
+// Weights are whole numbers of units, 2^-45 of the largest one, or coarser where all of a long row together would not fit 64 bits: sums depend on no order, so histograms may be summed by
+// atomics, and the roundings of a row of up to 2^20 tokens are together below a step of u.  (Units of 2^-30, one word each: without filters 25 us in place of 27, with them the same; but a row's many tokens
+// of 2^-31 each were then nothing, or twice what they are.)
 //
 // Bound: not by the row's bytes (256 rows of 128000 bf16 are 65 MB, 10 us), but by instructions and, with few rows, by the steps that follow each other.  A logit costs
-// a subtraction, two products, an exponential and its rounding to a whole number in the histogram and again in the sums: some 65 and 47 to 85 cycles per wavefront and element, 14 and 18 us of the 51.5
+// a subtraction, two products, an exponential and its rounding to units in the histogram and again in the sums: some 72 and 57 to 86 cycles per wavefront and element, 16 and 19 us of the 52
 // that those rows take with top-p; reading them and their maximum are 9, the borders, the candidates and the choice 6.  (Weights do not fit the registers beside the logits, to be computed once.)
-// Measured there: no filter 25 us, top-k of 50 22, top-p 51.5, all filters mixed 58, greedy 16.  One row of 32000 fp16: 11.5 us with top-k and top-p, 9.1 without, one launch: eight steps with
+// Measured there: no filter 27 us, top-k of 50 22.6, top-p 52, all filters mixed 59, greedy 16.  One row of 32000 fp16: 11.7 us with top-k and top-p, 9.6 without, one launch: eight steps with
 // barriers between them are all but 1.3 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -23,10 +25,11 @@ namespace rb {
 namespace sample {
 namespace {
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64, PER_THREAD = 2, BINS = PER_THREAD * THREADS, BIN_BITS = 11, PIECES = 64, LISTED = 2 * THREADS;
-static_assert(BINS == 1 << BIN_BITS);
-// (2048 bins of -log2 w are 0.015 wide; twice as many took the same time: what is saved among the candidates is spent on clearing and adding up)
-constexpr float RANGE = 31.f;      // -log2 of the weights that round to nothing
+constexpr int THREADS = 1024, WAVES = THREADS / 64, PER_THREAD = 3, BINS = PER_THREAD * THREADS, BIN_BITS = 11, PIECES = 64, LISTED = 2 * THREADS;
+static_assert(BINS >= 1 << BIN_BITS);
+// (3072 bins of -log2 w are 0.015 wide.  With 2048, more lanes meet in one: 256 rows of 128000 bf16, top-p, 59 us in place of 52, 48 of 131071 fp32 43 in place of 39; 4096 took the same time:
+// what is saved among the lanes and candidates is spent on clearing and adding up)
+constexpr float RANGE = 46.5f;      // -log2 of weights that round to nothing
 typedef unsigned long long Weight;
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
@@ -77,18 +80,38 @@ __device__ __forceinline__ int index_of(Place p) { return MAX_VOCAB - 1 - (int)(
 // What a row's weights come from.  (x - max) / T is taken from halves, which do not overflow, and times log2(e) / T in two parts: rounded once.
 struct Scale {
     float half_max, hi, lo;
+    int bits;      // the largest weight is 2^bits units: 2^45, or so many that all of a row, were they that large, fit 64 bits
+    __device__ __forceinline__ void units_for(int vocab) { bits = min(32 + __builtin_clz(vocab), 45); }
     // -log2 of x's weight; a larger x never has a larger one.  (NaN stays NaN: none)
     __device__ __forceinline__ float below(float x) const
     {
         const float d = __builtin_fmaf(x, -0.5f, half_max);
         return __builtin_fmaf(d, hi, d * lo);
     }
-    // in units of 2^-30, to the nearest: nothing beyond RANGE, for infinity and NaN
-    static __device__ __forceinline__ uint32_t weight(float below)
+    // The weight; zero for infinity and NaN
+    static __device__ __forceinline__ float share(float below) { return fminf(fmaxf(__builtin_amdgcn_exp2f(-below), 0.f), 1.f); }
+    // in units, to the nearest, ties to even: what is left in the lower bits of a number of 64 bits that has the unit as its last.  Nothing beyond RANGE
+    __device__ __forceinline__ Weight weight(float below) const
     {
-        uint32_t units;      // (the instruction gives 0 for NaN, where C++ says nothing)
-        asm("v_cvt_u32_f32 %0, %1" : "=v"(units) : "v"(__builtin_fmaf(__builtin_amdgcn_exp2f(-below), 0x1p+30f, 0.5f)));
-        return units;
+        const uint32_t high = (uint32_t)(1023 + 52 - bits) << 20;
+        const Weight sum = __builtin_bit_cast(Weight, (double)share(below) + __builtin_bit_cast(double, (Weight)high << 32));
+        return (Weight)((uint32_t)(sum >> 32) - high) << 32 | (uint32_t)sum;
+    }
+};
+// The sum of N weights in units, each rounded as above: to the nearest 2^-23, as the lower bits of 1 + w, and what that leaves as those of a number whose last bit is the unit.
+// (Four instructions of 32 bits a weight and no conversion.)
+template <int N> struct SumOf {
+    uint32_t upper = 0, lower = 0;
+    static __device__ __forceinline__ float offset(const Scale &scale) { return __uint_as_float((uint32_t)(127 + 23 - scale.bits) << 23 | 0x400000u); }      // (a multiple of 2^-23)
+    __device__ __forceinline__ void add(const Scale &scale, float below)
+    {
+        const float w = Scale::share(below), up = w + 1.f;
+        upper += __float_as_uint(up);
+        lower += __float_as_uint(w - (up - (1.f + offset(scale))));
+    }
+    __device__ __forceinline__ Weight units(const Scale &scale) const
+    {
+        return ((Weight)(upper - N * 0x3f800000u) << (scale.bits - 23)) + (Weight)(long long)(int)(lower - N * __float_as_uint(offset(scale)));
     }
 };
 
@@ -265,6 +288,7 @@ struct Row : Given {
         else if (min_p > 0.f)      // w >= min_p: x >= max + T log(min_p), the smallest float that is
             least = fmaxf(least, not_below((double)most + derived[1]));
         const double c = derived[0];
+        scale.units_for(vocab);
         scale.half_max = 0.5f * most;
         scale.hi = (float)c;
         if ((double)scale.hi > c) scale.hi = __uint_as_float(__float_as_uint(scale.hi) - 1u);      // (lo not below zero: where both parts overflow, so does their sum)
@@ -451,18 +475,18 @@ template <class E, class Elements_> __device__ __forceinline__ void histogram(Sh
 #pragma unroll
         for (int half = 0; half < E::N; half += 4) {
             float below[4];
-            uint32_t weight[4];
+            Weight weight[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) below[i] = R.scale.below(E::at(w, half + i));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) weight[i] = Scale::weight(below[i]);
+            for (int i = 0; i < 4; ++i) weight[i] = R.scale.weight(below[i]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float at = Row::bin_of(below[i]);
                 if (below[i] < RANGE && at < end) {
                     const int bin = (int)at;
                     if (R.by_count) atomicAdd(&S.counts[bin], 1u);
-                    if (R.by_weight) atomicAdd(&S.weights[bin], (Weight)weight[i]);
+                    if (R.by_weight) atomicAdd(&S.weights[bin], weight[i]);
                 }
             }
         }
@@ -542,14 +566,23 @@ __device__ __forceinline__ float bins_of_top_k(Shared &S, const Row &R, float la
     uint32_t *const tops = S.tops(), k = (uint32_t)R.top_k;
     if (below < RANGE) atomicAdd(&tops[(int)Row::bin_of(below)], 1u);
     __syncthreads();
-    static_assert(PER_THREAD == 2);
-    const uint32_t even = tops[2 * tid], odd = tops[2 * tid + 1], upto_lane = up_to_lane(even + odd);
+    static_assert(BINS * sizeof(uint32_t) <= sizeof(S.listed));
+    uint32_t own[PER_THREAD], here = 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) here += own[i] = tops[PER_THREAD * tid + i];
+    const uint32_t upto_lane = up_to_lane(here);
     if (lane == 63) S.wave_counts[BOUND][wave] = upto_lane;
     __syncthreads();
     uint32_t all;
-    const uint32_t upto = over_waves(upto_lane, S.wave_counts[BOUND], lane, wave, all), before = upto - even - odd;
+    const uint32_t upto = over_waves(upto_lane, S.wave_counts[BOUND], lane, wave, all);
+    uint32_t before = upto - here;
     if (all < k) return ALL_BINS;
-    if (before < k && upto >= k) S.reached[FIRST].bin = 2 * tid + (before + even < k);
+    if (before < k && upto >= k) {
+        int reached = PER_THREAD * tid;
+#pragma unroll
+        for (int i = 0; i < PER_THREAD - 1; ++i) reached += (before += own[i]) < k;
+        S.reached[FIRST].bin = reached;
+    }
     __syncthreads();
     const int bin = S.reached[FIRST].bin;
     return bin < BINS - 1 ? (float)(bin + 1) : ALL_BINS;
@@ -571,7 +604,7 @@ template <class E, class Elements_> __device__ __forceinline__ bool gather(Share
                 const uint32_t n = atomicAdd(&S.n_listed, 1u);
                 if (n < LISTED) S.found[n] = {x, (tile * 64 + lane) * E::N + i};
                 atomicAdd(&S.counts[bin], 1u);
-                atomicAdd(&S.weights[bin], (Weight)Scale::weight(below));
+                atomicAdd(&S.weights[bin], R.scale.weight(below));
             }
         }
     });
@@ -621,29 +654,26 @@ template <class E, bool MIN_P, class Elements_> __device__ __forceinline__ void 
     PieceSums sums(S, C, elements.from, lane);
     if (B.sure == BINS) {      // no filter but min-p's
         elements.each(R, end, [&](int tile, v4u w) {
-            Weight sum = 0;
+            SumOf<E::N> sum;
 #pragma unroll
-            for (int i = 0; i < E::N; i += 2) {
-                const float x = E::at(w, i), y = E::at(w, i + 1);
-                const uint32_t of_x = Scale::weight(R.scale.below(x)), of_y = Scale::weight(R.scale.below(y));
-                sum += (!MIN_P || x >= R.least ? of_x : 0u) + (!MIN_P || y >= R.least ? of_y : 0u);      // (two of them fit 32 bits)
+            for (int i = 0; i < E::N; ++i) {
+                const float x = E::at(w, i), below = R.scale.below(x);
+                sum.add(R.scale, !MIN_P || x >= R.least ? below : __builtin_inff());
             }
-            sums.add(tile, sum);
+            sums.add(tile, sum.units(R.scale));
         });
     } else {
         elements.each(R, end, [&](int tile, v4u w) {
-            Weight sum = 0;
+            SumOf<E::N> sum;
             bool any = false;
 #pragma unroll
             for (int half = 0; half < E::N; half += 4) {
-                uint32_t weight[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float x = E::at(w, half + i), below = R.scale.below(x), at = Row::bin_of(below);
                     any |= at < end && !(at < sure);
-                    weight[i] = at < sure && (!MIN_P || x >= R.least) ? Scale::weight(below) : 0u;
+                    sum.add(R.scale, at < sure && (!MIN_P || x >= R.least) ? below : __builtin_inff());
                 }
-                sum += weight[0] + weight[1], sum += weight[2] + weight[3];
             }
             uint32_t candidates = 0;      // one bit for each
             if (__ballot(any)) {
@@ -664,7 +694,7 @@ template <class E, bool MIN_P, class Elements_> __device__ __forceinline__ void 
                     }
                 }
             }
-            sums.add(tile, sum);
+            sums.add(tile, sum.units(R.scale));
         });
     }
     sums.end();
@@ -772,7 +802,7 @@ __device__ __forceinline__ Place resolve_all(Shared &S, const Row &R, const Elem
                 if (below < RANGE && p >= least && p >> (left + bits) == prefix) {
                     const int bin = (int)((1u << bits) - 1 - (uint32_t)(p >> left & ((1u << bits) - 1)));      // from the largest down
                     atomicAdd(&S.counts[bin], 1u);
-                    atomicAdd(&S.weights[bin], (Weight)Scale::weight(below));
+                    atomicAdd(&S.weights[bin], R.scale.weight(below));
                 }
             }
         });
@@ -803,9 +833,9 @@ template <class E> __device__ __forceinline__ Place settle(Shared &S, const Args
             const int bin = (int)Row::bin_of(below);
             const Weight what_for = B.candidate(bin);
             if (what_for)
-                S.listed[atomicAdd(&S.n_candidates, 1u)] = {place(f.x, f.index), Scale::weight(below) | what_for};
+                S.listed[atomicAdd(&S.n_candidates, 1u)] = {place(f.x, f.index), R.scale.weight(below) | what_for};
             else if (bin < B.sure && f.x >= R.least)
-                atomicAdd(&S.pieces[C.piece_of(f.index / Tiles<E>::TILE)], (Weight)Scale::weight(below));
+                atomicAdd(&S.pieces[C.piece_of(f.index / Tiles<E>::TILE)], R.scale.weight(below));
         }
         __syncthreads();
         const int n = (int)S.n_candidates;
@@ -827,7 +857,7 @@ template <class E> __device__ __forceinline__ Place settle(Shared &S, const Args
 #pragma unroll 1
             for (int i = 0; i < E::N; ++i) {
                 const float x = E::at(w, i), below = R.scale.below(x);
-                if (x >= R.least && place(x, (tile * 64 + lane) * E::N + i) >= border) sum += Scale::weight(below);
+                if (x >= R.least && place(x, (tile * 64 + lane) * E::N + i) >= border) sum += R.scale.weight(below);
             }
             sums.add(tile, sum);
         });
@@ -852,12 +882,12 @@ template <class E> __device__ __forceinline__ void pick(Shared &S, const Args &A
         const int tile = from + wave, at = (tile * 64 + lane) * E::N;
         v4u w = (v4u)(E::NONE);
         if (tile < to) w = Tiles<E>::as_row_says(R, tiles.is_cut(tile) ? tiles.load_cut(tile) : tiles.load(tile));
-        uint32_t own[E::N];
+        Weight own[E::N];
         Weight sum = 0;
 #pragma unroll
         for (int i = 0; i < E::N; ++i) {
             const float x = E::at(w, i);
-            own[i] = x >= R.least && place(x, at + i) >= border ? Scale::weight(R.scale.below(x)) : 0;
+            own[i] = x >= R.least && place(x, at + i) >= border ? R.scale.weight(R.scale.below(x)) : 0;
             sum += own[i];
         }
         Weight upto_lane = up_to_lane(sum), all;
