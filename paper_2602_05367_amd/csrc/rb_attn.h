@@ -264,6 +264,12 @@ __device__ __forceinline__ void meet()
 __device__ __forceinline__ int block_start(int first, int s, int group, int BM) { return (int)((long long)first * group / BM) + s; }
 inline long long block_numbers(long long tokens, int n_seqs, int group, int BM) { return tokens * group / BM + n_seqs; }
 
+// A launch of n workgroups that tell which they are by workgroup(): along x there may be fewer than 2^32 threads, so many workgroups are rows of ACROSS, and the last row's numbers go on
+// beyond n
+constexpr unsigned ACROSS = 1u << 22;
+inline dim3 workgroups(long long n) { return n <= ACROSS ? dim3((unsigned)n) : dim3(ACROSS, (unsigned)((n + ACROSS - 1) / ACROSS)); }
+__device__ __forceinline__ unsigned workgroup() { return blockIdx.y * ACROSS + blockIdx.x; }
+
 // lanes of which something is true, as a number with a sign: one less than none is -1
 __device__ __forceinline__ int lanes_of(unsigned long long mask) { return (int)__popcll(mask); }
 // the last of n places whose start is not beyond `value`, place 0 where all are (arrays that are not in order); a wavefront looks at 64 at a time

@@ -23,7 +23,8 @@ struct AppendArgs {
 template <class T, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append_kernel(const AppendArgs A)
 {
-    const int token = blockIdx.x / A.blocks, part = blockIdx.x % A.blocks, lane = threadIdx.x & 63;
+    const int token = workgroup() / A.blocks, part = workgroup() % A.blocks, lane = threadIdx.x & 63;
+    if (token >= A.tokens) return;
     const int pieces = A.dim / 8, unit = part * 256 + threadIdx.x, head = unit / pieces, piece = unit % pieces;
     const bool there = head < A.heads + 2 * A.kv_heads;
     const bool is_q = head < A.heads, is_v = head >= A.heads + A.kv_heads, turned = !is_v && piece * 8 < A.rotary;
@@ -107,7 +108,7 @@ extern "C" int rb_cache_append(const rb_cache *C, const rb_heads *H, const void 
     A.blocks = (int)(((long long)(A.heads + 2 * A.kv_heads) * (A.dim / 8) + 255) / 256);
     const long long n = (long long)tokens * A.blocks;
     if (n > 0x7fffffffll) return RB_ERR_SHAPE;
-    const dim3 grid((unsigned)n), threads(256);
+    const dim3 grid = workgroups(n), threads(256);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (H->dtype == RB_F16) {
         if (interleaved)

@@ -49,7 +49,8 @@ template <class T, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
 {
     const Cache8Args &C = A.c;
-    const int token = blockIdx.x / A.blocks, part = blockIdx.x % A.blocks, lane = threadIdx.x & 63;
+    const int token = workgroup() / A.blocks, part = workgroup() % A.blocks, lane = threadIdx.x & 63;
+    if (token >= C.tokens) return;
     const int first_unit = __builtin_amdgcn_readfirstlane(part * 256 + (threadIdx.x & 192)), unit = first_unit + lane;
     const bool queries = first_unit < A.query_units;      // (whole wavefronts)
     const int piece = unit & ((1 << A.lanes_shift) - 1), head = queries ? (unit >> A.lanes_shift) * QUERIES : (unit - A.query_units) >> A.lanes_shift;
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(256) void append8_kernel(const Append8Args A)
 template <class T>
 __global__ __launch_bounds__(256) void read8_kernel(const Cache8Args C, Address k_to, Address v_to, int waves)      // wavefronts of a token
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), token = wave / waves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(workgroup() * 4 + (threadIdx.x >> 6)), token = wave / waves;
     if (token >= C.tokens) return;
     const int pieces = C.dim / 16, unit = wave % waves * 64 + lane, head = unit / pieces, piece = unit % pieces;
     int s, end, length;
@@ -196,7 +197,7 @@ extern "C" int rb_cache8_append(const rb_cache8 *C, const rb_heads *H, const voi
     A.blocks = (int)((query_units + ((long long)2 * C->kv_heads << A.lanes_shift) + 255) / 256);
     const long long n = (long long)tokens * A.blocks;
     if (n > 0x7fffffffll) return RB_ERR_SHAPE;
-    const dim3 grid((unsigned)n), threads(256);
+    const dim3 grid = workgroups(n), threads(256);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (H->dtype == RB_F16) {
         if (interleaved)
@@ -227,8 +228,8 @@ extern "C" int rb_cache8_read(const rb_cache8 *C, const int32_t *first, const in
     if (n > 0x1fffffffll) return RB_ERR_SHAPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (C->dtype == RB_F16)
-        hipLaunchKernelGGL((read8_kernel<F16>), dim3((unsigned)n), dim3(256), 0, st, A, rb::address_of(k), rb::address_of(v), waves);
+        hipLaunchKernelGGL((read8_kernel<F16>), workgroups(n), dim3(256), 0, st, A, rb::address_of(k), rb::address_of(v), waves);
     else
-        hipLaunchKernelGGL((read8_kernel<BF16>), dim3((unsigned)n), dim3(256), 0, st, A, rb::address_of(k), rb::address_of(v), waves);
+        hipLaunchKernelGGL((read8_kernel<BF16>), workgroups(n), dim3(256), 0, st, A, rb::address_of(k), rb::address_of(v), waves);
     return hipGetLastError() == hipSuccess ? RB_OK : RB_ERR_HIP;
 }
