@@ -269,6 +269,8 @@ inline long long block_numbers(long long tokens, int n_seqs, int group, int BM) 
 constexpr unsigned ACROSS = 1u << 22;
 inline dim3 workgroups(long long n) { return n <= ACROSS ? dim3((unsigned)n) : dim3(ACROSS, (unsigned)((n + ACROSS - 1) / ACROSS)); }
 __device__ __forceinline__ unsigned workgroup() { return blockIdx.y * ACROSS + blockIdx.x; }
+// whether n of so many threads are few enough for one row
+inline bool one_launch(long long n, int threads) { return n * threads < 1ll << 32; }
 
 // lanes of which something is true, as a number with a sign: one less than none is -1
 __device__ __forceinline__ int lanes_of(unsigned long long mask) { return (int)__popcll(mask); }

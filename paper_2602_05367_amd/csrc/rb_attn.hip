@@ -371,7 +371,7 @@ size_t parts_workspace_bytes(int kv_heads, int group, int dim, int compute_units
 template <class T, int D> int launch_rows(Args A, bool paged, int compute_units, hipStream_t stream)
 {
     const long long blocks = block_numbers(A.tokens_q, A.n_seqs, A.group, BM) * A.kv_heads, n = blocks + (long long)A.wanted * A.kv_heads;      // (a block that has a share of x has at most x + 1)
-    if (n > 0x1fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    if (!one_launch(n, 256) || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     A.ordered = ordered_for(A.n_seqs, n, 2ll * compute_units);
     const dim3 grid((unsigned)n);
     if (paged) {

@@ -49,7 +49,7 @@ template <class T, int D> __global__ __launch_bounds__(256) void join_kernel(con
 template <class T, int D, class Start> int launch(const Args &A, int groups, hipStream_t stream, Start start)
 {
     const long long jobs = attn::block_numbers(A.tokens_q, A.n_seqs, A.group, ROWS) * A.kv_heads;
-    if (jobs > 0x7fffffffll) return RB_ERR_SHAPE;
+    if (!one_launch(jobs, 256)) return RB_ERR_SHAPE;      // (many more sequences than the search for one is made for)
     start(dim3((unsigned)(groups * A.kv_heads)), dim3(64 * WAVES));
     const int rows = (int)std::min((long long)ROWS, (long long)A.tokens_q * A.group), joined = rows_joined(jobs, rows);      // rows of one job, at most
     hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)jobs, (rows + joined - 1) / joined), dim3(256), 0, stream, A, groups * WAVES, joined);

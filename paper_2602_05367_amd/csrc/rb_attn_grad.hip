@@ -490,7 +490,7 @@ template <class T, int D> int launch(GradArgs A, int compute_units, hipStream_t 
 {
     const long long deltas = (long long)((A.tokens_q + 63) / 64) * A.heads;
     const long long keys = block_numbers(A.tokens_k, A.n_seqs, 1, BN) * A.kv_heads, queries = block_numbers(A.tokens_q, A.n_seqs, A.group, BN) * A.kv_heads;
-    if (deltas > 0x7fffffffll || keys > 0x7fffffffll || queries > 0x7fffffffll || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
+    if (!one_launch(deltas, 256) || !one_launch(keys, 512) || !one_launch(queries, 512) || (long long)A.tokens_q * A.group > 0x7fff0000ll) return RB_ERR_SHAPE;
     A.splits = splits_for(block_numbers(A.tokens_k, A.n_seqs, 1, BN), A.kv_heads, A.group, compute_units);
     A.ordered = ordered_for(A.n_seqs, queries, compute_units), A.ordered_keys = ordered_for(A.n_seqs, keys * A.splits, compute_units);
     hipLaunchKernelGGL((delta_kernel<T>), dim3((unsigned)deltas), dim3(256), 0, stream, A);
