@@ -499,7 +499,7 @@ int rb_attn_paged(const rb_cache *C, const void *q, long long q_token, long long
 
 /*
  * A cache in 8 bits: a paged cache as above, its elements e4m3 (8 bits: 4 of exponent, 3 of mantissa, no infinities) in units of one power of two per
- * token and key head, 2^(byte - 127), the bytes in k_exp and v_exp, contiguous [pages][kv_heads][page_tokens], 8-byte aligned.  dtype (RB_F16 or
+ * token and key head, 2^(byte - 127) (255: no number), the bytes in k_exp and v_exp, contiguous [pages][kv_heads][page_tokens], 8-byte aligned.  dtype (RB_F16 or
  * RB_BF16) is that of the tokens that enter it and of the queries.  dim is a multiple of 16 up to 128 (RB_ERR_UNSUPPORTED otherwise);
  * strides of k and v are in elements, multiples of 16, token_stride dim at least; elements of a head are contiguous, k and v 16-byte aligned.
  *
@@ -529,7 +529,10 @@ int rb_cache8_append(const rb_cache8 *C, const rb_heads *H, const void *q, const
 int rb_cache8_read(const rb_cache8 *C, const int32_t *first, const int32_t *lengths, const int32_t *table, int width,
                    int n_seqs, int tokens, void *k, void *v, void *stream);
 
-/* rb_attn_paged over it: the same arguments, refusals and results, of the values that the cache holds. */
+/*
+ * rb_attn_paged over it: the same arguments, refusals and results, of the values that the cache holds.  As there, calls of few tokens per sequence hold the softmax weights in two
+ * parts and others round them to dtype.  The former hold a weight times its value's unit in bf16's range: heads of values below 2^-110 lose bits.
+ */
 size_t rb_attn_cache8_workspace_bytes(const rb_cache8 *C, int heads, int n_seqs, int tokens);
 int rb_attn_cache8(const rb_cache8 *C, const void *q, long long q_token, long long q_head, int heads,
                    const int32_t *first, const int32_t *lengths, const int32_t *table, int width,

@@ -178,7 +178,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void few8_kernel(const Args A)
             start();
             rows_arrived();
         }
-        const auto unit = __builtin_amdgcn_permlane32_swap(exponent << 23, exponent << 23, false, false);      // of key lane % 32, and of its value
+        const uint32_t bits = max(exponent << 23, 0x400000u);      // (2^-127 is no normal number)
+        const auto unit = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);      // of key lane % 32, and of its value
         const float key_unit = __uint_as_float(unit[0]);
         if (lane < 32) units_w[lane] = __uint_as_float(unit[1]);
         loads_arrived<LEFT>();
