@@ -81,7 +81,7 @@ __device__ __forceinline__ Args with_shares(Args A, const Sums<Tiles> &tiles)
 // tokens in all, 312 workgroups, 11.5 and 16.8).
 //
 // Of a cache in 8 bits, elements come into registers, are widened to T in their units there, and stored into the tile that the rest of the kernel knows (512 and seven new tokens on 21513 positions,
-// 32 and 8 heads: 114 us and 14 for the join; of 16 bits, where tiles go into LDS past the registers, 90 to 100 and 14).
+// 32 and 8 heads: 115 us and 14 for the join; of 16 bits, where tiles go into LDS past the registers, 90 to 100 and 14).
 enum From { PACKED, PAGES, PAGES8 };      // where keys and values are: packed, in a cache, in a cache in 8 bits
 template <class T, int D, From FROM, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void rows_kernel(const Args A)

@@ -9,7 +9,7 @@ namespace attn {
 
 __device__ __forceinline__ float unit8(uint32_t exponent) { return __uint_as_float(exponent << 23); }      // (the conversions read a float's exponent alone)
 
-// eight elements times a unit, each exact in fp32 and rounded once
+// eight elements times a unit, each exact in fp32 and rounded once: exact in T too, but for fp16's last bits, below 2^-24, and what is beyond its largest number
 template <class T> __device__ __forceinline__ v4u widen8(v2u w, float unit);
 template <> __device__ __forceinline__ v4u widen8<F16>(v2u w, float unit)
 {
@@ -49,7 +49,7 @@ template <class T> __device__ __forceinline__ uint32_t narrow8(const float (&x)[
 }
 
 // 16 bytes per lane from a buffer to LDS, one lane's after the other's (a function of its own: inside of another, the host's compiler does not take the size).  Not kept by the caches: each
-// byte is used once (48 sequences of 250000 positions together: 110 us, kept 119)
+// byte is used once (48 sequences of 250000 positions together, the call: 111 us, kept 119)
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t offset)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, (int)offset, 0, 0, 2);

@@ -1,13 +1,14 @@
 // Attention of few new tokens per sequence over a paged cache in 8 bits: as rb_attn_few.hip, the time being that of reading the cache once.
 //
 // The same shares, one per wavefront.  Tiles of 32 keys go into LDS as they are, 8 bits an element, and are widened on their way to the matrix instructions: a key's elements
-// in units of their own, exactly, to the queries' type; a value's as they are, to bf16, their units going into the weights, which then have all the range of fp32 and two parts
-// of 16 bits, as good as 16 bits.  With half the bytes to a tile two of them per wavefront are on their way, and two workgroups share a compute unit.
+// in units of their own to the queries' type (exactly, but for fp16's last bits below 2^-24); a value's as they are, to bf16, their units going into the weights, which then have all the range of fp32
+// and two parts of 16 bits, as good as 16 bits.  With half the bytes to a tile two of them per wavefront are asked for ahead, and two workgroups share a compute unit.  Once in two tiles the
+// compiler waits for more than it has to: the loop may end between the two, and there it counts on the keys just asked for (heads of up to 64: on all loads, as half of the lanes make them).
 //
-// Bound: bytes of the cache that one long run of loads brings in.  48 sequences of 250000 positions together, 8 key heads of 128 elements (518 MB): 100 to 104 us (5.1 TB/s; a copy of 616 MB reaches 5.4),
-// and 7.5 for joining; one workgroup per compute unit 127.  Leaving out, for a measurement, the second part of the weights, the product with the values or the widening changed nothing; leaving out
-// the units' bytes, lines of their own among the elements', took off 4 %.  6 sequences of five drafted tokens, 40 heads (89 MB): 28 us and 7; one of 2000 tokens: 12.5 and 5, the chain of
-// finding the share, its pages, its first tiles and the join.
+// Bound: bytes of the cache that one long run of loads brings in, and that wait.  Kernels: 48 sequences of 250000 positions together, 8 key heads of 128 elements (518 MB, of which 521 are fetched): 103 us, 111 in
+// another run (4.7 to 5.0 TB/s; a copy of 616 MB reaches 5.4), and 7.4 for joining; vector instructions are 43 % of its time.  8 heads of 64, half the bytes: 100 us for the call, 110 with 128.  Leaving out, for a
+// measurement, the second part of the weights, the product with the values or the widening changed nothing; leaving out the units' bytes, lines of their own among the elements', with the wait for
+// them, took off 4 %.  6 sequences of five drafted tokens, 40 heads (89 MB): 28.5 us and 6.6; one of 2000 tokens: 12.4 and 5.1, the chain of finding the share, its pages, its first tiles and the join.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 
@@ -30,8 +31,8 @@ template <int D> struct Tile8 {
     static __device__ __forceinline__ int spread(int r) { return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3; }
 };
 
-// Heads of a token lie next to each other where pages are [tokens][heads][elements]: a workgroup's four wavefronts then read 512 bytes in a row in place of four times 128 (drafts over 40 heads 33.6 us
-// in all, 44.9 with a head to a workgroup; 48 sequences 110 both, 117 and 127 with loads that the caches keep)
+// Heads of a token lie next to each other where pages are [tokens][heads][elements]: a workgroup's four wavefronts then read 512 bytes in a row in place of four times 128 (calls: drafts over 40 heads 34 us,
+// 45 with a head to a workgroup; 48 sequences 111 both, 119 with loads that the caches keep)
 constexpr int XCDS = 8;
 __host__ __device__ __forceinline__ int heads_together(int kv_heads) { return kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1; }
 
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void few8_kernel(const Args A)
     loads_arrived();
 }
 
-// two workgroups per compute unit, shared out over the key heads (one each: 48 sequences 134 us in place of 110, drafts 38 in place of 34; a single sequence of 2000 tokens 17.0 in place of 17.5)
+// two workgroups per compute unit, shared out over the key heads (calls with one each: 48 sequences 134 us in place of 111, drafts 38 in place of 34; a single sequence of 2000 tokens 16.9 in place of 17.3)
 int groups_per_head(int kv_heads, int compute_units) { return std::max(2 * compute_units / kv_heads, 1); }
 
 template <class T, int D> int launch(Args A, int compute_units, hipStream_t stream)

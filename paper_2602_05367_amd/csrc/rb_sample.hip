@@ -357,8 +357,9 @@ template <class E> __device__ __forceinline__ float largest_of(v4u w)      // (N
     return t;
 }
 
-// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 22 and
-// 28 us, top-p 51.5 and 57, no filter 25 and 28, greedy 16 and 24).  Sixteen tiles are what a wavefront of 128 registers has room for.
+// Tiles kept in registers, or, HELD = 0, read anew each time, four at a time.  Held, the row is read once; read anew it comes from the L2 but waits for it each time (256 rows of 128000 bf16: top-k 22.6 and
+// 28 us, top-p 52 and 58, no filter 27 and 29, greedy 16 and 24; of 65536 fp32, top-p, 38 and 48).  Sixteen tiles are what a wavefront of 128 registers has room for; longer rows are read anew (256 of 128000 fp32: no
+// filter 49 us, top-p 79; of 152000 bf16 32 and 67).
 template <class E, int HELD> struct Elements : Tiles<E> {
     // word j of each tile: one place of a vector, so that a loop over the tiles is one copy of its body (sixteen do not fit the instruction cache)
     typedef uint32_t Words __attribute__((ext_vector_type(HELD ? HELD : 1)));
@@ -643,7 +644,7 @@ struct PieceSums {
     }
 };
 
-// Weights of the tokens that are left for sure, by pieces of the row; candidates into the list, as far as there is room.  Without min-p (!MIN_P) no logit is compared with its border (no filter 25 us for 26.5)
+// Weights of the tokens that are left for sure, by pieces of the row; candidates into the list, as far as there is room.  Without min-p (!MIN_P) no logit is compared with its border (256 rows of 128000 bf16, no filter, 27 us for 28)
 template <class E, bool MIN_P, class Elements_> __device__ __forceinline__ void collect(Shared &S, const Row &R, const Bins &B, const Cut &C, const Elements_ &elements, int lane)
 {
     const float sure = B.sure == BINS ? ALL_BINS : (float)B.sure, below_least = R.scale.below(R.least);
@@ -948,7 +949,7 @@ template <class E, int HELD> __global__ __launch_bounds__(THREADS) void row_kern
     pick<E>(S, A, row, R, border, C, lane, wave);
 }
 
-// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 39 us, one workgroup each 56; one row 24.5 and 52), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
+// Several workgroups do a row (48 rows of 131071 fp32 with top-p: 39 to 41 us, one workgroup each 56; one row 25 and 53), in four launches: its maximum; the histogram, which they add up in memory; what is left for sure and the candidates; the border and the
 // token.  What they hand on lies in the workspace.
 enum Step { MAXIMUM, HISTOGRAM, COLLECT };
 __device__ __forceinline__ float largest_of_row(const Parts &P, size_t first, int groups, int lane)
@@ -1042,9 +1043,9 @@ template <class E> __global__ __launch_bounds__(THREADS) void token_kernel(const
 constexpr int MAX_ROWS = 1 << 20;
 constexpr long long MAX_STRIDE = 1ll << 40;
 
-// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 24.6 us with 4096, 23.8 with 2048, 26.5 with 8192; four of 151936
-// fp32 26.0, 27.0 and 26.3); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 12.8 us, four launches 29; 7 rows
-// of 50001 bf16, no filter: 12.9 and 14.0.  From there on several are faster: 128000 bf16 with top-p 24.5 us, one workgroup 43.5, no filter 14.4 and 17.0)
+// Workgroups of a row: powers of two, as many as there are compute units for, of SHARE logits at least (one row of 128000 bf16, top-p: 24.9 us with 4096, 24.0 with 2048, 26.7 with 8192; four of 151936
+// fp32 25.9, 26.9 and 26.4); one, where that is a launch in place of four and has 8 tiles a wavefront at most (64 rows of 32000 fp32, top-k and top-p: 12.9 us, four launches 28.6; 7 rows
+// of 50001 bf16, no filter: 13.9 and 15.0.  From there on several are faster: 128000 bf16 with top-p 24.9 us, one workgroup 43.9, no filter 14.8 and 18.9)
 constexpr int SHARE = 4096, MOST_GROUPS = 64, SINGLE = 8 * WAVES;
 int compute_units() { return std::max(mx::device_groups(), 2); }
 int groups_of(int rows, int tiles, int tile, int compute_units)
@@ -1066,8 +1067,8 @@ template <class E> int launch(Args A, hipStream_t stream)
 {
     const int tiles = (A.vocab + Tiles<E>::TILE - 1) / Tiles<E>::TILE;
     const dim3 rows((unsigned)A.rows), threads(THREADS);
-    // With top-k alone a row's few tokens are found by one workgroup before several have met, if no row has more than 512 of them: one row of 128000 bf16, the first 50: 14.3 us, with sixteen
-    // workgroups 22.1; 300: 19.1 and 22.4; 1000, for which every bin counts, 37.4 and 22.8.  48 rows of 131071 fp32: 22.2 and 33.6; 27.5 and 34.8; 49.1 and 35.5.  One row of 200000 fp32: 24.7 and 21.4
+    // With top-k alone a row's few tokens are found by one workgroup before several have met, if no row has more than 512 of them: one row of 128000 bf16, the first 50: 14.5 us, with sixteen
+    // workgroups 22.1; 300: 19.5 and 22.5; 1000, for which every bin counts, 36.3 and 23.0.  48 rows of 131071 fp32: 22.6 and 32.6; 27.7 and 33.9; 46.7 and 34.5.  One row of 200000 fp32: 25.0 and 21.7
     A.groups = A.top_k && !A.top_p && tiles <= 32 * WAVES ? 1 : groups_of(A.rows, tiles, Tiles<E>::TILE, compute_units());
     if (A.groups > 1) {
         const int of_group = (tiles + A.groups - 1) / A.groups;
