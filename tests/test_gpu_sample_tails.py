@@ -116,3 +116,22 @@ def test_slopes():
             got = rb.rb_sample(x, torch.tensor([float(number)], device="cuda"))
             torch.cuda.synchronize()
             check(host, got, [float(number)])
+
+
+@pytest.mark.parametrize("vocab", [(1 << 19) - 1, 1 << 19, (1 << 22) - 1, 1 << 22])
+def test_the_largest_sums(vocab):
+    """All logits alike: every sum of weights is as large as it can be, and a whole number of the largest weight, so the token is known exactly."""
+    x = torch.full((1, vocab), 3.25, device="cuda")
+    for number in (0.0, 0.3, 0.5, 0.99999, 1 - 2.0 ** -24):
+        u = torch.tensor([number], device="cuda")
+        number = float(np.float32(number))
+        for top_k, top_p, temperature in ((0, 1.0, 1.0), (vocab - 5, 1.0, 0.01), (0, 0.75, INF), (vocab // 2, 0.999, 1.0), (7, 1.0, 1.0), (0, 1 - 2.0 ** -24, 1.0)):
+            given = {"temperature": torch.tensor([temperature], device="cuda")}
+            if top_k:
+                given["top_k"] = torch.tensor([top_k], dtype=torch.int32, device="cuda")
+            if top_p < 1:
+                given["top_p"] = torch.tensor([top_p], device="cuda")
+            left = top_k or vocab
+            left = -(-int(float(np.float32(top_p)) * 2 ** 24) * left // 2 ** 24) if top_p < 1 else left      # (fp32 numbers from 1/2 on are multiples of 2^-24)
+            got = rb.rb_sample(x, u, **given)
+            assert int(got) == int(number * 2 ** 149) * left // 2 ** 149, (vocab, number, top_k, top_p, temperature)
