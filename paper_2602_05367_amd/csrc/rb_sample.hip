@@ -27,7 +27,7 @@ namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64, PER_THREAD = 3, BINS = PER_THREAD * THREADS, BIN_BITS = 11, PIECES = 64, LISTED = 2 * THREADS;
 static_assert(BINS >= 1 << BIN_BITS);
-// (3072 bins of -log2 w are 0.015 wide.  With 2048, more lanes meet in one: 256 rows of 128000 bf16, top-p, 59 us in place of 52, 48 of 131071 fp32 43 in place of 39; 4096 took the same time:
+// (Three bins of -log2 w a thread are 0.015 wide.  With two, more lanes meet in one: 256 rows of 128000 bf16, top-p, 59 us in place of 52, 48 of 131071 fp32 43 in place of 39; four took the same time:
 // what is saved among the lanes and candidates is spent on clearing and adding up)
 constexpr float RANGE = 46.5f;      // -log2 of weights that round to nothing
 typedef unsigned long long Weight;
