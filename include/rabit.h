@@ -410,8 +410,9 @@ int rb_add(const uint16_t *a, const uint16_t *b, uint16_t *y, size_t n, void *st
  *
  * Sequences are packed one after the other: sequence s has the tokens first[s]
  * .. first[s + 1] - 1 (device int32 [n_seqs + 1], first[0] = 0, not decreasing;
- * lengths of zero are allowed; at most 2^24 tokens and 2^20 sequences, in attention fewer than 2^24 of kv_heads *
- * (n_seqs + tokens * heads / kv_heads / 32), in its gradient than 2^23 (RB_ERR_SHAPE)).  Tokens from
+ * lengths of zero are allowed; at most 2^24 tokens and 2^20 sequences.  Attention is a workgroup per block of
+ * rows, kv_heads * (n_seqs + tokens * heads / kv_heads / 128) at most (32 for 128 with few tokens per sequence over a
+ * cache), and takes fewer than 2^24 of them, its gradient 2^23: RB_ERR_SHAPE).  Tokens from
  * first[n_seqs] on (padding, where a call's number of tokens is fixed) belong to no sequence: they are not
  * read into any, and their rows of every result and gradient are left as they are.  The arrays are read on the
  * device; entries out of order or out of range give unspecified results, but
